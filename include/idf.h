@@ -425,6 +425,105 @@ int idf_profile_end(idf_streams *s, int max_kinds, idf_kernel_profile *out, int 
 enum { IDF_PEAK_COPY = 0, IDF_PEAK_FMA_F32 = 1, IDF_PEAK_MFMA_F32 = 2, IDF_PEAK_MFMA_BF16 = 3, IDF_PEAK_MFMA_I8 = 4 };
 int idf_measure_peak(int kind, void *dev_buf, size_t bytes, void *hip_stream, double *rate);
 
+/* Mixing the tokens of a stream -- what follows a net whose rows are feature vectors in time, with the property of the streaming core
+ * itself: a stream's state has a fixed size, whatever the length of the stream.  Three operators: norms of queries and keys with their
+ * rotation by position, attention over a sliding window with a rolling cache, and linear attention with a decay per head.
+ *   Tokens are packed: row t of q, k, v and out belongs to one token, rows of a segment follow each other, and segment s has the rows
+ * offsets[s] <= t < offsets[s + 1].  q is [token][head][value] with strides of its own (in elements; values of a head lie next to each
+ * other), so that q, k and v may be views of one projection.  Query head h reads key/value head h / (heads_q / heads_kv).  Precision is
+ * IDF_PREC_F32 or IDF_PREC_BF16 and holds for q, k, v, out and the caches; sums, statistics and states are float32.
+ *   All pointers are device pointers; the calls enqueue on hip_stream, allocate nothing, keep nothing and may be recorded into a graph:
+ * positions and lengths are read by the kernels.  What only the device can see is held in bounds there: offsets are cut to
+ * 0 .. n_tokens and to at most max_tokens per segment; a segment whose start is negative or whose stream id is none takes no part, and its rows
+ * of out are left as they are.  Two segments of one call must not name the same stream.
+ *   Workspaces (where asked for): any contents, 256-byte aligned, used until the work enqueued by the call is done.
+ * Errors: IDF_EINVAL (null pointers, sizes, strides), IDF_EUNSUPPORTED (precision, head sizes, alignment), IDF_ENOMEM (workspace too
+ * small), IDF_EDEVICE; nothing has been enqueued then, except by IDF_EDEVICE from a launch behind the first. */
+
+/* A matrix of tokens: values of head h of token t at base + t * token_stride + h * head_stride. */
+typedef struct {
+    void *base;
+    int64_t token_stride, head_stride;
+} idf_tokens;
+
+/* Radians per position of each pair of a rotation, f_i = base^(-2i/rotary_dim), i < rotary_dim / 2, to host memory, and the factor on
+ * cosine and sine that goes with them.  Stretched for contexts `factor` times the trained one:
+ *   IDF_ROTARY_LINEAR  f_i / factor;
+ *   IDF_ROTARY_BASE    base * factor^(rotary_dim / (rotary_dim - 2)) in place of base;
+ *   IDF_ROTARY_PARTS   pairs of at least `fast` turns within `trained` positions as they are, of at most `slow` turns divided by the
+ *                      factor, between them in proportion; amplitude 0.1 ln(factor) + 1.
+ * rotary_dim even, 2 .. 256 (4 at least for IDF_ROTARY_BASE); base > 1, factor >= 1, fast > slow >= 0, trained > 0. */
+enum { IDF_ROTARY_PLAIN = 0, IDF_ROTARY_LINEAR = 1, IDF_ROTARY_BASE = 2, IDF_ROTARY_PARTS = 3 };
+int idf_rotary_frequencies(int rotary_dim, double base, int scaling, double factor, double trained, double fast, double slow,
+                           double *frequencies, double *amplitude);
+
+/* Queries and keys of every token, each head normalised and turned by the token's position, in one pass:
+ *   y = weight * x / sqrt(mean(x^2) + eps) over the head (a null weight: y = x);
+ *   pairs (y_i, y_{i + rotary_dim/2}), or (y_2i, y_{2i+1}) where interleaved, i < rotary_dim / 2, by the angle position * frequencies[i]:
+ *   (a, b) -> amplitude * (a cos - b sin, b cos + a sin); values from rotary_dim on stay y.
+ * Angles are formed and reduced in float64.  q_out may be q and k_out may be k; else outputs must not overlap inputs.
+ *   head_dim <= 256, rotary_dim even and <= head_dim (0: no rotation), heads >= 0, weights float32 [head_dim], frequencies float64
+ * [rotary_dim / 2], positions int64 [n_tokens]. */
+typedef struct {
+    int precision, heads_q, heads_k, head_dim, rotary_dim, interleaved;
+    int64_t n_tokens;
+    idf_tokens q, k, q_out, k_out;
+    const int64_t *positions;
+    const double *frequencies;
+    const float *q_weight, *k_weight;
+    double amplitude;
+    float eps;
+} idf_norm_rotate_args;
+int idf_norm_rotate(const idf_norm_rotate_args *a, void *hip_stream);
+
+/* Attention over the last `window` tokens of a stream and its first `sinks` ones:
+ *   out_p = sum_j softmax_j(scale * q_p . k_j) v_j  over  j <= p with j > p - window or j < sinks.
+ * The cache of a stream is a ring, as the rows of a layer are: k_ring, v_ring [n_streams][slots][heads_kv][head_dim]; the token at
+ * position p lies in slot p where p < sinks, else in sinks + (p - sinks) mod (slots - sinks), slots - sinks >= window.  A segment attends
+ * over what its stream's ring holds from before and over its own tokens, and is then written to the ring (of a segment longer than the
+ * ring its newest tokens, and the first ones of the stream).  Slots that the stream has not written are never read.
+ *   starts: position of each segment's first token (NULL: 0); stream_ids: ring of each segment (NULL: segment s has ring s);
+ * offsets: see above (NULL: every segment has max_tokens tokens).  k_ring = v_ring = NULL: no cache, segments see themselves only.
+ *   head_dim a multiple of 16 bytes, <= 256; tokens' bases and strides multiples of 16 bytes; scale > 0. */
+typedef struct {
+    int precision, heads_q, heads_kv, head_dim;
+    int64_t n_tokens, max_tokens;
+    int n_segments, n_streams;
+    int64_t slots;
+    int window, sinks;
+    float scale;
+    idf_tokens q, k, v, out;
+    void *k_ring, *v_ring;
+    const int64_t *offsets, *starts;
+    const int32_t *stream_ids;
+    void *workspace;
+    size_t workspace_bytes;
+} idf_window_args;
+int idf_window_workspace(const idf_window_args *a, size_t *bytes);
+int idf_window_attend(const idf_window_args *a, void *hip_stream);
+
+/* Linear attention with a decay per key/value head, lambda = exp(log_decay):
+ *   S_t = lambda S_{t-1} + k_t^T v_t,   out_t = scale * q_t S_t,
+ * from the state S of the segment's stream before it to the one after it.  state_in, state_out: float32 [n_streams][heads_kv][dim_k][dim_v];
+ * they may be the same; state_in NULL: zeros; state_out NULL: not wanted.  A segment without tokens hands its state on.
+ *   dim_k, dim_v multiples of 16 bytes, dim_k <= 256; tokens' bases and strides multiples of 16 bytes; log_decay float32 [heads_kv], <= 0. */
+typedef struct {
+    int precision, heads_q, heads_kv, dim_k, dim_v;
+    int64_t n_tokens, max_tokens;
+    int n_segments, n_streams;
+    float scale;
+    idf_tokens q, k, v, out;
+    const float *log_decay;
+    const float *state_in;
+    float *state_out;
+    const int64_t *offsets;
+    const int32_t *stream_ids;
+    void *workspace;
+    size_t workspace_bytes;
+} idf_decay_args;
+int idf_decay_workspace(const idf_decay_args *a, size_t *bytes);
+int idf_decay_attend(const idf_decay_args *a, void *hip_stream);
+
 const char *idf_last_error(void);
 
 #ifdef __cplusplus

@@ -10,6 +10,10 @@
 
 namespace idf {
 
+// Sets the text of idf_last_error of this thread and returns the code.
+int fail(int code, const char *fmt, ...);
+int dev_fail(hipError_t e, const char *what);
+
 // Where and how a kernel is launched: plain, or bracketed by an event pair stamped at the
 // kernel's own start and end (profiling).
 struct LaunchCtx {
@@ -113,6 +117,13 @@ hipError_t launch_ring_move(const RingMove &a, const LaunchCtx &lc);
 size_t peak_sink_bytes(int blocks);
 double peak_ops(int kind, int blocks, int iters);
 hipError_t launch_peak(int kind, void *buf, size_t bytes, int blocks, int iters, const LaunchCtx &lc);
+
+// Mixing of tokens (arguments are checked; workspace sizes are those of the *_workspace functions).
+hipError_t launch_norm_rotate(const idf_norm_rotate_args &a, const LaunchCtx &lc);
+size_t window_workspace(const idf_window_args &a);
+hipError_t launch_window(const idf_window_args &a, const LaunchCtx &lc);
+size_t decay_workspace(const idf_decay_args &a);
+hipError_t launch_decay(const idf_decay_args &a, const LaunchCtx &lc);
 
 // Largest number of touched output rows one generic conv step can take for a layer with
 // c_out output channels (the host splits longer steps).

@@ -27,7 +27,9 @@ namespace {
 
 thread_local std::string g_err;
 
-int fail(int code, const char *fmt, ...)
+}  // namespace
+
+int idf::fail(int code, const char *fmt, ...)
 {
     char buf[512];
     va_list ap;
@@ -37,6 +39,13 @@ int fail(int code, const char *fmt, ...)
     g_err = buf;
     return code;
 }
+
+int idf::dev_fail(hipError_t e, const char *what)
+{
+    return fail(IDF_EDEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+namespace {
 
 size_t align_up(size_t v, size_t a = 256) { return (v + a - 1) / a * a; }
 
@@ -518,11 +527,6 @@ template <class F> int for_each_selection(const std::vector<std::pair<int, int>>
         i = j;
     }
     return IDF_OK;
-}
-
-int dev_fail(hipError_t e, const char *what)
-{
-    return fail(IDF_EDEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 
 // Launch context of the next kernel: plain, or with a fresh event pair while profiling.
