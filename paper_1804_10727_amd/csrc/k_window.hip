@@ -1,63 +1,515 @@
 // Attention over a sliding window and first tokens, with the ring that caches keys and values (idf_window_attend).
+//
+// Scores are formed transposed, S^T = K Q^T: a lane then holds the scores of one query row, so that the softmax's maximum and sum are kept
+// per lane, and what comes out of the matrix cores is the operand that O^T = V^T P^T takes, without a way through LDS.  Query heads that share
+// a key/value head are rows next to each other: row = token * group + head of the group.
+//   Sums, maxima and outputs are float32; in bfloat16 the weights exp(s - max) are rounded to bfloat16 for the product with V (their sum
+// is not): half a step of 2^-8 on each, independent from key to key, about as much as the rounding of the output.
 #include <algorithm>
 
 #include "idf.h"
-#include "seq_common.h"
+#include "seq_mfma.h"
 
 namespace idf {
 
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kStepRows = 16;                      // query rows of a segment and key/value head that the step kernel takes
+constexpr int kTileRows = 128;                     // query rows of a workgroup of the tile kernel
 
-// Where the key or value of a position lies: with the segment's own tokens, or in the ring.
-template <class T>
-__device__ __forceinline__ const T *held_row(const idf_window_args &a, const Segment &g, int64_t pos, const idf_tokens &own, const void *ring, int kv)
+// The keys that query positions first .. last see, as a list in order of position: first tokens of the stream, then from the beginning of
+// the oldest window on.  Entry i is entry of the ring or of the segment's own tokens; position p sees entry i if
+// i <= p - shift and (i > p - window - shift or i < n_first).
+struct Keys {
+    int n, n_first;            // entries, and how many of them are first tokens ahead of the window
+    int skip;                  // position of entry 0 where it is a first token
+    int own;                   // entries n_first + own .. are the segment's own, own token 0 being entry n_first + own (may be negative)
+    int first_own;             // the same for entries that are first tokens: entry i is own token i - first_own where not negative
+    uint32_t slot0, period;    // ring slot, counted behind the first tokens, of entry n_first
+    int64_t shift;             // position of entry i >= n_first is i + shift
+};
+
+__device__ __forceinline__ Keys keys_of(const idf_window_args &a, const Segment &g, int64_t p0, int64_t p1)
 {
-    if (pos >= g.start) return (const T *)own.base + (g.begin + (pos - g.start)) * own.token_stride + kv * own.head_stride;
-    const int64_t slot = pos < a.sinks ? pos : a.sinks + (pos - a.sinks) % (a.slots - a.sinks);
-    return (const T *)ring + ((g.ring * a.slots + slot) * a.heads_kv + kv) * a.head_dim;
+    Keys k;
+    const int64_t held = a.k_ring ? 0 : g.start;                 // (without a ring nothing from before the segment)
+    const int64_t first = min((int64_t)a.sinks, p1 + 1), skip = min(first, held), low = max(max(first, p0 - a.window + 1), held);
+    k.skip = (int)skip;
+    k.n_first = (int)(first - skip);
+    k.shift = low - k.n_first;
+    k.n = (int)(p1 - k.shift + 1);
+    k.own = (int)max(min(g.start - low, (int64_t)0x7fffffff), -(int64_t)0x7fffffff);
+    k.first_own = (int)min(g.start - skip, (int64_t)0x7fffffff);
+    k.period = a.k_ring ? (uint32_t)(a.slots - a.sinks) : 1u;
+    k.slot0 = low >= a.sinks ? (uint32_t)((low - a.sinks) % k.period) : 0u;
+    return k;
 }
 
-// One query row by one wave, key by key: scores of 64 keys at a time, a lane each, then the sum with a lane for every 64th value.  Only
-// keys that the query sees are read, so that whatever lies in the others cannot reach it.
+// Where a matrix of keys or values lies: own tokens and the ring of the segment's stream, from the head's first value on.
+template <class T> struct Held {
+    const T *own, *ring;
+    int64_t own_stride, ring_stride;
+    __device__ __forceinline__ Held(const idf_window_args &a, const Segment &g, const idf_tokens &t, const void *ring_base, int kv)
+    {
+        own = (const T *)t.base + g.begin * t.token_stride + kv * t.head_stride;
+        own_stride = t.token_stride;
+        ring_stride = (int64_t)a.heads_kv * a.head_dim;
+        ring = (const T *)ring_base + g.ring * a.slots * ring_stride + (int64_t)kv * a.head_dim;
+    }
+};
+
+// Entry i of the list (0 <= i < n): its place, for keys and values alike.
+struct Place { bool own; int64_t row; };
+__device__ __forceinline__ Place place_of(const idf_window_args &a, const Keys &k, int i)
+{
+    const int rel = i - k.n_first, t = rel < 0 ? i - k.first_own : rel - k.own;
+    Place p;
+    p.own = t >= 0;
+    uint32_t s = k.slot0 + (uint32_t)rel;
+    if (s >= k.period) s -= k.period;
+    p.row = p.own ? (int64_t)t : rel < 0 ? (int64_t)(k.skip + i) : (int64_t)a.sinks + s;
+    return p;
+}
+template <class T> __device__ __forceinline__ const T *at(const Held<T> &h, const Place &p)
+{
+    return p.own ? h.own + p.row * h.own_stride : h.ring + p.row * h.ring_stride;
+}
+
+// Partial results of rows whose keys are split over workgroups: [split][token][head][head_dim] sums, then [split][token][head] maximum (of
+// scores in units of log 2) and sum of weights.
+struct Partial {
+    float *o, *ml;
+    int splits;
+};
+__device__ __host__ __forceinline__ Partial partial_of(const idf_window_args &a, int splits)
+{
+    Partial p;
+    p.splits = splits;
+    p.o = (float *)a.workspace;
+    p.ml = p.o + (int64_t)splits * a.n_tokens * a.heads_q * a.head_dim;
+    return p;
+}
+
+// A row whose sums came out infinite or not a number: once more, by one wave, reading only the values that the row sees -- on the
+// matrix cores a weight of zero times an infinite value that another row of the tile sees would be no zero.
 template <int PREC>
-__global__ void __launch_bounds__(64) k_window_rows(idf_window_args a)
+__device__ __forceinline__ void exact_row(const idf_window_args &a, const Segment &g, const Keys &keys, int kv, int h, int t, int i0, int i1, const Partial &part, int split)
 {
     using E = Elem<PREC>;
     using T = typename E::type;
-    const int lane = threadIdx.x, h = blockIdx.y, kv = h / (a.heads_q / a.heads_kv);
-    const Segment g = segment_of(a, blockIdx.z, a.starts);
-    for (int t = blockIdx.x; t < g.len; t += gridDim.x) {
-        const int64_t p = g.start + t, floor = a.k_ring ? 0 : g.start;               // (without a ring nothing is held from before the segment)
-        const int64_t first = min((int64_t)a.sinks, p + 1), low = max(max(first, p - a.window + 1), floor), skip = min(first, floor);
-        const int64_t n_first = first - skip, n = n_first + max(p - low + 1, (int64_t)0);
-        const T *q = (const T *)a.q.base + (g.begin + t) * a.q.token_stride + h * a.q.head_stride;
-        float m = -__FLT_MAX__, l = 0.f, o[4] = {};
-        for (int64_t i0 = 0; i0 < n; i0 += 64) {
-            const int64_t i = min(i0 + lane, n - 1), pos = i < n_first ? skip + i : low + i - n_first;
-            const T *k = held_row<T>(a, g, pos, a.k, a.k_ring, kv);
-            float s = 0.f;
+    const int lane = threadIdx.x & 63;
+    const int64_t p = g.start + t, token = g.begin + t;
+    const int hi = (int)(p - keys.shift);
+    const int64_t lo = p - a.window - keys.shift;
+    const T *q = (const T *)a.q.base + token * a.q.token_stride + h * a.q.head_stride;
+    const Held<T> kh(a, g, a.k, a.k_ring, kv), vh(a, g, a.v, a.v_ring, kv);
+    float m = -__FLT_MAX__, l = 0.f, o[4] = {};
+    for (int b = i0; b < i1; b += 64) {
+        const int i = b + lane;
+        const bool seen = i < i1 && i <= hi && (i > lo || i < keys.n_first);
+        float s = -__builtin_inff();
+        if (seen) {
+            const T *k = at(kh, place_of(a, keys, i));
+            s = 0.f;
             for (int d = 0; d < a.head_dim; ++d) s += E::to_f32(q[d]) * E::to_f32(k[d]);
-            s = i0 + lane < n ? s * (a.scale * kLog2e) : -__builtin_inff();
-            const float m2 = fmaxf(m, wave_max(s)), w = exp2f(s - m2), fade = exp2f(m - m2);
-            m = m2;
-            l = l * fade + wave_sum(w);
+            s *= a.scale * kLog2e;
+        }
+        const unsigned long long all = __ballot(seen);
+        if (!all) continue;
+        // a NaN among the scores has to stay: the maximum alone would drop it, its weight does not
+        const float m2 = fmaxf(m, wave_max(s)), w = seen ? exp2f(s - m2) : 0.f, fade = exp2f(m - m2);
+        m = m2;
+        l = l * fade + wave_sum(w);
+        for (int c = 0; c < 4; ++c) o[c] *= fade;
+        for (int j = 0; j < 64; ++j) {
+            if (!(all >> j & 1)) continue;
+            const T *v = at(vh, place_of(a, keys, b + j));
+            const float wj = __shfl(w, j);
+            for (int c = 0; c < 4; ++c)
+                if (lane + 64 * c < a.head_dim) o[c] += wj * E::to_f32(v[lane + 64 * c]);
+        }
+    }
+    if (part.splits > 1) {
+        const int64_t row = ((int64_t)split * a.n_tokens + token) * a.heads_q + h;
+        for (int c = 0; c < 4; ++c)
+            if (lane + 64 * c < a.head_dim) part.o[row * a.head_dim + lane + 64 * c] = o[c];
+        if (lane == 0) { part.ml[2 * row] = m; part.ml[2 * row + 1] = l; }
+        return;
+    }
+    T *out = (T *)a.out.base + token * a.out.token_stride + h * a.out.head_stride;
+    for (int c = 0; c < 4; ++c)
+        if (lane + 64 * c < a.head_dim) out[lane + 64 * c] = E::from_f32(o[c] / l);
+}
+
+// ---- few rows on a long axis: single tokens, short segments ----
+
+// A workgroup takes the at most 16 query rows of one segment and key/value head and a part of the keys; its four waves take 16 NT of them at a
+// time, in turn, each with a softmax of its own, and are joined at the end.  Keys go from memory straight into the layout of the matrix
+// instruction, values through a piece of LDS that is the wave's own, to be read along the keys; both are asked for one round ahead.  No
+// barrier but the last.  Bound by memory: every row of the ring is read once.
+template <int PREC, int DP> struct StepShape {
+    static constexpr int NT = PREC == IDF_PREC_BF16 ? 2 : 1;                  // tiles of 16 keys
+    static constexpr int KEYS = 16 * NT;
+    static constexpr int STRIDE = DP + (PREC == IDF_PREC_BF16 ? 16 : 4);      // of a row of values in LDS: rows that are read together begin in banks of their own
+    static constexpr int ROW16 = DP / Elem<PREC>::VL;                         // pieces of 16 bytes in a row
+    static constexpr int LOADS = KEYS * ROW16 / 64;
+    static constexpr int WAVE_FLOATS = 16 * DP > KEYS * STRIDE / (4 / (int)sizeof(typename Elem<PREC>::type)) ? 16 * DP : KEYS * STRIDE / (4 / (int)sizeof(typename Elem<PREC>::type));
+};
+
+template <int PREC, int DP>
+__global__ void __launch_bounds__(256) k_window_step(idf_window_args a, int splits, bool append)
+{
+    using M = Mfma<PREC>;
+    using T = typename M::T;
+    using S = StepShape<PREC, DP>;
+    constexpr int NT = S::NT, KS = DP / 32, DT = DP / 16;
+    __shared__ __align__(16) float lds[4 * S::WAVE_FLOATS];
+    __shared__ float stats[2][4][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+    const int split = blockIdx.x, kv = blockIdx.y, group = a.heads_q / a.heads_kv;
+    const Segment g = segment_of(a, blockIdx.z, a.starts);
+    if (g.len == 0) return;
+    const int rows = min(g.len * group, kStepRows);
+    const Keys keys = keys_of(a, g, g.start, g.start + g.len - 1);
+    const Held<T> kh(a, g, a.k, a.k_ring, kv), vh(a, g, a.v, a.v_ring, kv);
+    const Partial part = partial_of(a, splits);
+
+    // this split's entries, whole tiles of them; the waves take them in turn
+    const int tiles = (keys.n + S::KEYS - 1) / S::KEYS, per = (tiles + splits - 1) / splits;
+    const int t0 = split * per, t1 = min(tiles, t0 + per);
+    const int my_t = col / group;                                             // the query row of this lane
+    const int my_h = kv * group + col - my_t * group;
+    const int64_t p = g.start + min(my_t, g.len - 1);
+    const int hi = (int)(p - keys.shift);
+    const int lo = (int)max(p - a.window - keys.shift, (int64_t)-1);
+    const float scale = a.scale * kLog2e;
+
+    typename M::frag q[KS];
+    {
+        const T *src = (const T *)a.q.base + (g.begin + my_t) * a.q.token_stride + my_h * a.q.head_stride;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) o[c] *= fade;
-            for (int j = 0; j < 64 && i0 + j < n; ++j) {
-                const int64_t i = i0 + j, pos = i < n_first ? skip + i : low + i - n_first;
-                const T *v = held_row<T>(a, g, pos, a.v, a.v_ring, kv);
-                const float wj = __shfl(w, j);
+        for (int s = 0; s < KS; ++s) q[s] = col < rows && 32 * s + 8 * grp < a.head_dim ? M::load(src + 32 * s + 8 * grp) : M::zero();
+    }
+
+    T *v_lds = (T *)(lds + wave * S::WAVE_FLOATS);
+    typename M::frag kf[NT][KS];
+    i32x4 vf[S::LOADS];
+    auto load = [&](int tile) IDF_INLINE {
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (lane + 64 * c < a.head_dim) o[c] += wj * E::to_f32(v[lane + 64 * c]);
+        for (int t = 0; t < NT; ++t) {
+            const T *src = at(kh, place_of(a, keys, min(tile * S::KEYS + 16 * t + col, keys.n - 1)));
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kf[t][s] = 32 * s + 8 * grp < a.head_dim ? M::load(src + 32 * s + 8 * grp) : M::zero();
+        }
+#pragma unroll
+        for (int j = 0; j < S::LOADS; ++j) {
+            const int piece = j * 64 + lane, r = piece / S::ROW16, c = (piece - r * S::ROW16) * M::VL, i = tile * S::KEYS + r;
+            vf[j] = i < keys.n && c < a.head_dim ? *(const i32x4 *)(at(vh, place_of(a, keys, i)) + c) : i32x4{0, 0, 0, 0};
+        }
+    };
+
+    f32x4 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -__FLT_MAX__, l = 0.f;
+    if (t0 + wave < t1) load(t0 + wave);
+    for (int tile = t0 + wave; tile < t1; tile += 4) {
+        f32x4 st[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            st[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) st[t] = M::mma16(kf[t][s], q[s], st[t]);
+        }
+        __builtin_amdgcn_wave_barrier();                                      // (LDS serves a wave in order: only the compiler has to keep it)
+#pragma unroll
+        for (int j = 0; j < S::LOADS; ++j) {
+            const int piece = j * 64 + lane, r = piece / S::ROW16, c = (piece - r * S::ROW16) * M::VL;
+            *(i32x4 *)(v_lds + r * S::STRIDE + c) = vf[j];
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (tile + 4 < t1) load(tile + 4);
+
+        float w[NT * 4], top = m;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = tile * S::KEYS + 16 * t + 4 * grp + e;
+                const bool seen = i <= hi && (i > lo || i < keys.n_first);
+                w[4 * t + e] = seen ? st[t][e] * scale : -__builtin_inff();
+                top = fmaxf(top, w[4 * t + e]);
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__ballot(top > m)) {
+            const float fade = __builtin_amdgcn_exp2f(m - top);
+            l *= fade;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= fade;
+            m = top;
+        }
+#pragma unroll
+        for (int e = 0; e < NT * 4; ++e) { w[e] = __builtin_amdgcn_exp2f(w[e] - m); l += w[e]; }
+        if constexpr (PREC == IDF_PREC_BF16) {
+            const bf16x8 pf = M::pack(w);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = M::mma16(read_column(v_lds, S::STRIDE, 16 * d, 4 * grp, 16 + 4 * grp), pf, o[d]);
+        } else {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v_lds[(4 * grp + e) * S::STRIDE + 16 * d + col], w[e], o[d], 0, 0, 0);
+        }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+
+    // the waves' rows joined: [wave][row][value]
+    __builtin_amdgcn_wave_barrier();
+    float *mine = lds + wave * S::WAVE_FLOATS;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *(f32x4 *)(mine + col * DP + 16 * d + 4 * grp) = o[d];
+    if (grp == 0) { stats[0][wave][col] = m; stats[1][wave][col] = l; }
+    __syncthreads();
+    bool bad = false;
+    constexpr int V4 = DP / 4;
+    for (int x = threadIdx.x; x < rows * V4; x += 256) {
+        const int r = x / V4, c = (x - r * V4) * 4;
+        float top = -__FLT_MAX__, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, stats[0][w][r]);
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float fade = __builtin_amdgcn_exp2f(stats[0][w][r] - top);
+            sum += fade * stats[1][w][r];
+            v += fade * *(const f32x4 *)(lds + w * S::WAVE_FLOATS + r * DP + c);
+        }
+        if (c >= a.head_dim) continue;
+        const int t = r / group, h = kv * group + r - t * group;
+        const int64_t token = g.begin + t;
+        const f32x4 none = v * 0.f;
+        bad |= !(none[0] + none[1] + none[2] + none[3] == 0.f);
+        if (splits > 1) {
+            const int64_t row = ((int64_t)split * a.n_tokens + token) * a.heads_q + h;
+            *(f32x4 *)(part.o + row * a.head_dim + c) = v;
+            if (c == 0) { part.ml[2 * row] = top; part.ml[2 * row + 1] = sum; }
+        } else {
+            Pack<T, 4> out;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out.v[e] = Elem<PREC>::from_f32(v[e] / sum);
+            *(Pack<T, 4> *)((T *)a.out.base + token * a.out.token_stride + h * a.out.head_stride + c) = out;
+        }
+    }
+    if (g.len > 1 && __syncthreads_or(bad))                                   // (a single token sees every key of its list)
+        for (int r = wave; r < rows; r += 4) {
+            const int t = r / group;
+            exact_row<PREC>(a, g, keys, kv, kv * group + r - t * group, t, t0 * S::KEYS, min(t1 * S::KEYS, keys.n), part, split);
+        }
+    // a single token into the ring: the slot that it takes held a token that no query sees any more
+    if (append && split == 0) {
+        const int64_t p = g.start, slot = p < a.sinks ? p : a.sinks + (p - a.sinks) % (int64_t)keys.period;
+        for (int c = threadIdx.x * M::VL; c < a.head_dim; c += 256 * M::VL) {
+            *(i32x4 *)(const_cast<T *>(kh.ring) + slot * kh.ring_stride + c) = *(const i32x4 *)(kh.own + c);
+            *(i32x4 *)(const_cast<T *>(vh.ring) + slot * vh.ring_stride + c) = *(const i32x4 *)(vh.own + c);
+        }
+    }
+}
+
+// ---- many rows ----
+
+// A workgroup takes 128 query rows of one segment and key/value head and walks over their keys; a wave has 32 of the rows.  Keys and values of a round
+// go through registers into LDS, the next round's being asked for while this one's are worked on.
+template <int PREC, int DP> struct TileShape {
+    static constexpr int KEYS = PREC == IDF_PREC_BF16 ? 64 : 32;
+    static constexpr int VL = Elem<PREC>::VL, ROW16 = DP / VL;
+    static constexpr int K_STRIDE = DP + VL;                                  // neighbouring rows begin 16 bytes apart in the banks
+    static constexpr int V_STRIDE = DP + (PREC == IDF_PREC_BF16 ? 16 : 4);
+    static constexpr int LOADS = (KEYS * ROW16 + 255) / 256;
+    static constexpr bool AHEAD = DP <= 128;                                  // (longer rows leave no registers for a round on its way)
+    static constexpr int LDS_BYTES = KEYS * (K_STRIDE + V_STRIDE) * (int)sizeof(typename Elem<PREC>::type);
+};
+
+template <int PREC, int DP>
+__global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 1) k_window_tile(idf_window_args a, int splits)
+{
+    using M = Mfma<PREC>;
+    using T = typename M::T;
+    using S = TileShape<PREC, DP>;
+    constexpr int KT = S::KEYS / 32, KS = DP / 16, DT = DP / 32;
+    extern __shared__ __align__(16) unsigned char raw[];
+    T *k_lds = (T *)raw, *v_lds = k_lds + S::KEYS * S::K_STRIDE;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int group = a.heads_q / a.heads_kv;
+    const int kv = blockIdx.x % a.heads_kv, seg = blockIdx.x / a.heads_kv;
+    const int split = blockIdx.z, tile = gridDim.y - 1 - blockIdx.y;          // long lists first
+    const Segment g = segment_of(a, seg, a.starts);
+    const int64_t rows = (int64_t)g.len * group, row0 = (int64_t)tile * kTileRows;
+    if (row0 >= rows) return;
+    const int64_t row_last = min(row0 + kTileRows, rows) - 1;
+    const Keys keys = keys_of(a, g, g.start + row0 / group, g.start + row_last / group);
+    const Held<T> kh(a, g, a.k, a.k_ring, kv), vh(a, g, a.v, a.v_ring, kv);
+    const Partial part = partial_of(a, splits);
+    const int rounds = (keys.n + S::KEYS - 1) / S::KEYS, per = (rounds + splits - 1) / splits;
+    const int t0 = split * per, t1 = min(rounds, t0 + per);
+
+    const int64_t my_row = row0 + wave * 32 + col;
+    const bool on = my_row < rows;
+    const int my_t = (int)(min(my_row, rows - 1) / group), my_h = kv * group + (int)(min(my_row, rows - 1) - (int64_t)my_t * group);
+    const int64_t p = g.start + my_t, token = g.begin + my_t;
+    const int hi = (int)(p - keys.shift);
+    const int lo = (int)max(p - a.window - keys.shift, (int64_t)-1);
+    const float scale = a.scale * kLog2e;
+    // what all rows of the wave see without a look at the mask
+    const int hi_all = (int)(g.start + min(row0 + wave * 32, rows - 1) / group - keys.shift);
+    const int lo_all = (int)max(g.start + min(row0 + wave * 32 + 31, rows - 1) / group - a.window - keys.shift, (int64_t)-1);
+
+    typename M::frag q[KS];
+    {
+        const T *src = (const T *)a.q.base + token * a.q.token_stride + my_h * a.q.head_stride;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = 16 * s + 8 * half < a.head_dim ? M::load(src + 16 * s + 8 * half) : M::zero();
+    }
+    i32x4 kr[S::LOADS], vr[S::LOADS];
+    auto load = [&](int t) IDF_INLINE {
+#pragma unroll
+        for (int j = 0; j < S::LOADS; ++j) {
+            const int piece = j * 256 + threadIdx.x, r = piece / S::ROW16, c = (piece - r * S::ROW16) * M::VL, i = t * S::KEYS + r;
+            const bool there = r < S::KEYS && i < keys.n && c < a.head_dim;
+            const Place pl = place_of(a, keys, min(i, keys.n - 1));
+            kr[j] = there ? *(const i32x4 *)(at(kh, pl) + c) : i32x4{0, 0, 0, 0};
+            vr[j] = there ? *(const i32x4 *)(at(vh, pl) + c) : i32x4{0, 0, 0, 0};
+        }
+    };
+    f32x16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    float m = -__FLT_MAX__, l = 0.f;
+    if (S::AHEAD && t0 < t1) load(t0);
+    for (int t = t0; t < t1; ++t) {
+        if (!S::AHEAD) load(t);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < S::LOADS; ++j) {
+            const int piece = j * 256 + threadIdx.x, r = piece / S::ROW16, c = (piece - r * S::ROW16) * M::VL;
+            if (S::KEYS * S::ROW16 % 256 && r >= S::KEYS) continue;
+            *(i32x4 *)(k_lds + r * S::K_STRIDE + c) = kr[j];
+            *(i32x4 *)(v_lds + r * S::V_STRIDE + c) = vr[j];
+        }
+        __syncthreads();
+        if (S::AHEAD && t + 1 < t1) load(t + 1);
+
+        f32x16 st[KT];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) st[kt][e] = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) st[kt] = M::mma32(M::load(k_lds + (32 * kt + col) * S::K_STRIDE + 16 * s + 8 * half), q[s], st[kt]);
+        }
+        const int i0 = t * S::KEYS;
+        if (!(i0 + S::KEYS - 1 <= hi_all && (i0 > lo_all || i0 + S::KEYS <= keys.n_first))) {
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int i = i0 + 32 * kt + 8 * (e / 4) + 4 * half + e % 4;
+                    if (!(i <= hi && (i > lo || i < keys.n_first))) st[kt][e] = -__builtin_inff();
+                }
+        }
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, st[kt][e]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        top = fmaxf(m, top * scale);
+        if (__ballot(top > m)) {
+            const float fade = __builtin_amdgcn_exp2f(m - top);
+            l *= fade;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= fade;
+            m = top;
+        }
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                st[kt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][e], scale, -m));
+                l += st[kt][e];
+            }
+#pragma unroll
+        for (int s = 0; s < 2 * KT; ++s) {
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = st[s / 2][8 * (s % 2) + e];
+            const typename M::frag pf = M::pack(w);
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+                o[d] = M::mma32(read_column(v_lds, S::V_STRIDE, 32 * d + (lane & 16), 16 * s + 4 * half, 16 * s + 8 + 4 * half), pf, o[d]);
+        }
+    }
+    l += __shfl_xor(l, 32);
+
+    float none = 0.f;
+    T *out = (T *)a.out.base + token * a.out.token_stride + my_h * a.out.head_stride;
+    const int64_t prow = ((int64_t)split * a.n_tokens + token) * a.heads_q + my_h;
+    const float r = 1.f / l;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const int c = 32 * d + 2 * e + 4 * half;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) none += o[d][e + x] * 0.f;
+            if (!on || c >= a.head_dim) continue;
+            if (splits > 1) {
+                *(f32x4 *)(part.o + prow * a.head_dim + c) = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
+            } else {
+                Pack<T, 4> w;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) w.v[x] = Elem<PREC>::from_f32(o[d][e + x] * r);
+                *(Pack<T, 4> *)(out + c) = w;
             }
         }
-        T *out = (T *)a.out.base + (g.begin + t) * a.out.token_stride + h * a.out.head_stride;
+    if (splits > 1 && on && half == 0) { part.ml[2 * prow] = m; part.ml[2 * prow + 1] = l; }
+    if (__ballot(!(none == 0.f)))
+        for (int x = 0; x < 32 && row0 + wave * 32 + x < rows; ++x) {
+            const int64_t row = row0 + wave * 32 + x;
+            const int t = (int)(row / group);
+            exact_row<PREC>(a, g, keys, kv, kv * group + (int)(row - (int64_t)t * group), t, t0 * S::KEYS, min(t1 * S::KEYS, keys.n), part, split);
+        }
+}
+
+// Splits joined: four values of a row by a thread.
+template <int PREC>
+__global__ void __launch_bounds__(256) k_window_join(idf_window_args a, int splits)
+{
+    using T = typename Elem<PREC>::type;
+    const Segment g = segment_of(a, blockIdx.y, a.starts);
+    const Partial part = partial_of(a, splits);
+    const int per_row = a.head_dim / 4;
+    const int64_t n = (int64_t)g.len * a.heads_q * per_row, step = a.n_tokens * a.heads_q;
+    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < n; x += (int64_t)gridDim.x * 256) {
+        const int64_t r = x / per_row, t = r / a.heads_q, token = g.begin + t;
+        const int c = (int)(x - r * per_row) * 4, h = (int)(r - t * a.heads_q);
+        const int64_t row = token * a.heads_q + h;
+        float top = -__FLT_MAX__, l = 0.f;
+        for (int s = 0; s < splits; ++s) top = fmaxf(top, part.ml[2 * (row + s * step)]);
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < splits; ++s) {
+            const float fade = __builtin_amdgcn_exp2f(part.ml[2 * (row + s * step)] - top);
+            l += fade * part.ml[2 * (row + s * step) + 1];
+            v += fade * *(const f32x4 *)(part.o + (row + s * step) * a.head_dim + c);
+        }
+        Pack<T, 4> w;
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (lane + 64 * c < a.head_dim) out[lane + 64 * c] = E::from_f32(o[c] / l);
+        for (int e = 0; e < 4; ++e) w.v[e] = Elem<PREC>::from_f32(v[e] / l);
+        *(Pack<T, 4> *)((T *)a.out.base + token * a.out.token_stride + h * a.out.head_stride + c) = w;
     }
 }
 
@@ -80,21 +532,61 @@ __global__ void __launch_bounds__(256) k_window_append(idf_window_args a, int ro
     }
 }
 
+// How a call is cut: which kernel, and into how many parts the keys go.
+struct Plan { bool step; int tiles, splits; };
+Plan plan_of(const idf_window_args &a)
+{
+    Plan p;
+    const int64_t rows = a.max_tokens * (a.heads_q / a.heads_kv);
+    p.step = rows <= kStepRows;
+    p.tiles = p.step ? 1 : (int)((rows + kTileRows - 1) / kTileRows);
+    const int64_t pairs = (int64_t)a.n_segments * a.heads_kv * p.tiles;
+    const int64_t keys = (a.k_ring ? std::min<int64_t>(a.window, a.slots) : 0) + a.sinks + std::min<int64_t>(a.max_tokens, a.window);
+    // two workgroups for every compute unit, and some rounds of keys for each of them
+    const int64_t least = p.step ? 256 : 512;
+    p.splits = (int)std::max<int64_t>(1, std::min((512 + pairs - 1) / pairs, keys / least));
+    if (pairs >= 384) p.splits = 1;
+    return p;
+}
+
+template <int PREC, int DP>
+hipError_t attend(const idf_window_args &a, const Plan &p, const LaunchCtx &lc)
+{
+    if (p.step)
+        return launch(k_window_step<PREC, DP>, dim3(p.splits, a.heads_kv, a.n_segments), dim3(256), 0, lc, a, p.splits, a.k_ring && a.max_tokens == 1);
+    constexpr int bytes = TileShape<PREC, DP>::LDS_BYTES;
+    if (bytes > 65536)
+        if (const hipError_t e = allow_lds<bytes>(Kernel<k_window_tile<PREC, DP>>{})) return e;
+    return launch(k_window_tile<PREC, DP>, dim3(a.n_segments * a.heads_kv, p.tiles, p.splits), dim3(256), bytes, lc, a, p.splits);
+}
+
+template <int PREC>
+hipError_t by_dim(const idf_window_args &a, const LaunchCtx &lc)
+{
+    const Plan p = plan_of(a);
+    hipError_t e = a.head_dim <= 64 ? attend<PREC, 64>(a, p, lc) : a.head_dim <= 96 ? attend<PREC, 96>(a, p, lc) : a.head_dim <= 128 ? attend<PREC, 128>(a, p, lc) : attend<PREC, 256>(a, p, lc);
+    if (e == hipSuccess && p.splits > 1) {
+        const int64_t n = a.max_tokens * a.heads_q * (a.head_dim / 4);
+        e = launch(k_window_join<PREC>, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 4096), a.n_segments), dim3(256), 0, lc, a, p.splits);
+    }
+    if (e == hipSuccess && a.k_ring && !(p.step && a.max_tokens == 1)) {
+        const int elem16 = Elem<PREC>::VL, row16 = a.heads_kv * a.head_dim / elem16;
+        e = launch(k_window_append, dim3((unsigned)std::min<int64_t>((a.max_tokens * row16 + 255) / 256, 4096), a.n_segments), dim3(256), 0, lc, a, row16, elem16);
+    }
+    return e;
+}
+
 }  // namespace
 
-size_t window_workspace(const idf_window_args &) { return 0; }
+size_t window_workspace(const idf_window_args &a)
+{
+    const Plan p = plan_of(a);
+    return p.splits > 1 ? (size_t)p.splits * a.n_tokens * a.heads_q * (a.head_dim + 2) * sizeof(float) : 0;
+}
 
 hipError_t launch_window(const idf_window_args &a, const LaunchCtx &lc)
 {
-    const dim3 grid((unsigned)std::min<int64_t>(a.max_tokens, 16384), a.heads_q, a.n_segments);
-    hipError_t e = a.precision == IDF_PREC_F32 ? launch(k_window_rows<IDF_PREC_F32>, grid, dim3(64), 0, lc, a)
-                                               : launch(k_window_rows<IDF_PREC_BF16>, grid, dim3(64), 0, lc, a);
-    if (e == hipSuccess && a.k_ring) {
-        const int elem16 = a.precision == IDF_PREC_F32 ? 4 : 8, row16 = a.heads_kv * a.head_dim / elem16;
-        const dim3 g((unsigned)std::min<int64_t>((a.max_tokens * row16 + 255) / 256, 4096), a.n_segments);
-        e = launch(k_window_append, g, dim3(256), 0, lc, a, row16, elem16);
-    }
-    return e;
+    return a.precision == IDF_PREC_F32 ? by_dim<IDF_PREC_F32>(a, lc) : by_dim<IDF_PREC_BF16>(a, lc);
 }
 
 }  // namespace idf

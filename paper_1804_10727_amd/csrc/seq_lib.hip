@@ -11,6 +11,9 @@ namespace {
 
 constexpr int kMostSegments = 65535;               // a launch's second or third axis
 constexpr int kMostHeads = 1024;
+constexpr int64_t kMostPairs = 1 << 23;            // segments times key/value heads: a launch's first axis
+constexpr int64_t kMostRows = 65535 * 128;         // query rows of a segment and key/value head: its second
+constexpr int64_t kMostSlots = 1 << 30;            // lists of keys are counted in 32 bits
 
 bool precision_ok(int p) { return p == IDF_PREC_F32 || p == IDF_PREC_BF16; }
 
@@ -37,6 +40,8 @@ int check_segments(const Args &a)
     if (a.n_segments > kMostSegments) return fail(IDF_EUNSUPPORTED, "%d segments: at most %d in a call", a.n_segments, kMostSegments);
     if (!a.offsets && (int64_t)a.n_segments * a.max_tokens != a.n_tokens)
         return fail(IDF_EINVAL, "%lld tokens are not %d segments of %lld", (long long)a.n_tokens, a.n_segments, (long long)a.max_tokens);
+    if ((int64_t)a.n_segments * a.heads_kv > kMostPairs || a.max_tokens * (a.heads_q / a.heads_kv) > kMostRows)
+        return fail(IDF_EUNSUPPORTED, "%d segments of up to %lld tokens with %d heads: more than a launch takes", a.n_segments, (long long)a.max_tokens, a.heads_q);
     if (!a.stream_ids && a.n_segments > a.n_streams) return fail(IDF_EINVAL, "%d segments of %d streams", a.n_segments, a.n_streams);
     if (!(a.scale > 0.f) || std::isinf(a.scale)) return fail(IDF_EINVAL, "scale %g", (double)a.scale);
     return IDF_OK;
@@ -51,7 +56,7 @@ int check_window(const idf_window_args *a)
     if (a->window < 1 || a->sinks < 0) return fail(IDF_EINVAL, "a window of %d tokens and %d first ones", a->window, a->sinks);
     if (!a->k_ring != !a->v_ring) return fail(IDF_EINVAL, "a ring of keys or values alone");
     if (a->k_ring) {
-        if (a->slots > INT_MAX || a->slots - a->sinks < a->window)
+        if (a->slots > kMostSlots || a->slots - a->sinks < a->window)
             return fail(IDF_EINVAL, "%lld slots for a window of %d tokens and %d first ones", (long long)a->slots, a->window, a->sinks);
         if (((uintptr_t)a->k_ring | (uintptr_t)a->v_ring) % 16) return fail(IDF_EUNSUPPORTED, "rings have to be 16-byte aligned");
     }
