@@ -2,7 +2,7 @@
 #include <algorithm>
 
 #include "idf.h"
-#include "seq_common.h"
+#include "seq_mfma.h"
 
 namespace idf {
 
@@ -74,6 +74,311 @@ __global__ void __launch_bounds__(256) k_decay_tokens(idf_decay_args a, int colu
             if (r0 + r < a.dim_k) *(f32x4 *)(a.state_out + state + (int64_t)(r0 + r) * a.dim_v + c0) = s[r];
 }
 
+// ---- segments of many tokens, 32 at a time ----
+
+// With S the state before a chunk of L <= 32 tokens, i and j tokens of it:
+//   O_i = lambda^(i+1) q_i S + sum_{j<=i} lambda^(i-j) (q_i . k_j) v_j,     S' = lambda^L S + sum_j k_j^T (lambda^(L-1-j) v_j),
+// matrix products throughout, no power of the decay above one.  A wave owns 32 columns of the state, in accumulators; scores are formed
+// transposed, K Q^T, by every wave for itself, so that what comes out is an operand of the next product; so is the state.  Keys and values
+// go through LDS, to be read along the tokens too, the next chunk's asked for while this one's are worked on.
+//   Roundings in bfloat16: scores times decay, and the state where it meets the queries, are rounded to bfloat16 (half a step of 2^-8, as the
+// output is).  The state itself stays float32: a decayed value, 24 bits, goes into the product as three bfloat16 numbers that add up to it.
+//   Bound by memory: q, k, v and out once, k and v twice where a segment is cut into parts.
+constexpr int kChunk = 32;
+constexpr int kPartLeast = 256;                    // tokens of a part of a segment, at least
+
+// Segments cut into parts along time, so that there is work for every compute unit: the state that each part leaves if it begins with none,
+// then the states that the parts begin with, then the parts themselves.
+struct Parts {
+    int n, tokens;             // parts of the longest segment, tokens of a part (a multiple of the chunk)
+    float *states;             // [segment][head][part][dim_k][dim_v]; nullptr for one part
+};
+
+__device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
+__device__ __forceinline__ float log2_of(float log_decay) { return fmaxf(log_decay * 1.4426950408889634f, -1e30f); }      // (a decay to nothing: times zero stays zero)
+
+template <int PREC, int DK, int NW>
+__global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 && NW == 4) ? 2 : 1) k_decay_chunks(idf_decay_args a, Parts parts, bool states_only, int blocks)
+{
+    using M = Mfma<PREC>;
+    using E = Elem<PREC>;
+    using T = typename M::T;
+    using frag = typename M::frag;
+    constexpr int KS = DK / 16, KT = DK / 32, VL = M::VL, THREADS = 64 * NW;
+    constexpr int K_STRIDE = DK + VL, V_STRIDE = 32 * NW + (PREC == IDF_PREC_BF16 ? 16 : 4);
+    constexpr int K_LOADS = kChunk * DK / VL / THREADS, V_LOADS = kChunk * 32 / VL / 64;
+    constexpr int BF = PREC == IDF_PREC_BF16;
+    constexpr int SCORE_STRIDE = kChunk + 4;
+    __shared__ __align__(16) T k_lds[kChunk * K_STRIDE], v_lds[kChunk * V_STRIDE];
+    __shared__ __align__(16) float score[kChunk * SCORE_STRIDE], fresh[2 * kChunk];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int part = gridDim.y - 1 - blockIdx.y;   // (the parts whose keys and values were read last are the first to be read again)
+    const int block = blockIdx.x % blocks, kv = blockIdx.x / blocks % a.heads_kv, seg = blockIdx.x / blocks / a.heads_kv;
+    const Segment g = segment_of(a, seg, nullptr);
+    const int first = part * parts.tokens;
+    const int len = min(g.len - first, parts.tokens);
+    const bool last = first + parts.tokens >= g.len;                          // the state behind this part is the segment's
+    if (!g.valid || (len <= 0 && part > 0) || (states_only && last)) return;
+    const int queries = a.heads_q / a.heads_kv;
+    const int c0 = block * 32 * NW;                                           // the workgroup's first column
+    const float l2 = log2_of(a.log_decay[kv]);
+    const bool own = c0 + 32 * wave + col < a.dim_v;
+
+    // row e of a state's tile: 16 (e / 8) + 8 half + e % 8, so that eight registers are eight rows in order
+    f32x16 s[KT];
+    const int64_t state = ((int64_t)g.ring * a.heads_kv + kv) * a.dim_k * a.dim_v;
+    float *mid = parts.states ? parts.states + ((int64_t)(seg * a.heads_kv + kv) * parts.n + part) * a.dim_k * a.dim_v : nullptr;
+    const float *from = states_only ? nullptr : mid ? mid : a.state_in ? a.state_in + state : nullptr;
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+    if (from && own)
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = 32 * t + 16 * (e / 8) + 8 * half + e % 8;
+                const float x = from[min(r, a.dim_k - 1) * a.dim_v + c0 + 32 * wave + col];
+                s[t][e] = r < a.dim_k ? x : 0.f;
+            }
+
+    // powers of the decay, by way of LDS: scale * lambda^(i-j) between tokens of a chunk, and what a token leaves at a whole chunk's end
+    for (int x = threadIdx.x; x < kChunk * kChunk; x += THREADS) {
+        const int i = x / kChunk, j = x % kChunk;
+        score[i * SCORE_STRIDE + j] = i >= j ? __builtin_amdgcn_exp2f((float)(i - j) * l2) * a.scale : 0.f;
+        if (i == 0) { fresh[j] = __builtin_amdgcn_exp2f((float)(kChunk - 1 - j) * l2); fresh[kChunk + j] = 0.f; }
+    }
+    const float faded = __builtin_amdgcn_exp2f((float)(col + 1) * l2) * a.scale;
+    // the decay of a whole chunk in two parts: it is applied again and again, and its own rounding would add up
+    // (the last chunk of the part may be a short one)
+    float keep[2], keep_low[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const double power = exp2((double)(x ? (len - 1) % kChunk + 1 : kChunk) * (double)l2);
+        keep[x] = uniform((float)power);
+        keep_low[x] = uniform((float)(power - (double)keep[x]));
+    }
+
+    const T *kb = (const T *)a.k.base + (g.begin + first) * a.k.token_stride + kv * a.k.head_stride;
+    const T *vb = (const T *)a.v.base + (g.begin + first) * a.v.token_stride + kv * a.v.head_stride;
+    i32x4 kr[K_LOADS], vr[V_LOADS];
+    auto load = [&](int t0) IDF_INLINE {
+#pragma unroll
+        for (int x = 0; x < K_LOADS; ++x) {
+            const int piece = x * THREADS + threadIdx.x, r = piece / (DK / VL), c = (piece - r * (DK / VL)) * VL;
+            kr[x] = t0 + r < len && c < a.dim_k ? *(const i32x4 *)(kb + (int64_t)(t0 + r) * a.k.token_stride + c) : i32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int x = 0; x < V_LOADS; ++x) {
+            const int piece = x * THREADS + threadIdx.x, r = piece / (32 * NW / VL), c = (piece - r * (32 * NW / VL)) * VL;
+            vr[x] = t0 + r < len && c0 + c < a.dim_v ? *(const i32x4 *)(vb + (int64_t)(t0 + r) * a.v.token_stride + c0 + c) : i32x4{0, 0, 0, 0};
+        }
+    };
+    if (len > 0) load(0);
+    for (int t0 = 0; t0 < len; t0 += kChunk) {
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < K_LOADS; ++x) {
+            const int piece = x * THREADS + threadIdx.x, r = piece / (DK / VL), c = (piece - r * (DK / VL)) * VL;
+            *(i32x4 *)(k_lds + r * K_STRIDE + c) = kr[x];
+        }
+#pragma unroll
+        for (int x = 0; x < V_LOADS; ++x) {
+            const int piece = x * THREADS + threadIdx.x, r = piece / (32 * NW / VL), c = (piece - r * (32 * NW / VL)) * VL;
+            *(i32x4 *)(v_lds + r * V_STRIDE + c) = vr[x];
+        }
+        __syncthreads();
+        const int n = min(kChunk, len - t0);
+        if (t0 + kChunk < len) load(t0 + kChunk);
+
+        // values of this wave's columns along the tokens: register x of piece p is token 16 p + 8 (x / 4) + 4 half + x % 4
+        frag v[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) v[p] = read_column(v_lds, V_STRIDE, 32 * wave + (lane & 16), 16 * p + 4 * half, 16 * p + 8 + 4 * half);
+
+        if (!states_only)
+            for (int h = kv * queries; h < (kv + 1) * queries; ++h) {
+                // a head's operands are formed in its turn: kept for the other heads of the group they would take the registers
+#pragma unroll
+                for (int t = 0; t < KT; ++t) asm volatile("" : "+v"(s[t])::"memory");
+                const int64_t token = g.begin + first + t0 + min(col, n - 1);
+                const T *qb = (const T *)a.q.base + token * a.q.token_stride + h * a.q.head_stride;
+                f32x16 w, o;
+                frag q[KS];
+#pragma unroll
+                for (int p = 0; p < KS; ++p) q[p] = 16 * p + 8 * half < a.dim_k ? M::load(qb + 16 * p + 8 * half) : M::zero();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) { w[e] = 0.f; o[e] = 0.f; }
+#pragma unroll
+                for (int p = 0; p < KS; ++p) {
+                    float sv[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sv[e] = s[p / 2][8 * (p % 2) + e];
+                    o = M::mma32(M::pack(sv), q[p], o);
+                    w = M::mma32(M::load(k_lds + col * K_STRIDE + 16 * p + 8 * half), q[p], w);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const f32x4 f = *(const f32x4 *)(score + col * SCORE_STRIDE + 2 * e + 4 * half);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) w[e + x] *= f[x];
+                }
+                o *= faded;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    float wv[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) wv[e] = w[8 * p + e];
+                    o = M::mma32(v[p], M::pack(wv), o);
+                }
+                float none = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) none += o[e] * 0.f;
+                if (__ballot(!(none == 0.f))) {
+                    // something infinite or not a number: a weight of zero times a later token's value is no zero then.  Once more, with the
+                    // tokens up to this one only
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = 0.f;
+#pragma unroll
+                    for (int p = 0; p < KS; ++p) {
+                        float sv[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sv[e] = s[p / 2][8 * (p % 2) + e];
+                        o = M::mma32(M::pack(sv), q[p], o);
+                    }
+                    o *= faded;
+#pragma unroll 1
+                    for (int j = 0; j < n; ++j) {
+                        float qk = 0.f;            // (a lane takes every other value, lane ^ 32 the ones between)
+#pragma unroll 1
+                        for (int d = half; d < a.dim_k; d += 2) qk += E::to_f32(qb[d]) * E::to_f32(k_lds[j * K_STRIDE + d]);
+                        qk += __shfl_xor(qk, 32);
+                        if (j > col) continue;
+                        qk *= __builtin_amdgcn_exp2f((float)(col - j) * l2) * a.scale;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] += qk * E::to_f32(v_lds[j * V_STRIDE + 32 * wave + 8 * (e / 4) + 4 * half + e % 4]);
+                    }
+                }
+                if (col < n) {
+                    T *out = (T *)a.out.base + token * a.out.token_stride + h * a.out.head_stride + c0 + 32 * wave + 4 * half;
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        Pack<T, 4> pk;
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) pk.v[x] = E::from_f32(o[e + x]);
+                        if (c0 + 32 * wave + 2 * e + 4 * half < a.dim_v) *(Pack<T, 4> *)(out + 2 * e) = pk;
+                    }
+                }
+            }
+
+        const float fade = n < kChunk ? keep[1] : keep[0], fade_low = n < kChunk ? keep_low[1] : keep_low[0];
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[t][e] = __builtin_fmaf(s[t][e], fade, s[t][e] * fade_low);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = E::to_f32(v[p][e]) * fresh[16 * p + 8 * (e / 4) + 4 * half + e % 4 + kChunk - n];
+            frag pieces[BF ? 3 : 1];
+            if constexpr (BF) {
+#pragma unroll
+                for (int y = 0; y < 3; ++y) {
+                    uint32_t u[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {  // the upper 16 bits, and what is left
+                        u[e] = __builtin_bit_cast(uint32_t, x[e]);
+                        x[e] -= __builtin_bit_cast(float, u[e] & 0xffff0000u);
+                    }
+                    i32x4 both;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) both[e] = (int)__builtin_amdgcn_perm(u[2 * e + 1], u[2 * e], 0x07060302u);
+                    pieces[y] = __builtin_bit_cast(frag, both);
+                }
+            } else {
+                pieces[0] = M::pack(x);
+            }
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                const frag k = read_rows_swapped(k_lds, K_STRIDE, 32 * t + (lane & 16), 16 * p + 4 * half, 16 * p + 8 + 4 * half);
+#pragma unroll
+                for (int y = 0; y < (BF ? 3 : 1); ++y) s[t] = M::mma32(k, pieces[y], s[t]);
+            }
+        }
+    }
+
+    float *to = states_only ? mid : last && a.state_out ? a.state_out + state : nullptr;
+    int row = 8 * half;
+    asm volatile("" : "+v"(row));                  // (places of the rows anew: kept from the beginning they would take the registers of the loop)
+    if (to && own)
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = 32 * t + 16 * (e / 8) + row + e % 8;
+                if (r < a.dim_k) to[r * a.dim_v + c0 + 32 * wave + col] = s[t][e];
+            }
+}
+
+// What each part begins with, in place of what it would leave by itself: in the order of the parts, four values by a thread.
+__global__ void __launch_bounds__(256) k_decay_scan(idf_decay_args a, Parts parts)
+{
+    const int kv = blockIdx.y % a.heads_kv, seg = blockIdx.y / a.heads_kv;
+    const int x = (blockIdx.x * 256 + threadIdx.x) * 4, size = a.dim_k * a.dim_v;
+    const Segment g = segment_of(a, seg, nullptr);
+    if (!g.valid || x >= size) return;
+    const int n = max(1, (g.len + parts.tokens - 1) / parts.tokens);
+    const float keep = (float)exp2((double)parts.tokens * (double)log2_of(a.log_decay[kv]));
+    float *at = parts.states + (int64_t)blockIdx.y * parts.n * size + x;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (a.state_in) s = *(const f32x4 *)(a.state_in + ((int64_t)g.ring * a.heads_kv + kv) * size + x);
+    for (int p = 0; p < n; ++p, at += size) {
+        f32x4 left = {0.f, 0.f, 0.f, 0.f};
+        if (p + 1 < n) left = *(const f32x4 *)at;
+        *(f32x4 *)at = s;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = __builtin_fmaf(s[e], keep, left[e]);
+    }
+}
+
+Parts parts_of(const idf_decay_args &a)
+{
+    Parts p;
+    p.states = nullptr;
+    const int64_t blocks = (int64_t)a.n_segments * a.heads_kv * ((a.dim_v + 127) / 128);
+    // two workgroups for every compute unit; a part is long next to the state that it reads and writes
+    const int64_t want = std::max<int64_t>(1, std::min((512 + blocks - 1) / blocks, a.max_tokens / kPartLeast));
+    p.tokens = (int)(((a.max_tokens + want - 1) / want + kChunk - 1) / kChunk * kChunk);
+    p.n = (int)((a.max_tokens + p.tokens - 1) / std::max(p.tokens, 1));
+    if (p.n <= 1) { p.n = 1; p.tokens = std::max(p.tokens, kChunk); }
+    return p;
+}
+
+// Rows of more than 128 values leave no registers for anything beside the state: they go token by token, whatever the length.
+bool by_token(const idf_decay_args &a) { return a.max_tokens <= 16 || a.dim_k > 128; }
+
+template <int PREC, int DK>
+hipError_t chunks(const idf_decay_args &a, const LaunchCtx &lc)
+{
+    Parts p = parts_of(a);
+    const int waves = a.dim_v <= 64 ? 2 : 4, blocks = (a.dim_v + 32 * waves - 1) / (32 * waves);
+    const dim3 grid((unsigned)((int64_t)a.n_segments * a.heads_kv * blocks), p.n);
+    auto go = [&](bool states_only) {
+        return waves == 2 ? launch(k_decay_chunks<PREC, DK, 2>, grid, dim3(128), 0, lc, a, p, states_only, blocks)
+                          : launch(k_decay_chunks<PREC, DK, 4>, grid, dim3(256), 0, lc, a, p, states_only, blocks);
+    };
+    hipError_t e = hipSuccess;
+    if (p.n > 1) {
+        p.states = (float *)a.workspace;
+        e = go(true);
+        if (e == hipSuccess)
+            e = launch(k_decay_scan, dim3((unsigned)((a.dim_k * a.dim_v + 1023) / 1024), a.n_segments * a.heads_kv), dim3(256), 0, lc, a, p);
+    }
+    return e == hipSuccess ? go(false) : e;
+}
+
 template <int PREC>
 hipError_t tokens(const idf_decay_args &a, const LaunchCtx &lc)
 {
@@ -84,13 +389,24 @@ hipError_t tokens(const idf_decay_args &a, const LaunchCtx &lc)
     return launch(k_decay_tokens<PREC, 32>, grid, dim3(256), 0, lc, a, column_groups);
 }
 
+template <int PREC>
+hipError_t by_shape(const idf_decay_args &a, const LaunchCtx &lc)
+{
+    if (by_token(a)) return tokens<PREC>(a, lc);
+    return a.dim_k <= 64 ? chunks<PREC, 64>(a, lc) : chunks<PREC, 128>(a, lc);
+}
+
 }  // namespace
 
-size_t decay_workspace(const idf_decay_args &) { return 0; }
+size_t decay_workspace(const idf_decay_args &a)
+{
+    const Parts p = parts_of(a);
+    return !by_token(a) && p.n > 1 ? (size_t)a.n_segments * a.heads_kv * p.n * a.dim_k * a.dim_v * sizeof(float) : 0;
+}
 
 hipError_t launch_decay(const idf_decay_args &a, const LaunchCtx &lc)
 {
-    return a.precision == IDF_PREC_F32 ? tokens<IDF_PREC_F32>(a, lc) : tokens<IDF_PREC_BF16>(a, lc);
+    return a.precision == IDF_PREC_F32 ? by_shape<IDF_PREC_F32>(a, lc) : by_shape<IDF_PREC_BF16>(a, lc);
 }
 
 }  // namespace idf

@@ -85,6 +85,26 @@ __device__ __forceinline__ f32x8 read_column(const float *lds, int stride, int c
     return f;
 }
 
+// The same with columns c + 4 .. c + 7 and c + 8 .. c + 11 of each 16 in each other's place: as rows of a 32 x 32 product they put eight
+// columns in order into a lane's registers.
+__device__ __forceinline__ bf16x8 read_rows_swapped(const __bf16 *lds, int stride, int c, int r0, int r1)
+{
+    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+    const int lane = threadIdx.x & 15, x = lane & 3, at = (lane >> 2) * stride + c + ((x & 1) << 3 | (x & 2) << 1);
+    const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(lds + r0 * stride + at));
+    const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(lds + r1 * stride + at));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+__device__ __forceinline__ f32x8 read_rows_swapped(const float *lds, int stride, int c, int r0, int r1)
+{
+    const int lane = threadIdx.x & 15, x = lane >> 2;
+    const float *at = lds + c + ((x & 1) << 3 | (x & 2) << 1 | (lane & 3));
+    f32x8 f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[i] = at[(r0 + i) * stride]; f[4 + i] = at[(r1 + i) * stride]; }
+    return f;
+}
+
 }  // namespace
 
 }  // namespace idf
