@@ -9,6 +9,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 _push = None                 # idf_push_segment on a tensor (csrc/push.cpp)
+_token_ops = None            # the operators that mix tokens, on tensors (csrc/tokens.cpp)
 
 IDF_OK, IDF_EINVAL, IDF_ENOMEM, IDF_ESTATE, IDF_EDEVICE, IDF_EUNSUPPORTED = 0, -1, -2, -3, -4, -5
 PREC = {"f32": 0, "bf16": 1, "i8": 2}
@@ -128,25 +129,45 @@ def load_library():
     return L
 
 
+def _load_extension(stem, path, build):
+    """An extension module, which needs torch's libraries in the process.  Built first, it alone, if this interpreter's and this torch's is
+    not there."""
+    import importlib.util
+    import sys
+    if not os.path.exists(path):
+        build()
+    name = f"{__package__}.{stem}"
+    spec = importlib.util.spec_from_file_location(name, path)
+    native = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(native)
+    sys.modules[name] = native
+    setattr(sys.modules[__package__], stem, native)
+    return native
+
+
 def load_push():
-    """Load the extension module of push.cpp, which needs torch's libraries in the process: with the first streams, whose pushes go through
-    it.  Built first, it alone, if this interpreter's and this torch's is not there."""
+    """The way of a push into the library: loaded with the first streams, whose pushes go through it."""
     global _push
     if _push is None:
         L = load_library()
-        import importlib.util
-        import sys
         from . import build as _build
-        path, name = _build.push_path(), __package__ + "._push"
-        if not os.path.exists(path):
-            _build.build_push()
-        spec = importlib.util.spec_from_file_location(name, path)
-        native = importlib.util.module_from_spec(spec)
-        spec.loader.exec_module(native)
-        sys.modules[name] = sys.modules[__package__]._push = native
+        native = _load_extension("_push", _build.push_path(), _build.build_push)
         native.bind(C.cast(L.idf_push_segment, C.c_void_p).value)
         _push = native.push
     return _push
+
+
+def load_tokens():
+    """The way of the operators that mix tokens into the library: loaded with the first call of one."""
+    global _token_ops
+    if _token_ops is None:
+        L = load_library()
+        from . import build as _build
+        native = _load_extension("_tokens", _build.tokens_path(), _build.build_tokens)
+        native.bind(*(C.cast(getattr(L, n), C.c_void_p).value for n in ("idf_norm_rotate", "idf_window_workspace", "idf_window_attend",
+                                                                         "idf_decay_workspace", "idf_decay_attend")))
+        _token_ops = native
+    return _token_ops
 
 
 PEAK_KINDS = {"copy": 0, "fma_f32": 1, "mfma_f32": 2, "mfma_bf16": 3, "mfma_i8": 4}

@@ -1,4 +1,4 @@
-"""Builds the HIP library (libidf.so) for gfx950 with hipcc, and the way into it from Python (push.cpp), in-tree."""
+"""Builds the HIP library (libidf.so) for gfx950 with hipcc, and the ways into it from Python (push.cpp, tokens.cpp), in-tree."""
 from __future__ import annotations
 
 import glob
@@ -13,6 +13,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libidf.so")
 PUSH_SRC = os.path.join(CSRC, "push.cpp")
+TOKENS_SRC = os.path.join(CSRC, "tokens.cpp")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -31,25 +32,35 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
 
 
-def push_path():
+def extension_path(stem):
     """The extension module of this interpreter and this torch: it is tied to the binary interfaces of both, and another one's is another file."""
     import torch
-    return os.path.join(HERE, f"_push.torch-{torch.__version__}{sysconfig.get_config_var('EXT_SUFFIX')}")
+    return os.path.join(HERE, f"{stem}.torch-{torch.__version__}{sysconfig.get_config_var('EXT_SUFFIX')}")
 
 
-def push_command(out):
-    """The extension module is host code against torch's own headers and libraries, which are in the process before it is loaded."""
+def push_path():
+    return extension_path("_push")
+
+
+def tokens_path():
+    return extension_path("_tokens")
+
+
+def push_command(out, src=PUSH_SRC):
+    """An extension module is host code against torch's own headers and libraries, which are in the process before it is loaded."""
     import torch
     from torch.utils.cpp_extension import include_paths, library_paths
-    return ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-o", out, PUSH_SRC,
-             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"] +
+    return ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-o", out, src,
+             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", os.path.join(ROOT, "include")] +
             [a for d in [sysconfig.get_paths()["include"]] + include_paths() for a in ("-isystem", d)] +
             ["-L" + d for d in library_paths()] + ["-ltorch_python", "-ltorch_cpu", "-lc10"])
 
 
 def up_to_date() -> bool:
-    push = push_path()
-    if not os.path.exists(LIB) or not os.path.exists(push) or os.path.getmtime(push) < os.path.getmtime(PUSH_SRC):
+    for path, made_of in ((push_path(), [PUSH_SRC]), (tokens_path(), [TOKENS_SRC, os.path.join(ROOT, "include", "idf.h")])):
+        if not os.path.exists(path) or any(os.path.getmtime(path) < os.path.getmtime(f) for f in made_of):
+            return False
+    if not os.path.exists(LIB):
         return False
     deps = sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
     return all(os.path.getmtime(LIB) >= os.path.getmtime(d) for d in deps)
@@ -68,17 +79,26 @@ def _run(cmd, verbose=False):
         raise RuntimeError(f"{cmd[0]} failed with code {proc.returncode}: {' '.join(cmd[-3:])}")
 
 
-def build_push(verbose: bool = False) -> str:
-    """Compile push.cpp into push_path() (put there whole: another process may be about to load it)."""
-    path = push_path()
+def _build_extension(path, src, verbose):
+    """Compile src into path (put there whole: another process may be about to load it)."""
     part = f"{path}.{os.getpid()}"
     try:
-        _run(push_command(part), verbose)
+        _run(push_command(part, src), verbose)
         os.replace(part, path)
     finally:
         if os.path.exists(part):
             os.remove(part)
     return path
+
+
+def build_push(verbose: bool = False) -> str:
+    """Compile push.cpp into push_path()."""
+    return _build_extension(push_path(), PUSH_SRC, verbose)
+
+
+def build_tokens(verbose: bool = False) -> str:
+    """Compile tokens.cpp into tokens_path()."""
+    return _build_extension(tokens_path(), TOKENS_SRC, verbose)
 
 
 def build_library(verbose: bool = False) -> str:
@@ -95,13 +115,14 @@ def build_library(verbose: bool = False) -> str:
 
 
 def build(force: bool = True, verbose: bool = False) -> str:
-    """Both of them; returns the library's path."""
+    """All of them; returns the library's path."""
     if not force and up_to_date():
         return LIB
-    with ThreadPoolExecutor(max_workers=1) as ex:
-        push = ex.submit(build_push, verbose)
+    with ThreadPoolExecutor(max_workers=2) as ex:
+        extensions = [ex.submit(f, verbose) for f in (build_push, build_tokens)]
         build_library(verbose)
-        push.result()
+        for e in extensions:
+            e.result()
     return LIB
 
 

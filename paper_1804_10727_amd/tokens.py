@@ -10,9 +10,11 @@ import math
 
 import numpy as np
 
-from .binding import _check, load_library
+from .binding import _check, load_library, load_tokens
 
 _PREC = {}
+_native = None               # csrc/tokens.cpp
+_current_stream = None
 SCALING = {None: 0, "linear": 1, "base": 2, "parts": 3}
 
 
@@ -42,6 +44,21 @@ class _Decay(C.Structure):
                 [(n, _Tokens) for n in ("q", "k", "v", "out")] +
                 [(n, C.c_void_p) for n in ("log_decay", "state_in", "state_out", "offsets", "stream_ids", "workspace")] +
                 [("workspace_bytes", C.c_size_t)])
+
+
+def _direct(name, q, *args):
+    """The call by way of compiled code: its outputs, or None where the arguments are not plain tensors and numbers of the usual kinds, or
+    are wrong: those go the long way round, by ctypes, which converts them or raises."""
+    global _native, _current_stream
+    if _native is None:
+        import torch
+        _native, _current_stream = load_tokens(), torch._C._cuda_getCurrentRawStream
+    if not getattr(q, "is_cuda", False):
+        return None
+    r = getattr(_native, name)(_current_stream(q.get_device()), q, *args)
+    if type(r) is int:
+        _check(r)
+    return r
 
 
 def _precision(t):
@@ -112,9 +129,14 @@ def rotary_frequencies(rotary_dim, base=10000.0, scaling=None, factor=1.0, train
 def norm_rotate(q, k, positions, frequencies, layout="half", amplitude=1.0, q_weight=None, k_weight=None, eps=1e-6, q_out=None, k_out=None):
     """Queries [token][head][value] and keys of the same tokens, each head normalised (where there is a weight) and turned by its token's
     position: (q, k) anew, or into q_out and k_out, which may be q and k (idf_norm_rotate).  layout "half" or "interleaved"."""
-    import torch
     if layout not in ("half", "interleaved"):
         raise ValueError(f"layout {layout!r}")
+    r = _direct("norm_rotate", q, k, positions, frequencies, int(layout == "interleaved"), amplitude, q_weight, k_weight, eps, q_out, k_out)
+    return r if r is not None else _norm_rotate(q, k, positions, frequencies, layout, amplitude, q_weight, k_weight, eps, q_out, k_out)
+
+
+def _norm_rotate(q, k, positions, frequencies, layout, amplitude, q_weight, k_weight, eps, q_out, k_out):
+    import torch
     q, k = _rows(q, q, "q", aligned=False), _rows(k, q, "k", aligned=False)
     n, hq, d = q.shape
     if k.shape[0] != n or k.shape[2] != d:
@@ -163,6 +185,11 @@ def window_attend(q, k, v, k_ring=None, v_ring=None, starts=None, *, window, sin
 
     starts: int64, position of each segment's first token.  Without offsets all segments have one length; with offsets (int64, one more
     than segments) max_tokens is the longest one's.  stream_ids: int32, the ring of each segment.  scale: 1 / sqrt(head size)."""
+    r = _direct("window_attend", q, k, v, k_ring, v_ring, starts, window, sinks, scale, offsets, max_tokens, stream_ids, out)
+    return r if r is not None else _window_attend(q, k, v, k_ring, v_ring, starts, window, sinks, scale, offsets, max_tokens, stream_ids, out)
+
+
+def _window_attend(q, k, v, k_ring, v_ring, starts, window, sinks, scale, offsets, max_tokens, stream_ids, out):
     import torch
     q, k, v = _rows(q, q, "q"), _rows(k, q, "k"), _rows(v, q, "v")
     n, hq, d = q.shape
@@ -200,6 +227,11 @@ def decay_attend(q, k, v, log_decay, state=None, state_out=None, *, scale=None, 
     """Linear attention of packed segments with a decay per key/value head, from `state` (float32 [stream][head][key value][value], None:
     zeros) into `state_out` (None: not wanted; may be `state`) (idf_decay_attend).  Segments as in window_attend; n_segments where
     neither states nor ids say how many there are.  scale: 1 / sqrt(key size)."""
+    r = _direct("decay_attend", q, k, v, log_decay, state, state_out, scale, offsets, max_tokens, n_segments, stream_ids, out)
+    return r if r is not None else _decay_attend(q, k, v, log_decay, state, state_out, scale, offsets, max_tokens, n_segments, stream_ids, out)
+
+
+def _decay_attend(q, k, v, log_decay, state, state_out, scale, offsets, max_tokens, n_segments, stream_ids, out):
     import torch
     q, k, v = _rows(q, q, "q"), _rows(k, q, "k"), _rows(v, q, "v")
     n, hq, dk = q.shape

@@ -405,3 +405,65 @@ def test_same_bits_every_time():
     q, k, v = (normal(g, 4000, 1, 64, dtype=torch.bfloat16).to(DEV) for _ in range(3))
     a = [idf.decay_attend(q, k, v, torch.tensor([-0.01], device=DEV)) for _ in range(3)]
     assert torch.equal(a[0], a[1]) and torch.equal(a[0], a[2])
+
+
+# ---- the two ways into the library ----
+
+def test_both_ways_into_the_library_agree(monkeypatch):
+    """Compiled code takes plain tensors; what it leaves goes by ctypes, with the same results and outputs where they were asked for."""
+    from paper_1804_10727_amd import tokens
+    g = torch.Generator().manual_seed(30)
+    q, k, v = (normal(g, 6, h, 64, dtype=torch.bfloat16).to(DEV) for h in (4, 2, 2))
+    rings = [normal(g, 3, 12, 2, 64, dtype=torch.bfloat16).to(DEV) for _ in range(2)]
+    starts = torch.tensor([30, 4, 0], device=DEV)
+    positions = torch.arange(6, device=DEV)
+    f, _ = idf.rotary_frequencies(64, device=DEV)
+    w = torch.rand(64, generator=g).to(DEV)
+    state = torch.randn(3, 2, 64, 64, generator=g).to(DEV)
+    log_decay = torch.tensor([-0.1, -0.2], device=DEV)
+    offsets = torch.tensor([0, 3, 4, 6], device=DEV)
+    ids = torch.tensor([2, 0, 1], dtype=torch.int32, device=DEV)
+
+    def everything():
+        r, s = [x.clone() for x in rings], state.clone()
+        into = torch.zeros_like(q)
+        got = [*idf.norm_rotate(q, k, positions, f, q_weight=w), *idf.norm_rotate(q, k, positions, f, layout="interleaved", amplitude=2, q_out=into),
+               idf.window_attend(q, k, v, *r, starts, window=10, sinks=2), idf.window_attend(q, k, v, *r, starts, window=10, sinks=1, offsets=offsets, max_tokens=3),
+               idf.window_attend(q, k, v, window=4, scale=1), idf.window_attend(q[:3], k[:3], v[:3], *r, starts, window=12, stream_ids=ids, out=into[:3]),
+               idf.decay_attend(q, k, v, log_decay, s, s), idf.decay_attend(q, k, v, log_decay, offsets=offsets, max_tokens=3),
+               idf.decay_attend(q, k, v, log_decay, n_segments=2), idf.decay_attend(q, k, v, log_decay, s, None, stream_ids=ids)]
+        return got + [into, *r, s]
+    want = everything()
+    called = []
+    real = tokens._direct
+    monkeypatch.setattr(tokens, "_direct", lambda name, *a: called.append((name, real(name, *a) is not None)))
+    got = everything()
+    assert len(called) == 10 and all(taken for _, taken in called)
+    # (each call ran both ways here: what is updated in place went twice, so only what is not is compared)
+    for i in (0, 1, 2, 3, 6, 9, 10):
+        assert torch.equal(got[i], want[i]), i
+    monkeypatch.setattr(tokens, "_direct", lambda *a: None)
+    for a, b in zip(everything(), want):
+        assert torch.equal(a, b)
+
+
+def test_python_refuses_on_the_gpu():
+    q = torch.zeros(4, 2, 64, device=DEV)
+    f, _ = idf.rotary_frequencies(64, device=DEV)
+    ring = torch.zeros(2, 8, 2, 64, device=DEV)
+    p = torch.zeros(4, dtype=torch.int64, device=DEV)
+    for call in (lambda: idf.norm_rotate(q, q, p[:3], f), lambda: idf.norm_rotate(q, q, p.int(), f), lambda: idf.norm_rotate(q, q, p, f.float()),
+                 lambda: idf.norm_rotate(q, q[:3], p, f), lambda: idf.norm_rotate(q, q, p, f, q_weight=f), lambda: idf.norm_rotate(q, q, p, f, q_out=q[:3]),
+                 lambda: idf.norm_rotate(q, q.cpu(), p, f), lambda: idf.norm_rotate(q, q, p.cpu(), f),
+                 lambda: idf.window_attend(q, q, q[:3], window=4), lambda: idf.window_attend(q, q, q, ring, window=4), lambda: idf.window_attend(q, q, q, ring, ring[:1], window=4),
+                 lambda: idf.window_attend(q, q, q, ring.bfloat16(), ring.bfloat16(), window=4), lambda: idf.window_attend(q, q, q, window=4, offsets=p),
+                 lambda: idf.window_attend(q, q, q, ring[:, ::2], ring[:, ::2], window=4), lambda: idf.window_attend(q, q, q, window=4, starts=p[:3]),
+                 lambda: idf.window_attend(q, q, q, window=4, out=q[:, :, ::2]), lambda: idf.decay_attend(q, q, q, p), lambda: idf.decay_attend(q, q, q, p.float()),
+                 lambda: idf.decay_attend(q, q, q, p[:2].float(), torch.zeros(1, 2, 64, 32, device=DEV)), lambda: idf.decay_attend(q, q, q, p[:2].float(), n_segments=3),
+                 lambda: idf.decay_attend(q, q, q, p[:2].float(), torch.zeros(1, 2, 64, 64, device=DEV), torch.zeros(2, 2, 64, 64, device=DEV))):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: idf.norm_rotate(q.half(), q.half(), p, f), lambda: idf.window_attend(q, q, q, window=0), lambda: idf.window_attend(q, q, q, ring, ring, window=9),
+                 lambda: idf.window_attend(q, q, q, window=4, scale=-1.0), lambda: idf.decay_attend(q, q, q, p[:2].float(), scale=float("nan"))):
+        with pytest.raises(idf.IdfError):
+            call()
