@@ -327,7 +327,8 @@ template <int PREC, int DP> struct TileShape {
     static constexpr int VL = Elem<PREC>::VL, ROW16 = DP / VL;
     static constexpr int K_STRIDE = DP + VL;                                  // neighbouring rows begin 16 bytes apart in the banks
     static constexpr int V_STRIDE = DP + (PREC == IDF_PREC_BF16 ? 16 : 4);
-    static constexpr int LOADS = (KEYS * ROW16 + 255) / 256;
+    static constexpr int LOADS = KEYS * ROW16 / 256;
+    static_assert(KEYS * ROW16 % 256 == 0, "a round is loaded whole");
     static constexpr bool AHEAD = DP <= 128;                                  // (longer rows leave no registers for a round on its way)
     static constexpr int LDS_BYTES = KEYS * (K_STRIDE + V_STRIDE) * (int)sizeof(typename Elem<PREC>::type);
 };
@@ -372,12 +373,51 @@ __global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = 16 * s + 8 * half < a.head_dim ? M::load(src + 16 * s + 8 * half) : M::zero();
     }
+    // Rounds whose entries lie behind each other, all own tokens or all in the ring without its end between them, are read from one address on;
+    // the others (first tokens, the ring's end, the list's) look for the place of each entry.
+    const int r0 = threadIdx.x / S::ROW16, c0 = (threadIdx.x - r0 * S::ROW16) * M::VL;
+    const bool in_row = c0 < a.head_dim;
+    const int64_t k_step = kh.own_stride, v_step = vh.own_stride, ring_step = kh.ring_stride;
+    constexpr int64_t kFar = ((int64_t)1 << 31) / S::KEYS / (int)sizeof(T) - DP;
+    const bool own_flat = k_step >= 0 && v_step >= 0 && k_step < kFar && v_step < kFar, ring_flat = ring_step < kFar;
     i32x4 kr[S::LOADS], vr[S::LOADS];
     auto load = [&](int t) IDF_INLINE {
+        const int i0 = t * S::KEYS, rel = i0 - keys.n_first;
+        const T *kb = nullptr, *vb = nullptr;
+        int ks = 0, vs = 0;
+        if (i0 + S::KEYS <= keys.n && rel >= 0) {
+            if (own_flat && rel >= keys.own) {
+                kb = kh.own + (int64_t)(rel - keys.own) * k_step; vb = vh.own + (int64_t)(rel - keys.own) * v_step;
+                ks = (int)k_step; vs = (int)v_step;
+            } else if (ring_flat && rel + S::KEYS <= keys.own) {
+                uint32_t s = keys.slot0 + (uint32_t)rel;
+                if (s >= keys.period) s -= keys.period;
+                if (s + S::KEYS <= keys.period) {
+                    kb = kh.ring + (a.sinks + (int64_t)s) * ring_step; vb = vh.ring + (a.sinks + (int64_t)s) * ring_step;
+                    ks = vs = (int)ring_step;
+                }
+            }
+        }
+        if (kb) {
+            const uint32_t ko = (uint32_t)(r0 * ks + c0) * sizeof(T), vo = (uint32_t)(r0 * vs + c0) * sizeof(T);
+#pragma unroll
+            for (int j = 0; j < S::LOADS; ++j) {
+                constexpr int rows = 256 / S::ROW16;
+                if constexpr (256 % S::ROW16 == 0) {
+                    kr[j] = in_row ? *(const i32x4 *)((const char *)(kb + (int64_t)(j * rows) * ks) + ko) : i32x4{0, 0, 0, 0};
+                    vr[j] = in_row ? *(const i32x4 *)((const char *)(vb + (int64_t)(j * rows) * vs) + vo) : i32x4{0, 0, 0, 0};
+                } else {
+                    const int piece = j * 256 + threadIdx.x, r = piece / S::ROW16, c = (piece - r * S::ROW16) * M::VL;
+                    kr[j] = c < a.head_dim ? *(const i32x4 *)(kb + r * ks + c) : i32x4{0, 0, 0, 0};
+                    vr[j] = c < a.head_dim ? *(const i32x4 *)(vb + r * vs + c) : i32x4{0, 0, 0, 0};
+                }
+            }
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < S::LOADS; ++j) {
-            const int piece = j * 256 + threadIdx.x, r = piece / S::ROW16, c = (piece - r * S::ROW16) * M::VL, i = t * S::KEYS + r;
-            const bool there = r < S::KEYS && i < keys.n && c < a.head_dim;
+            const int piece = j * 256 + threadIdx.x, r = piece / S::ROW16, c = (piece - r * S::ROW16) * M::VL, i = i0 + r;
+            const bool there = i < keys.n && c < a.head_dim;
             const Place pl = place_of(a, keys, min(i, keys.n - 1));
             kr[j] = there ? *(const i32x4 *)(at(kh, pl) + c) : i32x4{0, 0, 0, 0};
             vr[j] = there ? *(const i32x4 *)(at(vh, pl) + c) : i32x4{0, 0, 0, 0};
@@ -396,7 +436,6 @@ __global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 
 #pragma unroll
         for (int j = 0; j < S::LOADS; ++j) {
             const int piece = j * 256 + threadIdx.x, r = piece / S::ROW16, c = (piece - r * S::ROW16) * M::VL;
-            if (S::KEYS * S::ROW16 % 256 && r >= S::KEYS) continue;
             *(i32x4 *)(k_lds + r * S::K_STRIDE + c) = kr[j];
             *(i32x4 *)(v_lds + r * S::V_STRIDE + c) = vr[j];
         }
@@ -427,8 +466,11 @@ __global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, st[kt][e]);
         top = fmaxf(top, __shfl_xor(top, 32));
-        top = fmaxf(m, top * scale);
-        if (__ballot(top > m)) {
+        // the maximum that weights are taken against may lag behind by a factor of 2^8, far from any overflow: outputs are scaled anew only
+        // where it falls back further
+        top *= scale;
+        if (__ballot(top > m + 8.f)) {
+            top = fmaxf(m, top);
             const float fade = __builtin_amdgcn_exp2f(m - top);
             l *= fade;
 #pragma unroll
