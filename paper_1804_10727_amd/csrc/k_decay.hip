@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
     constexpr int K_LOADS = kChunk * DK / VL / THREADS, V_LOADS = kChunk * 32 / VL / 64;
     constexpr int BF = PREC == IDF_PREC_BF16;
     constexpr int SCORE_STRIDE = kChunk + 4;
-    __shared__ __align__(16) T k_lds[kChunk * K_STRIDE], v_lds[kChunk * V_STRIDE];
+    __shared__ __align__(16) T k_both[2][kChunk * K_STRIDE], q_both[2][kChunk * K_STRIDE], v_both[2][kChunk * V_STRIDE];
     __shared__ __align__(16) float score[kChunk * SCORE_STRIDE], fresh[2 * kChunk];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
     const int part = gridDim.y - 1 - blockIdx.y;   // (the parts whose keys and values were read last are the first to be read again)
@@ -150,64 +150,74 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
         if (i == 0) { fresh[j] = __builtin_amdgcn_exp2f((float)(kChunk - 1 - j) * l2); fresh[kChunk + j] = 0.f; }
     }
     const float faded = __builtin_amdgcn_exp2f((float)(col + 1) * l2) * a.scale;
-    // the decay of a whole chunk in two parts: it is applied again and again, and its own rounding would add up
-    // (the last chunk of the part may be a short one)
-    float keep[2], keep_low[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const double power = exp2((double)(x ? (len - 1) % kChunk + 1 : kChunk) * (double)l2);
-        keep[x] = uniform((float)power);
-        keep_low[x] = uniform((float)(power - (double)keep[x]));
-    }
+    // The decay of a whole chunk is applied again and again, and its own rounding would add up: each factor takes back what those before it
+    // were off (drift: what has been applied over what should have been).
+    const double whole = exp2((double)kChunk * (double)l2), inverse = whole > 1e-30 ? 1.0 / whole : 0.0;
+    double drift = 1.0;
+    const float fade_short = uniform((float)exp2((double)((max(len, 1) - 1) % kChunk + 1) * (double)l2));        // (the last chunk of the part may be a short one)
 
+    // A step is a chunk for one of the heads.  While one is worked on, what the next one needs is written from registers into the other half
+    // of LDS, and what the one behind it needs is asked for.
     const T *kb = (const T *)a.k.base + (g.begin + first) * a.k.token_stride + kv * a.k.head_stride;
     const T *vb = (const T *)a.v.base + (g.begin + first) * a.v.token_stride + kv * a.v.head_stride;
-    i32x4 kr[K_LOADS], vr[V_LOADS];
-    auto load = [&](int t0) IDF_INLINE {
+    const T *qb = (const T *)a.q.base + (g.begin + first) * a.q.token_stride + kv * queries * a.q.head_stride;
+    const int heads = states_only ? 1 : queries;
+    struct Step { int t0, h; };
+    auto next_of = [&](Step x) { return x.h + 1 < heads ? Step{x.t0, x.h + 1} : Step{x.t0 + kChunk, 0}; };
+    i32x4 kr[K_LOADS], qr[K_LOADS], vr[V_LOADS];
+    auto load = [&](const Step &x) IDF_INLINE {
+        if (x.t0 >= len) return;
 #pragma unroll
-        for (int x = 0; x < K_LOADS; ++x) {
-            const int piece = x * THREADS + threadIdx.x, r = piece / (DK / VL), c = (piece - r * (DK / VL)) * VL;
-            kr[x] = t0 + r < len && c < a.dim_k ? *(const i32x4 *)(kb + (int64_t)(t0 + r) * a.k.token_stride + c) : i32x4{0, 0, 0, 0};
+        for (int y = 0; y < K_LOADS; ++y) {
+            const int piece = y * THREADS + threadIdx.x, r = piece / (DK / VL), c = (piece - r * (DK / VL)) * VL;
+            const bool there = x.t0 + r < len && c < a.dim_k;
+            if (x.h == 0) kr[y] = there ? *(const i32x4 *)(kb + (int64_t)(x.t0 + r) * a.k.token_stride + c) : i32x4{0, 0, 0, 0};
+            if (!states_only) qr[y] = there ? *(const i32x4 *)(qb + (int64_t)(x.t0 + r) * a.q.token_stride + x.h * a.q.head_stride + c) : i32x4{0, 0, 0, 0};
         }
+        if (x.h == 0)
 #pragma unroll
-        for (int x = 0; x < V_LOADS; ++x) {
-            const int piece = x * THREADS + threadIdx.x, r = piece / (32 * NW / VL), c = (piece - r * (32 * NW / VL)) * VL;
-            vr[x] = t0 + r < len && c0 + c < a.dim_v ? *(const i32x4 *)(vb + (int64_t)(t0 + r) * a.v.token_stride + c0 + c) : i32x4{0, 0, 0, 0};
-        }
+            for (int y = 0; y < V_LOADS; ++y) {
+                const int piece = y * THREADS + threadIdx.x, r = piece / (32 * NW / VL), c = (piece - r * (32 * NW / VL)) * VL;
+                vr[y] = x.t0 + r < len && c0 + c < a.dim_v ? *(const i32x4 *)(vb + (int64_t)(x.t0 + r) * a.v.token_stride + c0 + c) : i32x4{0, 0, 0, 0};
+            }
     };
-    if (len > 0) load(0);
-    for (int t0 = 0; t0 < len; t0 += kChunk) {
-        __syncthreads();
+    auto store = [&](const Step &x, int step) IDF_INLINE {
+        if (x.t0 >= len) return;
+        T *k_to = k_both[x.t0 / kChunk & 1], *v_to = v_both[x.t0 / kChunk & 1], *q_to = q_both[step & 1];
 #pragma unroll
-        for (int x = 0; x < K_LOADS; ++x) {
-            const int piece = x * THREADS + threadIdx.x, r = piece / (DK / VL), c = (piece - r * (DK / VL)) * VL;
-            *(i32x4 *)(k_lds + r * K_STRIDE + c) = kr[x];
+        for (int y = 0; y < K_LOADS; ++y) {
+            const int piece = y * THREADS + threadIdx.x, r = piece / (DK / VL), c = (piece - r * (DK / VL)) * VL;
+            if (x.h == 0) *(i32x4 *)(k_to + r * K_STRIDE + c) = kr[y];
+            if (!states_only) *(i32x4 *)(q_to + r * K_STRIDE + c) = qr[y];
         }
+        if (x.h == 0)
 #pragma unroll
-        for (int x = 0; x < V_LOADS; ++x) {
-            const int piece = x * THREADS + threadIdx.x, r = piece / (32 * NW / VL), c = (piece - r * (32 * NW / VL)) * VL;
-            *(i32x4 *)(v_lds + r * V_STRIDE + c) = vr[x];
-        }
+            for (int y = 0; y < V_LOADS; ++y) {
+                const int piece = y * THREADS + threadIdx.x, r = piece / (32 * NW / VL), c = (piece - r * (32 * NW / VL)) * VL;
+                *(i32x4 *)(v_to + r * V_STRIDE + c) = vr[y];
+            }
+    };
+    Step now = {0, 0}, ahead = next_of(now);
+    load(now);
+    store(now, 0);
+    load(ahead);
+    for (int step = 0; now.t0 < len; ++step) {
         __syncthreads();
-        const int n = min(kChunk, len - t0);
-        if (t0 + kChunk < len) load(t0 + kChunk);
+        store(ahead, step + 1);
+        const Step then = next_of(ahead);
+        load(then);
+        const int t0 = now.t0, n = min(kChunk, len - t0), h = now.h;
+        const T *k_lds = k_both[t0 / kChunk & 1], *v_lds = v_both[t0 / kChunk & 1], *q_lds = q_both[step & 1];
+        now = ahead;
+        ahead = then;
 
         // values of this wave's columns along the tokens: register x of piece p is token 16 p + 8 (x / 4) + 4 half + x % 4
         frag v[2];
 #pragma unroll
         for (int p = 0; p < 2; ++p) v[p] = read_column(v_lds, V_STRIDE, 32 * wave + (lane & 16), 16 * p + 4 * half, 16 * p + 8 + 4 * half);
 
-        if (!states_only)
-            for (int h = kv * queries; h < (kv + 1) * queries; ++h) {
-                // a head's operands are formed in its turn: kept for the other heads of the group they would take the registers
-#pragma unroll
-                for (int t = 0; t < KT; ++t) asm volatile("" : "+v"(s[t])::"memory");
-                const int64_t token = g.begin + first + t0 + min(col, n - 1);
-                const T *qb = (const T *)a.q.base + token * a.q.token_stride + h * a.q.head_stride;
+        if (!states_only) {
                 f32x16 w, o;
-                frag q[KS];
-#pragma unroll
-                for (int p = 0; p < KS; ++p) q[p] = 16 * p + 8 * half < a.dim_k ? M::load(qb + 16 * p + 8 * half) : M::zero();
 #pragma unroll
                 for (int e = 0; e < 16; ++e) { w[e] = 0.f; o[e] = 0.f; }
 #pragma unroll
@@ -215,8 +225,9 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
                     float sv[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sv[e] = s[p / 2][8 * (p % 2) + e];
-                    o = M::mma32(M::pack(sv), q[p], o);
-                    w = M::mma32(M::load(k_lds + col * K_STRIDE + 16 * p + 8 * half), q[p], w);
+                    const frag q = M::load(q_lds + col * K_STRIDE + 16 * p + 8 * half);
+                    o = M::mma32(M::pack(sv), q, o);
+                    w = M::mma32(M::load(k_lds + col * K_STRIDE + 16 * p + 8 * half), q, w);
                 }
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
@@ -245,14 +256,14 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
                         float sv[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) sv[e] = s[p / 2][8 * (p % 2) + e];
-                        o = M::mma32(M::pack(sv), q[p], o);
+                        o = M::mma32(M::pack(sv), M::load(q_lds + col * K_STRIDE + 16 * p + 8 * half), o);
                     }
                     o *= faded;
 #pragma unroll 1
                     for (int j = 0; j < n; ++j) {
                         float qk = 0.f;            // (a lane takes every other value, lane ^ 32 the ones between)
 #pragma unroll 1
-                        for (int d = half; d < a.dim_k; d += 2) qk += E::to_f32(qb[d]) * E::to_f32(k_lds[j * K_STRIDE + d]);
+                        for (int d = half; d < a.dim_k; d += 2) qk += E::to_f32(q_lds[col * K_STRIDE + d]) * E::to_f32(k_lds[j * K_STRIDE + d]);
                         qk += __shfl_xor(qk, 32);
                         if (j > col) continue;
                         qk *= __builtin_amdgcn_exp2f((float)(col - j) * l2) * a.scale;
@@ -261,7 +272,7 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
                     }
                 }
                 if (col < n) {
-                    T *out = (T *)a.out.base + token * a.out.token_stride + h * a.out.head_stride + c0 + 32 * wave + 4 * half;
+                    T *out = (T *)a.out.base + (g.begin + first + t0 + col) * a.out.token_stride + (kv * queries + h) * a.out.head_stride + c0 + 32 * wave + 4 * half;
 #pragma unroll
                     for (int e = 0; e < 16; e += 4) {
                         Pack<T, 4> pk;
@@ -272,11 +283,14 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
                 }
             }
 
-        const float fade = n < kChunk ? keep[1] : keep[0], fade_low = n < kChunk ? keep_low[1] : keep_low[0];
+        if (h + 1 < heads) continue;
+        float fade = fade_short;
+        if (n == kChunk) {
+            fade = uniform((float)(whole * (2.0 - drift)));                   // (2 - x is 1 / x so near to one)
+            if (inverse > 0.0) drift *= (double)fade * inverse;
+        }
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[t][e] = __builtin_fmaf(s[t][e], fade, s[t][e] * fade_low);
+        for (int t = 0; t < KT; ++t) s[t] *= fade;
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
             float x[8];

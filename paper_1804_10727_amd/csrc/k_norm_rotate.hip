@@ -14,6 +14,7 @@ namespace idf {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kGroups = 1024;                      // workgroups that go on from tokens to tokens: four for a compute unit
 constexpr int kDeep = 4;                           // heads that a group of lanes has in flight
 
 // P: values of a piece; N: pairs of pieces of a lane (2 only where single values make a head longer than 64 lanes can hold)
@@ -23,9 +24,13 @@ __global__ void __launch_bounds__(kThreads) k_norm_rotate(idf_norm_rotate_args a
     using E = Elem<PREC>;
     using T = typename E::type;
     using Piece = Pack<T, P>;
-    extern __shared__ float2 turn[];               // [tokens_per_group][rotary_dim / 2]: amplitude * (cos, sin)
-    const int half = a.rotary_dim / 2, heads = a.heads_q + a.heads_k;
+    extern __shared__ float2 lds[];                // weights of queries and keys, then twice [tokens_per_group][rotary_dim / 2]: amplitude * (cos, sin)
+    const int half = a.rotary_dim / 2, heads = a.heads_q + a.heads_k, padded = (a.head_dim + 3) / 4 * 4;
+    float *weights = (float *)lds;
+    float2 *turn = lds + padded;
+    const int table = tokens_per_group * half;
     const int lane = threadIdx.x & ((1 << lanes_log2) - 1), group = threadIdx.x >> lanes_log2, groups = kThreads >> lanes_log2;
+    const float per_head = 1.f / (float)heads;
 
     // where this lane's pieces begin, and the pair whose angle the first value has
     int at0[N], at1[N], pair[N];
@@ -42,70 +47,99 @@ __global__ void __launch_bounds__(kThreads) k_norm_rotate(idf_norm_rotate_args a
         }
     }
 
-    for (int64_t token0 = (int64_t)blockIdx.x * tokens_per_group; token0 < a.n_tokens; token0 += (int64_t)gridDim.x * tokens_per_group)
-    for (int row0 = 0, tokens = (int)min((int64_t)tokens_per_group, a.n_tokens - token0), rows = tokens * heads; row0 < rows; row0 += groups * kDeep) {
-        Piece x0[kDeep][N], x1[kDeep][N];
-        T *to[kDeep];
-        const float *weight[kDeep];
-        int token[kDeep];
+    // A workgroup goes through its tokens as the groups of lanes take their heads, kDeep each at a time; the values of the next time, and
+    // the angles where they belong to further tokens, are fetched and formed while this time's are worked on.
+    struct Where { int64_t token0; int row0; };
+    auto tokens_of = [&](const Where &w) { return (int)min((int64_t)tokens_per_group, a.n_tokens - w.token0); };
+    auto next_of = [&](Where w) {
+        w.row0 += groups * kDeep;
+        if (w.row0 >= tokens_of(w) * heads) { w.row0 = 0; w.token0 += (int64_t)gridDim.x * tokens_per_group; }
+        return w;
+    };
+    struct Head { int t, h; bool on, key; };
+    auto head_of = [&](const Where &w, int u) {
+        Head r;
+        const int row = w.row0 + u * groups + group;
+        r.on = row < tokens_of(w) * heads;
+        r.t = r.on ? (int)(((float)row + 0.5f) * per_head) : 0;                // (fewer than 2^16 rows: the quotient is exact)
+        r.h = r.on ? row - r.t * heads : 0;
+        r.key = r.h >= a.heads_q;
+        if (r.key) r.h -= a.heads_q;
+        return r;
+    };
+    auto fetch = [&](const Where &w, Piece (&x)[kDeep][N][2]) IDF_INLINE {
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) {
-            const int row = row0 + u * groups + group;
-            const bool on = row < rows;
-            const int t = on ? row / heads : 0, h = on ? row - t * heads : 0;
-            const bool is_k = h >= a.heads_q;
-            const idf_tokens &from = is_k ? a.k : a.q, &out = is_k ? a.k_out : a.q_out;
-            const int hh = is_k ? h - a.heads_q : h;
-            const T *src = (const T *)from.base + (token0 + t) * from.token_stride + hh * from.head_stride;
-            to[u] = on ? (T *)out.base + (token0 + t) * out.token_stride + hh * out.head_stride : nullptr;
-            weight[u] = is_k ? a.k_weight : a.q_weight;
-            token[u] = t;
+            const Head r = head_of(w, u);
+            const idf_tokens &from = r.key ? a.k : a.q;
+            const T *src = (const T *)from.base + (w.token0 + r.t) * from.token_stride + r.h * from.head_stride;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                x0[u][n] = Piece{}; x1[u][n] = Piece{};
-                if (on && at0[n] < a.head_dim) x0[u][n] = *(const Piece *)(src + at0[n]);
-                if (on && at1[n] < a.head_dim) x1[u][n] = *(const Piece *)(src + at1[n]);
+                x[u][n][0] = Piece{}; x[u][n][1] = Piece{};
+                if (r.on && at0[n] < a.head_dim) x[u][n][0] = *(const Piece *)(src + at0[n]);
+                if (r.on && at1[n] < a.head_dim) x[u][n][1] = *(const Piece *)(src + at1[n]);
             }
         }
-        if (row0 == 0) {
-            __syncthreads();                       // (the angles of the tokens before are no longer read)
-            for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
-                const int t = i / half;
-                // quarter turns, reduced to the nearest whole one while still in 64 bits: what is left is small where a cosine or sine is
-                const double quarters = (double)a.positions[token0 + t] * a.frequencies[i - t * half] * 0.63661977236758134308;
-                const double whole = __builtin_rint(quarters);
-                float s, c;
-                sincospif(0.5f * (float)(quarters - whole), &s, &c);
-                const int quadrant = (int)(whole - 4.0 * __builtin_floor(0.25 * whole));
-                if (quadrant & 1) { const float was = c; c = -s; s = was; }
-                if (quadrant & 2) { c = -c; s = -s; }
-                turn[i] = make_float2((float)(a.amplitude * (double)c), (float)(a.amplitude * (double)s));
-            }
-            __syncthreads();
+    };
+    auto form_angles = [&](const Where &w, float2 *to) IDF_INLINE {
+        const int n = tokens_of(w) * half;
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            const int t = i / half;
+            // quarter turns, reduced to the nearest whole one while still in 64 bits: what is left is small where a cosine or sine is
+            const double quarters = (double)a.positions[w.token0 + t] * a.frequencies[i - t * half] * 0.63661977236758134308;
+            const double whole = __builtin_rint(quarters);
+            float s, c;
+            sincospif(0.5f * (float)(quarters - whole), &s, &c);
+            const int quadrant = (int)(whole - 4.0 * __builtin_floor(0.25 * whole));
+            if (quadrant & 1) { const float was = c; c = -s; s = was; }
+            if (quadrant & 2) { c = -c; s = -s; }
+            to[i] = make_float2((float)(a.amplitude * (double)c), (float)(a.amplitude * (double)s));
         }
+    };
+
+    Where at = {(int64_t)blockIdx.x * tokens_per_group, 0};
+    if (at.token0 >= a.n_tokens) return;
+    Piece x[kDeep][N][2];
+    fetch(at, x);
+    for (int i = threadIdx.x; i < 2 * padded; i += kThreads) {
+        const float *w = i < padded ? a.q_weight : a.k_weight;
+        const int d = i < padded ? i : i - padded;
+        weights[i] = w && d < a.head_dim ? w[d] : 1.f;
+    }
+    form_angles(at, turn);
+    __syncthreads();
+    for (int buffer = 0;;) {
+        const Where ahead = next_of(at);
+        const bool more = ahead.token0 < a.n_tokens, other_tokens = more && ahead.row0 == 0;
+        Piece next[kDeep][N][2];
+        if (more) fetch(ahead, next);
+        if (other_tokens) form_angles(ahead, turn + (buffer ^ 1) * table);
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) {
+            const Head r = head_of(at, u);
             float y0[N][P], y1[N][P], sum = 0.f;
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
                 for (int e = 0; e < P; ++e) {
-                    y0[n][e] = E::to_f32(x0[u][n].v[e]); y1[n][e] = E::to_f32(x1[u][n].v[e]);
+                    y0[n][e] = E::to_f32(x[u][n][0].v[e]); y1[n][e] = E::to_f32(x[u][n][1].v[e]);
                     sum += y0[n][e] * y0[n][e] + y1[n][e] * y1[n][e];
                 }
             for (int m = 1; m < 1 << lanes_log2; m <<= 1) sum += __shfl_xor(sum, m);
-            if (!to[u]) continue;
-            if (weight[u]) {
+            if (!r.on) continue;
+            if (r.key ? a.k_weight : a.q_weight) {
                 const float norm = 1.f / sqrtf(sum / (float)a.head_dim + a.eps);
+                const float *w = weights + (r.key ? padded : 0);
 #pragma unroll
-                for (int n = 0; n < N; ++n)
+                for (int n = 0; n < N; ++n) {
+                    const Pack<float, P> w0 = at0[n] < a.head_dim ? *(const Pack<float, P> *)(w + at0[n]) : Pack<float, P>{}, w1 = at1[n] < a.head_dim ? *(const Pack<float, P> *)(w + at1[n]) : Pack<float, P>{};
 #pragma unroll
-                    for (int e = 0; e < P; ++e) {
-                        if (at0[n] < a.head_dim) y0[n][e] *= norm * weight[u][at0[n] + e];
-                        if (at1[n] < a.head_dim) y1[n][e] *= norm * weight[u][at1[n] + e];
-                    }
+                    for (int e = 0; e < P; ++e) { y0[n][e] *= norm * w0.v[e]; y1[n][e] *= norm * w1.v[e]; }
+                }
             }
-            const float2 *cs = turn + token[u] * half;
+            const float2 *cs = turn + buffer * table + r.t * half;
+            const idf_tokens &out = r.key ? a.k_out : a.q_out;
+            T *to = (T *)out.base + (at.token0 + r.t) * out.token_stride + r.h * out.head_stride;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 if (turned[n]) {
@@ -129,10 +163,17 @@ __global__ void __launch_bounds__(kThreads) k_norm_rotate(idf_norm_rotate_args a
                 Piece o0, o1;
 #pragma unroll
                 for (int e = 0; e < P; ++e) { o0.v[e] = E::from_f32(y0[n][e]); o1.v[e] = E::from_f32(y1[n][e]); }
-                if (at0[n] < a.head_dim) *(Piece *)(to[u] + at0[n]) = o0;
-                if (at1[n] < a.head_dim) *(Piece *)(to[u] + at1[n]) = o1;
+                if (at0[n] < a.head_dim) *(Piece *)(to + at0[n]) = o0;
+                if (at1[n] < a.head_dim) *(Piece *)(to + at1[n]) = o1;
             }
         }
+        if (!more) break;
+        if (other_tokens) { __syncthreads(); buffer ^= 1; }
+        at = ahead;
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+#pragma unroll
+            for (int n = 0; n < N; ++n) { x[u][n][0] = next[u][n][0]; x[u][n][1] = next[u][n][1]; }
     }
 }
 
@@ -157,9 +198,10 @@ hipError_t go(const idf_norm_rotate_args &a, const LaunchCtx &lc)
     const int heads = a.heads_q + a.heads_k, groups = kThreads >> lanes_log2;
     // as many tokens as the groups take in one go, but workgroups for every compute unit first
     int64_t per = std::max(1, groups * kDeep / heads);
-    per = std::max<int64_t>(1, std::min<int64_t>({per, a.n_tokens / 1024, 32}));
-    const int64_t grid = std::min<int64_t>((a.n_tokens + per - 1) / per, 1 << 20);
-    return launch(k_norm_rotate<PREC, P, N>, dim3((unsigned)grid), dim3(kThreads), (size_t)per * (a.rotary_dim / 2) * sizeof(float2), lc, a, lanes_log2, (int)per);
+    per = std::max<int64_t>(1, std::min<int64_t>({per, a.n_tokens / 1024, 16}));
+    const int64_t grid = std::min<int64_t>((a.n_tokens + per - 1) / per, kGroups);
+    const size_t bytes = ((size_t)(a.head_dim + 3) / 4 * 4 + 2 * (size_t)per * (a.rotary_dim / 2)) * sizeof(float2);
+    return launch(k_norm_rotate<PREC, P, N>, dim3((unsigned)grid), dim3(kThreads), bytes, lc, a, lanes_log2, (int)per);
 }
 
 template <int PREC>

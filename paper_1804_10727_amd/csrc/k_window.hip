@@ -16,6 +16,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStepRows = 16;                      // query rows of a segment and key/value head that the step kernel takes
+constexpr int kMostSplits = 64;                    // parts of a list of keys: a wave joins them, a lane each
 constexpr int kTileRows = 128;                     // query rows of a workgroup of the tile kernel
 
 // The keys that query positions first .. last see, as a list in order of position: first tokens of the stream, then from the beginning of
@@ -158,7 +159,7 @@ template <int PREC, int DP> struct StepShape {
 };
 
 template <int PREC, int DP>
-__global__ void __launch_bounds__(256) k_window_step(idf_window_args a, int splits, bool append)
+__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_window_step(idf_window_args a, int splits, bool append)
 {
     using M = Mfma<PREC>;
     using T = typename M::T;
@@ -527,31 +528,53 @@ __global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 
         }
 }
 
-// Splits joined: four values of a row by a thread.
+// Splits joined.  A workgroup takes a row, each of its waves every fourth split: its lanes first the maximum and sum of a split each, whose
+// shares then go from lane to lane while a lane adds up four values of the row, with splits side by side where the row leaves lanes.  All of
+// a wave's reads are on their way together: one after the other, each would wait for memory.
 template <int PREC>
-__global__ void __launch_bounds__(256) k_window_join(idf_window_args a, int splits)
+__global__ void __launch_bounds__(256) k_window_join(idf_window_args a, int splits, int lanes_log2)
 {
     using T = typename Elem<PREC>::type;
+    constexpr int kAhead = 8;
+    __shared__ __align__(16) float sums[4][256];
     const Segment g = segment_of(a, blockIdx.y, a.starts);
     const Partial part = partial_of(a, splits);
-    const int per_row = a.head_dim / 4;
-    const int64_t n = (int64_t)g.len * a.heads_q * per_row, step = a.n_tokens * a.heads_q;
-    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < n; x += (int64_t)gridDim.x * 256) {
-        const int64_t r = x / per_row, t = r / a.heads_q, token = g.begin + t;
-        const int c = (int)(x - r * per_row) * 4, h = (int)(r - t * a.heads_q);
-        const int64_t row = token * a.heads_q + h;
-        float top = -__FLT_MAX__, l = 0.f;
-        for (int s = 0; s < splits; ++s) top = fmaxf(top, part.ml[2 * (row + s * step)]);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c = (lane & ((1 << lanes_log2) - 1)) * 4, first = wave + 4 * (lane >> lanes_log2), step = 4 * (64 >> lanes_log2);
+    const int64_t n = (int64_t)g.len * a.heads_q, apart = a.n_tokens * a.heads_q;
+    for (int64_t x = blockIdx.x; x < n; x += gridDim.x) {
+        const int64_t t = x / a.heads_q, token = g.begin + t, row = token * a.heads_q + (x - t * a.heads_q);
+        float m = -__FLT_MAX__, l = 0.f;
+        if (lane < splits) { m = part.ml[2 * (row + lane * apart)]; l = part.ml[2 * (row + lane * apart) + 1]; }
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < splits; ++s) {
-            const float fade = __builtin_amdgcn_exp2f(part.ml[2 * (row + s * step)] - top);
-            l += fade * part.ml[2 * (row + s * step) + 1];
-            v += fade * *(const f32x4 *)(part.o + (row + s * step) * a.head_dim + c);
+        float share = 0.f, sum = 0.f;
+        for (int s0 = 0; s0 < splits; s0 += kAhead * step) {
+            f32x4 in[kAhead];
+#pragma unroll
+            for (int y = 0; y < kAhead; ++y) {
+                const int s = s0 + first + y * step;
+                in[y] = s < splits && c < a.head_dim ? *(const f32x4 *)(part.o + (row + s * apart) * a.head_dim + c) : f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+            if (s0 == 0) {
+                share = __builtin_amdgcn_exp2f(m - wave_max(m));
+                sum = wave_sum(lane < splits ? l * share : 0.f);
+            }
+#pragma unroll
+            for (int y = 0; y < kAhead; ++y) v += __shfl(share, s0 + first + y * step) * in[y];
         }
+        for (int mask = 1 << lanes_log2; mask < 64; mask <<= 1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], mask);
+        __syncthreads();                           // (the row before has been read)
+        if (first < 4 && c < a.head_dim) *(f32x4 *)(sums[wave] + c) = v;
+        __syncthreads();
+        if (threadIdx.x * 4 >= a.head_dim) continue;
+        const int at = threadIdx.x * 4;
+        v = *(const f32x4 *)(sums[0] + at) + *(const f32x4 *)(sums[1] + at) + *(const f32x4 *)(sums[2] + at) + *(const f32x4 *)(sums[3] + at);
         Pack<T, 4> w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w.v[e] = Elem<PREC>::from_f32(v[e] / l);
-        *(Pack<T, 4> *)((T *)a.out.base + token * a.out.token_stride + h * a.out.head_stride + c) = w;
+        for (int e = 0; e < 4; ++e) w.v[e] = Elem<PREC>::from_f32(v[e] / sum);
+        *(Pack<T, 4> *)((T *)a.out.base + token * a.out.token_stride + (x - t * a.heads_q) * a.out.head_stride + at) = w;
     }
 }
 
@@ -586,7 +609,7 @@ Plan plan_of(const idf_window_args &a)
     const int64_t keys = (a.k_ring ? std::min<int64_t>(a.window, a.slots) : 0) + a.sinks + std::min<int64_t>(a.max_tokens, a.window);
     // two workgroups for every compute unit, and some rounds of keys for each of them
     const int64_t least = p.step ? 256 : 512;
-    p.splits = (int)std::max<int64_t>(1, std::min((512 + pairs - 1) / pairs, keys / least));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(512 + pairs - 1) / pairs, keys / least, kMostSplits}));
     if (pairs >= 384) p.splits = 1;
     return p;
 }
@@ -608,8 +631,9 @@ hipError_t by_dim(const idf_window_args &a, const LaunchCtx &lc)
     const Plan p = plan_of(a);
     hipError_t e = a.head_dim <= 64 ? attend<PREC, 64>(a, p, lc) : a.head_dim <= 96 ? attend<PREC, 96>(a, p, lc) : a.head_dim <= 128 ? attend<PREC, 128>(a, p, lc) : attend<PREC, 256>(a, p, lc);
     if (e == hipSuccess && p.splits > 1) {
-        const int64_t n = a.max_tokens * a.heads_q * (a.head_dim / 4);
-        e = launch(k_window_join<PREC>, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 4096), a.n_segments), dim3(256), 0, lc, a, p.splits);
+        int lanes_log2 = 0;
+        while (4 << lanes_log2 < a.head_dim) ++lanes_log2;
+        e = launch(k_window_join<PREC>, dim3((unsigned)std::min<int64_t>(a.max_tokens * a.heads_q, 8192), a.n_segments), dim3(256), 0, lc, a, p.splits, lanes_log2);
     }
     if (e == hipSuccess && a.k_ring && !(p.step && a.max_tokens == 1)) {
         const int elem16 = Elem<PREC>::VL, row16 = a.heads_kv * a.head_dim / elem16;
