@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_window_step(idf_wind
     {
         const T *src = (const T *)a.q.base + (g.begin + my_t) * a.q.token_stride + my_h * a.q.head_stride;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) q[s] = col < rows && 32 * s + 8 * grp < a.head_dim ? M::load(src + 32 * s + 8 * grp) : M::zero();
+        for (int s = 0; s < KS; ++s) q[s] = col < rows ? M::load(src + 32 * s + 8 * grp, a.head_dim - 32 * s - 8 * grp) : M::zero();
     }
 
     T *v_lds = (T *)(lds + wave * S::WAVE_FLOATS);
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_window_step(idf_wind
         for (int t = 0; t < NT; ++t) {
             const T *src = at(kh, place_of(a, keys, min(tile * S::KEYS + 16 * t + col, keys.n - 1)));
 #pragma unroll
-            for (int s = 0; s < KS; ++s) kf[t][s] = 32 * s + 8 * grp < a.head_dim ? M::load(src + 32 * s + 8 * grp) : M::zero();
+            for (int s = 0; s < KS; ++s) kf[t][s] = M::load(src + 32 * s + 8 * grp, a.head_dim - 32 * s - 8 * grp);
         }
 #pragma unroll
         for (int j = 0; j < S::LOADS; ++j) {
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 
     {
         const T *src = (const T *)a.q.base + token * a.q.token_stride + my_h * a.q.head_stride;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) q[s] = 16 * s + 8 * half < a.head_dim ? M::load(src + 16 * s + 8 * half) : M::zero();
+        for (int s = 0; s < KS; ++s) q[s] = M::load(src + 16 * s + 8 * half, a.head_dim - 16 * s - 8 * half);
     }
     // Rounds whose entries lie behind each other, all own tokens or all in the ring without its end between them, are read from one address on;
     // the others (first tokens, the ring's end, the list's) look for the place of each entry.

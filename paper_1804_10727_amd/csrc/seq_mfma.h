@@ -21,6 +21,8 @@ template <> struct Mfma<IDF_PREC_BF16> {
     static constexpr int VL = 8;
     static __device__ __forceinline__ frag zero() { return __builtin_bit_cast(frag, i32x4{0, 0, 0, 0}); }
     static __device__ __forceinline__ frag load(const T *p) { return *(const frag *)p; }
+    // of a row that has n values from p on (n a multiple of VL; zeros behind them, nothing read there)
+    static __device__ __forceinline__ frag load(const T *p, int n) { return n > 0 ? load(p) : zero(); }
     // D[16][16] += A[16][32] B[32][16]: a lane holds row (A) or column (B) lane % 16 and, of the summed axis, 8 (lane / 16) + 0 .. 7; of D column
     // lane % 16, rows 4 (lane / 16) + 0 .. 3
     static __device__ __forceinline__ f32x4 mma16(const frag &a, const frag &b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -42,6 +44,13 @@ template <> struct Mfma<IDF_PREC_F32> {
     static __device__ __forceinline__ frag load(const T *p)
     {
         const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    static __device__ __forceinline__ frag load(const T *p, int n)
+    {
+        f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+        if (n > 0) a = *(const f32x4 *)p;
+        if (n > 4) b = *(const f32x4 *)(p + 4);
         return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
     static __device__ __forceinline__ f32x4 mma16(const frag &a, const frag &b, f32x4 c)

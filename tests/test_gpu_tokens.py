@@ -149,6 +149,22 @@ def test_window_segments(dtype, hq, hkv, d, window, sinks, room):
     window_streams(dtype, hq, hkv, d, window, sinks, room, pushes, seed=window + d)
 
 
+@pytest.mark.parametrize("d", [4, 12, 20, 60, 68, 100, 132, 252])
+def test_window_odd_heads(d):
+    """Float32 heads whose end lies inside a fragment of eight values: what lies behind it, here NaN, is not read."""
+    g = torch.Generator().manual_seed(d)
+    pushes = [[1, 1], [13, 2], [1, 1], [90, 200], [3, 1], [1, 1]]
+    window_streams(torch.float32, 2, 1, d, 30, 2, 0, pushes, seed=d)
+    for lengths in ((1, 1), (4, 3), (70, 9)):
+        n = sum(lengths)
+        q, k, v = (torch.full((n, h, d + 4), float("nan"), device=DEV)[:, :, :d].copy_(normal(g, n, h, d, dtype=torch.float32)) for h in (3, 1, 1))
+        offsets = torch.tensor((0,) + lengths).cumsum(0)
+        out = idf.window_attend(q, k, v, window=30, offsets=offsets.to(DEV), max_tokens=max(lengths))
+        for at, m in zip(offsets.tolist(), lengths):
+            want, size, score = oracle.Attention(30, 0, 1 / np.sqrt(d)).push(*(f64(x[at:at + m]) for x in (q, k, v)))
+            within(out[at:at + m], want, W * np.abs(want) + (4 * (d + 8) * W * score[..., None] + 2 * 46 * W) * size)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
 def test_window_long(dtype):
     """Few rows on a long axis, and many of them."""
