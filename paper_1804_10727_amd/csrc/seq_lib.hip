@@ -11,7 +11,7 @@ namespace {
 
 constexpr int kMostSegments = 65535;               // a launch's second or third axis
 constexpr int kMostHeads = 1024;
-constexpr int64_t kMostPairs = 1 << 23;            // segments times key/value heads: a launch's first axis
+constexpr int64_t kMostPairs = 1 << 23;            // segments times key/value heads (times columns by 64): a launch's first axis, 2^32 threads
 constexpr int64_t kMostRows = 65535 * 128;         // query rows of a segment and key/value head: its second
 constexpr int64_t kMostSlots = 1 << 30;            // lists of keys are counted in 32 bits
 
@@ -70,6 +70,8 @@ int check_decay(const idf_decay_args *a)
     const int vl = a->precision == IDF_PREC_F32 ? 4 : 8;
     if (a->dim_k < vl || a->dim_k > 256 || a->dim_k % vl || a->dim_v < vl || a->dim_v % vl || a->dim_v > 4096)
         return fail(IDF_EUNSUPPORTED, "heads of %d and %d values", a->dim_k, a->dim_v);
+    if ((int64_t)a->n_segments * a->heads_kv * ((a->dim_v + 63) / 64) > kMostPairs)
+        return fail(IDF_EUNSUPPORTED, "%d segments with %d heads of %d values: more than a launch takes", a->n_segments, a->heads_kv, a->dim_v);
     if (((uintptr_t)a->state_in | (uintptr_t)a->state_out) % 16) return fail(IDF_EUNSUPPORTED, "states have to be 16-byte aligned");
     return IDF_OK;
 }

@@ -74,6 +74,13 @@ def test_decay_refuses(kw, want):
     assert code("idf_decay_attend", decay_args(**kw)) == want and idf.load_library().idf_last_error()
 
 
+def test_decay_refuses_more_workgroups_than_a_launch_takes():
+    many = dict(heads_q=1024, heads_kv=1024, n_segments=8192, n_streams=8192, n_tokens=8192, max_tokens=1)
+    assert code("idf_decay_attend", decay_args(**many, dim_v=128)) == -5
+    nb = C.c_size_t()
+    assert idf.load_library().idf_decay_workspace(C.byref(decay_args(**many, dim_v=64)), C.byref(nb)) == 0 and nb.value == 0
+
+
 def test_null_arguments_and_nothing_to_do():
     for fn in ("idf_norm_rotate", "idf_window_attend", "idf_decay_attend", "idf_window_workspace", "idf_decay_workspace"):
         assert code(fn, None) == -1
