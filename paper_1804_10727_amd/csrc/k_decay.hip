@@ -1,5 +1,6 @@
 // Linear attention with a decay per head (idf_decay_attend).
 #include <algorithm>
+#include <type_traits>
 
 #include "idf.h"
 #include "seq_mfma.h"
@@ -97,8 +98,8 @@ struct Parts {
 __device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
 __device__ __forceinline__ float log2_of(float log_decay) { return fmaxf(log_decay * 1.4426950408889634f, -1e30f); }      // (a decay to nothing: times zero stays zero)
 
-template <int PREC, int DK, int NW>
-__global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 && NW == 4) ? 2 : 1) k_decay_chunks(idf_decay_args a, Parts parts, bool states_only, int blocks)
+template <int PREC, int DK, int NW, bool states_only>
+__global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 && NW == 4) ? 2 : 1) k_decay_chunks(idf_decay_args a, Parts parts, int blocks)
 {
     using M = Mfma<PREC>;
     using E = Elem<PREC>;
@@ -108,7 +109,7 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
     constexpr int K_STRIDE = DK + VL, V_STRIDE = 32 * NW + (PREC == IDF_PREC_BF16 ? 16 : 4);
     constexpr int K_LOADS = kChunk * DK / VL / THREADS, V_LOADS = kChunk * 32 / VL / 64;
     constexpr int BF = PREC == IDF_PREC_BF16;
-    constexpr int SCORE_STRIDE = kChunk + 4;
+    constexpr int SCORE_STRIDE = kChunk + 4, STAGES = states_only ? 2 : 1;
     __shared__ __align__(16) T k_both[2][kChunk * K_STRIDE], q_both[2][kChunk * K_STRIDE], v_both[2][kChunk * V_STRIDE];
     __shared__ __align__(16) float score[kChunk * SCORE_STRIDE], fresh[2 * kChunk];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
@@ -122,9 +123,11 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
     const int queries = a.heads_q / a.heads_kv;
     const int c0 = block * 32 * NW;                                           // the workgroup's first column
     const float l2 = log2_of(a.log_decay[kv]);
-    const bool own = c0 + 32 * wave + col < a.dim_v;
+    const int my_c = c0 + 32 * wave + ((col & 0x13) | (col & 4) << 1 | (col & 8) >> 1);
+    const bool own = my_c < a.dim_v;
 
-    // row e of a state's tile: 16 (e / 8) + 8 half + e % 8, so that eight registers are eight rows in order
+    // row e of a state's tile: 16 (e / 8) + 8 half + e % 8, so that eight registers are eight rows in order; columns 4 .. 7 and 8 .. 11 of
+    // each 16 are in each other's place, so that of an output, too, a lane has eight values in order
     f32x16 s[KT];
     const int64_t state = ((int64_t)g.ring * a.heads_kv + kv) * a.dim_k * a.dim_v;
     float *mid = parts.states ? parts.states + ((int64_t)(seg * a.heads_kv + kv) * parts.n + part) * a.dim_k * a.dim_v : nullptr;
@@ -139,7 +142,7 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int r = 32 * t + 16 * (e / 8) + 8 * half + e % 8;
-                const float x = from[min(r, a.dim_k - 1) * a.dim_v + c0 + 32 * wave + col];
+                const float x = from[min(r, a.dim_k - 1) * a.dim_v + my_c];
                 s[t][e] = r < a.dim_k ? x : 0.f;
             }
 
@@ -157,64 +160,71 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
     const float fade_short = uniform((float)exp2((double)((max(len, 1) - 1) % kChunk + 1) * (double)l2));        // (the last chunk of the part may be a short one)
 
     // A step is a chunk for one of the heads.  While one is worked on, what the next one needs is written from registers into the other half
-    // of LDS, and what the one behind it needs is asked for.
+    // of LDS, and what the one behind it needs is on its way; where nothing is stored between the loads, what the next but one needs, too.
     const T *kb = (const T *)a.k.base + (g.begin + first) * a.k.token_stride + kv * a.k.head_stride;
     const T *vb = (const T *)a.v.base + (g.begin + first) * a.v.token_stride + kv * a.v.head_stride;
     const T *qb = (const T *)a.q.base + (g.begin + first) * a.q.token_stride + kv * queries * a.q.head_stride;
     const int heads = states_only ? 1 : queries;
     struct Step { int t0, h; };
     auto next_of = [&](Step x) { return x.h + 1 < heads ? Step{x.t0, x.h + 1} : Step{x.t0 + kChunk, 0}; };
-    i32x4 kr[K_LOADS], qr[K_LOADS], vr[V_LOADS];
-    auto load = [&](const Step &x) IDF_INLINE {
-        if (x.t0 >= len) return;
+    // Loads are issued whether there is something to load or not, from the nearest place that there is, and become zeros on their way into
+    // LDS: behind a branch the compiler would have to wait for all of them instead of the oldest.
+    i32x4 kr[STAGES][K_LOADS], qr[STAGES][K_LOADS], vr[STAGES][V_LOADS];
+    auto load = [&](const Step &x, int stage) IDF_INLINE {
+        if (STAGES == 1 && x.t0 >= len) return;
 #pragma unroll
         for (int y = 0; y < K_LOADS; ++y) {
             const int piece = y * THREADS + threadIdx.x, r = piece / (DK / VL), c = (piece - r * (DK / VL)) * VL;
-            const bool there = x.t0 + r < len && c < a.dim_k;
-            if (x.h == 0) kr[y] = there ? *(const i32x4 *)(kb + (int64_t)(x.t0 + r) * a.k.token_stride + c) : i32x4{0, 0, 0, 0};
-            if (!states_only) qr[y] = there ? *(const i32x4 *)(qb + (int64_t)(x.t0 + r) * a.q.token_stride + x.h * a.q.head_stride + c) : i32x4{0, 0, 0, 0};
+            if constexpr (STAGES == 2) {
+                kr[stage][y] = *(const i32x4 *)(kb + (int64_t)min(x.t0 + r, len - 1) * a.k.token_stride + min(c, a.dim_k - VL));
+            } else {
+                const bool there = x.t0 + r < len && c < a.dim_k;
+                if (x.h == 0) kr[stage][y] = there ? *(const i32x4 *)(kb + (int64_t)(x.t0 + r) * a.k.token_stride + c) : i32x4{0, 0, 0, 0};
+                qr[stage][y] = there ? *(const i32x4 *)(qb + (int64_t)(x.t0 + r) * a.q.token_stride + x.h * a.q.head_stride + c) : i32x4{0, 0, 0, 0};
+            }
         }
         if (x.h == 0)
 #pragma unroll
             for (int y = 0; y < V_LOADS; ++y) {
-                const int piece = y * THREADS + threadIdx.x, r = piece / (32 * NW / VL), c = (piece - r * (32 * NW / VL)) * VL;
-                vr[y] = x.t0 + r < len && c0 + c < a.dim_v ? *(const i32x4 *)(vb + (int64_t)(x.t0 + r) * a.v.token_stride + c0 + c) : i32x4{0, 0, 0, 0};
+                const int piece = y * THREADS + threadIdx.x, r = piece / (32 * NW / VL), c = c0 + (piece - r * (32 * NW / VL)) * VL;
+                if constexpr (STAGES == 2) vr[stage][y] = *(const i32x4 *)(vb + (int64_t)min(x.t0 + r, len - 1) * a.v.token_stride + min(c, a.dim_v - VL));
+                else vr[stage][y] = x.t0 + r < len && c < a.dim_v ? *(const i32x4 *)(vb + (int64_t)(x.t0 + r) * a.v.token_stride + c) : i32x4{0, 0, 0, 0};
             }
     };
-    auto store = [&](const Step &x, int step) IDF_INLINE {
-        if (x.t0 >= len) return;
+    auto store = [&](const Step &x, int step, int stage) IDF_INLINE {
+        if (STAGES == 1 && x.t0 >= len) return;
         T *k_to = k_both[x.t0 / kChunk & 1], *v_to = v_both[x.t0 / kChunk & 1], *q_to = q_both[step & 1];
+        const i32x4 none = {0, 0, 0, 0};
 #pragma unroll
         for (int y = 0; y < K_LOADS; ++y) {
             const int piece = y * THREADS + threadIdx.x, r = piece / (DK / VL), c = (piece - r * (DK / VL)) * VL;
-            if (x.h == 0) *(i32x4 *)(k_to + r * K_STRIDE + c) = kr[y];
-            if (!states_only) *(i32x4 *)(q_to + r * K_STRIDE + c) = qr[y];
+            const bool there = STAGES == 1 || (x.t0 + r < len && c < a.dim_k);
+            if (x.h == 0) *(i32x4 *)(k_to + r * K_STRIDE + c) = there ? kr[stage][y] : none;
+            if (!states_only) *(i32x4 *)(q_to + r * K_STRIDE + c) = there ? qr[stage][y] : none;
         }
         if (x.h == 0)
 #pragma unroll
             for (int y = 0; y < V_LOADS; ++y) {
                 const int piece = y * THREADS + threadIdx.x, r = piece / (32 * NW / VL), c = (piece - r * (32 * NW / VL)) * VL;
-                *(i32x4 *)(v_to + r * V_STRIDE + c) = vr[y];
+                *(i32x4 *)(v_to + r * V_STRIDE + c) = STAGES == 1 || (x.t0 + r < len && c0 + c < a.dim_v) ? vr[stage][y] : none;
             }
     };
-    Step now = {0, 0}, ahead = next_of(now);
-    load(now);
-    store(now, 0);
-    load(ahead);
-    for (int step = 0; now.t0 < len; ++step) {
+    Step now = {0, 0}, ahead = next_of(now), beyond = next_of(ahead);
+    auto step_of = [&](int step, int stage) IDF_INLINE {
         __syncthreads();
-        store(ahead, step + 1);
-        const Step then = next_of(ahead);
-        load(then);
+        store(ahead, step + 1, stage);
+        const Step then = next_of(beyond);
+        load(STAGES == 2 ? then : beyond, stage);
         const int t0 = now.t0, n = min(kChunk, len - t0), h = now.h;
         const T *k_lds = k_both[t0 / kChunk & 1], *v_lds = v_both[t0 / kChunk & 1], *q_lds = q_both[step & 1];
         now = ahead;
-        ahead = then;
+        ahead = beyond;
+        beyond = then;
 
         // values of this wave's columns along the tokens: register x of piece p is token 16 p + 8 (x / 4) + 4 half + x % 4
         frag v[2];
 #pragma unroll
-        for (int p = 0; p < 2; ++p) v[p] = read_column(v_lds, V_STRIDE, 32 * wave + (lane & 16), 16 * p + 4 * half, 16 * p + 8 + 4 * half);
+        for (int p = 0; p < 2; ++p) v[p] = read_rows_swapped(v_lds, V_STRIDE, 32 * wave + (lane & 16), 16 * p + 4 * half, 16 * p + 8 + 4 * half);
 
         if (!states_only) {
                 f32x16 w, o;
@@ -268,22 +278,23 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
                         if (j > col) continue;
                         qk *= __builtin_amdgcn_exp2f((float)(col - j) * l2) * a.scale;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] += qk * E::to_f32(v_lds[j * V_STRIDE + 32 * wave + 8 * (e / 4) + 4 * half + e % 4]);
+                        for (int e = 0; e < 16; ++e) o[e] += qk * E::to_f32(v_lds[j * V_STRIDE + 32 * wave + 16 * (e / 8) + 8 * half + e % 8]);
                     }
                 }
                 if (col < n) {
-                    T *out = (T *)a.out.base + (g.begin + first + t0 + col) * a.out.token_stride + (kv * queries + h) * a.out.head_stride + c0 + 32 * wave + 4 * half;
+                    const int c = c0 + 32 * wave + 8 * half;
+                    T *out = (T *)a.out.base + (g.begin + first + t0 + col) * a.out.token_stride + (kv * queries + h) * a.out.head_stride + c;
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        Pack<T, 4> pk;
+                    for (int e = 0; e < 16; e += VL) {
+                        Pack<T, VL> pk;
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) pk.v[x] = E::from_f32(o[e + x]);
-                        if (c0 + 32 * wave + 2 * e + 4 * half < a.dim_v) *(Pack<T, 4> *)(out + 2 * e) = pk;
+                        for (int x = 0; x < VL; ++x) pk.v[x] = E::from_f32(o[e + x]);
+                        if (c + 16 * (e / 8) + e % 8 < a.dim_v) *(Pack<T, VL> *)(out + 16 * (e / 8) + e % 8) = pk;
                     }
                 }
             }
 
-        if (h + 1 < heads) continue;
+        if (h + 1 < heads) return;
         float fade = fade_short;
         if (n == kChunk) {
             fade = uniform((float)(whole * (2.0 - drift)));                   // (2 - x is 1 / x so near to one)
@@ -321,6 +332,17 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
                 for (int y = 0; y < (BF ? 3 : 1); ++y) s[t] = M::mma32(k, pieces[y], s[t]);
             }
         }
+    };
+    if (len > 0) {
+        load(now, 0);
+        store(now, 0, 0);
+        load(ahead, 0);
+        if (STAGES == 2) load(beyond, STAGES - 1);
+        for (int step = 0; now.t0 < len; step += STAGES) {
+            step_of(step, 0);
+            if (STAGES == 1 || now.t0 >= len) continue;
+            step_of(step + 1, STAGES - 1);
+        }
     }
 
     float *to = states_only ? mid : last && a.state_out ? a.state_out + state : nullptr;
@@ -332,7 +354,7 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 &&
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int r = 32 * t + 16 * (e / 8) + row + e % 8;
-                if (r < a.dim_k) to[r * a.dim_v + c0 + 32 * wave + col] = s[t][e];
+                if (r < a.dim_k) to[r * a.dim_v + my_c] = s[t][e];
             }
 }
 
@@ -379,18 +401,18 @@ hipError_t chunks(const idf_decay_args &a, const LaunchCtx &lc)
     Parts p = parts_of(a);
     const int waves = a.dim_v <= 64 ? 2 : 4, blocks = (a.dim_v + 32 * waves - 1) / (32 * waves);
     const dim3 grid((unsigned)((int64_t)a.n_segments * a.heads_kv * blocks), p.n);
-    auto go = [&](bool states_only) {
-        return waves == 2 ? launch(k_decay_chunks<PREC, DK, 2>, grid, dim3(128), 0, lc, a, p, states_only, blocks)
-                          : launch(k_decay_chunks<PREC, DK, 4>, grid, dim3(256), 0, lc, a, p, states_only, blocks);
+    auto go = [&](auto states_only) {
+        constexpr bool S = decltype(states_only)::value;
+        return waves == 2 ? launch(k_decay_chunks<PREC, DK, 2, S>, grid, dim3(128), 0, lc, a, p, blocks) : launch(k_decay_chunks<PREC, DK, 4, S>, grid, dim3(256), 0, lc, a, p, blocks);
     };
     hipError_t e = hipSuccess;
     if (p.n > 1) {
         p.states = (float *)a.workspace;
-        e = go(true);
+        e = go(std::true_type{});
         if (e == hipSuccess)
             e = launch(k_decay_scan, dim3((unsigned)((a.dim_k * a.dim_v + 1023) / 1024), a.n_segments * a.heads_kv), dim3(256), 0, lc, a, p);
     }
-    return e == hipSuccess ? go(false) : e;
+    return e == hipSuccess ? go(std::false_type{}) : e;
 }
 
 template <int PREC>
