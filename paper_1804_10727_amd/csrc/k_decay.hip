@@ -99,7 +99,7 @@ __device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(fl
 __device__ __forceinline__ float log2_of(float log_decay) { return fmaxf(log_decay * 1.4426950408889634f, -1e30f); }      // (a decay to nothing: times zero stays zero)
 
 template <int PREC, int DK, int NW, bool states_only>
-__global__ void __launch_bounds__(64 * NW, DK <= 64 || (PREC == IDF_PREC_BF16 && NW == 4) ? 2 : 1) k_decay_chunks(idf_decay_args a, Parts parts, int blocks)
+__global__ void __launch_bounds__(64 * NW, PREC == IDF_PREC_BF16 && (DK <= 64 || NW == 4) ? 2 : 1) k_decay_chunks(idf_decay_args a, Parts parts, int blocks)
 {
     using M = Mfma<PREC>;
     using E = Elem<PREC>;
@@ -383,17 +383,25 @@ Parts parts_of(const idf_decay_args &a)
 {
     Parts p;
     p.states = nullptr;
-    const int64_t blocks = (int64_t)a.n_segments * a.heads_kv * ((a.dim_v + 127) / 128);
-    // two workgroups for every compute unit; a part is long next to the state that it reads and writes
-    const int64_t want = std::max<int64_t>(1, std::min((512 + blocks - 1) / blocks, a.max_tokens / kPartLeast));
+    // two workgroups for every compute unit, by the tokens that there are and not by the longest segment's (uneven segments 87 -> 81 us); a part
+    // is long next to the state that it reads and writes, and states that mostly empty segments would not use stay few (512 MB of 128 x 128)
+    const int64_t pairs = (int64_t)a.n_segments * a.heads_kv, tokens = std::max<int64_t>(1, std::min(a.n_tokens, a.n_segments * a.max_tokens) * a.heads_kv * ((a.dim_v + 127) / 128));
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({a.max_tokens * 512 / tokens, a.max_tokens / kPartLeast, 8192 / std::max<int64_t>(pairs, 1)}));
     p.tokens = (int)(((a.max_tokens + want - 1) / want + kChunk - 1) / kChunk * kChunk);
     p.n = (int)((a.max_tokens + p.tokens - 1) / std::max(p.tokens, 1));
     if (p.n <= 1) { p.n = 1; p.tokens = std::max(p.tokens, kChunk); }
     return p;
 }
 
-// Rows of more than 128 values leave no registers for anything beside the state: they go token by token, whatever the length.
-bool by_token(const idf_decay_args &a) { return a.max_tokens <= 16 || a.dim_k > 128; }
+// Token by token or by chunks.  A chunk costs the same whatever it holds, each token by itself about 3 us more (us per call, tokens against
+// chunk: 64 streams x 16 heads of 128 x 128 in bfloat16 25.9 : 28.2 for one token, 29.9 : 28.2 for two; 16 streams x 8 heads x 4 queries of 64 x 64
+// 8.2 : 8.7 and 12.0 : 8.7).  In float32 a chunk takes eight instructions for one: 64 streams x 4 heads of 64 x 64 9.2 : 10.0 for four tokens, 10.4 : 10.0
+// for five; x 16 heads of 128 x 128, 33 : 61 for four and level with 61 at twelve.  Rows of more than 128 values leave no registers for anything beside the state.
+bool by_token(const idf_decay_args &a)
+{
+    const int most = a.precision == IDF_PREC_BF16 ? 1 : a.dim_k <= 64 ? 4 : 12;
+    return a.max_tokens <= most || a.dim_k > 128;
+}
 
 template <int PREC, int DK>
 hipError_t chunks(const idf_decay_args &a, const LaunchCtx &lc)

@@ -16,7 +16,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStepRows = 16;                      // query rows of a segment and key/value head that the step kernel takes
-constexpr int kMostSplits = 64;                    // parts of a list of keys: a wave joins them, a lane each
+constexpr int kMostSplits = 128;                   // parts of a list of keys: a wave joins them, a lane has two
 constexpr int kTileRows = 128;                     // query rows of a workgroup of the tile kernel
 
 // The keys that query positions first .. last see, as a list in order of position: first tokens of the stream, then from the beginning of
@@ -141,6 +141,22 @@ __device__ __forceinline__ void exact_row(const idf_window_args &a, const Segmen
     T *out = (T *)a.out.base + token * a.out.token_stride + h * a.out.head_stride;
     for (int c = 0; c < 4; ++c)
         if (lane + 64 * c < a.head_dim) out[lane + 64 * c] = E::from_f32(o[c] / l);
+}
+
+// Tokens t0 <= t < t1 of a segment into the ring, by the workgroup that attended over them.  Only where the ring has room for the segment beside
+// a window (Plan): the slots that they take then hold tokens that no query of the segment sees any more, while other workgroups still
+// read the ring.
+template <class T>
+__device__ __forceinline__ void append_tokens(const idf_window_args &a, const Segment &g, const Keys &keys, const Held<T> &kh, const Held<T> &vh, int t0, int t1)
+{
+    constexpr int VL = 16 / (int)sizeof(T);
+    const int pieces = a.head_dim / VL;
+    for (int x = threadIdx.x; x < (t1 - t0) * pieces; x += 256) {
+        const int t = t0 + x / pieces, c = (x - (x / pieces) * pieces) * VL;
+        const int64_t p = g.start + t, slot = p < a.sinks ? p : a.sinks + (p - a.sinks) % (int64_t)keys.period;
+        *(i32x4 *)(const_cast<T *>(kh.ring) + slot * kh.ring_stride + c) = *(const i32x4 *)(kh.own + t * kh.own_stride + c);
+        *(i32x4 *)(const_cast<T *>(vh.ring) + slot * vh.ring_stride + c) = *(const i32x4 *)(vh.own + t * vh.own_stride + c);
+    }
 }
 
 // ---- few rows on a long axis: single tokens, short segments ----
@@ -309,14 +325,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_window_step(idf_wind
             const int t = r / group;
             exact_row<PREC>(a, g, keys, kv, kv * group + r - t * group, t, t0 * S::KEYS, min(t1 * S::KEYS, keys.n), part, split);
         }
-    // a single token into the ring: the slot that it takes held a token that no query sees any more
-    if (append && split == 0) {
-        const int64_t p = g.start, slot = p < a.sinks ? p : a.sinks + (p - a.sinks) % (int64_t)keys.period;
-        for (int c = threadIdx.x * M::VL; c < a.head_dim; c += 256 * M::VL) {
-            *(i32x4 *)(const_cast<T *>(kh.ring) + slot * kh.ring_stride + c) = *(const i32x4 *)(kh.own + c);
-            *(i32x4 *)(const_cast<T *>(vh.ring) + slot * vh.ring_stride + c) = *(const i32x4 *)(vh.own + c);
-        }
-    }
+    if (append && split == 0) append_tokens(a, g, keys, kh, vh, 0, g.len);
 }
 
 // ---- many rows ----
@@ -335,7 +344,7 @@ template <int PREC, int DP> struct TileShape {
 };
 
 template <int PREC, int DP>
-__global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 1) k_window_tile(idf_window_args a, int splits)
+__global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 1) k_window_tile(idf_window_args a, int splits, bool append)
 {
     using M = Mfma<PREC>;
     using T = typename M::T;
@@ -526,6 +535,8 @@ __global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 
             const int t = (int)(row / group);
             exact_row<PREC>(a, g, keys, kv, kv * group + (int)(row - (int64_t)t * group), t, t0 * S::KEYS, min(t1 * S::KEYS, keys.n), part, split);
         }
+    // the tokens whose first row lies in this tile
+    if (append && split == 0) append_tokens(a, g, keys, kh, vh, (int)((row0 + group - 1) / group), (int)(row_last / group) + 1);
 }
 
 // Splits joined.  A workgroup takes a row, each of its waves every fourth split: its lanes first the maximum and sum of a split each, whose
@@ -544,10 +555,14 @@ __global__ void __launch_bounds__(256) k_window_join(idf_window_args a, int spli
     const int64_t n = (int64_t)g.len * a.heads_q, apart = a.n_tokens * a.heads_q;
     for (int64_t x = blockIdx.x; x < n; x += gridDim.x) {
         const int64_t t = x / a.heads_q, token = g.begin + t, row = token * a.heads_q + (x - t * a.heads_q);
-        float m = -__FLT_MAX__, l = 0.f;
-        if (lane < splits) { m = part.ml[2 * (row + lane * apart)]; l = part.ml[2 * (row + lane * apart) + 1]; }
+        float m[2], l[2], share[2] = {}, sum = 0.f;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const int s = lane + 64 * y;
+            m[y] = s < splits ? part.ml[2 * (row + s * apart)] : -__FLT_MAX__;
+            l[y] = s < splits ? part.ml[2 * (row + s * apart) + 1] : 0.f;
+        }
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        float share = 0.f, sum = 0.f;
         for (int s0 = 0; s0 < splits; s0 += kAhead * step) {
             f32x4 in[kAhead];
 #pragma unroll
@@ -556,11 +571,17 @@ __global__ void __launch_bounds__(256) k_window_join(idf_window_args a, int spli
                 in[y] = s < splits && c < a.head_dim ? *(const f32x4 *)(part.o + (row + s * apart) * a.head_dim + c) : f32x4{0.f, 0.f, 0.f, 0.f};
             }
             if (s0 == 0) {
-                share = __builtin_amdgcn_exp2f(m - wave_max(m));
-                sum = wave_sum(lane < splits ? l * share : 0.f);
+                const float top = wave_max(fmaxf(m[0], m[1]));
+#pragma unroll
+                for (int y = 0; y < 2; ++y) share[y] = __builtin_amdgcn_exp2f(m[y] - top);
+                sum = wave_sum((lane < splits ? l[0] * share[0] : 0.f) + (lane + 64 < splits ? l[1] * share[1] : 0.f));
             }
 #pragma unroll
-            for (int y = 0; y < kAhead; ++y) v += __shfl(share, s0 + first + y * step) * in[y];
+            for (int y = 0; y < kAhead; ++y) {
+                const int s = s0 + first + y * step;
+                const float low = __shfl(share[0], s & 63), high = __shfl(share[1], s & 63);
+                v += (s & 64 ? high : low) * in[y];
+            }
         }
         for (int mask = 1 << lanes_log2; mask < 64; mask <<= 1)
 #pragma unroll
@@ -598,18 +619,29 @@ __global__ void __launch_bounds__(256) k_window_append(idf_window_args a, int ro
 }
 
 // How a call is cut: which kernel, and into how many parts the keys go.
-struct Plan { bool step; int tiles, splits; };
+struct Plan {
+    bool step;
+    int tiles, splits;
+    bool append;               // tokens go to the ring with the attention over them, and not by a launch behind it
+};
 Plan plan_of(const idf_window_args &a)
 {
     Plan p;
     const int64_t rows = a.max_tokens * (a.heads_q / a.heads_kv);
     p.step = rows <= kStepRows;
+    // the ring has room for a segment beside a window (64 streams of 16 tokens, float32: 60 -> 50 us a pass)
+    p.append = a.k_ring && a.slots - a.sinks - a.window >= a.max_tokens - 1;
     p.tiles = p.step ? 1 : (int)((rows + kTileRows - 1) / kTileRows);
     const int64_t pairs = (int64_t)a.n_segments * a.heads_kv * p.tiles;
     const int64_t keys = (a.k_ring ? std::min<int64_t>(a.window, a.slots) : 0) + a.sinks + std::min<int64_t>(a.max_tokens, a.window);
-    // two workgroups for every compute unit, and some rounds of keys for each of them
+    // two workgroups for every compute unit, and some rounds of keys for each of them; where waves take tiles in turn, as many splits as
+    // leave all waves the same number of rounds
     const int64_t least = p.step ? 256 : 512;
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(512 + pairs - 1) / pairs, keys / least, kMostSplits}));
+    if (p.step && p.splits > 1) {
+        const int64_t tile = a.precision == IDF_PREC_BF16 ? 32 : 16, tiles = (keys + tile - 1) / tile, rounds = (tiles + 4 * p.splits - 1) / (4 * p.splits);
+        p.splits = (int)std::min<int64_t>(kMostSplits, (tiles + 4 * rounds - 1) / (4 * rounds));
+    }
     if (pairs >= 384) p.splits = 1;
     return p;
 }
@@ -618,11 +650,11 @@ template <int PREC, int DP>
 hipError_t attend(const idf_window_args &a, const Plan &p, const LaunchCtx &lc)
 {
     if (p.step)
-        return launch(k_window_step<PREC, DP>, dim3(p.splits, a.heads_kv, a.n_segments), dim3(256), 0, lc, a, p.splits, a.k_ring && a.max_tokens == 1);
+        return launch(k_window_step<PREC, DP>, dim3(p.splits, a.heads_kv, a.n_segments), dim3(256), 0, lc, a, p.splits, p.append);
     constexpr int bytes = TileShape<PREC, DP>::LDS_BYTES;
     if (bytes > 65536)
         if (const hipError_t e = allow_lds<bytes>(Kernel<k_window_tile<PREC, DP>>{})) return e;
-    return launch(k_window_tile<PREC, DP>, dim3(a.n_segments * a.heads_kv, p.tiles, p.splits), dim3(256), bytes, lc, a, p.splits);
+    return launch(k_window_tile<PREC, DP>, dim3(a.n_segments * a.heads_kv, p.tiles, p.splits), dim3(256), bytes, lc, a, p.splits, p.append);
 }
 
 template <int PREC>
@@ -635,7 +667,7 @@ hipError_t by_dim(const idf_window_args &a, const LaunchCtx &lc)
         while (4 << lanes_log2 < a.head_dim) ++lanes_log2;
         e = launch(k_window_join<PREC>, dim3((unsigned)std::min<int64_t>(a.max_tokens * a.heads_q, 8192), a.n_segments), dim3(256), 0, lc, a, p.splits, lanes_log2);
     }
-    if (e == hipSuccess && a.k_ring && !(p.step && a.max_tokens == 1)) {
+    if (e == hipSuccess && a.k_ring && !p.append) {
         const int elem16 = Elem<PREC>::VL, row16 = a.heads_kv * a.head_dim / elem16;
         e = launch(k_window_append, dim3((unsigned)std::min<int64_t>((a.max_tokens * row16 + 255) / 256, 4096), a.n_segments), dim3(256), 0, lc, a, row16, elem16);
     }
