@@ -336,7 +336,7 @@ template <int PREC, int DP> struct TileShape {
     static constexpr int KEYS = PREC == IDF_PREC_BF16 ? 64 : 32;
     static constexpr int VL = Elem<PREC>::VL, ROW16 = DP / VL;
     static constexpr int K_STRIDE = DP + VL;                                  // neighbouring rows begin 16 bytes apart in the banks
-    static constexpr int V_STRIDE = DP + (PREC == IDF_PREC_BF16 ? 16 : 4);
+    static constexpr int V_STRIDE = DP + (PREC != IDF_PREC_BF16 ? 4 : DP % 64 ? 0 : 32);      // four rows by 64 bytes are read together: rows begin 16 banks apart
     static constexpr int LOADS = KEYS * ROW16 / 256;
     static_assert(KEYS * ROW16 % 256 == 0, "a round is loaded whole");
     static constexpr bool AHEAD = DP <= 128;                                  // (longer rows leave no registers for a round on its way)
