@@ -11,7 +11,8 @@ namespace {
 
 // The recurrence itself, token by token.  A wave owns 32 columns of the state of one key/value head: eight lanes side by side hold four
 // columns each, eight lanes below each other ROWS rows each, so that a token costs two multiply-adds per value of the state and a sum
-// over eight lanes per query; nothing is shared between waves.
+// over eight lanes per query; nothing is shared between waves.  Bound by memory: the state is
+// read and written once (64 streams x 16 heads of 128 x 128, a token each: 29 us, 4.7 TB/s).
 template <int PREC, int ROWS>
 __global__ void __launch_bounds__(256) k_decay_tokens(idf_decay_args a, int column_groups)
 {
@@ -84,7 +85,10 @@ __global__ void __launch_bounds__(256) k_decay_tokens(idf_decay_args a, int colu
 // go through LDS, to be read along the tokens too, the next chunk's asked for while this one's are worked on.
 //   Roundings in bfloat16: scores times decay, and the state where it meets the queries, are rounded to bfloat16 (half a step of 2^-8, as the
 // output is).  The state itself stays float32: a decayed value, 24 bits, goes into the product as three bfloat16 numbers that add up to it.
-//   Bound by memory: q, k, v and out once, k and v twice where a segment is cut into parts.
+//   Bound by memory: q, k, v and out once, k and v twice where a segment is cut into parts (one prompt of 65536 tokens, 16 heads of 128 x 128 in
+// bfloat16: 410 us, of them 140 for the states of the parts, 17 for the scan and 250 for the outputs, 4.3 TB/s; loads of the outputs' pass
+// two chunks ahead took longer, 512 us in all: between stores they are waited for all the same).  Short calls by latency: 64 streams of 16 tokens,
+// 4 heads of 64 x 64 in float32, 10 us.
 constexpr int kChunk = 32;
 constexpr int kPartLeast = 256;                    // tokens of a part of a segment, at least
 

@@ -164,7 +164,8 @@ __device__ __forceinline__ void append_tokens(const idf_window_args &a, const Se
 // A workgroup takes the at most 16 query rows of one segment and key/value head and a part of the keys; its four waves take 16 NT of them at a
 // time, in turn, each with a softmax of its own, and are joined at the end.  Keys go from memory straight into the layout of the matrix
 // instruction, values through a piece of LDS that is the wave's own, to be read along the keys; both are asked for one round ahead.  No
-// barrier but the last.  Bound by memory: every row of the ring is read once.
+// barrier but the last.  Bound by memory: every row of the ring is read once (64 streams on 4096 keys of 8 x 128 in bfloat16: 197 us, 5.5 TB/s; 64
+// streams of 16 tokens on 1000 keys of 8 x 64 in float32: 54 us, 5.1 TB/s; one stream on 16384 keys, split: 21.5 us with the join, 3.1 TB/s).
 template <int PREC, int DP> struct StepShape {
     static constexpr int NT = PREC == IDF_PREC_BF16 ? 2 : 1;                  // tiles of 16 keys
     static constexpr int KEYS = 16 * NT;
@@ -331,7 +332,11 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_window_step(idf_wind
 // ---- many rows ----
 
 // A workgroup takes 128 query rows of one segment and key/value head and walks over their keys; a wave has 32 of the rows.  Keys and values of a round
-// go through registers into LDS, the next round's being asked for while this one's are worked on.
+// go through registers into LDS, the next round's being asked for while this one's are worked on.  Bound by the vector units and the matrix cores
+// together: of 128 values a head, a round costs a wave 32 matrix instructions of 32 cycles and some 170 others, 32 of them exponentials of 16 cycles;
+// of 64 values, half the former and the same of the latter, which is why these run four waves to a SIMD (three: 273 us, four: 263, uneven
+// segments).  Two prompts of 16384 tokens, 32 heads of 128 on a window of 4096: 2060 us, 935 TFLOP/s.  Two halves of LDS with one barrier a round
+// instead of two took longer (2182 : 2158 us), reads from LDS held ahead of the products as long (2076 : 2065).
 template <int PREC, int DP> struct TileShape {
     static constexpr int KEYS = PREC == IDF_PREC_BF16 ? 64 : 32;
     static constexpr int VL = Elem<PREC>::VL, ROW16 = DP / VL;
@@ -344,7 +349,7 @@ template <int PREC, int DP> struct TileShape {
 };
 
 template <int PREC, int DP>
-__global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 1) k_window_tile(idf_window_args a, int splits, bool append)
+__global__ void __launch_bounds__(256, PREC != IDF_PREC_BF16 || DP > 128 ? 1 : DP > 64 ? 2 : 4) k_window_tile(idf_window_args a, int splits, bool append)
 {
     using M = Mfma<PREC>;
     using T = typename M::T;
@@ -452,6 +457,8 @@ __global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 
         __syncthreads();
         if (S::AHEAD && t + 1 < t1) load(t + 1);
 
+        // a wave in its products goes first: those of another on the same SIMD, in its softmax, fill what it leaves (two long prompts 2158 -> 2065 us)
+        __builtin_amdgcn_s_setprio(1);
         f32x16 st[KT];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
@@ -460,6 +467,7 @@ __global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 
 #pragma unroll
             for (int s = 0; s < KS; ++s) st[kt] = M::mma32(M::load(k_lds + (32 * kt + col) * S::K_STRIDE + 16 * s + 8 * half), q[s], st[kt]);
         }
+        __builtin_amdgcn_s_setprio(0);
         const int i0 = t * S::KEYS;
         if (!(i0 + S::KEYS - 1 <= hi_all && (i0 > lo_all || i0 + S::KEYS <= keys.n_first))) {
 #pragma unroll
@@ -494,6 +502,7 @@ __global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 
                 st[kt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][e], scale, -m));
                 l += st[kt][e];
             }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int s = 0; s < 2 * KT; ++s) {
             float w[8];
@@ -504,6 +513,7 @@ __global__ void __launch_bounds__(256, DP <= 128 && PREC == IDF_PREC_BF16 ? 2 : 
             for (int d = 0; d < DT; ++d)
                 o[d] = M::mma32(read_column(v_lds, S::V_STRIDE, 32 * d + (lane & 16), 16 * s + 4 * half, 16 * s + 8 + 4 * half), pf, o[d]);
         }
+        __builtin_amdgcn_s_setprio(0);
     }
     l += __shfl_xor(l, 32);
 
