@@ -1,0 +1,104 @@
+"""Live signals whose rows are mixed over time: the streaming net makes feature rows of what comes in, every finished row is a token, and
+two layers on top look back over the stream -- one attends to a window and the first tokens, one carries a decaying sum.  Rings and states
+have a fixed size, as the net's rolling buffers do: memory does not grow with the signal.
+
+    python -m paper_1804_10727_amd.mixing [--streams 64] [--samples 4000] [--segment 16] [--window 256]
+
+Weights are random (there is nothing to train on here): what it shows is how the calls go together.
+"""
+from __future__ import annotations
+
+import argparse
+import time
+
+from .tokens import decay_attend, norm_rotate, rotary_frequencies, window_attend
+
+
+class TokenMixer:
+    """The two layers for `n_streams` streams of rows of `channels` values; push() takes what is new of each."""
+
+    def __init__(self, channels, n_streams, heads=4, kv_heads=2, dim=64, window=256, sinks=4, room=16, dtype=None, device="cuda:0", seed=0):
+        import torch
+        g = torch.Generator().manual_seed(seed)
+        dtype = torch.float32 if dtype is None else dtype
+        self.heads, self.kv_heads, self.dim, self.window, self.sinks = heads, kv_heads, dim, window, sinks
+        width = (heads + 2 * kv_heads) * dim
+
+        def weights(rows, cols):
+            return (torch.randn(rows, cols, generator=g) / rows ** 0.5).to(device, dtype)
+        self.project, self.back = ([weights(*s) for _ in range(2)] for s in ((channels, width), (heads * dim, channels)))
+        self.q_weight, self.k_weight = (1 + 0.1 * torch.randn(dim, generator=g).to(device) for _ in range(2))
+        self.frequencies, self.amplitude = rotary_frequencies(dim, device=device)
+        self.log_decay = -torch.exp2(-torch.arange(3, 3 + kv_heads, dtype=torch.float32)).to(device)
+        # room for a segment beside the window: its tokens then go to the ring in the launch that attends over them
+        self.rings = [torch.zeros(n_streams, sinks + window + room, kv_heads, dim, dtype=dtype, device=device) for _ in range(2)]
+        self.state = torch.zeros(n_streams, kv_heads, dim, dim, device=device)
+        self.starts = torch.zeros(n_streams, dtype=torch.int64, device=device)
+
+    def state_bytes(self):
+        """Per stream, whatever its length."""
+        return sum(t[0].numel() * t.element_size() for t in (*self.rings, self.state, self.starts))
+
+    def _split(self, x, layer):
+        return (x @ self.project[layer]).unflatten(1, (-1, self.dim)).split([self.heads, self.kv_heads, self.kv_heads], 1)
+
+    def push(self, x, counts=None):
+        """x: the new rows of all streams behind each other, [rows][channels]; counts: how many of each stream (None: the same of all)."""
+        import torch
+        n = torch.full_like(self.starts, x.shape[0] // self.starts.numel()) if counts is None else torch.as_tensor(counts, device=x.device)
+        ends = n.cumsum(0)
+        segments = {} if counts is None else dict(offsets=torch.cat([ends.new_zeros(1), ends]), max_tokens=int(max(counts)))
+        positions = torch.arange(x.shape[0], device=x.device) + torch.repeat_interleave(self.starts - ends + n, n, output_size=x.shape[0])
+        q, k, v = self._split(x, 0)
+        norm_rotate(q, k, positions, self.frequencies, amplitude=self.amplitude, q_weight=self.q_weight, k_weight=self.k_weight, q_out=q, k_out=k)
+        seen = window_attend(q, k, v, *self.rings, self.starts, window=self.window, sinks=self.sinks, **segments)
+        x = x + seen.flatten(1) @ self.back[0]
+        q, k, v = self._split(x, 1)
+        carried = decay_attend(q, k, v, self.log_decay, self.state, self.state, **segments)
+        self.starts += n
+        return x + carried.flatten(1) @ self.back[1]
+
+
+def listen(wl, segment, mixer):
+    """The workload's signals pushed `segment` samples at a time through the net and the mixer: yields the rows that came out of each push,
+    [streams][rows][channels]."""
+    from . import Streams, net_from_workload
+    from .binding import input_tensor
+    net = net_from_workload(wl)
+    st = Streams(net, wl["streams"], max_seg_rows=segment)
+    x = input_tensor(wl)
+    for at in range(0, x.shape[1], segment):
+        st.push_segment(x[:, at:at + segment].contiguous())
+        rows, _, counts = st.read_outputs(segment)
+        n = int(counts[0])                         # (all streams are pushed together)
+        if n:
+            tokens = rows[:, :n].flatten(2).to(mixer.project[0].dtype).flatten(0, 1)
+            yield mixer.push(tokens).unflatten(0, (wl["streams"], n))
+    st.close()
+    net.destroy()
+
+
+def main():
+    ap = argparse.ArgumentParser()
+    ap.add_argument("--streams", type=int, default=64)
+    ap.add_argument("--samples", type=int, default=4000)
+    ap.add_argument("--segment", type=int, default=16)
+    ap.add_argument("--window", type=int, default=256)
+    args = ap.parse_args()
+    import torch
+    import workloads
+    wl = workloads.make(2, streams=args.streams, length=args.samples)
+    for run in range(2):                           # (the first one loads)
+        mixer = TokenMixer(wl["layers"][-1]["c_out"], args.streams, window=args.window, room=args.segment)
+        torch.cuda.synchronize()
+        began = time.perf_counter()
+        rows = [r.shape[1] for r in listen(wl, args.segment, mixer)]
+        torch.cuda.synchronize()
+        took = time.perf_counter() - began
+    pushes = -(-args.samples // args.segment)
+    print(f"{args.streams} signals of {args.samples} samples, {args.segment} at a time: {sum(rows)} rows of each mixed over the last {args.window}; "
+          f"{1e6 * took / pushes:.0f} us per push, {mixer.state_bytes()} bytes of rings and states per stream")
+
+
+if __name__ == "__main__":
+    main()

@@ -1,6 +1,6 @@
 """The operators that mix the tokens of streams (include/idf.h, last section) on torch tensors: argument marshalling only.
 
-Everything is enqueued on the current stream of the tensors' device.  Packed tokens [token][head][value]; a tensor whose values lie
+Everything is enqueued on the current stream of the tensors' device; outputs carry no gradients.  Packed tokens [token][head][value]; a tensor whose values lie
 apart, or whose rows do not begin at multiples of 16 bytes where the library asks for that, is copied first.
 """
 from __future__ import annotations
