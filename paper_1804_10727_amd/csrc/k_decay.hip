@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(256) k_decay_tokens(idf_decay_args a, int colu
 //   Roundings in bfloat16: scores times decay, and the state where it meets the queries, are rounded to bfloat16 (half a step of 2^-8, as the
 // output is).  The state itself stays float32: a decayed value, 24 bits, goes into the product as three bfloat16 numbers that add up to it.
 //   Bound by memory: q, k, v and out once, k and v twice where a segment is cut into parts (one prompt of 65536 tokens, 16 heads of 128 x 128 in
-// bfloat16: 410 us, of them 140 for the states of the parts, 17 for the scan and 250 for the outputs, 4.3 TB/s; loads of the outputs' pass
+// bfloat16: 405 us, of them 140 for the states of the parts, 17 for the scan and 250 for the outputs, 4.3 TB/s; loads of the outputs' pass
 // two chunks ahead took longer, 512 us in all: between stores they are waited for all the same).  Short calls by latency: 64 streams of 16 tokens,
 // 4 heads of 64 x 64 in float32, 10 us.
 constexpr int kChunk = 32;
@@ -299,18 +299,24 @@ __global__ void __launch_bounds__(64 * NW, PREC == IDF_PREC_BF16 && (DK <= 64 ||
             }
 
         if (h + 1 < heads) return;
-        float fade = fade_short;
-        if (n == kChunk) {
-            fade = uniform((float)(whole * (2.0 - drift)));                   // (2 - x is 1 / x so near to one)
-            if (inverse > 0.0) drift *= (double)fade * inverse;
-        }
+        // what this chunk's last token leaves at the end of the part, where only that is asked for: nothing is faded on the way then
+        float left = 1.f;
+        if constexpr (states_only) {
+            left = __builtin_amdgcn_exp2f((float)(len - t0 - n) * l2);
+        } else {
+            float fade = fade_short;
+            if (n == kChunk) {
+                fade = uniform((float)(whole * (2.0 - drift)));               // (2 - x is 1 / x so near to one)
+                if (inverse > 0.0) drift *= (double)fade * inverse;
+            }
 #pragma unroll
-        for (int t = 0; t < KT; ++t) s[t] *= fade;
+            for (int t = 0; t < KT; ++t) s[t] *= fade;
+        }
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
             float x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = E::to_f32(v[p][e]) * fresh[16 * p + 8 * (e / 4) + 4 * half + e % 4 + kChunk - n];
+            for (int e = 0; e < 8; ++e) x[e] = E::to_f32(v[p][e]) * (fresh[16 * p + 8 * (e / 4) + 4 * half + e % 4 + kChunk - n] * left);
             frag pieces[BF ? 3 : 1];
             if constexpr (BF) {
 #pragma unroll
