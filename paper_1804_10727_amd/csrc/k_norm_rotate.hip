@@ -16,10 +16,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kGroups = 1024;                      // workgroups that go on from tokens to tokens: four for a compute unit
-constexpr int kDeep = 4;                           // heads that a group of lanes has in flight
+constexpr int kMostDeep = 4;                       // heads that a group of lanes has in flight
 
 // P: values of a piece; N: pairs of pieces of a lane (2 only where single values make a head longer than 64 lanes can hold)
-template <int PREC, int P, int N>
+template <int PREC, int P, int N, int kDeep>
 __global__ void __launch_bounds__(kThreads) k_norm_rotate(idf_norm_rotate_args a, int lanes_log2, int tokens_per_group)
 {
     using E = Elem<PREC>;
@@ -198,11 +198,14 @@ hipError_t go(const idf_norm_rotate_args &a, const LaunchCtx &lc)
     while ((1 << lanes_log2) < pieces && lanes_log2 < 6) ++lanes_log2;
     const int heads = a.heads_q + a.heads_k, groups = kThreads >> lanes_log2;
     // as many tokens as the groups take in one go, but workgroups for every compute unit first
-    int64_t per = std::max(1, groups * kDeep / heads);
+    int64_t per = std::max(1, groups * kMostDeep / heads);
     per = std::max<int64_t>(1, std::min<int64_t>({per, a.n_tokens / 1024, 16}));
     const int64_t grid = std::min<int64_t>((a.n_tokens + per - 1) / per, kGroups);
     const size_t bytes = ((size_t)(a.head_dim + 3) / 4 * 4 + 2 * (size_t)per * (a.rotary_dim / 2)) * sizeof(float2);
-    return launch(k_norm_rotate<PREC, P, N>, dim3((unsigned)grid), dim3(kThreads), bytes, lc, a, lanes_log2, (int)per);
+    // few tokens: every group of lanes has one head and is done
+    if (per * heads <= groups && grid * per >= a.n_tokens)
+        return launch(k_norm_rotate<PREC, P, N, 1>, dim3((unsigned)grid), dim3(kThreads), bytes, lc, a, lanes_log2, (int)per);
+    return launch(k_norm_rotate<PREC, P, N, kMostDeep>, dim3((unsigned)grid), dim3(kThreads), bytes, lc, a, lanes_log2, (int)per);
 }
 
 template <int PREC>
