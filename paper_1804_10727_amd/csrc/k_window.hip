@@ -77,6 +77,40 @@ template <class T> __device__ __forceinline__ const T *at(const Held<T> &h, cons
     return p.own ? h.own + p.row * h.own_stride : h.ring + p.row * h.ring_stride;
 }
 
+// Rounds whose entries lie behind each other, all own tokens or all in the ring without its end between them, are read from one address on;
+// the others (first tokens, the ring's end, the list's) look for the place of each entry.
+struct Flat {
+    bool own, ring;            // rows near enough to each other for offsets of 32 bits
+    template <class T> struct Round {
+        const T *k, *v;        // nullptr: no such round
+        int k_step, v_step;
+    };
+    template <class T> __device__ __forceinline__ Flat(const Held<T> &kh, const Held<T> &vh, int entries, int row)
+    {
+        const int64_t far = ((int64_t)1 << 31) / entries / (int)sizeof(T) - row;
+        own = kh.own_stride >= 0 && vh.own_stride >= 0 && kh.own_stride < far && vh.own_stride < far;
+        ring = kh.ring_stride < far;
+    }
+    template <class T> __device__ __forceinline__ Round<T> round(const idf_window_args &a, const Keys &keys, const Held<T> &kh, const Held<T> &vh, int i0, int entries) const
+    {
+        Round<T> f = {nullptr, nullptr, 0, 0};
+        const int rel = i0 - keys.n_first;
+        if (i0 + entries > keys.n || rel < 0) return f;
+        if (own && rel >= keys.own) {
+            f.k = kh.own + (int64_t)(rel - keys.own) * kh.own_stride; f.v = vh.own + (int64_t)(rel - keys.own) * vh.own_stride;
+            f.k_step = (int)kh.own_stride; f.v_step = (int)vh.own_stride;
+        } else if (ring && rel + entries <= keys.own) {
+            uint32_t s = keys.slot0 + (uint32_t)rel;
+            if (s >= keys.period) s -= keys.period;
+            if (s + entries <= keys.period) {
+                f.k = kh.ring + (a.sinks + (int64_t)s) * kh.ring_stride; f.v = vh.ring + (a.sinks + (int64_t)s) * vh.ring_stride;
+                f.k_step = f.v_step = (int)kh.ring_stride;
+            }
+        }
+        return f;
+    }
+};
+
 // Partial results of rows whose keys are split over workgroups: [split][token][head][head_dim] sums, then [split][token][head] maximum (of
 // scores in units of log 2) and sum of weights.
 struct Partial {
@@ -164,8 +198,8 @@ __device__ __forceinline__ void append_tokens(const idf_window_args &a, const Se
 // A workgroup takes the at most 16 query rows of one segment and key/value head and a part of the keys; its four waves take 16 NT of them at a
 // time, in turn, each with a softmax of its own, and are joined at the end.  Keys go from memory straight into the layout of the matrix
 // instruction, values through a piece of LDS that is the wave's own, to be read along the keys; both are asked for one round ahead.  No
-// barrier but the last.  Bound by memory: every row of the ring is read once (64 streams on 4096 keys of 8 x 128 in bfloat16: 197 us, 5.5 TB/s; 64
-// streams of 16 tokens on 1000 keys of 8 x 64 in float32: 54 us, 5.1 TB/s; one stream on 16384 keys, split: 21.5 us with the join, 3.1 TB/s).
+// barrier but the last.  Bound by memory: every row of the ring is read once (64 streams on 4096 keys of 8 x 128 in bfloat16: 193 us, 5.6 TB/s; 64
+// streams of 16 tokens on 1000 keys of 8 x 64 in float32: 54 to 56 us, 5 TB/s; one stream on 16384 keys, split: 21 us with the join, 3.2 TB/s).
 template <int PREC, int DP> struct StepShape {
     static constexpr int NT = PREC == IDF_PREC_BF16 ? 2 : 1;                  // tiles of 16 keys
     static constexpr int KEYS = 16 * NT;
@@ -184,7 +218,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_window_step(idf_wind
     constexpr int NT = S::NT, KS = DP / 32, DT = DP / 16;
     __shared__ __align__(16) float lds[4 * S::WAVE_FLOATS];
     __shared__ float stats[2][4][16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
     const int split = blockIdx.x, kv = blockIdx.y, group = a.heads_q / a.heads_kv;
     const Segment g = segment_of(a, blockIdx.z, a.starts);
     if (g.len == 0) return;
@@ -213,16 +247,39 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_window_step(idf_wind
     T *v_lds = (T *)(lds + wave * S::WAVE_FLOATS);
     typename M::frag kf[NT][KS];
     i32x4 vf[S::LOADS];
+    const int r0 = lane / S::ROW16, c0 = (lane - r0 * S::ROW16) * M::VL;
+    const Flat flat(kh, vh, S::KEYS, DP);
     auto load = [&](int tile) IDF_INLINE {
+        const int i0 = tile * S::KEYS;
+        if (const auto f = flat.round(a, keys, kh, vh, i0, S::KEYS); f.k) {
+            const uint32_t ko = (uint32_t)(col * f.k_step + 8 * grp) * sizeof(T), vo = (uint32_t)(r0 * f.v_step + c0) * sizeof(T);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const T *src = (const T *)((const char *)(f.k + (int64_t)(16 * t) * f.k_step) + ko);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kf[t][s] = M::load(src + 32 * s, a.head_dim - 32 * s - 8 * grp);
+            }
+#pragma unroll
+            for (int j = 0; j < S::LOADS; ++j) {
+                if constexpr (64 % S::ROW16 == 0) {
+                    constexpr int rows = 64 / S::ROW16;
+                    vf[j] = c0 < a.head_dim ? *(const i32x4 *)((const char *)(f.v + (int64_t)(j * rows) * f.v_step) + vo) : i32x4{0, 0, 0, 0};
+                } else {
+                    const int piece = j * 64 + lane, r = piece / S::ROW16, c = (piece - r * S::ROW16) * M::VL;
+                    vf[j] = c < a.head_dim ? *(const i32x4 *)(f.v + r * f.v_step + c) : i32x4{0, 0, 0, 0};
+                }
+            }
+            return;
+        }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const T *src = at(kh, place_of(a, keys, min(tile * S::KEYS + 16 * t + col, keys.n - 1)));
+            const T *src = at(kh, place_of(a, keys, min(i0 + 16 * t + col, keys.n - 1)));
 #pragma unroll
             for (int s = 0; s < KS; ++s) kf[t][s] = M::load(src + 32 * s + 8 * grp, a.head_dim - 32 * s - 8 * grp);
         }
 #pragma unroll
         for (int j = 0; j < S::LOADS; ++j) {
-            const int piece = j * 64 + lane, r = piece / S::ROW16, c = (piece - r * S::ROW16) * M::VL, i = tile * S::KEYS + r;
+            const int piece = j * 64 + lane, r = piece / S::ROW16, c = (piece - r * S::ROW16) * M::VL, i = i0 + r;
             vf[j] = i < keys.n && c < a.head_dim ? *(const i32x4 *)(at(vh, place_of(a, keys, i)) + c) : i32x4{0, 0, 0, 0};
         }
     };
@@ -335,7 +392,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_window_step(idf_wind
 // go through registers into LDS, the next round's being asked for while this one's are worked on.  Bound by the vector units and the matrix cores
 // together: of 128 values a head, a round costs a wave 32 matrix instructions of 32 cycles and some 170 others, 32 of them exponentials of 16 cycles;
 // of 64 values, half the former and the same of the latter, which is why these run four waves to a SIMD (three: 273 us, four: 263, uneven
-// segments).  Two prompts of 16384 tokens, 32 heads of 128 on a window of 4096: 2060 us, 935 TFLOP/s.  Two halves of LDS with one barrier a round
+// segments).  Two prompts of 16384 tokens, 32 heads of 128 on a window of 4096: 2030 us, 948 TFLOP/s.  Two halves of LDS with one barrier a round
 // instead of two took longer (2182 : 2158 us), reads from LDS held ahead of the products as long (2076 : 2065).
 template <int PREC, int DP> struct TileShape {
     static constexpr int KEYS = PREC == IDF_PREC_BF16 ? 64 : 32;
@@ -388,32 +445,15 @@ __global__ void __launch_bounds__(256, PREC != IDF_PREC_BF16 || DP > 128 ? 1 : D
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = M::load(src + 16 * s + 8 * half, a.head_dim - 16 * s - 8 * half);
     }
-    // Rounds whose entries lie behind each other, all own tokens or all in the ring without its end between them, are read from one address on;
-    // the others (first tokens, the ring's end, the list's) look for the place of each entry.
     const int r0 = threadIdx.x / S::ROW16, c0 = (threadIdx.x - r0 * S::ROW16) * M::VL;
     const bool in_row = c0 < a.head_dim;
-    const int64_t k_step = kh.own_stride, v_step = vh.own_stride, ring_step = kh.ring_stride;
-    constexpr int64_t kFar = ((int64_t)1 << 31) / S::KEYS / (int)sizeof(T) - DP;
-    const bool own_flat = k_step >= 0 && v_step >= 0 && k_step < kFar && v_step < kFar, ring_flat = ring_step < kFar;
+    const Flat flat(kh, vh, S::KEYS, DP);
     i32x4 kr[S::LOADS], vr[S::LOADS];
     auto load = [&](int t) IDF_INLINE {
-        const int i0 = t * S::KEYS, rel = i0 - keys.n_first;
-        const T *kb = nullptr, *vb = nullptr;
-        int ks = 0, vs = 0;
-        if (i0 + S::KEYS <= keys.n && rel >= 0) {
-            if (own_flat && rel >= keys.own) {
-                kb = kh.own + (int64_t)(rel - keys.own) * k_step; vb = vh.own + (int64_t)(rel - keys.own) * v_step;
-                ks = (int)k_step; vs = (int)v_step;
-            } else if (ring_flat && rel + S::KEYS <= keys.own) {
-                uint32_t s = keys.slot0 + (uint32_t)rel;
-                if (s >= keys.period) s -= keys.period;
-                if (s + S::KEYS <= keys.period) {
-                    kb = kh.ring + (a.sinks + (int64_t)s) * ring_step; vb = vh.ring + (a.sinks + (int64_t)s) * ring_step;
-                    ks = vs = (int)ring_step;
-                }
-            }
-        }
-        if (kb) {
+        const int i0 = t * S::KEYS;
+        if (const auto f = flat.round(a, keys, kh, vh, i0, S::KEYS); f.k) {
+            const T *kb = f.k, *vb = f.v;
+            const int ks = f.k_step, vs = f.v_step;
             const uint32_t ko = (uint32_t)(r0 * ks + c0) * sizeof(T), vo = (uint32_t)(r0 * vs + c0) * sizeof(T);
 #pragma unroll
             for (int j = 0; j < S::LOADS; ++j) {

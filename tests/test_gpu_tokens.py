@@ -149,6 +149,32 @@ def test_window_segments(dtype, hq, hkv, d, window, sinks, room):
     window_streams(dtype, hq, hkv, d, window, sinks, room, pushes, seed=window + d)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("hq,hkv,d,window,sinks", [(6, 2, 64, 33, 2), (2, 2, 128, 16, 0), (16, 1, 96, 70, 40), (7, 1, 32, 1, 1)])
+def test_window_rings_with_room_for_segments(dtype, hq, hkv, d, window, sinks):
+    """The attention itself writes the ring while it is read: heads that leave tokens on two tiles, first tokens, slots that wrap."""
+    window_streams(dtype, hq, hkv, d, window, sinks, 199, [[5, 1, 0], [200, 43, 129], [1, 1, 1], [64, 200, 2], [128, 7, 200], [2, 1, 3]], seed=d)
+    window_streams(dtype, hq, hkv, d, window, sinks, 3, [[4, 2, 1], [1, 4, 0], [4, 4, 4], [3, 3, 3]] * 3, seed=d + 1)
+
+
+def test_window_single_rows_split_many_times():
+    """Lists of keys in more parts than a wave has lanes; first tokens ahead of them."""
+    g = torch.Generator().manual_seed(15)
+    d, window, sinks, start = 64, 40000, 3, 100000
+    for dtype in TYPES:
+        q, k, v = (normal(g, 1, h, d, dtype=dtype) for h in (2, 1, 1))
+        rings = [normal(g, 1, sinks + window, 1, d, dtype=dtype) for _ in range(2)]
+        out = idf.window_attend(*(x.to(DEV) for x in (q, k, v, *rings)), torch.tensor([start], device=DEV), window=window, sinks=sinks)
+        slot = sinks + (start - sinks) % window                        # it holds the one token that has left the window
+        seen = [np.concatenate([np.delete(f64(r[0, :, 0]), slot, 0), f64(x[:, 0])]) for r, x in zip(rings, (k, v))]
+        for h in range(2):
+            s = seen[0] @ f64(q[0, h]) / 8
+            w = np.exp(s - s.max())
+            w /= w.sum()
+            want, size, score = w @ seen[1], w @ np.abs(seen[1]), (np.abs(seen[0]) @ np.abs(f64(q[0, h]))).max() / 8
+            within(out[0, h], want, half_step(dtype) * np.abs(want) + (rounded(dtype) + 4 * (d + 8) * W * score + 2 * (window + 19) * W) * size)
+
+
 @pytest.mark.parametrize("d", [4, 12, 20, 60, 68, 100, 132, 252])
 def test_window_odd_heads(d):
     """Float32 heads whose end lies inside a fragment of eight values: what lies behind it, here NaN, is not read."""
@@ -307,6 +333,14 @@ def decay_case(dtype, hq, hkv, dk, dv, lengths, seed=0, with_state=True, ragged=
 @pytest.mark.parametrize("lengths", [(1, 1, 1), (1, 0, 1), (2, 5, 16, 3), (63, 64, 65, 0, 1), (130, 17)])
 def test_decay(dtype, hq, hkv, dk, dv, lengths):
     decay_case(dtype, hq, hkv, dk, dv, lengths, seed=dk + len(lengths))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("hq,hkv,dk,dv", [(2, 1, 64, 64), (2, 2, 128, 80), (1, 1, 200, 64)])
+@pytest.mark.parametrize("lengths", [(2, 1, 0), (4, 3, 2), (12, 0, 7), (13, 1, 5)])
+def test_decay_few_tokens(dtype, hq, hkv, dk, dv, lengths):
+    """Both sides of the line between tokens one by one and chunks."""
+    decay_case(dtype, hq, hkv, dk, dv, lengths, seed=sum(lengths))
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
