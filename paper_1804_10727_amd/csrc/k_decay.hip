@@ -90,7 +90,6 @@ __global__ void __launch_bounds__(256) k_decay_tokens(idf_decay_args a, int colu
 // two chunks ahead took longer, 512 us in all: between stores they are waited for all the same).  Short calls by latency: 64 streams of 16 tokens,
 // 4 heads of 64 x 64 in float32, 10 us.
 constexpr int kChunk = 32;
-constexpr int kPartLeast = 256;                    // tokens of a part of a segment, at least
 
 // Segments cut into parts along time, so that there is work for every compute unit: the state that each part leaves if it begins with none,
 // then the states that the parts begin with, then the parts themselves.
@@ -368,7 +367,8 @@ __global__ void __launch_bounds__(64 * NW, PREC == IDF_PREC_BF16 && (DK <= 64 ||
             }
 }
 
-// What each part begins with, in place of what it would leave by itself: in the order of the parts, four values by a thread.
+// What each part begins with, in place of what it would leave by itself: in the order of the parts, four values by a thread, what eight parts
+// leave being read at a time (16 heads x 32 parts of 128 x 128: 17.5 us one after the other, 14.3 so).
 __global__ void __launch_bounds__(256) k_decay_scan(idf_decay_args a, Parts parts)
 {
     const int kv = blockIdx.y % a.heads_kv, seg = blockIdx.y / a.heads_kv;
@@ -380,12 +380,18 @@ __global__ void __launch_bounds__(256) k_decay_scan(idf_decay_args a, Parts part
     float *at = parts.states + (int64_t)blockIdx.y * parts.n * size + x;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (a.state_in) s = *(const f32x4 *)(a.state_in + ((int64_t)g.ring * a.heads_kv + kv) * size + x);
-    for (int p = 0; p < n; ++p, at += size) {
-        f32x4 left = {0.f, 0.f, 0.f, 0.f};
-        if (p + 1 < n) left = *(const f32x4 *)at;
-        *(f32x4 *)at = s;
+    constexpr int kAhead = 8;
+    for (int p0 = 0; p0 < n; p0 += kAhead, at += (int64_t)kAhead * size) {
+        f32x4 left[kAhead];                        // (what lies in the last part's place is read and not used)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = __builtin_fmaf(s[e], keep, left[e]);
+        for (int y = 0; y < kAhead; ++y) left[y] = *(const f32x4 *)(at + (int64_t)min(y, n - 1 - p0) * size);
+#pragma unroll
+        for (int y = 0; y < kAhead; ++y) {
+            if (p0 + y >= n) break;
+            *(f32x4 *)(at + (int64_t)y * size) = s;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] = __builtin_fmaf(s[e], keep, left[y][e]);
+        }
     }
 }
 
@@ -393,10 +399,16 @@ Parts parts_of(const idf_decay_args &a)
 {
     Parts p;
     p.states = nullptr;
-    // two workgroups for every compute unit, by the tokens that there are and not by the longest segment's (uneven segments 87 -> 81 us); a part
+    // as many workgroups as the machine holds, by the tokens that there are and not by the longest segment's (uneven segments 87 -> 81 us); a part
     // is long next to the state that it reads and writes, and states that mostly empty segments would not use stay few (512 MB of 128 x 128)
     const int64_t pairs = (int64_t)a.n_segments * a.heads_kv, tokens = std::max<int64_t>(1, std::min(a.n_tokens, a.n_segments * a.max_tokens) * a.heads_kv * ((a.dim_v + 127) / 128));
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({a.max_tokens * 512 / tokens, a.max_tokens / kPartLeast, 8192 / std::max<int64_t>(pairs, 1)}));
+    // Where few workgroups run, a part's chunks follow each other by latency: up to sixteen parts, of a chunk at least, then of 128 tokens; the two
+    // launches more pay from 256 tokens on, 128 in float32 (us per call with parts of 256 tokens and so: 400 tokens, 16 heads of 128 x 128 32 -> 24; 800
+    // tokens, a head of 64 x 64 30 -> 15, in float32 68 -> 24).
+    const int64_t held = a.precision == IDF_PREC_F32 && a.dim_k > 64 ? 256 : 512;        // workgroups of the machine: by their LDS one or two to a compute unit
+    const int64_t part = std::min<int64_t>(std::max<int64_t>(a.max_tokens / 16, kChunk), 128);
+    const int64_t most = a.max_tokens < (a.precision == IDF_PREC_BF16 ? 256 : 128) ? 1 : a.max_tokens / part;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({a.max_tokens * held / tokens, most, 8192 / std::max<int64_t>(pairs, 1)}));
     p.tokens = (int)(((a.max_tokens + want - 1) / want + kChunk - 1) / kChunk * kChunk);
     p.n = (int)((a.max_tokens + p.tokens - 1) / std::max(p.tokens, 1));
     if (p.n <= 1) { p.n = 1; p.tokens = std::max(p.tokens, kChunk); }

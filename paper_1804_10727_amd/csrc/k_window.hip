@@ -674,6 +674,29 @@ struct Plan {
     int tiles, splits;
     bool append;               // tokens go to the ring with the attention over them, and not by a launch behind it
 };
+// Into how many parts a list of keys goes: the number with the least estimated time.  A workgroup's rounds follow each other, at a time each that
+// is latency where few of them run (measured, us: four tiles of the step kernel 1.4 in bfloat16, 0.9 + 0.0075 per value of a head in float32; a round
+// of the tile kernel 1.0 + 0.006, and 1.3 + 0.0275); no more workgroups than the compute units hold; a join is a launch of 4 to
+// 5 us and reads every row of every part.  Against parts of 256 keys (step) or 512 (tile) at least, us per pass: one stream, four heads of 128 on
+// one, 1500 keys 14.2 -> 11.1, in float32 19.2 -> 11.8; 40 tokens, eight heads on two, 500 keys 27.7 -> 15.9, 95.5 -> 21.3; 1200 tokens, 600 keys,
+// where the join costs more than it brings, 45.6 -> 29.4.
+int splits_of(const idf_window_args &a, bool step, int64_t pairs, int64_t keys)
+{
+    const bool bf = a.precision == IDF_PREC_BF16;
+    const int64_t round = step ? (bf ? 128 : 64) : bf ? 64 : 32, rounds = (keys + round - 1) / round, held = !step && !bf && a.head_dim > 64 ? 256 : 512;
+    const double each = step ? (bf ? 1.4 : 0.9 + 0.0075 * a.head_dim) : bf ? 1.0 + 0.006 * a.head_dim : 1.3 + 0.0275 * a.head_dim;
+    const double rows = (double)std::min<int64_t>(a.n_tokens, a.n_segments * a.max_tokens) * a.heads_q;
+    int best = 1;
+    double least = 0.0;
+    for (int64_t per = rounds; per >= 1; per = per > 8 ? per * 7 / 8 : per - 1) {
+        const int64_t n = (rounds + per - 1) / per;
+        if (n > 1 && (n > kMostSplits || pairs * n > held)) break;
+        const double us = per * each + (n > 1 ? (step ? 4.2 : 5.0) + rows * (1.6e-3 + 1e-6 * n * a.head_dim) : 0.0);
+        if (n == 1 || us < least) { least = us; best = (int)n; }
+    }
+    return best;
+}
+
 Plan plan_of(const idf_window_args &a)
 {
     Plan p;
@@ -683,16 +706,9 @@ Plan plan_of(const idf_window_args &a)
     p.append = a.k_ring && a.slots - a.sinks - a.window >= a.max_tokens - 1;
     p.tiles = p.step ? 1 : (int)((rows + kTileRows - 1) / kTileRows);
     const int64_t pairs = (int64_t)a.n_segments * a.heads_kv * p.tiles;
-    const int64_t keys = (a.k_ring ? std::min<int64_t>(a.window, a.slots) : 0) + a.sinks + std::min<int64_t>(a.max_tokens, a.window);
-    // two workgroups for every compute unit, and some rounds of keys for each of them; where waves take tiles in turn, as many splits as
-    // leave all waves the same number of rounds
-    const int64_t least = p.step ? 256 : 512;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(512 + pairs - 1) / pairs, keys / least, kMostSplits}));
-    if (p.step && p.splits > 1) {
-        const int64_t tile = a.precision == IDF_PREC_BF16 ? 32 : 16, tiles = (keys + tile - 1) / tile, rounds = (tiles + 4 * p.splits - 1) / (4 * p.splits);
-        p.splits = (int)std::min<int64_t>(kMostSplits, (tiles + 4 * rounds - 1) / (4 * rounds));
-    }
-    if (pairs >= 384) p.splits = 1;
+    const int64_t own = p.step ? a.max_tokens : std::min<int64_t>(a.max_tokens, kTileRows / (a.heads_q / a.heads_kv) + 1);
+    const int64_t keys = std::min<int64_t>(a.window, a.k_ring ? a.slots : a.max_tokens) + a.sinks + own;
+    p.splits = splits_of(a, p.step, pairs, keys);
     return p;
 }
 
