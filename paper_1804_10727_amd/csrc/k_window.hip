@@ -683,7 +683,7 @@ struct Plan {
 int splits_of(const idf_window_args &a, bool step, int64_t pairs, int64_t keys)
 {
     const bool bf = a.precision == IDF_PREC_BF16;
-    const int64_t round = step ? (bf ? 128 : 64) : bf ? 64 : 32, rounds = (keys + round - 1) / round, held = !step && !bf && a.head_dim > 64 ? 256 : 512;
+    const int64_t round = step ? (bf ? 128 : 64) : bf ? 64 : 32, rounds = (keys + round - 1) / round, held = 512;
     const double each = step ? (bf ? 1.4 : 0.9 + 0.0075 * a.head_dim) : bf ? 1.0 + 0.006 * a.head_dim : 1.3 + 0.0275 * a.head_dim;
     const double rows = (double)std::min<int64_t>(a.n_tokens, a.n_segments * a.max_tokens) * a.heads_q;
     int best = 1;
