@@ -14,6 +14,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libidf.so")
 PUSH_SRC = os.path.join(CSRC, "push.cpp")
 TOKENS_SRC = os.path.join(CSRC, "tokens.cpp")
+# Asked for here, before there are threads: while one thread reads the interpreter's configuration for the first time, another finds it half read.
+EXT_SUFFIX = sysconfig.get_config_var("EXT_SUFFIX")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -35,7 +37,7 @@ def sources():
 def extension_path(stem):
     """The extension module of this interpreter and this torch: it is tied to the binary interfaces of both, and another one's is another file."""
     import torch
-    return os.path.join(HERE, f"{stem}.torch-{torch.__version__}{sysconfig.get_config_var('EXT_SUFFIX')}")
+    return os.path.join(HERE, f"{stem}.torch-{torch.__version__}{EXT_SUFFIX}")
 
 
 def push_path():

@@ -177,3 +177,13 @@ def test_oracle_decay():
     want = np.einsum("thd,jd,tj,je->the", q, k[:, 0], lam, v[:, 0]) + np.einsum("thd,de,t->the", q, s0[0], np.exp(-0.3 * np.arange(1, 10)))
     assert np.allclose(out, 0.7 * want)
     assert np.allclose(end[0], np.exp(-2.7) * s0[0] + np.einsum("j,jd,je->de", np.exp(-0.3 * np.arange(8, -1, -1)), k[:, 0], v[:, 0]))
+
+
+def test_extension_names_do_not_depend_on_the_thread_that_asks(monkeypatch):
+    """Threads of a build that ask for the interpreter's configuration while another reads it get None: names come from what was read at import."""
+    import sysconfig
+
+    from paper_1804_10727_amd import build
+    want = sysconfig.get_config_var("EXT_SUFFIX")
+    monkeypatch.setattr(sysconfig, "get_config_var", lambda name: None)
+    assert want and build.push_path().endswith(want) and build.tokens_path().endswith(want)
