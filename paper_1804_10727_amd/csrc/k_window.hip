@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_window_step(idf_wind
 // go through registers into LDS, the next round's being asked for while this one's are worked on.  Bound by the vector units and the matrix cores
 // together: of 128 values a head, a round costs a wave 32 matrix instructions of 32 cycles and some 170 others, 32 of them exponentials of 16 cycles;
 // of 64 values, half the former and the same of the latter, which is why these run four waves to a SIMD (three: 273 us, four: 263, uneven
-// segments).  Two prompts of 16384 tokens, 32 heads of 128 on a window of 4096: 2030 us, 948 TFLOP/s.  Two halves of LDS with one barrier a round
+// segments).  Two prompts of 16384 tokens, 32 heads of 128 on a window of 4096: 1990 to 2140 us by the machine, 900 to 965 TFLOP/s.  Two halves of LDS with one barrier a round
 // instead of two took longer (2182 : 2158 us), reads from LDS held ahead of the products as long (2076 : 2065).
 template <int PREC, int DP> struct TileShape {
     static constexpr int KEYS = PREC == IDF_PREC_BF16 ? 64 : 32;
