@@ -395,22 +395,27 @@ __global__ void __launch_bounds__(256) k_decay_scan(idf_decay_args a, Parts part
     }
 }
 
+// Tokens of the longest segment that there can be: max_tokens is a bound only.  A call without tokens has segments all the same, which hand
+// their states on.
+int64_t longest(const idf_decay_args &a) { return std::min(a.max_tokens, a.n_tokens); }
+
 Parts parts_of(const idf_decay_args &a)
 {
     Parts p;
     p.states = nullptr;
+    const int64_t max_tokens = longest(a);
     // as many workgroups as the machine holds, by the tokens that there are and not by the longest segment's (uneven segments 87 -> 81 us); a part
     // is long next to the state that it reads and writes, and states that mostly empty segments would not use stay few (512 MB of 128 x 128)
-    const int64_t pairs = (int64_t)a.n_segments * a.heads_kv, tokens = std::max<int64_t>(1, std::min(a.n_tokens, a.n_segments * a.max_tokens) * a.heads_kv * ((a.dim_v + 127) / 128));
+    const int64_t pairs = (int64_t)a.n_segments * a.heads_kv, tokens = std::max<int64_t>(1, std::min(a.n_tokens, a.n_segments * max_tokens) * a.heads_kv * ((a.dim_v + 127) / 128));
     // Where few workgroups run, a part's chunks follow each other by latency: up to sixteen parts, of a chunk at least, then of 128 tokens; the two
     // launches more pay from 256 tokens on, 128 in float32 (us per call with parts of 256 tokens and so: 400 tokens, 16 heads of 128 x 128 32 -> 24; 800
     // tokens, a head of 64 x 64 30 -> 15, in float32 68 -> 24).
     const int64_t held = a.precision == IDF_PREC_F32 && a.dim_k > 64 ? 256 : 512;        // workgroups of the machine: by their LDS one or two to a compute unit
-    const int64_t part = std::min<int64_t>(std::max<int64_t>(a.max_tokens / 16, kChunk), 128);
-    const int64_t most = a.max_tokens < (a.precision == IDF_PREC_BF16 ? 256 : 128) ? 1 : a.max_tokens / part;
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({a.max_tokens * held / tokens, most, 8192 / std::max<int64_t>(pairs, 1)}));
-    p.tokens = (int)(((a.max_tokens + want - 1) / want + kChunk - 1) / kChunk * kChunk);
-    p.n = (int)((a.max_tokens + p.tokens - 1) / std::max(p.tokens, 1));
+    const int64_t part = std::min<int64_t>(std::max<int64_t>(max_tokens / 16, kChunk), 128);
+    const int64_t most = max_tokens < (a.precision == IDF_PREC_BF16 ? 256 : 128) ? 1 : max_tokens / part;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({max_tokens * held / tokens, most, 8192 / std::max<int64_t>(pairs, 1)}));
+    p.tokens = (int)(((max_tokens + want - 1) / want + kChunk - 1) / kChunk * kChunk);
+    p.n = (int)((max_tokens + p.tokens - 1) / std::max(p.tokens, 1));
     if (p.n <= 1) { p.n = 1; p.tokens = std::max(p.tokens, kChunk); }
     return p;
 }
@@ -422,7 +427,7 @@ Parts parts_of(const idf_decay_args &a)
 bool by_token(const idf_decay_args &a)
 {
     const int most = a.precision == IDF_PREC_BF16 ? 1 : a.dim_k <= 64 ? 4 : 12;
-    return a.max_tokens <= most || a.dim_k > 128;
+    return longest(a) <= most || a.dim_k > 128;
 }
 
 template <int PREC, int DK>

@@ -170,7 +170,7 @@ int idf_decay_workspace(const idf_decay_args *a, size_t *bytes)
 {
     if (!bytes) return fail(IDF_EINVAL, "null argument");
     if (int rc = check_decay(a)) return rc;
-    *bytes = a->n_segments && a->n_tokens && a->max_tokens ? decay_workspace(*a) : 0;
+    *bytes = decay_workspace(*a);
     return IDF_OK;
 }
 
@@ -185,9 +185,9 @@ int idf_decay_attend(const idf_decay_args *a, void *hip_stream)
         if (!rc) rc = check_tokens("k", a->k, a->precision, false, a->n_tokens, a->heads_kv, a->dim_k);
         if (!rc) rc = check_tokens("v", a->v, a->precision, false, a->n_tokens, a->heads_kv, a->dim_v);
         if (!rc) rc = check_tokens("out", a->out, a->precision, true, a->n_tokens, a->heads_q, a->dim_v);
-        if (!rc) rc = check_workspace(a->workspace, a->workspace_bytes, decay_workspace(*a));
         if (rc) return rc;
     }
+    if (int rc = check_workspace(a->workspace, a->workspace_bytes, decay_workspace(*a))) return rc;
     LaunchCtx lc;
     lc.st = (hipStream_t)hip_stream;
     const hipError_t e = launch_decay(*a, lc);
