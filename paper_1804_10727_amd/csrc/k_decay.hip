@@ -99,7 +99,11 @@ struct Parts {
 };
 
 __device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
-__device__ __forceinline__ float log2_of(float log_decay) { return fmaxf(log_decay * 1.4426950408889634f, -1e30f); }      // (a decay to nothing: times zero stays zero)
+__device__ __forceinline__ float log2_of(float log_decay)
+{
+    const float x = log_decay * 1.4426950408889634f;
+    return x < -1e30f ? -1e30f : x;                // (a decay to nothing: times zero stays zero; a maximum would drop what is not a number)
+}
 
 template <int PREC, int DK, int NW, bool states_only>
 __global__ void __launch_bounds__(64 * NW, PREC == IDF_PREC_BF16 && (DK <= 64 || NW == 4) ? 2 : 1) k_decay_chunks(idf_decay_args a, Parts parts, int blocks)

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_1804_10727_amd as idf
-from test_gpu_tokens import DEV, TYPES
+from test_gpu_tokens import DEV, TYPES, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +29,21 @@ def test_decay_without_tokens_hands_states_on(dtype, in_place, dk, monkeypatch):
             assert out.shape == (0, 2, 64) and torch.equal(into, state)
             idf.decay_attend(q, q, v, log_decay, None, into, offsets=offsets, max_tokens=max_tokens)
             assert torch.equal(into, torch.zeros_like(state))           # (no states: zeros are handed on)
+
+
+# ---- values that are infinite or not a number ----
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 5, 20, 70, 600])
+def test_decay_that_is_not_a_number(dtype, n):
+    """One head's decay is NaN: all that this head gives is, token by token, in chunks and in parts; the other head's is as without it."""
+    g = torch.Generator().manual_seed(41)
+    q, k, v = (normal(g, n, 2, 64, dtype=dtype).to(DEV) for _ in range(3))
+    state = torch.randn(1, 2, 64, 64, generator=g).to(DEV)
+    got = []
+    for first in (-0.1, float("nan")):
+        end = torch.empty_like(state)
+        got.append((idf.decay_attend(q, k, v, torch.tensor([first, -0.2], device=DEV), state, end), end))
+    (want, want_end), (out, end) = got
+    assert torch.isfinite(want).all() and torch.isnan(out[:, 0]).all() and torch.isnan(end[:, 0]).all()
+    assert torch.equal(out[:, 1], want[:, 1]) and torch.equal(end[:, 1], want_end[:, 1])
