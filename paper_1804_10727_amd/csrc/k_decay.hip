@@ -105,8 +105,92 @@ __device__ __forceinline__ float log2_of(float log_decay)
     return x < -1e30f ? -1e30f : x;                // (a decay to nothing: times zero stays zero; a maximum would drop what is not a number)
 }
 
+template <int N> __device__ __forceinline__ bool finite(const f32x16 (&s)[N])
+{
+    float none[4] = {};
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) none[e % 4] += s[t][e] * 0.f;
+    return none[0] + none[1] + (none[2] + none[3]) == 0.f;
+}
+
+// What a wave does in k_decay_chunks, once more, by the recurrence, where something infinite or not a number came into a state that had begun without:
+// three parts of an infinite value are no number, nor is an infinite key times a part that is zero, nor an infinite value times the zeros behind a
+// key that is shorter than DK.  Outputs that are finite are as they should be and stay.  Lanes side by side hold a column of the state each, either half
+// of the wave half of its rows.  False: the state had begun so.
 template <int PREC, int DK, int NW, bool states_only>
-__global__ void __launch_bounds__(64 * NW, PREC == IDF_PREC_BF16 && (DK <= 64 || NW == 4) ? 2 : 1) k_decay_chunks(idf_decay_args a, Parts parts, int blocks)
+__device__ __forceinline__ bool part_by_tokens(const idf_decay_args &a, const Parts &parts, int blocks, int x, int y, int thread, bool good)
+{
+    using M = Mfma<PREC>;
+    using E = Elem<PREC>;
+    using T = typename M::T;
+    constexpr int ROWS = DK / 16;                  // times eight rows
+    const int part = gridDim.y - 1 - y, kv = x / blocks % a.heads_kv, seg = x / blocks / a.heads_kv;
+    const int c = x % blocks * 32 * NW + (thread & ~63) / 2 + (thread & 31), half = thread >> 5 & 1;
+    const Segment g = segment_of(a, seg, nullptr);
+    const int first = part * parts.tokens, len = min(g.len - first, parts.tokens), queries = a.heads_q / a.heads_kv;
+    const bool own = c < a.dim_v, last = first + parts.tokens >= g.len;
+    const int64_t state = ((int64_t)g.ring * a.heads_kv + kv) * a.dim_k * a.dim_v + c;
+    float *mid = parts.states ? parts.states + ((int64_t)(seg * a.heads_kv + kv) * parts.n + part) * a.dim_k * a.dim_v + c : nullptr;
+    const float *from = states_only ? nullptr : mid ? mid : a.state_in ? a.state_in + state : nullptr;
+    float s[ROWS][8], none = 0.f;
+#pragma unroll
+    for (int p = 0; p < ROWS; ++p)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int r = 16 * p + 8 * half + e;
+            s[p][e] = from && own && r < a.dim_k ? from[r * a.dim_v] : 0.f;
+            none += s[p][e] * 0.f;
+        }
+    if (!__ballot(!good && none == 0.f)) return false;
+    __threadfence_block();                         // (outputs are written once more)
+    const float lambda = __builtin_amdgcn_exp2f(log2_of(a.log_decay[kv]));
+    const T *k = (const T *)a.k.base + (g.begin + first) * a.k.token_stride + kv * a.k.head_stride;
+    const T *v = (const T *)a.v.base + (g.begin + first) * a.v.token_stride + kv * a.v.head_stride + c;
+#pragma unroll 1
+    for (int t = 0; t < len; ++t, k += a.k.token_stride, v += a.v.token_stride) {
+        const float vc = own ? E::to_f32(*v) : 0.f;
+#pragma unroll
+        for (int p = 0; p < ROWS; ++p) {
+            const int r = 16 * p + 8 * half;
+            const typename M::frag f = M::load(k + r, a.dim_k - r);
+            if (r < a.dim_k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[p][e] = __builtin_fmaf(E::to_f32(f[e]), vc, lambda * s[p][e]);
+        }
+        if constexpr (!states_only)
+#pragma unroll 1
+            for (int h = kv * queries; h < (kv + 1) * queries; ++h) {
+                const int64_t token = g.begin + first + t;
+                const T *q = (const T *)a.q.base + token * a.q.token_stride + h * a.q.head_stride;
+                float o = 0.f;
+#pragma unroll
+                for (int p = 0; p < ROWS; ++p) {
+                    const int r = 16 * p + 8 * half;
+                    const typename M::frag f = M::load(q + r, a.dim_k - r);
+                    if (r < a.dim_k)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) o = __builtin_fmaf(E::to_f32(f[e]), s[p][e], o);
+                }
+                o += __shfl_xor(o, 32);
+                if (own && half == 0 && !(o * 0.f == 0.f)) ((T *)a.out.base)[token * a.out.token_stride + h * a.out.head_stride + c] = E::from_f32(a.scale * o);
+            }
+    }
+    float *to = states_only ? mid : last && a.state_out ? a.state_out + state : nullptr;
+    if (to && own)
+#pragma unroll
+        for (int p = 0; p < ROWS; ++p)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (16 * p + 8 * half + e < a.dim_k) to[(16 * p + 8 * half + e) * a.dim_v] = s[p][e];
+    return true;
+}
+
+// (bfloat16, keys of up to 64, four waves: held to the 168 registers of three waves to a SIMD at the price of two spilled ones outside the loop --
+// with two waves uneven segments took 94 us in place of 80)
+template <int PREC, int DK, int NW, bool states_only>
+__global__ void __launch_bounds__(64 * NW, PREC != IDF_PREC_BF16 ? 1 : NW == 4 ? (DK <= 64 ? 3 : 2) : DK <= 64 ? 2 : 1) k_decay_chunks(idf_decay_args a, Parts parts, int blocks)
 {
     using M = Mfma<PREC>;
     using E = Elem<PREC>;
@@ -358,6 +442,11 @@ __global__ void __launch_bounds__(64 * NW, PREC == IDF_PREC_BF16 && (DK <= 64 ||
         }
     }
 
+    if (const bool good = finite(s); __builtin_expect(__ballot(!good) != 0, 0)) {
+        int x = blockIdx.x, y = blockIdx.y, thread = threadIdx.x;
+        asm volatile("" : "+s"(x), "+s"(y), "+v"(thread));                    // (everything anew: kept from the beginning it would take the registers of the loop)
+        if (part_by_tokens<PREC, DK, NW, states_only>(a, parts, blocks, x, y, thread, good)) return;
+    }
     float *to = states_only ? mid : last && a.state_out ? a.state_out + state : nullptr;
     int row = 8 * half;
     asm volatile("" : "+v"(row));                  // (places of the rows anew: kept from the beginning they would take the registers of the loop)

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_1804_10727_amd as idf
-from test_gpu_tokens import DEV, TYPES, normal
+from test_gpu_tokens import DEV, TYPES, W, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +47,53 @@ def test_decay_that_is_not_a_number(dtype, n):
     (want, want_end), (out, end) = got
     assert torch.isfinite(want).all() and torch.isnan(out[:, 0]).all() and torch.isnan(end[:, 0]).all()
     assert torch.equal(out[:, 1], want[:, 1]) and torch.equal(end[:, 1], want_end[:, 1])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("dk", [64, 96, 128])
+@pytest.mark.parametrize("n,at", [(1, 0), (4, 1), (40, 0), (40, 33), (40, 39), (600, 7), (600, 130), (600, 599)])
+def test_decay_infinite_keys_and_values_stay_in_the_state(dtype, dk, n, at):
+    """S gains k^T v: infinite of its sign where one of the two is infinite and the other is not zero, and stays so; the rest is as without it."""
+    g = torch.Generator().manual_seed(42)
+    q, k, v = (normal(g, n, 1, d, dtype=dtype) for d in (dk, dk, 64))
+    log_decay = torch.tensor([-0.02], device=DEV)
+
+    def end(k, v):
+        s = torch.randn(1, 1, dk, 64, generator=torch.Generator().manual_seed(43)).to(DEV)
+        idf.decay_attend(q.to(DEV), k.to(DEV), v.to(DEV), log_decay, s, s)
+        return s[0, 0].cpu()
+    want = end(k, v)
+    size = float((k.double().abs().amax() * v.double().abs().amax()) * min(n, 60) + 5)
+    for row, col, bad in ((None, 3, float("inf")), (None, 60, -float("inf")), (5, None, float("inf")), (dk - 1, None, -float("inf"))):
+        kk, vv = k.clone(), v.clone()
+        if row is None:
+            vv[at, 0, col] = bad
+            gained = torch.sign(k[at, 0].float())[:, None] * bad * torch.ones(1, 64)
+            hit = torch.zeros(dk, 64, dtype=torch.bool)
+            hit[:, col] = True
+        else:
+            kk[at, 0, row] = bad
+            gained = torch.ones(dk, 1) * bad * torch.sign(v[at, 0].float())[None, :]
+            hit = torch.zeros(dk, 64, dtype=torch.bool)
+            hit[row] = True
+        got = end(kk, vv)
+        assert torch.equal(got[hit], gained[hit]), (row, col)
+        # (the rest by another way in one chunk: float32 sums of 2 n terms in another order)
+        assert torch.allclose(got[~hit], want[~hit], rtol=0, atol=4 * (n + 16) * W * size), (row, col)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("dk", [40, 64, 96])
+@pytest.mark.parametrize("n,at", [(1, 0), (20, 3), (600, 130)])
+def test_decay_infinite_keys_and_values_in_outputs(dtype, dk, n, at):
+    """Of queries, keys and values that are all positive an infinite one gives infinity, from its token on, and nothing but that."""
+    g = torch.Generator().manual_seed(46)
+    q, k, v = (normal(g, n, 1, d, dtype=dtype).abs() + 0.1 for d in (dk, dk, 64))
+    log_decay = torch.tensor([-0.02], device=DEV)
+    for column, bad in ((7, "value"), (slice(None), "key")):
+        kk, vv = k.clone(), v.clone()
+        (vv if bad == "value" else kk)[at, 0, 7] = float("inf")
+        out = idf.decay_attend(q.to(DEV), kk.to(DEV), vv.to(DEV), log_decay)[:, 0]
+        hit = torch.zeros(n, 64, dtype=torch.bool, device=DEV)
+        hit[at:, column] = True
+        assert torch.all(out[hit] == float("inf")) and torch.isfinite(out[~hit]).all(), bad
