@@ -147,9 +147,12 @@ __global__ void __launch_bounds__(kThreads) k_norm_rotate(idf_norm_rotate_args a
                     if (P > 1 && a.interleaved) {
 #pragma unroll
                         for (int e = 0; e + 1 < P; e += 2) {
-                            const float2 r = cs[pair[n] + e / 2], s = at1[n] < a.rotary_dim ? cs[pair[n] + P / 2 + e / 2] : make_float2(1.f, 0.f);
-                            const float p = y0[n][e], q = y0[n][e + 1], v = y1[n][e], w = y1[n][e + 1];
+                            const float2 r = cs[pair[n] + e / 2];
+                            const float p = y0[n][e], q = y0[n][e + 1];
                             y0[n][e] = p * r.x - q * r.y; y0[n][e + 1] = q * r.x + p * r.y;
+                            if (at1[n] >= a.rotary_dim) continue;             // (not turned by nothing: zero times infinite is no zero)
+                            const float2 s = cs[pair[n] + P / 2 + e / 2];
+                            const float v = y1[n][e], w = y1[n][e + 1];
                             y1[n][e] = v * s.x - w * s.y; y1[n][e + 1] = w * s.x + v * s.y;
                         }
                     } else {

@@ -97,3 +97,22 @@ def test_decay_infinite_keys_and_values_in_outputs(dtype, dk, n, at):
         hit = torch.zeros(n, 64, dtype=torch.bool, device=DEV)
         hit[at:, column] = True
         assert torch.all(out[hit] == float("inf")) and torch.isfinite(out[~hit]).all(), bad
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("d,r", [(64, 8), (64, 24), (64, 4), (80, 20), (18, 6)])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_values_behind_the_rotated_ones_stay_by_themselves(dtype, layout, d, r, bad):
+    """What is not turned is copied: an infinite value there makes nothing else infinite, nor its neighbour not a number."""
+    g = torch.Generator().manual_seed(44)
+    x = normal(g, 3, 2, d, dtype=dtype)
+    positions, f = torch.tensor([0, 5, 1000], device=DEV), torch.linspace(0.1, 1, r // 2, dtype=torch.float64, device=DEV)
+    want, _ = idf.norm_rotate(x.to(DEV), x.to(DEV), positions, f, layout=layout)
+    for c in range(r, d):
+        y = x.clone()
+        y[:, :, c] = bad
+        got, _ = idf.norm_rotate(y.to(DEV), y.to(DEV), positions, f, layout=layout)
+        w = want.clone()
+        w[:, :, c] = bad
+        assert torch.equal(torch.nan_to_num(got.float(), nan=12345.0), torch.nan_to_num(w.float(), nan=12345.0)), c
