@@ -9,12 +9,38 @@ namespace idf {
 
 namespace {
 
+// A decay that is applied again and again, as the largest float32 number not above it and the rest: one rounded number would be off in the same
+// direction each time (half a step of 2^-25: after 4000 tokens 1e-4, where the roundings of the state cancel to 1e-6).  Both are positive wherever
+// the decay is, so that an infinite state stays infinite.
+struct Factor {
+    float high, low;
+    __device__ __forceinline__ float times(float s) const { return __builtin_fmaf(high, s, low * s); }
+};
+__device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
+// high + rest, a rest of half a step of it at most, either sign.
+__device__ __forceinline__ Factor factor_of(float high, float rest)
+{
+    if (rest < 0.f) {                              // (one step down; exact, as the two are of one size)
+        const float down = __builtin_bit_cast(float, __builtin_bit_cast(int, high) - 1);
+        rest += high - down;
+        high = down;
+    }
+    return {uniform(high), uniform(fmaxf(rest, high * 0x1p-60f))};
+}
+// exp(log_decay).  Where it is near one, by what it lacks, to 2^-23 of that; where not, what has been multiplied a few times is gone.
+__device__ __forceinline__ Factor factor_of(float log_decay)
+{
+    if (log_decay < -0.5f) return factor_of(expf(log_decay), 0.f);
+    const float lacks = expm1f(log_decay), high = 1.f + lacks;
+    return factor_of(high, lacks - (high - 1.f));
+}
+
 // The recurrence itself, token by token.  A wave owns 32 columns of the state of one key/value head: eight lanes side by side hold four
-// columns each, eight lanes below each other ROWS rows each, so that a token costs two multiply-adds per value of the state and a sum
+// columns each, eight lanes below each other ROWS rows each, so that a token costs four multiply-adds per value of the state and a sum
 // over eight lanes per query; nothing is shared between waves.  Bound by memory: the state is
-// read and written once (64 streams x 16 heads of 128 x 128, a token each: 29 us, 4.7 TB/s).
+// read and written once (64 streams x 16 heads of 128 x 128, a token each: 29.6 us, 4.6 TB/s).
 template <int PREC, int ROWS>
-__global__ void __launch_bounds__(256) k_decay_tokens(idf_decay_args a, int column_groups)
+__global__ void __launch_bounds__(256, ROWS == 8 ? 3 : 1) k_decay_tokens(idf_decay_args a, int column_groups)
 {
     using E = Elem<PREC>;
     using T = typename E::type;
@@ -24,7 +50,7 @@ __global__ void __launch_bounds__(256) k_decay_tokens(idf_decay_args a, int colu
     const Segment g = segment_of(a, blockIdx.y, nullptr);
     if (!g.valid) return;
     const int queries = a.heads_q / a.heads_kv;
-    const float lambda = expf(a.log_decay[kv]);
+    const Factor lambda = factor_of(a.log_decay[kv]);
     const bool on = c0 < a.dim_v;
     const int64_t state = ((int64_t)g.ring * a.heads_kv + kv) * a.dim_k * a.dim_v;
     f32x4 s[ROWS];
@@ -45,7 +71,7 @@ __global__ void __launch_bounds__(256) k_decay_tokens(idf_decay_args a, int colu
         for (int r = 0; r < ROWS; ++r) {
             const float kr = r0 + r < a.dim_k ? E::to_f32(k[r0 + r]) : 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[r][e] = __builtin_fmaf(kr, vv[e], lambda * s[r][e]);
+            for (int e = 0; e < 4; ++e) s[r][e] = __builtin_fmaf(kr, vv[e], lambda.times(s[r][e]));
         }
         for (int h = kv * queries; h < (kv + 1) * queries; ++h) {
             const T *q = (const T *)a.q.base + row * a.q.token_stride + h * a.q.head_stride;
@@ -98,7 +124,6 @@ struct Parts {
     float *states;             // [segment][head][part][dim_k][dim_v]; nullptr for one part
 };
 
-__device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
 __device__ __forceinline__ float log2_of(float log_decay)
 {
     const float x = log_decay * 1.4426950408889634f;
@@ -469,7 +494,8 @@ __global__ void __launch_bounds__(256) k_decay_scan(idf_decay_args a, Parts part
     const Segment g = segment_of(a, seg, nullptr);
     if (!g.valid || x >= size) return;
     const int n = max(1, (g.len + parts.tokens - 1) / parts.tokens);
-    const float keep = (float)exp2((double)parts.tokens * (double)log2_of(a.log_decay[kv]));
+    const double whole = exp2((double)parts.tokens * (double)log2_of(a.log_decay[kv]));
+    const Factor keep = factor_of((float)whole, (float)(whole - (double)(float)whole));
     float *at = parts.states + (int64_t)blockIdx.y * parts.n * size + x;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (a.state_in) s = *(const f32x4 *)(a.state_in + ((int64_t)g.ring * a.heads_kv + kv) * size + x);
@@ -483,7 +509,7 @@ __global__ void __launch_bounds__(256) k_decay_scan(idf_decay_args a, Parts part
             if (p0 + y >= n) break;
             *(f32x4 *)(at + (int64_t)y * size) = s;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[e] = __builtin_fmaf(s[e], keep, left[y][e]);
+            for (int e = 0; e < 4; ++e) s[e] = keep.times(s[e]) + left[y][e];
         }
     }
 }

@@ -1,4 +1,5 @@
 """The operators that mix tokens where calls are at their edges: no tokens, values that are infinite or not a number, positions far out."""
+import numpy as np
 import pytest
 import torch
 
@@ -116,3 +117,34 @@ def test_values_behind_the_rotated_ones_stay_by_themselves(dtype, layout, d, r, 
         w = want.clone()
         w[:, :, c] = bad
         assert torch.equal(torch.nan_to_num(got.float(), nan=12345.0), torch.nan_to_num(w.float(), nan=12345.0)), c
+
+
+# ---- long streams of slow decays ----
+
+def relative(state, start, log_decay, n):
+    """Mean over each head's values of the relative error of what n tokens without keys have left."""
+    want = start.double() * torch.exp(log_decay.double() * n)[None, :, None, None]
+    return ((state.double() - want) / want).mean(dim=(0, 2, 3)).abs().cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+def test_decay_rounding_of_a_factor_does_not_add_up(dtype):
+    """A state that nothing is added to, token by token and by parts: float32 roundings of the state, in either direction, cancel over its
+    many values; a factor that is off by half a step of float32 would be off in the same direction for all of them.
+
+    Each of n products rounds by at most W.  A slow decay leaves a value nearly where it is, so that its roundings can all be alike, but not those of
+    another value: errors of up to n W, independent from value to value, evenly spread (a root of 3 less), leave a mean over m values of at most
+    6 n W / sqrt(3 m)."""
+    log_decay = -torch.tensor([5e-4, 3.3e-4, 1e-4, 2.7e-5, 1e-6, 4e-3], device=DEV)
+    h = len(log_decay)
+    g = torch.Generator().manual_seed(45)
+    for n, dk, steps in ((4000, 256, 4000), (65536, 64, 65536 // 128 + 4)):        # tokens; parts of 128 tokens, and the last one's chunks
+        start = (1 + torch.rand(1, h, dk, 64, generator=g)).to(DEV)
+        q, k, v = (torch.zeros(n, h, d, dtype=dtype, device=DEV) for d in (dk, dk, 64))
+        end = torch.empty_like(start)
+        idf.decay_attend(q, k, v, log_decay, start, end)
+        keep = (log_decay * n > -60).cpu().numpy()
+        off = relative(end, start, log_decay, n)
+        # (the exponent of a part is formed from a float32 logarithm: n |log_decay| W)
+        bound = 6 * steps * W / np.sqrt(3 * dk * 64) + n * log_decay.abs().cpu().numpy() * W
+        assert np.all(off[keep] <= bound[keep]), (n, off / bound)
