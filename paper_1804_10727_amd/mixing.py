@@ -45,9 +45,19 @@ class TokenMixer:
     def push(self, x, counts=None):
         """x: the new rows of all streams behind each other, [rows][channels]; counts: how many of each stream (None: the same of all)."""
         import torch
-        n = torch.full_like(self.starts, x.shape[0] // self.starts.numel()) if counts is None else torch.as_tensor(counts, device=x.device)
+        streams = self.starts.numel()
+        # (on the GPU nothing would refuse wrong counts: positions are laid out for so many rows)
+        if counts is None:
+            if x.shape[0] % streams:
+                raise ValueError(f"{x.shape[0]} rows are not as many of each of {streams} streams")
+            n = torch.full_like(self.starts, x.shape[0] // streams)
+        else:
+            counts = torch.as_tensor(counts)
+            if counts.dtype.is_floating_point or counts.shape != (streams,) or int(counts.min()) < 0 or int(counts.sum()) != x.shape[0]:
+                raise ValueError(f"{x.shape[0]} rows of {streams} streams, {counts.tolist()} of each")
+            n = counts.to(x.device, torch.int64)
         ends = n.cumsum(0)
-        segments = {} if counts is None else dict(offsets=torch.cat([ends.new_zeros(1), ends]), max_tokens=int(max(counts)))
+        segments = {} if counts is None else dict(offsets=torch.cat([ends.new_zeros(1), ends]), max_tokens=int(counts.max()))
         positions = torch.arange(x.shape[0], device=x.device) + torch.repeat_interleave(self.starts - ends + n, n, output_size=x.shape[0])
         q, k, v = self._split(x, 0)
         norm_rotate(q, k, positions, self.frequencies, amplitude=self.amplitude, q_weight=self.q_weight, k_weight=self.k_weight, q_out=q, k_out=k)
