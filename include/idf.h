@@ -437,7 +437,7 @@ int idf_measure_peak(int kind, void *dev_buf, size_t bytes, void *hip_stream, do
  * 0 .. n_tokens and to at most max_tokens per segment; a segment whose start is negative or whose stream id is none takes no part, and its rows
  * of out are left as they are.  Two segments of one call must not name the same stream, and out must not overlap q, k, v or a cache.
  *   Workspaces (where asked for): any contents, 256-byte aligned, used until the work enqueued by the call is done.
- * Errors: IDF_EINVAL (null pointers, sizes, strides), IDF_EUNSUPPORTED (precision, head sizes, alignment), IDF_ENOMEM (workspace too
+ * Errors: IDF_EINVAL (null pointers, sizes, strides, outputs whose own rows share places), IDF_EUNSUPPORTED (precision, head sizes, alignment), IDF_ENOMEM (workspace too
  * small), IDF_EDEVICE; nothing has been enqueued then, except by IDF_EDEVICE from a launch behind the first. */
 
 /* A matrix of tokens: values of head h of token t at base + t * token_stride + h * head_stride. */

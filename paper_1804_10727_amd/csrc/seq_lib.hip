@@ -1,4 +1,5 @@
 // Entry points of the operators that mix the tokens of streams: checks of arguments; what is launched is decided in the k_*.hip files.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 
@@ -17,6 +18,22 @@ constexpr int64_t kMostSlots = 1 << 30;            // lists of keys are counted 
 
 bool precision_ok(int p) { return p == IDF_PREC_F32 || p == IDF_PREC_BF16; }
 
+// Whether two rows of dim values, at token * token_stride + head * head_stride, share a place: for each distance between heads the two distances
+// between tokens that come nearest to it.  (Signs do not matter: tokens may be as far apart in either direction.)
+bool rows_overlap(const idf_tokens &t, int64_t n_tokens, int heads, int dim)
+{
+    using Wide = __int128;
+    const Wide token = t.token_stride < 0 ? -(Wide)t.token_stride : (Wide)t.token_stride, head = t.head_stride < 0 ? -(Wide)t.head_stride : (Wide)t.head_stride;
+    if ((n_tokens > 1 && token < dim) || (heads > 1 && head < dim)) return true;
+    if (n_tokens <= 1 || heads <= 1 || token >= (heads - 1) * head + dim || head >= (n_tokens - 1) * token + dim) return false;
+    for (int h = 1; h < heads; ++h) {
+        const Wide at = h * head, before = std::min<Wide>(at / token, n_tokens - 1);
+        if (at - before * token < dim) return true;
+        if (before + 1 < n_tokens && (before + 1) * token - at < dim) return true;
+    }
+    return false;
+}
+
 // A matrix of tokens that 16-byte pieces are read from or written to.
 int check_tokens(const char *what, const idf_tokens &t, int precision, bool out, int64_t n_tokens, int heads, int dim)
 {
@@ -24,8 +41,7 @@ int check_tokens(const char *what, const idf_tokens &t, int precision, bool out,
     if (!t.base) return fail(IDF_EINVAL, "%s: null pointer", what);
     if ((uintptr_t)t.base % 16 || t.token_stride % vl || t.head_stride % vl)
         return fail(IDF_EUNSUPPORTED, "%s: base and strides have to be multiples of 16 bytes", what);
-    if (out && ((heads > 1 && std::llabs(t.head_stride) < dim) || (n_tokens > 1 && std::llabs(t.token_stride) < dim)))
-        return fail(IDF_EINVAL, "%s: rows overlap", what);
+    if (out && rows_overlap(t, n_tokens, heads, dim)) return fail(IDF_EINVAL, "%s: rows overlap", what);
     return IDF_OK;
 }
 
@@ -132,8 +148,7 @@ int idf_norm_rotate(const idf_norm_rotate_args *a, void *hip_stream)
         const char *names[] = {"q", "k", "q_out", "k_out"};
         if (!each[i]->base) return fail(IDF_EINVAL, "%s: null pointer", names[i]);
         if ((uintptr_t)each[i]->base % eb) return fail(IDF_EINVAL, "%s: not aligned to its values", names[i]);
-        if (i >= 2 && ((heads > 1 && std::llabs(each[i]->head_stride) < a->head_dim) || (a->n_tokens > 1 && std::llabs(each[i]->token_stride) < a->head_dim)))
-            return fail(IDF_EINVAL, "%s: rows overlap", names[i]);
+        if (i >= 2 && rows_overlap(*each[i], a->n_tokens, heads, a->head_dim)) return fail(IDF_EINVAL, "%s: rows overlap", names[i]);
     }
     if (a->rotary_dim && (!a->positions || !a->frequencies)) return fail(IDF_EINVAL, "a rotation without positions or frequencies");
     LaunchCtx lc;

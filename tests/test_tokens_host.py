@@ -75,3 +75,40 @@ def decay_plans(rt):
 
 def test_decay_launches_parts_only_into_a_workspace(runtime):
     host_runtime.run(runtime, "test_tokens_host", "decay_plans")
+
+
+def overlapping(rt):
+    import ctypes as C
+    import random
+
+    from paper_1804_10727_amd import binding, tokens
+    L = binding.load_library()
+    rng = random.Random(5)
+    seen = set()
+    for _ in range(4000):
+        n, heads, dim = rng.choice([1, 2, 3, 7]), rng.choice([1, 2, 3, 8]), 8
+        token, head = (rng.choice([0, 4, 8, 12, 16, 20, 24, 40, 64, 68, 72, 200]) * rng.choice([1, 1, -1]) for _ in range(2))
+        places = [(t * token + h * head + c) for t in range(n) for h in range(heads) for c in range(dim)]
+        apart = len(set(places)) == len(places)
+        seen.add(apart)
+        inside, out = tokens._Tokens(AT, heads * dim, dim), tokens._Tokens(AT, token, head)
+        w = tokens._Window(0, heads, heads, dim, n, n, 1, 1, 0, 8, 0, 0.25, inside, inside, inside, out, None, None, None, None, None, None, 0)
+        d = tokens._Decay(0, heads, heads, dim, dim, n, n, 1, 1, 0.25, inside, inside, inside, out, AT, None, None, None, None, None, 0)
+        r = tokens._NormRotate(0, heads, heads, dim, 0, 0, n, inside, inside, out, inside, None, None, None, None, 1.0, 1e-6)
+        s = tokens._NormRotate(0, heads, heads, dim, 0, 0, n, inside, inside, inside, out, None, None, None, None, 1.0, 1e-6)
+        for fn, a in (("idf_window_attend", w), ("idf_decay_attend", d), ("idf_norm_rotate", r), ("idf_norm_rotate", s)):
+            rt.host_begin()
+            rc = getattr(L, fn)(C.byref(a), None)
+            assert rc == (0 if apart else -1) and (rt.host_launches(None) > 0) == apart, (fn, n, heads, token, head)
+            assert apart or b"overlap" in L.idf_last_error()
+    assert seen == {False, True}
+    # strides as large as they can be
+    for token, head in ((1 << 62, 8), (8, 1 << 62), (-(1 << 63), 8), (-(1 << 63), -(1 << 63)), ((1 << 63) - 8, -(1 << 63)), ((1 << 62) + 4, 1 << 62)):
+        a = tokens._Window(0, 2, 2, 8, 2, 2, 1, 1, 0, 8, 0, 0.25, inside, inside, inside, tokens._Tokens(AT, token, head), None, None, None, None, None, None, 0)
+        rt.host_begin()
+        assert L.idf_window_attend(C.byref(a), None) == (-1 if abs(token) == abs(head) or abs(abs(token) - abs(head)) < 8 else 0), (token, head)
+
+
+def test_outputs_whose_rows_overlap_are_refused(runtime):
+    """Rows of tokens and heads by two strides, against the set of all their places."""
+    host_runtime.run(runtime, "test_tokens_host", "overlapping")
