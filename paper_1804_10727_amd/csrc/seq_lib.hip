@@ -14,6 +14,8 @@ constexpr int kMostSegments = 65535;               // a launch's second or third
 constexpr int kMostHeads = 1024;
 constexpr int64_t kMostPairs = 1 << 23;            // segments times key/value heads (times columns by 64): a launch's first axis, 2^32 threads
 constexpr int64_t kMostRows = 65535 * 128;         // query rows of a segment and key/value head: its second
+constexpr int64_t kMostTokens = 1 << 30;           // of a segment: places behind its last chunk are counted in 32 bits
+constexpr int64_t kMostByToken = 1 << 23;          // the same where tokens follow each other one by one: more would hold the machine for a minute
 constexpr int64_t kMostSlots = 1 << 30;            // lists of keys are counted in 32 bits
 
 bool precision_ok(int p) { return p == IDF_PREC_F32 || p == IDF_PREC_BF16; }
@@ -56,8 +58,8 @@ int check_segments(const Args &a)
     if (a.n_segments > kMostSegments) return fail(IDF_EUNSUPPORTED, "%d segments: at most %d in a call", a.n_segments, kMostSegments);
     if (!a.offsets && (int64_t)a.n_segments * a.max_tokens != a.n_tokens)
         return fail(IDF_EINVAL, "%lld tokens are not %d segments of %lld", (long long)a.n_tokens, a.n_segments, (long long)a.max_tokens);
-    if ((int64_t)a.n_segments * a.heads_kv > kMostPairs || a.max_tokens * (a.heads_q / a.heads_kv) > kMostRows)
-        return fail(IDF_EUNSUPPORTED, "%d segments of up to %lld tokens with %d heads: more than a launch takes", a.n_segments, (long long)a.max_tokens, a.heads_q);
+    if ((int64_t)a.n_segments * a.heads_kv > kMostPairs)
+        return fail(IDF_EUNSUPPORTED, "%d segments with %d heads: more than a launch takes", a.n_segments, a.heads_kv);
     if (!a.stream_ids && a.n_segments > a.n_streams) return fail(IDF_EINVAL, "%d segments of %d streams", a.n_segments, a.n_streams);
     if (!(a.scale > 0.f) || std::isinf(a.scale)) return fail(IDF_EINVAL, "scale %g", (double)a.scale);
     return IDF_OK;
@@ -67,6 +69,8 @@ int check_window(const idf_window_args *a)
 {
     if (!a) return fail(IDF_EINVAL, "null argument");
     if (int rc = check_segments(*a)) return rc;
+    if (a->max_tokens * (a->heads_q / a->heads_kv) > kMostRows)
+        return fail(IDF_EUNSUPPORTED, "segments of up to %lld tokens with %d heads on %d: more than a launch takes", (long long)a->max_tokens, a->heads_q, a->heads_kv);
     const int vl = a->precision == IDF_PREC_F32 ? 4 : 8;
     if (a->head_dim < vl || a->head_dim > 256 || a->head_dim % vl) return fail(IDF_EUNSUPPORTED, "heads of %d values", a->head_dim);
     if (a->window < 1 || a->sinks < 0) return fail(IDF_EINVAL, "a window of %d tokens and %d first ones", a->window, a->sinks);
@@ -86,6 +90,8 @@ int check_decay(const idf_decay_args *a)
     const int vl = a->precision == IDF_PREC_F32 ? 4 : 8;
     if (a->dim_k < vl || a->dim_k > 256 || a->dim_k % vl || a->dim_v < vl || a->dim_v % vl || a->dim_v > 4096)
         return fail(IDF_EUNSUPPORTED, "heads of %d and %d values", a->dim_k, a->dim_v);
+    if (std::min(a->max_tokens, a->n_tokens) > (a->dim_k > 128 ? kMostByToken : kMostTokens))
+        return fail(IDF_EUNSUPPORTED, "segments of up to %lld tokens with keys of %d values", (long long)a->max_tokens, a->dim_k);
     if ((int64_t)a->n_segments * a->heads_kv * ((a->dim_v + 63) / 64) > kMostPairs)
         return fail(IDF_EUNSUPPORTED, "%d segments with %d heads of %d values: more than a launch takes", a->n_segments, a->heads_kv, a->dim_v);
     if (((uintptr_t)a->state_in | (uintptr_t)a->state_out) % 16) return fail(IDF_EUNSUPPORTED, "states have to be 16-byte aligned");

@@ -148,3 +148,28 @@ def test_decay_rounding_of_a_factor_does_not_add_up(dtype):
         # (the exponent of a part is formed from a float32 logarithm: n |log_decay| W)
         bound = 6 * steps * W / np.sqrt(3 * dk * 64) + n * log_decay.abs().cpu().numpy() * W
         assert np.all(off[keep] <= bound[keep]), (n, off / bound)
+
+
+# ---- many rows ----
+
+def test_decay_more_query_rows_than_a_launch_axis():
+    """9 000 tokens of 1 024 query heads on one: each head as by itself."""
+    g = torch.Generator(DEV).manual_seed(47)
+    q, k, v = (torch.randn(9000, h, 8, generator=g, device=DEV).bfloat16() for h in (1024, 1, 1))
+    log_decay = torch.tensor([-0.01], device=DEV)
+    out = idf.decay_attend(q, k, v, log_decay)
+    for h in (0, 511, 1023):
+        assert torch.equal(out[:, h:h + 1], idf.decay_attend(q[:, h:h + 1].contiguous(), k, v, log_decay))
+
+
+def test_a_push_of_the_mixer_without_rows():
+    from paper_1804_10727_amd.mixing import TokenMixer
+    g = torch.Generator().manual_seed(48)
+    a, b = (TokenMixer(32, 3, heads=2, kv_heads=1, dim=32, window=8) for _ in range(2))
+    for counts in ((2, 0, 1), (0, 0, 0), (1, 30, 2)):
+        x = torch.randn(sum(counts), 32, generator=g).to(DEV)
+        y = a.push(x, counts)
+        assert y.shape == x.shape
+        if sum(counts):
+            assert torch.equal(y, b.push(x, counts))
+    assert a.starts.tolist() == [3, 30, 3] and torch.equal(a.state, b.state)

@@ -112,3 +112,21 @@ def overlapping(rt):
 def test_outputs_whose_rows_overlap_are_refused(runtime):
     """Rows of tokens and heads by two strides, against the set of all their places."""
     host_runtime.run(runtime, "test_tokens_host", "overlapping")
+
+
+def long_segments(rt):
+    from paper_1804_10727_amd import tokens
+    for n_tokens, max_tokens, heads_q, segments in ((9000000, 9000000, 1, 1), (10000, 10000, 1024, 1), (100, 1 << 30, 4, 3), (0, (1 << 31) - 1, 4, 3), (1 << 30, (1 << 31) - 1, 1, 1)):
+        a = decay_args(1, max_tokens, n_tokens, segments=segments, heads=1)
+        a.heads_q, a.q, a.out = heads_q, *[tokens._Tokens(AT, heads_q * 64, 64)] * 2
+        need = workspace(a)
+        a.workspace, a.workspace_bytes = AT, need
+        assert attend(rt, a) == 0 and rt.host_launches(None) == (3 if need else 1), (n_tokens, max_tokens)
+    assert attend(rt, decay_args(1, (1 << 30) + 1, (1 << 30) + 1, segments=1, heads=1)) == -5
+    assert attend(rt, decay_args(1, 1 << 23, 1 << 23, segments=1, heads=1, dim_k=256)) == 0      # (token by token)
+    assert attend(rt, decay_args(1, 1 << 24, 1 << 24, segments=1, heads=1, dim_k=256)) == -5
+
+
+def test_decay_takes_segments_that_the_window_does_not(runtime):
+    """The decayed attention has no axis of query rows: segments are cut into parts, and tokens counted in 32 bits."""
+    host_runtime.run(runtime, "test_tokens_host", "long_segments")
