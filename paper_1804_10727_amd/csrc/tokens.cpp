@@ -6,6 +6,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 
 #include <climits>
 #include <cmath>
@@ -49,7 +50,9 @@ const at::Tensor *tensor(PyObject *o)
 {
     if (o == Py_None) return nullptr;
     need(THPVariable_CheckExact(o));
-    return &THPVariable_Unpack(o);
+    const at::Tensor &t = THPVariable_Unpack(o);
+    need(!t.requires_grad() || !c10::GradMode::is_enabled());                // (refused there: there is no backward pass)
+    return &t;
 }
 
 int precision(const at::Tensor &t)

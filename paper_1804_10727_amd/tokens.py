@@ -1,6 +1,7 @@
 """The operators that mix the tokens of streams (include/idf.h, last section) on torch tensors: argument marshalling only.
 
-Everything is enqueued on the current stream of the tensors' device; outputs carry no gradients.  Packed tokens [token][head][value]; a tensor whose values lie
+Everything is enqueued on the current stream of the tensors' device.  There is no backward pass: tensors that require gradients are refused
+where gradients are recorded, taken under torch.no_grad().  Packed tokens [token][head][value]; a tensor whose values lie
 apart, or whose rows do not begin at multiples of 16 bytes where the library asks for that, is copied first.
 """
 from __future__ import annotations
@@ -59,6 +60,13 @@ def _direct(name, q, *args):
     if type(r) is int:
         _check(r)
     return r
+
+
+def _no_gradients(**tensors):
+    import torch
+    for what, t in tensors.items():
+        if torch.is_grad_enabled() and getattr(t, "requires_grad", False):
+            raise ValueError(f"{what} requires gradients, and there is no backward pass: detach it, or call under torch.no_grad()")
 
 
 def _precision(t):
@@ -137,6 +145,7 @@ def norm_rotate(q, k, positions, frequencies, layout="half", amplitude=1.0, q_we
 
 def _norm_rotate(q, k, positions, frequencies, layout, amplitude, q_weight, k_weight, eps, q_out, k_out):
     import torch
+    _no_gradients(q=q, k=k, frequencies=frequencies, q_weight=q_weight, k_weight=k_weight, q_out=q_out, k_out=k_out)
     q, k = _rows(q, q, "q", aligned=False), _rows(k, q, "k", aligned=False)
     n, hq, d = q.shape
     if k.shape[0] != n or k.shape[2] != d:
@@ -191,6 +200,7 @@ def window_attend(q, k, v, k_ring=None, v_ring=None, starts=None, *, window, sin
 
 def _window_attend(q, k, v, k_ring, v_ring, starts, window, sinks, scale, offsets, max_tokens, stream_ids, out):
     import torch
+    _no_gradients(q=q, k=k, v=v, k_ring=k_ring, v_ring=v_ring, out=out)
     q, k, v = _rows(q, q, "q"), _rows(k, q, "k"), _rows(v, q, "v")
     n, hq, d = q.shape
     hkv = k.shape[1]
@@ -233,6 +243,7 @@ def decay_attend(q, k, v, log_decay, state=None, state_out=None, *, scale=None, 
 
 def _decay_attend(q, k, v, log_decay, state, state_out, scale, offsets, max_tokens, n_segments, stream_ids, out):
     import torch
+    _no_gradients(q=q, k=k, v=v, log_decay=log_decay, state=state, state_out=state_out, out=out)
     q, k, v = _rows(q, q, "q"), _rows(k, q, "k"), _rows(v, q, "v")
     n, hq, dk = q.shape
     hkv, dv = v.shape[1:]

@@ -173,3 +173,30 @@ def test_a_push_of_the_mixer_without_rows():
         if sum(counts):
             assert torch.equal(y, b.push(x, counts))
     assert a.starts.tolist() == [3, 30, 3] and torch.equal(a.state, b.state)
+
+
+# ---- gradients ----
+
+def test_tensors_that_require_gradients_are_refused():
+    """There is no backward pass: nothing is read, written or lost silently; without recording they are tensors as any other."""
+    q, k, v = (torch.randn(4, h, 64, device=DEV) for h in (2, 1, 1))
+    f, _ = idf.rotary_frequencies(64, device=DEV)
+    rings = [torch.zeros(1, 8, 1, 64, device=DEV) for _ in range(2)]
+    p, w, state, into = torch.arange(4, device=DEV), torch.ones(64, device=DEV), torch.zeros(1, 1, 64, 64, device=DEV), torch.empty(4, 2, 64, device=DEV)
+    log_decay, start = torch.tensor([-0.1], device=DEV), torch.zeros(1, dtype=torch.int64, device=DEV)
+    calls = ((idf.norm_rotate, (q, k, p, f), dict(q_weight=w, k_weight=w.clone(), q_out=into, k_out=torch.empty_like(k))),
+             (idf.window_attend, (q, k, v, *rings, start), dict(window=8, out=into)),
+             (idf.decay_attend, (q, k, v, log_decay, state, state.clone()), dict(out=into)))
+    for call, args, kw in calls:
+        call(*args, **kw)
+        for t in [*args, *kw.values()]:
+            if not torch.is_tensor(t) or not t.is_floating_point():
+                continue
+            t.requires_grad_(True)
+            before = [x.detach().clone() for x in [*args, *kw.values()] if torch.is_tensor(x)]
+            with pytest.raises(ValueError, match="gradients"):
+                call(*args, **kw)
+            assert all(torch.equal(a, b) for a, b in zip(before, [x for x in [*args, *kw.values()] if torch.is_tensor(x)]))
+            with torch.no_grad():
+                call(*args, **kw)
+            t.requires_grad_(False)
