@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import paper_1804_10727_amd as idf
-from test_gpu_tokens import DEV, TYPES, W, normal
+from oracle import tokens as oracle
+from test_gpu_tokens import DEV, TYPES, W, decay_case, f64, half_step, normal, rounded, within
 
 pytestmark = pytest.mark.gpu
 
@@ -200,3 +201,57 @@ def test_tensors_that_require_gradients_are_refused():
             with torch.no_grad():
                 call(*args, **kw)
             t.requires_grad_(False)
+
+
+# ---- positions far out, offsets that lie, long keys ----
+
+def turns(p, f):
+    """Cosine and sine of the exact product of a whole number and a float64 one."""
+    from decimal import Decimal, getcontext
+    getcontext().prec = 90
+    pi = Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534211706798")
+    angle = float((Decimal(p) * Decimal(f)) % (2 * pi))
+    return np.cos(angle), np.sin(angle)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rotation_at_positions_beyond_32_bits(dtype, layout):
+    """Angles are float64: the product with the frequency, the number of quarter turns in one radian and the product with that are rounded once each,
+    2^-53 of the angle.  The rest, taken to a quarter turn, is float32 as anywhere (test_norm_rotate)."""
+    g = torch.Generator().manual_seed(49)
+    positions = [0, 3, 1 << 24, (1 << 31) - 1, (1 << 31) + 7, (1 << 34) + 12345, (1 << 40) + 99, -(1 << 35) - 1]
+    d = 64
+    f, amplitude = idf.rotary_frequencies(d, scaling="parts", factor=8.0)
+    x = normal(g, len(positions), 2, d, dtype=dtype)
+    got, _ = idf.norm_rotate(x.to(DEV), x.to(DEV), torch.tensor(positions, device=DEV), f.to(DEV), layout=layout, amplitude=amplitude)
+    want, bound = f64(x).copy(), np.zeros(x.shape)
+    for i in range(d // 2):
+        a, b = (i, i + d // 2) if layout == "half" else (2 * i, 2 * i + 1)
+        for t, p in enumerate(positions):
+            c, s = (amplitude * y for y in turns(p, f[i].item()))
+            u, v = f64(x)[t, :, a], f64(x)[t, :, b]
+            want[t, :, a], want[t, :, b] = u * c - v * s, v * c + u * s
+            size = amplitude * (np.abs(u) + np.abs(v))
+            bound[t, :, a] = bound[t, :, b] = size * (3 * 2.0 ** -53 * abs(p) * f[i].item() + 32 * W)
+    within(got, want, half_step(dtype) * np.abs(want) + bound)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("m", [4, 200])
+def test_window_offsets_that_lie_cut_segments_where_they_can(dtype, m):
+    """Ends behind the next beginning are cut to the longest segment, ends ahead of their beginning leave nothing, and all to the tokens there are."""
+    g = torch.Generator().manual_seed(50)
+    n = 3 * m
+    q, k, v = (normal(g, n, h, 64, dtype=dtype) for h in (2, 1, 1))
+    out = torch.full((n, 2, 64), 9.0, dtype=dtype, device=DEV)
+    idf.window_attend(*(x.to(DEV) for x in (q, k, v)), window=1000, offsets=torch.tensor([-5, m, 2 * m + 5, 2 * m, 1 << 40], device=DEV), max_tokens=m, out=out)
+    for rows in (slice(0, m), slice(m, 2 * m), slice(2 * m, n)):
+        want, size, score = oracle.Attention(1000, 0, 1 / 8).push(*(f64(x[rows]) for x in (q, k, v)))
+        within(out[rows], want, half_step(dtype) * np.abs(want) + (rounded(dtype) + 4 * 72 * W * score[..., None] + 2 * (m + 16) * W) * size, rows)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(256, 64), (136, 40)])
+def test_decay_long_segments_of_long_keys(dtype, dk, dv):
+    decay_case(dtype, 2, 1, dk, dv, (1500, 3, 0, 129), seed=dk)

@@ -187,3 +187,14 @@ def test_extension_names_do_not_depend_on_the_thread_that_asks(monkeypatch):
     want = sysconfig.get_config_var("EXT_SUFFIX")
     monkeypatch.setattr(sysconfig, "get_config_var", lambda name: None)
     assert want and build.push_path().endswith(want) and build.tokens_path().endswith(want)
+
+
+def test_calls_of_many_parts_need_their_workspace():
+    L = idf.load_library()
+    for fn, a in (("window", window_args(heads_q=1, precision=1, head_dim=16, n_tokens=1, max_tokens=1, window=1 << 20, slots=1 << 20)),
+                  ("decay", decay_args(heads_q=1, precision=1, n_tokens=1 << 20, max_tokens=1 << 20))):
+        nb = C.c_size_t()
+        assert getattr(L, f"idf_{fn}_workspace")(C.byref(a), C.byref(nb)) == 0 and nb.value > 0
+        for at, size, want in ((None, 0, -2), (None, nb.value, -2), (AT, nb.value - 1, -2), (AT + 16, nb.value, -1)):
+            a.workspace, a.workspace_bytes = at, size
+            assert code(f"idf_{fn}_attend", a) == want, (fn, at, size)
