@@ -506,7 +506,9 @@ int idf_window_attend(const idf_window_args *a, void *hip_stream);
  *   S_t = lambda S_{t-1} + k_t^T v_t,   out_t = scale * q_t S_t,
  * from the state S of the segment's stream before it to the one after it.  state_in, state_out: float32 [n_streams][heads_kv][dim_k][dim_v];
  * they may be the same; state_in NULL: zeros; state_out NULL: not wanted.  A segment without tokens hands its state on.
- *   dim_k, dim_v multiples of 16 bytes, dim_k <= 256; tokens' bases and strides multiples of 16 bytes; log_decay float32 [heads_kv], <= 0. */
+ *   dim_k, dim_v multiples of 16 bytes, dim_k <= 256, dim_v <= 4096; tokens' bases and strides multiples of 16 bytes; log_decay float32 [heads_kv],
+ * <= 0.  Segments of up to 2^30 tokens.  Keys of more than 128 values go token by token, some 4 to 6 us each whatever the number of heads: for single tokens
+ * and short segments; at most 2^23 of them in a segment. */
 typedef struct {
     int precision, heads_q, heads_kv, dim_k, dim_v;
     int64_t n_tokens, max_tokens;

@@ -112,9 +112,10 @@ __global__ void __launch_bounds__(256, ROWS == 8 ? 3 : 1) k_decay_tokens(idf_dec
 //   Roundings in bfloat16: scores times decay, and the state where it meets the queries, are rounded to bfloat16 (half a step of 2^-8, as the
 // output is).  The state itself stays float32: a decayed value, 24 bits, goes into the product as three bfloat16 numbers that add up to it.
 //   Bound by memory: q, k, v and out once, k and v twice where a segment is cut into parts (one prompt of 65536 tokens, 16 heads of 128 x 128 in
-// bfloat16: 405 us, of them 140 for the states of the parts, 17 for the scan and 250 for the outputs, 4.3 TB/s; loads of the outputs' pass
+// bfloat16: 400 to 418 us by the machine, of them 136 to 146 for the states of the parts, 14 for the scan and 250 to 277 for the outputs, 4 TB/s;
+// matrix cores and LDS a third of the time, waves waiting for 34 to 40 %; loads of the outputs' pass
 // two chunks ahead took longer, 512 us in all: between stores they are waited for all the same).  Short calls by latency: 64 streams of 16 tokens,
-// 4 heads of 64 x 64 in float32, 10 us.
+// 4 heads of 64 x 64 in float32, 10.2 us.
 constexpr int kChunk = 32;
 
 // Segments cut into parts along time, so that there is work for every compute unit: the state that each part leaves if it begins with none,
@@ -212,8 +213,8 @@ __device__ __forceinline__ bool part_by_tokens(const idf_decay_args &a, const Pa
     return true;
 }
 
-// (bfloat16, keys of up to 64, four waves: held to the 168 registers of three waves to a SIMD at the price of two spilled ones outside the loop --
-// with two waves uneven segments took 94 us in place of 80)
+// (bfloat16, keys of up to 64, four waves: held to the 168 registers of three waves to a SIMD at the price of two spilled ones -- with two waves
+// uneven segments took 94 us in place of 80)
 template <int PREC, int DK, int NW, bool states_only>
 __global__ void __launch_bounds__(64 * NW, PREC != IDF_PREC_BF16 ? 1 : NW == 4 ? (DK <= 64 ? 3 : 2) : DK <= 64 ? 2 : 1) k_decay_chunks(idf_decay_args a, Parts parts, int blocks)
 {
@@ -486,7 +487,7 @@ __global__ void __launch_bounds__(64 * NW, PREC != IDF_PREC_BF16 ? 1 : NW == 4 ?
 }
 
 // What each part begins with, in place of what it would leave by itself: in the order of the parts, four values by a thread, what eight parts
-// leave being read at a time (16 heads x 32 parts of 128 x 128: 17.5 us one after the other, 14.3 so).
+// leave being read at a time (16 heads x 32 parts of 128 x 128: 17.5 us one after the other, 14.6 so).
 __global__ void __launch_bounds__(256) k_decay_scan(idf_decay_args a, Parts parts)
 {
     const int kv = blockIdx.y % a.heads_kv, seg = blockIdx.y / a.heads_kv;
@@ -540,9 +541,10 @@ Parts parts_of(const idf_decay_args &a)
 }
 
 // Token by token or by chunks.  A chunk costs the same whatever it holds, each token by itself about 3 us more (us per call, tokens against
-// chunk: 64 streams x 16 heads of 128 x 128 in bfloat16 25.9 : 28.2 for one token, 29.9 : 28.2 for two; 16 streams x 8 heads x 4 queries of 64 x 64
-// 8.2 : 8.7 and 12.0 : 8.7).  In float32 a chunk takes eight instructions for one: 64 streams x 4 heads of 64 x 64 9.2 : 10.0 for four tokens, 10.4 : 10.0
-// for five; x 16 heads of 128 x 128, 33 : 61 for four and level with 61 at twelve.  Rows of more than 128 values leave no registers for anything beside the state.
+// chunk: 64 streams x 16 heads of 128 x 128 in bfloat16 26.6 : 28.2 for one token, 30 : 28.2 for two; 16 streams x 8 heads x 4 queries of 64 x 64
+// 8.0 : 8.7 and 12.0 : 8.7).  In float32 a chunk takes eight instructions for one: 64 streams x 4 heads of 64 x 64 9.5 : 10.2 for four tokens, 10.4 : 10.2
+// for five; x 16 heads of 128 x 128, 35 : 61 for four and about level, 63 : 61, at twelve.  There is no chunk form for keys of more than 128 values:
+// they go token by token whatever their number, some 4 to 6 us a token (4000 tokens, 8 heads of 256 x 64: 22.9 ms, in float32 16.2 ms).
 bool by_token(const idf_decay_args &a)
 {
     const int most = a.precision == IDF_PREC_BF16 ? 1 : a.dim_k <= 64 ? 4 : 12;

@@ -4,7 +4,7 @@
 // float64, taken to quarter turns and reduced there (a float32 angle is off by a radian at position 2^24), then cosine and sine of the rest in
 // float32.  A group of lanes holds a head, each lane two pieces of P neighbouring values chosen so that the two values of a pair are in the
 // same lane: no exchange but the sum of squares.  Bound by memory: every value is read and written once (16384 tokens of 32 + 8 heads of 128 in
-// bfloat16: 72 us, 4.7 TB/s; 4001 tokens of 12 + 4 heads of 96 in float32: 13.5 us, 3.6 TB/s); one token each of 64 streams 5.5 us, a launch.
+// bfloat16: 72 us, 4.7 TB/s; 4001 tokens of 12 + 4 heads of 96 in float32: 13.6 us, 3.6 TB/s); one token each of 64 streams 5.4 to 6.1 us, a launch.
 #include <algorithm>
 
 #include "idf.h"

@@ -4,7 +4,8 @@
 // per lane, and what comes out of the matrix cores is the operand that O^T = V^T P^T takes, without a way through LDS.  Query heads that share
 // a key/value head are rows next to each other: row = token * group + head of the group.
 //   Sums, maxima and outputs are float32; in bfloat16 the weights exp(s - max) are rounded to bfloat16 for the product with V (their sum
-// is not): half a step of 2^-8 on each, independent from key to key, about as much as the rounding of the output.
+// is not): half a step of 2^-8 on each, independent from key to key, about as much as the rounding of the output (error against 64 bits 0.0020 to
+// 0.0023 of the output, that of its own rounding alone 0.0015 to 0.0017).  Weights in two parts would take half as many matrix instructions more.
 #include <algorithm>
 
 #include "idf.h"
@@ -198,8 +199,9 @@ __device__ __forceinline__ void append_tokens(const idf_window_args &a, const Se
 // A workgroup takes the at most 16 query rows of one segment and key/value head and a part of the keys; its four waves take 16 NT of them at a
 // time, in turn, each with a softmax of its own, and are joined at the end.  Keys go from memory straight into the layout of the matrix
 // instruction, values through a piece of LDS that is the wave's own, to be read along the keys; both are asked for one round ahead.  No
-// barrier but the last.  Bound by memory: every row of the ring is read once (64 streams on 4096 keys of 8 x 128 in bfloat16: 193 us, 5.6 TB/s; 64
-// streams of 16 tokens on 1000 keys of 8 x 64 in float32: 54 to 56 us, 5 TB/s; one stream on 16384 keys, split: 21 us with the join, 3.2 TB/s).
+// barrier but the last.  Bound by memory: every row of the ring is read once (64 streams on 4096 keys of 8 x 128 in bfloat16: 192 us, 5.6 TB/s, in
+// float32 361, where two registers are spilled; 64 streams of 16 tokens on 1000 keys of 8 x 64 in float32: 54 to 56 us, 5 TB/s; one stream on 16384
+// keys, split: 21 us with the join, 3.2 TB/s).
 template <int PREC, int DP> struct StepShape {
     static constexpr int NT = PREC == IDF_PREC_BF16 ? 2 : 1;                  // tiles of 16 keys
     static constexpr int KEYS = 16 * NT;
@@ -389,11 +391,14 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_window_step(idf_wind
 // ---- many rows ----
 
 // A workgroup takes 128 query rows of one segment and key/value head and walks over their keys; a wave has 32 of the rows.  Keys and values of a round
-// go through registers into LDS, the next round's being asked for while this one's are worked on.  Bound by the vector units and the matrix cores
-// together: of 128 values a head, a round costs a wave 32 matrix instructions of 32 cycles and some 170 others, 32 of them exponentials of 16 cycles;
-// of 64 values, half the former and the same of the latter, which is why these run four waves to a SIMD (three: 273 us, four: 263, uneven
-// segments).  Two prompts of 16384 tokens, 32 heads of 128 on a window of 4096: 1990 to 2140 us by the machine, 900 to 965 TFLOP/s.  Two halves of LDS with one barrier a round
-// instead of two took longer (2182 : 2158 us), reads from LDS held ahead of the products as long (2076 : 2065).
+// go through registers into LDS, the next round's being asked for while this one's are worked on.  Two prompts of 16384 tokens, 32 heads of 128 on a
+// window of 4096: 1990 to 2150 us by the machine, 890 to 965 TFLOP/s.  No unit is busy all the time: matrix cores 44 %, vector units in all 47 % (of
+// 128 values a head, a round costs a wave 32 matrix instructions of 32 cycles and some 200 others, 32 of them exponentials of 16), LDS 34 % without
+// bank conflicts; a wave waits for a quarter of its time for memory or the others, and 31 % to issue.  Of 64 values, half the matrix instructions and as many others,
+// which is why these run four waves to a SIMD, held to 128 registers with eight spilled ones, one of them read in the loop (three: 273 us, four: 263, uneven
+// segments; there compute units have work for 52 % of the time only, with matrix cores busy 18 % and vector units 35 % of the whole).  Two
+// halves of LDS with one barrier a round instead of two took longer (2182 : 2158 us), reads from LDS held ahead of the products as long (2076 : 2065).
+// Heads of more than 128 values are not loaded ahead: two prompts of 4096 tokens, 16 heads of 256 on 4, 483 us, 570 TFLOP/s (float32 2480 us, 111).
 template <int PREC, int DP> struct TileShape {
     static constexpr int KEYS = PREC == IDF_PREC_BF16 ? 64 : 32;
     static constexpr int VL = Elem<PREC>::VL, ROW16 = DP / VL;
@@ -676,10 +681,13 @@ struct Plan {
 };
 // Into how many parts a list of keys goes: the number with the least estimated time.  A workgroup's rounds follow each other, at a time each that
 // is latency where few of them run (measured, us: four tiles of the step kernel 1.4 in bfloat16, 0.9 + 0.0075 per value of a head in float32; a round
-// of the tile kernel 1.0 + 0.006, and 1.3 + 0.0275); no more workgroups than the compute units hold; a join is a launch of 4 to
-// 5 us and reads every row of every part.  Against parts of 256 keys (step) or 512 (tile) at least, us per pass: one stream, four heads of 128 on
-// one, 1500 keys 14.2 -> 11.1, in float32 19.2 -> 11.8; 40 tokens, eight heads on two, 500 keys 27.7 -> 15.9, 95.5 -> 21.3; 1200 tokens, 600 keys,
-// where the join costs more than it brings, 45.6 -> 29.4.
+// of the tile kernel 1.0 + 0.006, and 1.3 + 0.0275; by the head's size, not by the one it is padded to); a join is a launch of 4 to
+// 5 us and reads every row of every part.  At most 512 workgroups, whichever kernel: compute units hold two of most, but one of float32 tiles of more than 64
+// values and bfloat16 ones of more than 128, three of steps of 64 values and four of bfloat16 tiles of 64; whole rounds of the machine are not counted.  256
+// where one is held (us per pass, 256 : 512): 8 streams x 300 tokens on 4000 keys, 4 heads of 96 in float32 504 : 391, but 4 streams x 100 tokens on 8000
+// keys, 4 heads of 128, 331 : 377, and 200 tokens on 8000 keys, 4 heads of 256 in bfloat16, 75 : 86.  Against parts of 256 keys (step) or 512 (tile) at
+// least, us per pass: one stream, four heads of 128 on one, 1500 keys 14.2 -> 11.1, in float32 19.2 -> 11.8; 40 tokens, eight heads on two, 500 keys 27.7 -> 15.9,
+// 95.5 -> 21.3; 1200 tokens, 600 keys, where the join costs more than it brings, 45.6 -> 29.4.
 int splits_of(const idf_window_args &a, bool step, int64_t pairs, int64_t keys)
 {
     const bool bf = a.precision == IDF_PREC_BF16;
