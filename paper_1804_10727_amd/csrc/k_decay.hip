@@ -181,9 +181,11 @@ __device__ __forceinline__ bool part_by_tokens(const idf_decay_args &a, const Pa
         for (int p = 0; p < ROWS; ++p) {
             const int r = 16 * p + 8 * half;
             const typename M::frag f = M::load(k + r, a.dim_k - r);
-            if (r < a.dim_k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[p][e] = __builtin_fmaf(E::to_f32(f[e]), vc, lambda * s[p][e]);
+            for (int e0 = 0; e0 < 8; e0 += M::VL)                             // (zeros behind the key would meet infinities)
+                if (r + e0 < a.dim_k)
+#pragma unroll
+                    for (int e = e0; e < e0 + M::VL; ++e) s[p][e] = __builtin_fmaf(E::to_f32(f[e]), vc, lambda * s[p][e]);
         }
         if constexpr (!states_only)
 #pragma unroll 1

@@ -255,3 +255,18 @@ def test_window_offsets_that_lie_cut_segments_where_they_can(dtype, m):
 @pytest.mark.parametrize("dk,dv", [(256, 64), (136, 40)])
 def test_decay_long_segments_of_long_keys(dtype, dk, dv):
     decay_case(dtype, 2, 1, dk, dv, (1500, 3, 0, 129), seed=dk)
+
+
+@pytest.mark.parametrize("dk", [4, 36, 68, 124])
+@pytest.mark.parametrize("n,at", [(20, 3), (300, 130)])
+def test_decay_infinite_values_with_keys_that_end_inside_a_fragment(dk, n, at):
+    """Float32 keys of 4 mod 8 values: what fills the last fragment takes no part."""
+    g = torch.Generator().manual_seed(51)
+    q, k, v = (normal(g, n, 1, d, dtype=torch.float32).abs() + 0.1 for d in (dk, dk, 64))
+    v[at, 0, 7] = float("inf")
+    end = torch.empty(1, 1, dk, 64, device=DEV)
+    out = idf.decay_attend(q.to(DEV), k.to(DEV), v.to(DEV), torch.tensor([-0.02], device=DEV), None, end)[:, 0]
+    hit = torch.zeros(n, 64, dtype=torch.bool, device=DEV)
+    hit[at:, 7] = True
+    assert torch.all(out[hit] == float("inf")) and torch.isfinite(out[~hit]).all()
+    assert torch.all(end[..., 7] == float("inf")) and torch.isfinite(end[..., :7]).all() and torch.isfinite(end[..., 8:]).all()
