@@ -27,6 +27,7 @@ __device__ __forceinline__ Factor factor_of(float high, float rest)
     }
     return {uniform(high), uniform(fmaxf(rest, high * 0x1p-60f))};
 }
+__device__ __forceinline__ Factor factor_of(double decay) { return factor_of((float)decay, (float)(decay - (double)(float)decay)); }
 // exp(log_decay).  Where it is near one, by what it lacks, to 2^-23 of that; where not, what has been multiplied a few times is gone.
 __device__ __forceinline__ Factor factor_of(float log_decay)
 {
@@ -215,7 +216,7 @@ __device__ __forceinline__ bool part_by_tokens(const idf_decay_args &a, const Pa
     return true;
 }
 
-// (bfloat16, keys of up to 64, four waves: held to the 168 registers of three waves to a SIMD at the price of two spilled ones -- with two waves
+// (bfloat16, keys of up to 64, four waves: held to the 168 registers of three waves to a SIMD at the price of a spilled one -- with two waves
 // uneven segments took 94 us in place of 80)
 template <int PREC, int DK, int NW, bool states_only>
 __global__ void __launch_bounds__(64 * NW, PREC != IDF_PREC_BF16 ? 1 : NW == 4 ? (DK <= 64 ? 3 : 2) : DK <= 64 ? 2 : 1) k_decay_chunks(idf_decay_args a, Parts parts, int blocks)
@@ -273,10 +274,11 @@ __global__ void __launch_bounds__(64 * NW, PREC != IDF_PREC_BF16 ? 1 : NW == 4 ?
     }
     const float faded = __builtin_amdgcn_exp2f((float)(col + 1) * l2) * a.scale;
     // The decay of a whole chunk is applied again and again, and its own rounding would add up: each factor takes back what those before it
-    // were off (drift: what has been applied over what should have been).
+    // were off (drift: what has been applied over what should have been), and the last one of the call, which may be of a short chunk, leaves nothing
+    // for the next call to add to.
     const double whole = exp2((double)kChunk * (double)l2), inverse = whole > 1e-30 ? 1.0 / whole : 0.0;
     double drift = 1.0;
-    const float fade_short = uniform((float)exp2((double)((max(len, 1) - 1) % kChunk + 1) * (double)l2));        // (the last chunk of the part may be a short one)
+    const double short_one = exp2((double)((max(len, 1) - 1) % kChunk + 1) * (double)l2);
 
     // A step is a chunk for one of the heads.  While one is worked on, what the next one needs is written from registers into the other half
     // of LDS, and what the one behind it needs is on its way; where nothing is stored between the loads, what the next but one needs, too.
@@ -419,13 +421,18 @@ __global__ void __launch_bounds__(64 * NW, PREC != IDF_PREC_BF16 ? 1 : NW == 4 ?
         if constexpr (states_only) {
             left = __builtin_amdgcn_exp2f((float)(len - t0 - n) * l2);
         } else {
-            float fade = fade_short;
-            if (n == kChunk) {
-                fade = uniform((float)(whole * (2.0 - drift)));               // (2 - x is 1 / x so near to one)
+            if (t0 + kChunk < len) {
+                const float fade = uniform((float)(whole * (2.0 - drift)));   // (2 - x is 1 / x so near to one)
                 if (inverse > 0.0) drift *= (double)fade * inverse;
-            }
 #pragma unroll
-            for (int t = 0; t < KT; ++t) s[t] *= fade;
+                for (int t = 0; t < KT; ++t) s[t] *= fade;
+            } else {
+                const Factor fade = factor_of(short_one * (2.0 - drift));
+#pragma unroll
+                for (int t = 0; t < KT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[t][e] = fade.times(s[t][e]);
+            }
         }
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
@@ -497,8 +504,7 @@ __global__ void __launch_bounds__(256) k_decay_scan(idf_decay_args a, Parts part
     const Segment g = segment_of(a, seg, nullptr);
     if (!g.valid || x >= size) return;
     const int n = max(1, (g.len + parts.tokens - 1) / parts.tokens);
-    const double whole = exp2((double)parts.tokens * (double)log2_of(a.log_decay[kv]));
-    const Factor keep = factor_of((float)whole, (float)(whole - (double)(float)whole));
+    const Factor keep = factor_of(exp2((double)parts.tokens * (double)log2_of(a.log_decay[kv])));
     float *at = parts.states + (int64_t)blockIdx.y * parts.n * size + x;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (a.state_in) s = *(const f32x4 *)(a.state_in + ((int64_t)g.ring * a.heads_kv + kv) * size + x);

@@ -270,3 +270,20 @@ def test_decay_infinite_values_with_keys_that_end_inside_a_fragment(dk, n, at):
     hit[at:, 7] = True
     assert torch.all(out[hit] == float("inf")) and torch.isfinite(out[~hit]).all()
     assert torch.all(end[..., 7] == float("inf")) and torch.isfinite(end[..., :7]).all() and torch.isfinite(end[..., 8:]).all()
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,calls", [(16, 4000), (32, 3000), (77, 1500)])
+def test_decay_rounding_of_a_factor_does_not_add_up_over_calls(dtype, n, calls):
+    """The same where a stream brings a few tokens at a time: bounds as above, of the chunks that the calls have; the exponent of a chunk is formed
+    from a float32 logarithm in units of log 2, which is rounded twice."""
+    log_decay = -torch.tensor([5e-4, 3.3e-4, 1e-4, 2.7e-5, 1e-6], device=DEV)
+    h = len(log_decay)
+    g = torch.Generator().manual_seed(52)
+    start = (1 + torch.rand(4, h, 64, 64, generator=g)).to(DEV)
+    state = start.clone()
+    q = torch.zeros(4 * n, h, 64, dtype=dtype, device=DEV)
+    out = torch.empty_like(q)
+    for _ in range(calls):
+        idf.decay_attend(q, q, q, log_decay, state, state, out=out)
+    off = relative(state, start, log_decay, n * calls)
+    bound = 6 * calls * -(-n // 32) * W / np.sqrt(3 * 4 * 64 * 64) + 2 * n * calls * log_decay.abs().cpu().numpy() * W
+    assert np.all(off <= bound), off / bound
