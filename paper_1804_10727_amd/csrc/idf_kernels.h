@@ -119,6 +119,9 @@ double peak_ops(int kind, int blocks, int iters);
 hipError_t launch_peak(int kind, void *buf, size_t bytes, int blocks, int iters, const LaunchCtx &lc);
 
 // Mixing of tokens (arguments are checked; workspace sizes are those of the *_workspace functions).
+// Tokens of the longest segment that there can be: max_tokens is a bound only, and calls are planned by this.  (A call of the decayed attention
+// without tokens has segments all the same, which hand their states on.)
+template <class Args> inline int64_t longest(const Args &a) { return a.max_tokens < a.n_tokens ? a.max_tokens : a.n_tokens; }
 hipError_t launch_norm_rotate(const idf_norm_rotate_args &a, const LaunchCtx &lc);
 size_t window_workspace(const idf_window_args &a);
 hipError_t launch_window(const idf_window_args &a, const LaunchCtx &lc);

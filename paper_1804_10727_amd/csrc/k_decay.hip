@@ -523,10 +523,6 @@ __global__ void __launch_bounds__(256) k_decay_scan(idf_decay_args a, Parts part
     }
 }
 
-// Tokens of the longest segment that there can be: max_tokens is a bound only.  A call without tokens has segments all the same, which hand
-// their states on.
-int64_t longest(const idf_decay_args &a) { return std::min(a.max_tokens, a.n_tokens); }
-
 Parts parts_of(const idf_decay_args &a)
 {
     Parts p;

@@ -693,7 +693,7 @@ int splits_of(const idf_window_args &a, bool step, int64_t pairs, int64_t keys)
     const bool bf = a.precision == IDF_PREC_BF16;
     const int64_t round = step ? (bf ? 128 : 64) : bf ? 64 : 32, rounds = (keys + round - 1) / round, held = 512;
     const double each = step ? (bf ? 1.4 : 0.9 + 0.0075 * a.head_dim) : bf ? 1.0 + 0.006 * a.head_dim : 1.3 + 0.0275 * a.head_dim;
-    const double rows = (double)std::min<int64_t>(a.n_tokens, a.n_segments * a.max_tokens) * a.heads_q;
+    const double rows = (double)std::min<int64_t>(a.n_tokens, a.n_segments * longest(a)) * a.heads_q;
     int best = 1;
     double least = 0.0;
     for (int64_t per = rounds; per >= 1; per = per > 8 ? per * 7 / 8 : per - 1) {
@@ -708,14 +708,14 @@ int splits_of(const idf_window_args &a, bool step, int64_t pairs, int64_t keys)
 Plan plan_of(const idf_window_args &a)
 {
     Plan p;
-    const int64_t rows = a.max_tokens * (a.heads_q / a.heads_kv);
+    const int64_t rows = longest(a) * (a.heads_q / a.heads_kv);
     p.step = rows <= kStepRows;
     // the ring has room for a segment beside a window (64 streams of 16 tokens, float32: 60 -> 50 us a pass)
-    p.append = a.k_ring && a.slots - a.sinks - a.window >= a.max_tokens - 1;
+    p.append = a.k_ring && a.slots - a.sinks - a.window >= longest(a) - 1;
     p.tiles = p.step ? 1 : (int)((rows + kTileRows - 1) / kTileRows);
     const int64_t pairs = (int64_t)a.n_segments * a.heads_kv * p.tiles;
-    const int64_t own = p.step ? a.max_tokens : std::min<int64_t>(a.max_tokens, kTileRows / (a.heads_q / a.heads_kv) + 1);
-    const int64_t keys = std::min<int64_t>(a.window, a.k_ring ? a.slots : a.max_tokens) + a.sinks + own;
+    const int64_t own = p.step ? longest(a) : std::min<int64_t>(longest(a), kTileRows / (a.heads_q / a.heads_kv) + 1);
+    const int64_t keys = std::min<int64_t>(a.window, a.k_ring ? a.slots : longest(a)) + a.sinks + own;
     p.splits = splits_of(a, p.step, pairs, keys);
     return p;
 }
@@ -739,11 +739,11 @@ hipError_t by_dim(const idf_window_args &a, const LaunchCtx &lc)
     if (e == hipSuccess && p.splits > 1) {
         int lanes_log2 = 0;
         while (4 << lanes_log2 < a.head_dim) ++lanes_log2;
-        e = launch(k_window_join<PREC>, dim3((unsigned)std::min<int64_t>(a.max_tokens * a.heads_q, 8192), a.n_segments), dim3(256), 0, lc, a, p.splits, lanes_log2);
+        e = launch(k_window_join<PREC>, dim3((unsigned)std::min<int64_t>(longest(a) * a.heads_q, 8192), a.n_segments), dim3(256), 0, lc, a, p.splits, lanes_log2);
     }
     if (e == hipSuccess && a.k_ring && !p.append) {
         const int elem16 = Elem<PREC>::VL, row16 = a.heads_kv * a.head_dim / elem16;
-        e = launch(k_window_append, dim3((unsigned)std::min<int64_t>((a.max_tokens * row16 + 255) / 256, 4096), a.n_segments), dim3(256), 0, lc, a, row16, elem16);
+        e = launch(k_window_append, dim3((unsigned)std::min<int64_t>((longest(a) * row16 + 255) / 256, 4096), a.n_segments), dim3(256), 0, lc, a, row16, elem16);
     }
     return e;
 }

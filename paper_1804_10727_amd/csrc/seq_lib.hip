@@ -69,8 +69,8 @@ int check_window(const idf_window_args *a)
 {
     if (!a) return fail(IDF_EINVAL, "null argument");
     if (int rc = check_segments(*a)) return rc;
-    if (a->max_tokens * (a->heads_q / a->heads_kv) > kMostRows)
-        return fail(IDF_EUNSUPPORTED, "segments of up to %lld tokens with %d heads on %d: more than a launch takes", (long long)a->max_tokens, a->heads_q, a->heads_kv);
+    if (longest(*a) * (a->heads_q / a->heads_kv) > kMostRows)
+        return fail(IDF_EUNSUPPORTED, "segments of up to %lld tokens with %d heads on %d: more than a launch takes", (long long)longest(*a), a->heads_q, a->heads_kv);
     const int vl = a->precision == IDF_PREC_F32 ? 4 : 8;
     if (a->head_dim < vl || a->head_dim > 256 || a->head_dim % vl) return fail(IDF_EUNSUPPORTED, "heads of %d values", a->head_dim);
     if (a->window < 1 || a->sinks < 0) return fail(IDF_EINVAL, "a window of %d tokens and %d first ones", a->window, a->sinks);
@@ -90,8 +90,8 @@ int check_decay(const idf_decay_args *a)
     const int vl = a->precision == IDF_PREC_F32 ? 4 : 8;
     if (a->dim_k < vl || a->dim_k > 256 || a->dim_k % vl || a->dim_v < vl || a->dim_v % vl || a->dim_v > 4096)
         return fail(IDF_EUNSUPPORTED, "heads of %d and %d values", a->dim_k, a->dim_v);
-    if (std::min(a->max_tokens, a->n_tokens) > (a->dim_k > 128 ? kMostByToken : kMostTokens))
-        return fail(IDF_EUNSUPPORTED, "segments of up to %lld tokens with keys of %d values", (long long)a->max_tokens, a->dim_k);
+    if (longest(*a) > (a->dim_k > 128 ? kMostByToken : kMostTokens))
+        return fail(IDF_EUNSUPPORTED, "segments of up to %lld tokens with keys of %d values", (long long)longest(*a), a->dim_k);
     if ((int64_t)a->n_segments * a->heads_kv * ((a->dim_v + 63) / 64) > kMostPairs)
         return fail(IDF_EUNSUPPORTED, "%d segments with %d heads of %d values: more than a launch takes", a->n_segments, a->heads_kv, a->dim_v);
     if (((uintptr_t)a->state_in | (uintptr_t)a->state_out) % 16) return fail(IDF_EUNSUPPORTED, "states have to be 16-byte aligned");

@@ -287,3 +287,21 @@ def test_decay_rounding_of_a_factor_does_not_add_up_over_calls(dtype, n, calls):
     off = relative(state, start, log_decay, n * calls)
     bound = 6 * calls * -(-n // 32) * W / np.sqrt(3 * 4 * 64 * 64) + 2 * n * calls * log_decay.abs().cpu().numpy() * W
     assert np.all(off <= bound), off / bound
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("lengths", [(1, 0, 1), (3, 1, 2), (20, 0, 7), (150, 0, 200)])
+def test_bounds_beyond_the_tokens_change_nothing(dtype, lengths):
+    g = torch.Generator().manual_seed(53)
+    n = sum(lengths)
+    q, k, v = (normal(g, n, h, 64, dtype=dtype).to(DEV) for h in (4, 1, 1))
+    offsets, starts = torch.tensor((0,) + lengths).cumsum(0).to(DEV), torch.tensor([50, 3, 1000], device=DEV)
+    rings = [normal(g, 3, 250, 1, 64, dtype=dtype).to(DEV) for _ in range(2)]
+    state, log_decay = torch.randn(3, 1, 64, 64, generator=g).to(DEV), torch.tensor([-0.1], device=DEV)
+    want = None
+    for max_tokens in (n, n + 1, 4096, 1 << 24):
+        r, s = [x.clone() for x in rings], state.clone()
+        got = [idf.window_attend(q, k, v, *r, starts, window=40, sinks=2, offsets=offsets, max_tokens=max_tokens), *r,
+               idf.decay_attend(q, k, v, log_decay, s, s, offsets=offsets, max_tokens=max_tokens), s]
+        want = want or got
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), max_tokens

@@ -130,3 +130,31 @@ def long_segments(rt):
 def test_decay_takes_segments_that_the_window_does_not(runtime):
     """The decayed attention has no axis of query rows: segments are cut into parts, and tokens counted in 32 bits."""
     host_runtime.run(runtime, "test_tokens_host", "long_segments")
+
+
+def bounds_beyond_the_tokens(rt):
+    import ctypes as C
+
+    from paper_1804_10727_amd import binding, tokens
+    L = binding.load_library()
+
+    def call(n_tokens, max_tokens, room, heads_q=16):
+        q, k = tokens._Tokens(AT, heads_q * 64, 64), tokens._Tokens(AT, 64, 64)
+        a = tokens._Window(1, heads_q, 1, 64, n_tokens, max_tokens, 2, 2, 40 + room, 40, 0, 0.125, q, k, k, q, AT, AT, AT, AT, None, None, 0)
+        nb = C.c_size_t()
+        if L.idf_window_workspace(C.byref(a), C.byref(nb)):
+            return "refused"
+        a.workspace, a.workspace_bytes = AT, nb.value
+        rt.host_begin()
+        assert L.idf_window_attend(C.byref(a), None) == 0 and rt.host_error() == b""
+        return nb.value, {k: rt.host_launches(k) for k in (None, b"k_window_step", b"k_window_tile", b"k_window_append")}
+    for n_tokens, room in ((1, 0), (1, 5), (10, 0), (10, 9), (300, 0), (300, 299)):
+        exact = call(n_tokens, n_tokens, room)
+        for max_tokens in (4096, 1 << 24, (1 << 31) - 1):
+            assert call(n_tokens, max_tokens, room) == exact, (n_tokens, room, max_tokens)
+    assert call(1 << 20, 1 << 20, 0) == "refused"
+
+
+def test_window_goes_by_the_tokens_there_are(runtime):
+    """A bound on the tokens of a segment beyond all tokens of the call is no reason to refuse it or to launch for more."""
+    host_runtime.run(runtime, "test_tokens_host", "bounds_beyond_the_tokens")
