@@ -145,7 +145,7 @@ template <int N> __device__ __forceinline__ bool finite(const f32x16 (&s)[N])
 // What a wave does in k_decay_chunks, once more, by the recurrence, where something infinite or not a number came into a state that had begun without:
 // three parts of an infinite value are no number, nor is an infinite key times a part that is zero, nor an infinite value times the zeros behind a
 // key that is shorter than DK.  Outputs that are finite are as they should be and stay.  Lanes side by side hold a column of the state each, either half
-// of the wave half of its rows.  False: the state had begun so.
+// of the wave half of its rows.  False: the state had begun so, or the decay is not a number and nothing else can come of it.
 template <int PREC, int DK, int NW, bool states_only>
 __device__ __forceinline__ bool part_by_tokens(const idf_decay_args &a, const Parts &parts, int blocks, int x, int y, int thread, bool good)
 {
@@ -170,9 +170,9 @@ __device__ __forceinline__ bool part_by_tokens(const idf_decay_args &a, const Pa
             s[p][e] = from && own && r < a.dim_k ? from[r * a.dim_v] : 0.f;
             none += s[p][e] * 0.f;
         }
-    if (!__ballot(!good && none == 0.f)) return false;
-    __threadfence_block();                         // (outputs are written once more)
     const float lambda = __builtin_amdgcn_exp2f(log2_of(a.log_decay[kv]));
+    if (lambda != lambda || !__ballot(!good && none == 0.f)) return false;
+    __threadfence_block();                         // (outputs are written once more)
     const T *k = (const T *)a.k.base + (g.begin + first) * a.k.token_stride + kv * a.k.head_stride;
     const T *v = (const T *)a.v.base + (g.begin + first) * a.v.token_stride + kv * a.v.head_stride + c;
 #pragma unroll 1
