@@ -216,7 +216,7 @@ __device__ __forceinline__ bool part_by_tokens(const idf_decay_args &a, const Pa
     return true;
 }
 
-// (bfloat16, keys of up to 64, four waves: held to the 168 registers of three waves to a SIMD at the price of a spilled one -- with two waves
+// (bfloat16, keys of up to 64, four waves: held to the 168 registers of three waves to a SIMD at the price of three spilled ones -- with two waves
 // uneven segments took 94 us in place of 80)
 template <int PREC, int DK, int NW, bool states_only>
 __global__ void __launch_bounds__(64 * NW, PREC != IDF_PREC_BF16 ? 1 : NW == 4 ? (DK <= 64 ? 3 : 2) : DK <= 64 ? 2 : 1) k_decay_chunks(idf_decay_args a, Parts parts, int blocks)
@@ -330,6 +330,44 @@ __global__ void __launch_bounds__(64 * NW, PREC != IDF_PREC_BF16 ? 1 : NW == 4 ?
                 *(i32x4 *)(v_to + r * V_STRIDE + c) = STAGES == 1 || (x.t0 + r < len && c0 + c < a.dim_v) ? vr[stage][y] : none;
             }
     };
+    // values of this wave's columns along the tokens: register x of piece p is token 16 p + 8 (x / 4) + 4 half + x % 4
+    auto read_values = [&](const T *v_lds, frag (&v)[2]) IDF_INLINE {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) v[p] = read_rows_swapped(v_lds, V_STRIDE, 32 * wave + (lane & 16), 16 * p + 4 * half, 16 * p + 8 + 4 * half);
+    };
+    // what the n tokens of a chunk add to the state, each weighed by what it leaves at the chunk's end, and that by `left`
+    auto gain = [&](const frag (&v)[2], const T *k_lds, int n, float left) IDF_INLINE {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = E::to_f32(v[p][e]) * (fresh[16 * p + 8 * (e / 4) + 4 * half + e % 4 + kChunk - n] * left);
+            frag pieces[BF ? 3 : 1];
+            if constexpr (BF) {
+#pragma unroll
+                for (int y = 0; y < 3; ++y) {
+                    uint32_t u[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {  // the upper 16 bits, and what is left
+                        u[e] = __builtin_bit_cast(uint32_t, x[e]);
+                        x[e] -= __builtin_bit_cast(float, u[e] & 0xffff0000u);
+                    }
+                    i32x4 both;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) both[e] = (int)__builtin_amdgcn_perm(u[2 * e + 1], u[2 * e], 0x07060302u);
+                    pieces[y] = __builtin_bit_cast(frag, both);
+                }
+            } else {
+                pieces[0] = M::pack(x);
+            }
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                const frag k = read_rows_swapped(k_lds, K_STRIDE, 32 * t + (lane & 16), 16 * p + 4 * half, 16 * p + 8 + 4 * half);
+#pragma unroll
+                for (int y = 0; y < (BF ? 3 : 1); ++y) s[t] = M::mma32(k, pieces[y], s[t]);
+            }
+        }
+    };
     Step now = {0, 0}, ahead = next_of(now), beyond = next_of(ahead);
     auto step_of = [&](int step, int stage) IDF_INLINE {
         __syncthreads();
@@ -342,10 +380,8 @@ __global__ void __launch_bounds__(64 * NW, PREC != IDF_PREC_BF16 ? 1 : NW == 4 ?
         ahead = beyond;
         beyond = then;
 
-        // values of this wave's columns along the tokens: register x of piece p is token 16 p + 8 (x / 4) + 4 half + x % 4
         frag v[2];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) v[p] = read_rows_swapped(v_lds, V_STRIDE, 32 * wave + (lane & 16), 16 * p + 4 * half, 16 * p + 8 + 4 * half);
+        read_values(v_lds, v);
 
         if (!states_only) {
                 f32x16 w, o;
@@ -417,52 +453,14 @@ __global__ void __launch_bounds__(64 * NW, PREC != IDF_PREC_BF16 ? 1 : NW == 4 ?
 
         if (h + 1 < heads) return;
         // what this chunk's last token leaves at the end of the part, where only that is asked for: nothing is faded on the way then
-        float left = 1.f;
         if constexpr (states_only) {
-            left = __builtin_amdgcn_exp2f((float)(len - t0 - n) * l2);
-        } else {
-            if (t0 + kChunk < len) {
-                const float fade = uniform((float)(whole * (2.0 - drift)));   // (2 - x is 1 / x so near to one)
-                if (inverse > 0.0) drift *= (double)fade * inverse;
+            gain(v, k_lds, n, __builtin_amdgcn_exp2f((float)(len - t0 - n) * l2));
+        } else if (t0 + kChunk < len) {
+            const float fade = uniform((float)(whole * (2.0 - drift)));       // (2 - x is 1 / x so near to one)
+            if (inverse > 0.0) drift *= (double)fade * inverse;
 #pragma unroll
-                for (int t = 0; t < KT; ++t) s[t] *= fade;
-            } else {
-                const Factor fade = factor_of(short_one * (2.0 - drift));
-#pragma unroll
-                for (int t = 0; t < KT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[t][e] = fade.times(s[t][e]);
-            }
-        }
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = E::to_f32(v[p][e]) * (fresh[16 * p + 8 * (e / 4) + 4 * half + e % 4 + kChunk - n] * left);
-            frag pieces[BF ? 3 : 1];
-            if constexpr (BF) {
-#pragma unroll
-                for (int y = 0; y < 3; ++y) {
-                    uint32_t u[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {  // the upper 16 bits, and what is left
-                        u[e] = __builtin_bit_cast(uint32_t, x[e]);
-                        x[e] -= __builtin_bit_cast(float, u[e] & 0xffff0000u);
-                    }
-                    i32x4 both;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) both[e] = (int)__builtin_amdgcn_perm(u[2 * e + 1], u[2 * e], 0x07060302u);
-                    pieces[y] = __builtin_bit_cast(frag, both);
-                }
-            } else {
-                pieces[0] = M::pack(x);
-            }
-#pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                const frag k = read_rows_swapped(k_lds, K_STRIDE, 32 * t + (lane & 16), 16 * p + 4 * half, 16 * p + 8 + 4 * half);
-#pragma unroll
-                for (int y = 0; y < (BF ? 3 : 1); ++y) s[t] = M::mma32(k, pieces[y], s[t]);
-            }
+            for (int t = 0; t < KT; ++t) s[t] *= fade;
+            gain(v, k_lds, kChunk, 1.f);
         }
     };
     if (len > 0) {
@@ -474,6 +472,17 @@ __global__ void __launch_bounds__(64 * NW, PREC != IDF_PREC_BF16 ? 1 : NW == 4 ?
             step_of(step, 0);
             if (STAGES == 1 || now.t0 >= len) continue;
             step_of(step + 1, STAGES - 1);
+        }
+        if constexpr (!states_only) {              // the last chunk, which is still in LDS (within the loop the state's registers would be copied for it)
+            const int t0 = (len - 1) / kChunk * kChunk;
+            const Factor fade = factor_of(short_one * (2.0 - drift));
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[t][e] = fade.times(s[t][e]);
+            frag v[2];
+            read_values(v_both[t0 / kChunk & 1], v);
+            gain(v, k_both[t0 / kChunk & 1], len - t0, 1.f);
         }
     }
 
