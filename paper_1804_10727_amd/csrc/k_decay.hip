@@ -113,8 +113,8 @@ __global__ void __launch_bounds__(256, ROWS == 8 ? 3 : 1) k_decay_tokens(idf_dec
 //   Roundings in bfloat16: scores times decay, and the state where it meets the queries, are rounded to bfloat16 (half a step of 2^-8, as the
 // output is).  The state itself stays float32: a decayed value, 24 bits, goes into the product as three bfloat16 numbers that add up to it.
 //   Bound by memory: q, k, v and out once, k and v twice where a segment is cut into parts (one prompt of 65536 tokens, 16 heads of 128 x 128 in
-// bfloat16: 400 to 418 us by the machine, of them 136 to 146 for the states of the parts, 14 for the scan and 250 to 277 for the outputs, 4 TB/s;
-// matrix cores and LDS a third of the time, waves waiting for 35 to 40 %; loads of the outputs' pass
+// bfloat16: 400 to 418 us by the machine, of them 135 to 145 for the states of the parts, 14 for the scan and 240 to 275 for the outputs, 4 TB/s;
+// matrix cores and LDS a third of the time, waves waiting for 33 to 40 %; loads of the outputs' pass
 // two chunks ahead took longer, 512 us in all: between stores they are waited for all the same).  Short calls by latency: 64 streams of 16 tokens,
 // 4 heads of 64 x 64 in float32, 10.2 us.
 constexpr int kChunk = 32;

@@ -392,11 +392,11 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_window_step(idf_wind
 
 // A workgroup takes 128 query rows of one segment and key/value head and walks over their keys; a wave has 32 of the rows.  Keys and values of a round
 // go through registers into LDS, the next round's being asked for while this one's are worked on.  Two prompts of 16384 tokens, 32 heads of 128 on a
-// window of 4096: 1990 to 2150 us by the machine, 890 to 965 TFLOP/s.  No unit is busy all the time: matrix cores 44 %, vector units in all 47 % (of
+// window of 4096: 1990 to 2150 us by the machine, 890 to 965 TFLOP/s.  No unit is busy all the time: matrix cores 44 %, vector units in all 46 % (of
 // 128 values a head, a round costs a wave 32 matrix instructions of 32 cycles and some 200 others, 32 of them exponentials of 16), LDS 34 % without
 // bank conflicts; a wave waits for a quarter of its time for memory or the others, and 31 % to issue.  Of 64 values, half the matrix instructions and as many others,
 // which is why these run four waves to a SIMD, held to 128 registers with eight spilled ones, one of them read in the loop (three: 273 us, four: 263, uneven
-// segments; there compute units have work for 54 % of the time only, with matrix cores busy 19 % and vector units 36 % of the whole).  Two
+// segments; there compute units have work for 53 % of the time only, with matrix cores busy 18 % and vector units 36 % of the whole).  Two
 // halves of LDS with one barrier a round instead of two took longer (2182 : 2158 us), reads from LDS held ahead of the products as long (2076 : 2065).
 // Heads of more than 128 values are not loaded ahead: two prompts of 4096 tokens, 16 heads of 256 on 4, 483 us, 570 TFLOP/s (float32 2480 us, 111).
 template <int PREC, int DP> struct TileShape {
