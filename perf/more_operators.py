@@ -206,12 +206,12 @@ def _run_own(s):
         return idf.project_rows(s["x"], s["weight"], s["weight_scales"], bias=s["bias"])
     ragged = {} if s["offsets"] is None else dict(offsets=s["offsets"], max_tokens=s["max_tokens"])
     if c["op"] == "append":
-        ring = idf.Ring4(*s["ring"])
-        idf.ring4_append(s["k"], s["v"], ring, s["starts"], sinks=c["sinks"], frequencies=s["frequencies"], layout=c["layout"],
+        ring = idf.NibbleRing(*s["ring"])
+        idf.nibble_append(s["k"], s["v"], ring, s["starts"], sinks=c["sinks"], frequencies=s["frequencies"], layout=c["layout"],
                          amplitude=s["amplitude"], k_weight=s["k_weight"], eps=1e-6, **ragged)
-        return idf.ring4_values(ring)
+        return idf.nibble_values(ring)
     if c["op"] == "attend":
-        return idf.ring4_attend(s["q"], idf.Ring4(*s["ring"]), s["starts"], window=c["window"], sinks=c["sinks"], **ragged)
+        return idf.nibble_attend(s["q"], idf.NibbleRing(*s["ring"]), s["starts"], window=c["window"], sinks=c["sinks"], **ragged)
     if not c["train"]:
         return idf.gate_scan(s["x"], s["gates"], state=s["state"], state_out=s["state_out"], **ragged), s["state_out"]
     # as a training program has them: leaves that record, a forward and a backward pass
