@@ -526,6 +526,149 @@ typedef struct {
 int idf_decay_workspace(const idf_decay_args *a, size_t *bytes);
 int idf_decay_attend(const idf_decay_args *a, void *hip_stream);
 
+/* The same layers in few bits, and a recurrence with one state per channel: rows times 8-bit weights, a ring of 4-bit blocks in place of
+ * the one that idf_window_attend reads, and a gated recurrence that has a backward pass.  Tokens, segments, streams, workspaces, what is held in
+ * bounds on the device, and errors as above. */
+
+/* A matrix: value c of row r at base + (r * row_stride + c) * size of a value. */
+typedef struct {
+    void *base;
+    int64_t row_stride;
+} idf_rows;
+
+/* Rows in 8 bits with a scale each: codes = x * 127 / max|x| of the row to the nearest whole number (halfway: to the even one), scale = max|x| / 127.
+ * A row of zeros has the scale zero; a row with a value that is not finite has codes of zero and a scale that is not a number.
+ *   codes [n_rows][cols rounded up to 16], the rest of a row filled with zeros, 16-byte aligned; scales float32 [n_rows].  For the rows of a matrix of
+ * weights as for tokens.  precision IDF_PREC_F32 or IDF_PREC_BF16; 1 <= cols <= 65536. */
+typedef struct {
+    int precision, cols;
+    int64_t n_rows;
+    idf_rows x;
+    int8_t *codes;
+    float *scales;
+} idf_quantize_args;
+int idf_quantize_rows(const idf_quantize_args *a, void *hip_stream);
+
+/* out[r][n] = x_scale[r] * weight_scales[n] * sum_c x[r][c] * weights[n][c] + bias[n], the sum of 8-bit codes in 32-bit integers, exact.
+ *   precision: that of x.  IDF_PREC_F32, IDF_PREC_BF16: rows are taken to codes and scales as by idf_quantize_rows, within the call;
+ * IDF_PREC_I8: codes with x_scales [n_rows], cols and x.row_stride multiples of 16 and x.base 16-byte aligned.  out_precision IDF_PREC_F32 or
+ * IDF_PREC_BF16.  weights int8 [n_out][cols rounded up to 16], 16-byte aligned; weight_scales, bias float32 [n_out], bias NULL: none.  out must not
+ * overlap an input.  cols <= 65536, n_out <= 2^24. */
+typedef struct {
+    int precision, out_precision, cols, n_out;
+    int64_t n_rows;
+    idf_rows x, out;
+    const float *x_scales;
+    const int8_t *weights;
+    const float *weight_scales, *bias;
+    void *workspace;
+    size_t workspace_bytes;
+} idf_project_args;
+int idf_project_workspace(const idf_project_args *a, size_t *bytes);
+int idf_project_rows(const idf_project_args *a, void *hip_stream);
+
+/* A ring of keys and values in 4 bits.  A block is 32 neighbouring values of a head and one power of two 2^e, held as the byte e + 127 (255: the block is
+ * not a number).  A value is a sign (bit 3) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^e; the even one of two neighbours lies in the low bits of
+ * a byte.  e is the smallest with all of the block at most 7 * 2^e (so that nothing is off by more than half the widest step), -100 <= e <= 125; values go to the
+ * nearest one there is (halfway: to the one of even bits), beyond 6 to 6.  A block that holds a value that is not finite is not a number.  Every
+ * value that a block can hold is one of bfloat16, and 17 bytes hold what takes 64 there.
+ *   codes [n_streams][heads_kv][slots][head_dim / 2], scales [n_streams][heads_kv][slots][head_dim / 32], codes 16-byte aligned; head_dim a multiple of
+ * 32, <= 256.  The token at position p lies in slot p where p < sinks, else in sinks + (p - sinks) mod (slots - sinks). */
+typedef struct {
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+} idf_nibble_ring;
+
+/* Segments' keys and values into their streams' rings, keys normalised and turned on the way as by idf_norm_rotate (a null weight: not
+ * normalised; rotary_dim 0: not turned), in float64: a code does not depend on how that is rounded.  Of a segment longer than the ring its newest tokens are
+ * written, and the first ones of the stream.  slots > sinks.  k and v need not be aligned.  starts NULL: 0. */
+typedef struct {
+    int precision, heads_kv, head_dim, rotary_dim, interleaved;
+    int64_t n_tokens, max_tokens;
+    int n_segments, n_streams;
+    int64_t slots;
+    int sinks;
+    double amplitude, eps;
+    idf_tokens k, v;
+    idf_nibble_ring ring;
+    const double *frequencies;
+    const float *k_weight;
+    const int64_t *offsets, *starts;
+    const int32_t *stream_ids;
+} idf_nibble_append_args;
+int idf_nibble_append(const idf_nibble_append_args *a, void *hip_stream);
+
+/* idf_window_attend over what the ring holds alone: the queries' own tokens have been appended before.  starts: position of each segment's first
+ * query.  The ring has to have room for a segment beside a window, slots - sinks >= window + max_tokens - 1 (of the tokens that there are), since its later
+ * tokens take the slots of earlier ones.  Whatever the ring holds of positions beyond the segment's last query, and of positions that fell out of the window,
+ * is not seen.  The values are those of idf_nibble_values, exactly. */
+typedef struct {
+    int precision, heads_q, heads_kv, head_dim;
+    int64_t n_tokens, max_tokens;
+    int n_segments, n_streams;
+    int64_t slots;
+    int window, sinks;
+    float scale;
+    idf_tokens q, out;
+    idf_nibble_ring ring;
+    const int64_t *offsets, *starts;
+    const int32_t *stream_ids;
+    void *workspace;
+    size_t workspace_bytes;
+} idf_nibble_attend_args;
+int idf_nibble_attend_workspace(const idf_nibble_attend_args *a, size_t *bytes);
+int idf_nibble_attend(const idf_nibble_attend_args *a, void *hip_stream);
+
+/* What the rings stand for: k, v [n_streams][slots][heads_kv][head_dim] of the precision, a ring as idf_window_attend takes it.  Nothing is lost. */
+typedef struct {
+    int precision, heads_kv, head_dim, n_streams;
+    int64_t slots;
+    idf_nibble_ring ring;
+    void *k, *v;
+} idf_nibble_values_args;
+int idf_nibble_values(const idf_nibble_values_args *a, void *hip_stream);
+
+/* A gated recurrence per channel:  h_t = a_t h_{t-1} + (1 - a_t) x_t,  a_t = 1 / (1 + exp(-g_t)),  out_t = h_t,
+ * with gates held to -87 .. 87 (neither what is kept nor what is taken in is ever nothing: an infinite state stays infinite).  state_in, state_out: float32
+ * [n_streams][channels], from the state of the segment's stream before it to the one after it, as in idf_decay_attend.  States are float32 throughout.
+ *   marks (NULL: not wanted): what the backward pass needs beside x and gates, states within the segments, idf_gate_scan_marks bytes, 256-byte
+ * aligned.  Rows need no alignment beyond their values'.  1 <= channels <= 2^20; segments of up to 2^30 tokens. */
+typedef struct {
+    int precision, channels;
+    int64_t n_tokens, max_tokens;
+    int n_segments, n_streams;
+    idf_rows x, gates, out;
+    const float *state_in;
+    float *state_out, *marks;
+    const int64_t *offsets;
+    const int32_t *stream_ids;
+    void *workspace;
+    size_t workspace_bytes;
+} idf_gate_scan_args;
+int idf_gate_scan_marks(const idf_gate_scan_args *a, size_t *bytes);
+int idf_gate_scan_workspace(const idf_gate_scan_args *a, size_t *bytes);
+int idf_gate_scan(const idf_gate_scan_args *a, void *hip_stream);
+
+/* Its gradients, for the same x, gates, offsets, ids and the marks that the forward call left:
+ *   l_t = grad_out_t + a_{t+1} l_{t+1} (the last one with grad_end in place of a l),  grad_x_t = (1 - a_t) l_t,
+ *   grad_gates_t = l_t (h_{t-1} - x_t) a_t (1 - a_t),  grad_state = a_1 l_1.
+ * grad_out.base, grad_end (of state_out) NULL: zeros; grad_state (of state_in) NULL: not wanted.  grad_end and grad_state float32 [n_streams][channels], may be
+ * the same; a segment without tokens hands grad_end on.  Rows of grad_x and grad_gates that none of the segments has are set to zero. */
+typedef struct {
+    int precision, channels;
+    int64_t n_tokens, max_tokens;
+    int n_segments, n_streams;
+    idf_rows x, gates, grad_out, grad_x, grad_gates;
+    const float *grad_end;
+    float *grad_state;
+    const float *marks;
+    const int64_t *offsets;
+    const int32_t *stream_ids;
+    void *workspace;
+    size_t workspace_bytes;
+} idf_gate_scan_backward_args;
+int idf_gate_scan_backward_workspace(const idf_gate_scan_backward_args *a, size_t *bytes);
+int idf_gate_scan_backward(const idf_gate_scan_backward_args *a, void *hip_stream);
+
 const char *idf_last_error(void);
 
 #ifdef __cplusplus

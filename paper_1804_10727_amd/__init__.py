@@ -6,4 +6,5 @@ PyTorch is used for device memory and streams.
 """
 from .binding import (IdfError, Net, Streams, create_net, lib_path, load_library,  # noqa: F401
                       measure_peak, net_from_workload, open_streams)
-from .tokens import decay_attend, norm_rotate, rotary_frequencies, window_attend  # noqa: F401
+from .tokens import (NibbleRing, decay_attend, gate_scan, gate_scan_backward, gate_scan_recorded, nibble_append, nibble_attend,  # noqa: F401
+                     nibble_ring, nibble_values, norm_rotate, project_rows, quantize_rows, rotary_frequencies, window_attend)

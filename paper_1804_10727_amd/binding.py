@@ -9,6 +9,9 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 _push = None                 # idf_push_segment on a tensor (csrc/push.cpp)
+TOKEN_OPS = ("idf_norm_rotate", "idf_window_workspace", "idf_window_attend", "idf_decay_workspace", "idf_decay_attend", "idf_quantize_rows",
+             "idf_project_workspace", "idf_project_rows", "idf_nibble_append", "idf_nibble_attend_workspace", "idf_nibble_attend", "idf_nibble_values",
+             "idf_gate_scan_workspace", "idf_gate_scan", "idf_gate_scan_backward_workspace", "idf_gate_scan_backward", "idf_gate_scan_marks")
 _token_ops = None            # the operators that mix tokens, on tensors (csrc/tokens.cpp)
 
 IDF_OK, IDF_EINVAL, IDF_ENOMEM, IDF_ESTATE, IDF_EDEVICE, IDF_EUNSUPPORTED = 0, -1, -2, -3, -4, -5
@@ -20,7 +23,9 @@ EXPORTS = ["idf_create_net", "idf_create_net_columnwise", "idf_destroy_net", "id
            "idf_push_segment", "idf_set_push_batching", "idf_read_outputs", "idf_reset_streams", "idf_get_stats", "idf_count_issued_macs", "idf_get_issued_macs", "idf_set_event_path", "idf_rows_pushed",
            "idf_layer_kernel", "idf_last_error", "idf_profile_begin", "idf_profile_end", "idf_enable_head",
            "idf_read_head", "idf_query_head_units_bytes", "idf_enable_head_units", "idf_read_head_units", "idf_push_pixels", "idf_query_eager_bytes", "idf_enable_eager", "idf_read_announced", "idf_read_announced_rows", "idf_eager_state_bytes", "idf_snapshot_bytes", "idf_snapshot", "idf_restore", "idf_create_net_volume", "idf_measure_peak",
-           "idf_rotary_frequencies", "idf_norm_rotate", "idf_window_workspace", "idf_window_attend", "idf_decay_workspace", "idf_decay_attend"]
+           "idf_rotary_frequencies", "idf_norm_rotate", "idf_window_workspace", "idf_window_attend", "idf_decay_workspace", "idf_decay_attend",
+           "idf_quantize_rows", "idf_project_workspace", "idf_project_rows", "idf_nibble_append", "idf_nibble_attend_workspace", "idf_nibble_attend", "idf_nibble_values",
+           "idf_gate_scan_marks", "idf_gate_scan_workspace", "idf_gate_scan", "idf_gate_scan_backward_workspace", "idf_gate_scan_backward"]
 
 
 class IdfError(RuntimeError):
@@ -120,7 +125,7 @@ def load_library():
     L.idf_restore.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]
     L.idf_read_head.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]
     L.idf_measure_peak.argtypes = [C.c_int, C.c_void_p, C.c_size_t, C.c_void_p, C.POINTER(C.c_double)]
-    for name in ("idf_norm_rotate", "idf_window_workspace", "idf_window_attend", "idf_decay_workspace", "idf_decay_attend"):
+    for name in TOKEN_OPS:
         getattr(L, name).argtypes = [C.c_void_p, C.c_void_p]
     L.idf_rotary_frequencies.argtypes = [C.c_int, C.c_double, C.c_int] + [C.c_double] * 4 + [C.c_void_p, C.POINTER(C.c_double)]
     L.idf_profile_begin.argtypes = [C.c_void_p]
@@ -164,8 +169,7 @@ def load_tokens():
         L = load_library()
         from . import build as _build
         native = _load_extension("_tokens", _build.tokens_path(), _build.build_tokens)
-        native.bind(*(C.cast(getattr(L, n), C.c_void_p).value for n in ("idf_norm_rotate", "idf_window_workspace", "idf_window_attend",
-                                                                         "idf_decay_workspace", "idf_decay_attend")))
+        native.bind(*(C.cast(getattr(L, n), C.c_void_p).value for n in TOKEN_OPS))
         _token_ops = native
     return _token_ops
 

@@ -127,6 +127,18 @@ size_t window_workspace(const idf_window_args &a);
 hipError_t launch_window(const idf_window_args &a, const LaunchCtx &lc);
 size_t decay_workspace(const idf_decay_args &a);
 hipError_t launch_decay(const idf_decay_args &a, const LaunchCtx &lc);
+hipError_t launch_quantize_rows(const idf_quantize_args &a, const LaunchCtx &lc);
+size_t project_workspace(const idf_project_args &a);
+hipError_t launch_project_rows(const idf_project_args &a, const LaunchCtx &lc);
+hipError_t launch_nibble_append(const idf_nibble_append_args &a, const LaunchCtx &lc);
+hipError_t launch_nibble_values(const idf_nibble_values_args &a, const LaunchCtx &lc);
+size_t nibble_attend_workspace(const idf_nibble_attend_args &a);
+hipError_t launch_nibble_attend(const idf_nibble_attend_args &a, const LaunchCtx &lc);
+size_t gate_scan_marks(int64_t n_tokens, int n_segments, int channels);
+size_t gate_scan_workspace(const idf_gate_scan_args &a);
+hipError_t launch_gate_scan(const idf_gate_scan_args &a, const LaunchCtx &lc);
+size_t gate_scan_workspace(const idf_gate_scan_backward_args &a);
+hipError_t launch_gate_scan_backward(const idf_gate_scan_backward_args &a, const LaunchCtx &lc);
 
 // Largest number of touched output rows one generic conv step can take for a layer with
 // c_out output channels (the host splits longer steps).

@@ -9,15 +9,13 @@
 #include <algorithm>
 
 #include "idf.h"
-#include "seq_mfma.h"
+#include "seq_split.h"
 
 namespace idf {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStepRows = 16;                      // query rows of a segment and key/value head that the step kernel takes
-constexpr int kMostSplits = 128;                   // parts of a list of keys: a wave joins them, a lane has two
 constexpr int kTileRows = 128;                     // query rows of a workgroup of the tile kernel
 
 // The keys that query positions first .. last see, as a list in order of position: first tokens of the stream, then from the beginning of
@@ -111,21 +109,6 @@ struct Flat {
         return f;
     }
 };
-
-// Partial results of rows whose keys are split over workgroups: [split][token][head][head_dim] sums, then [split][token][head] maximum (of
-// scores in units of log 2) and sum of weights.
-struct Partial {
-    float *o, *ml;
-    int splits;
-};
-__device__ __host__ __forceinline__ Partial partial_of(const idf_window_args &a, int splits)
-{
-    Partial p;
-    p.splits = splits;
-    p.o = (float *)a.workspace;
-    p.ml = p.o + (int64_t)splits * a.n_tokens * a.heads_q * a.head_dim;
-    return p;
-}
 
 // A row whose sums came out infinite or not a number: once more, by one wave, reading only the values that the row sees -- on the
 // matrix cores a weight of zero times an infinite value that another row of the tile sees would be no zero.
@@ -594,66 +577,6 @@ __global__ void __launch_bounds__(256, PREC != IDF_PREC_BF16 || DP > 128 ? 1 : D
     if (append && split == 0) append_tokens(a, g, keys, kh, vh, (int)((row0 + group - 1) / group), (int)(row_last / group) + 1);
 }
 
-// Splits joined.  A workgroup takes a row, each of its waves every fourth split: its lanes first the maximum and sum of a split each, whose
-// shares then go from lane to lane while a lane adds up four values of the row, with splits side by side where the row leaves lanes.  All of
-// a wave's reads are on their way together: one after the other, each would wait for memory.
-template <int PREC>
-__global__ void __launch_bounds__(256) k_window_join(idf_window_args a, int splits, int lanes_log2)
-{
-    using T = typename Elem<PREC>::type;
-    constexpr int kAhead = 8;
-    __shared__ __align__(16) float sums[4][256];
-    const Segment g = segment_of(a, blockIdx.y, a.starts);
-    const Partial part = partial_of(a, splits);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c = (lane & ((1 << lanes_log2) - 1)) * 4, first = wave + 4 * (lane >> lanes_log2), step = 4 * (64 >> lanes_log2);
-    const int64_t n = (int64_t)g.len * a.heads_q, apart = a.n_tokens * a.heads_q;
-    for (int64_t x = blockIdx.x; x < n; x += gridDim.x) {
-        const int64_t t = x / a.heads_q, token = g.begin + t, row = token * a.heads_q + (x - t * a.heads_q);
-        float m[2], l[2], share[2] = {}, sum = 0.f;
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int s = lane + 64 * y;
-            m[y] = s < splits ? part.ml[2 * (row + s * apart)] : -__FLT_MAX__;
-            l[y] = s < splits ? part.ml[2 * (row + s * apart) + 1] : 0.f;
-        }
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int s0 = 0; s0 < splits; s0 += kAhead * step) {
-            f32x4 in[kAhead];
-#pragma unroll
-            for (int y = 0; y < kAhead; ++y) {
-                const int s = s0 + first + y * step;
-                in[y] = s < splits && c < a.head_dim ? *(const f32x4 *)(part.o + (row + s * apart) * a.head_dim + c) : f32x4{0.f, 0.f, 0.f, 0.f};
-            }
-            if (s0 == 0) {
-                const float top = wave_max(fmaxf(m[0], m[1]));
-#pragma unroll
-                for (int y = 0; y < 2; ++y) share[y] = __builtin_amdgcn_exp2f(m[y] - top);
-                sum = wave_sum((lane < splits ? l[0] * share[0] : 0.f) + (lane + 64 < splits ? l[1] * share[1] : 0.f));
-            }
-#pragma unroll
-            for (int y = 0; y < kAhead; ++y) {
-                const int s = s0 + first + y * step;
-                const float low = __shfl(share[0], s & 63), high = __shfl(share[1], s & 63);
-                v += (s & 64 ? high : low) * in[y];
-            }
-        }
-        for (int mask = 1 << lanes_log2; mask < 64; mask <<= 1)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], mask);
-        __syncthreads();                           // (the row before has been read)
-        if (first < 4 && c < a.head_dim) *(f32x4 *)(sums[wave] + c) = v;
-        __syncthreads();
-        if (threadIdx.x * 4 >= a.head_dim) continue;
-        const int at = threadIdx.x * 4;
-        v = *(const f32x4 *)(sums[0] + at) + *(const f32x4 *)(sums[1] + at) + *(const f32x4 *)(sums[2] + at) + *(const f32x4 *)(sums[3] + at);
-        Pack<T, 4> w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w.v[e] = Elem<PREC>::from_f32(v[e] / sum);
-        *(Pack<T, 4> *)((T *)a.out.base + token * a.out.token_stride + (x - t * a.heads_q) * a.out.head_stride + at) = w;
-    }
-}
-
 // The segments' tokens into their rings, behind the attention that still reads what they take the place of.  Of a segment longer than
 // the ring the newest tokens are written, so that no slot is written twice.
 __global__ void __launch_bounds__(256) k_window_append(idf_window_args a, int row16, int elem16)
@@ -736,11 +659,7 @@ hipError_t by_dim(const idf_window_args &a, const LaunchCtx &lc)
 {
     const Plan p = plan_of(a);
     hipError_t e = a.head_dim <= 64 ? attend<PREC, 64>(a, p, lc) : a.head_dim <= 96 ? attend<PREC, 96>(a, p, lc) : a.head_dim <= 128 ? attend<PREC, 128>(a, p, lc) : attend<PREC, 256>(a, p, lc);
-    if (e == hipSuccess && p.splits > 1) {
-        int lanes_log2 = 0;
-        while (4 << lanes_log2 < a.head_dim) ++lanes_log2;
-        e = launch(k_window_join<PREC>, dim3((unsigned)std::min<int64_t>(longest(a) * a.heads_q, 8192), a.n_segments), dim3(256), 0, lc, a, p.splits, lanes_log2);
-    }
+    if (e == hipSuccess && p.splits > 1) e = join_splits<PREC>(a, p.splits, lc);
     if (e == hipSuccess && a.k_ring && !p.append) {
         const int elem16 = Elem<PREC>::VL, row16 = a.heads_kv * a.head_dim / elem16;
         e = launch(k_window_append, dim3((unsigned)std::min<int64_t>((longest(a) * row16 + 255) / 256, 4096), a.n_segments), dim3(256), 0, lc, a, row16, elem16);
@@ -753,7 +672,7 @@ hipError_t by_dim(const idf_window_args &a, const LaunchCtx &lc)
 size_t window_workspace(const idf_window_args &a)
 {
     const Plan p = plan_of(a);
-    return p.splits > 1 ? (size_t)p.splits * a.n_tokens * a.heads_q * (a.head_dim + 2) * sizeof(float) : 0;
+    return split_workspace(a, p.splits);
 }
 
 hipError_t launch_window(const idf_window_args &a, const LaunchCtx &lc)

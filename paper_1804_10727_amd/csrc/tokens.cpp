@@ -11,30 +11,45 @@
 #include <climits>
 #include <cmath>
 #include <cstdint>
+#include <cstring>
 
 #include "idf.h"
 
 namespace {
 
-int (*norm_rotate_fn)(const idf_norm_rotate_args *, void *);
-int (*window_workspace_fn)(const idf_window_args *, size_t *);
-int (*window_fn)(const idf_window_args *, void *);
-int (*decay_workspace_fn)(const idf_decay_args *, size_t *);
-int (*decay_fn)(const idf_decay_args *, void *);
+// The library's functions, in the order in which bind takes them.
+struct Functions {
+    int (*norm_rotate)(const idf_norm_rotate_args *, void *);
+    int (*window_workspace)(const idf_window_args *, size_t *);
+    int (*window)(const idf_window_args *, void *);
+    int (*decay_workspace)(const idf_decay_args *, size_t *);
+    int (*decay)(const idf_decay_args *, void *);
+    int (*quantize)(const idf_quantize_args *, void *);
+    int (*project_workspace)(const idf_project_args *, size_t *);
+    int (*project)(const idf_project_args *, void *);
+    int (*nibble_append)(const idf_nibble_append_args *, void *);
+    int (*nibble_workspace)(const idf_nibble_attend_args *, size_t *);
+    int (*nibble_attend)(const idf_nibble_attend_args *, void *);
+    int (*nibble_values)(const idf_nibble_values_args *, void *);
+    int (*gate_workspace)(const idf_gate_scan_args *, size_t *);
+    int (*gate)(const idf_gate_scan_args *, void *);
+    int (*gate_back_workspace)(const idf_gate_scan_backward_args *, size_t *);
+    int (*gate_back)(const idf_gate_scan_backward_args *, void *);
+    int (*gate_marks)(const idf_gate_scan_args *, size_t *);
+} fn;
+constexpr int kFunctions = sizeof(Functions) / sizeof(void *);
+bool bound;
 
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    if (n != 5) { PyErr_SetString(PyExc_TypeError, "five addresses"); return nullptr; }
-    void *p[5];
-    for (int i = 0; i < 5; ++i) {
+    if (n != kFunctions) { PyErr_Format(PyExc_TypeError, "%d addresses", kFunctions); return nullptr; }
+    void *p[kFunctions];
+    for (int i = 0; i < kFunctions; ++i) {
         p[i] = PyLong_AsVoidPtr(args[i]);
         if (PyErr_Occurred()) return nullptr;
     }
-    norm_rotate_fn = reinterpret_cast<decltype(norm_rotate_fn)>(p[0]);
-    window_workspace_fn = reinterpret_cast<decltype(window_workspace_fn)>(p[1]);
-    window_fn = reinterpret_cast<decltype(window_fn)>(p[2]);
-    decay_workspace_fn = reinterpret_cast<decltype(decay_workspace_fn)>(p[3]);
-    decay_fn = reinterpret_cast<decltype(decay_fn)>(p[4]);
+    std::memcpy(&fn, p, sizeof(fn));
+    bound = true;
     Py_RETURN_NONE;
 }
 
@@ -99,11 +114,11 @@ double real(PyObject *o)
     return v;
 }
 
-template <class A> int call(int (*fn)(const A *, void *), const A &a, void *stream)
+template <class A> int call(int (*f)(const A *, void *), const A &a, void *stream)
 {
     int rc;
     Py_BEGIN_ALLOW_THREADS
-    rc = fn(&a, stream);
+    rc = f(&a, stream);
     Py_END_ALLOW_THREADS
     return rc;
 }
@@ -134,7 +149,7 @@ template <class F> PyObject *entry(F f)
 // norm_rotate(stream, q, k, positions, frequencies, interleaved, amplitude, q_weight, k_weight, eps, q_out, k_out)
 PyObject *norm_rotate(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    if (n != 12 || !norm_rotate_fn) { PyErr_SetString(PyExc_TypeError, "norm_rotate takes 12 arguments"); return nullptr; }
+    if (n != 12 || !bound) { PyErr_SetString(PyExc_TypeError, "norm_rotate takes 12 arguments"); return nullptr; }
     return entry([&]() -> PyObject * {
         void *stream = reinterpret_cast<void *>((uintptr_t)whole(args[0]));
         const at::Tensor *q = tensor(args[1]), *k = tensor(args[2]), *pos = tensor(args[3]), *freq = tensor(args[4]);
@@ -160,7 +175,7 @@ PyObject *norm_rotate(PyObject *, PyObject *const *args, Py_ssize_t n)
         const at::Tensor q_out = output(tensor(args[10]), q->sizes(), *q), k_out = output(tensor(args[11]), k->sizes(), *q);
         a.q_out = rows(q_out, *q, false);
         a.k_out = rows(k_out, *q, false);
-        const int rc = call(norm_rotate_fn, a, stream);
+        const int rc = call(fn.norm_rotate, a, stream);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
         PyObject *both = PyTuple_New(2);
         if (!both) throw Unusual();
@@ -188,7 +203,7 @@ template <class A> void segments(A &a, const at::Tensor &q, const at::Tensor *of
 // window_attend(stream, q, k, v, k_ring, v_ring, starts, window, sinks, scale, offsets, max_tokens, stream_ids, out)
 PyObject *window_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    if (n != 14 || !window_fn) { PyErr_SetString(PyExc_TypeError, "window_attend takes 14 arguments"); return nullptr; }
+    if (n != 14 || !bound) { PyErr_SetString(PyExc_TypeError, "window_attend takes 14 arguments"); return nullptr; }
     return entry([&]() -> PyObject * {
         void *stream = reinterpret_cast<void *>((uintptr_t)whole(args[0]));
         const at::Tensor *q = tensor(args[1]), *k = tensor(args[2]), *v = tensor(args[3]), *k_ring = tensor(args[4]), *v_ring = tensor(args[5]);
@@ -225,14 +240,14 @@ PyObject *window_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
         const c10::DeviceGuard guard(q->device());
         const at::Tensor out = output(tensor(args[13]), q->sizes(), *q);
         a.out = rows(out, *q, true);
-        int rc = window_workspace_fn(&a, &a.workspace_bytes);
+        int rc = fn.window_workspace(&a, &a.workspace_bytes);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
         at::Tensor ws;                             // (held until the work is enqueued)
         if (a.workspace_bytes) {
             ws = at::empty({(int64_t)a.workspace_bytes}, q->options().dtype(at::kByte));
             a.workspace = ws.data_ptr();
         }
-        rc = call(window_fn, a, stream);
+        rc = call(fn.window, a, stream);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
         return args[13] != Py_None ? Py_NewRef(args[13]) : THPVariable_Wrap(out);
     });
@@ -241,7 +256,7 @@ PyObject *window_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
 // decay_attend(stream, q, k, v, log_decay, state, state_out, scale, offsets, max_tokens, n_segments, stream_ids, out)
 PyObject *decay_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    if (n != 13 || !decay_fn) { PyErr_SetString(PyExc_TypeError, "decay_attend takes 13 arguments"); return nullptr; }
+    if (n != 13 || !bound) { PyErr_SetString(PyExc_TypeError, "decay_attend takes 13 arguments"); return nullptr; }
     return entry([&]() -> PyObject * {
         void *stream = reinterpret_cast<void *>((uintptr_t)whole(args[0]));
         const at::Tensor *q = tensor(args[1]), *k = tensor(args[2]), *v = tensor(args[3]), *log_decay = tensor(args[4]), *in = tensor(args[5]), *to = tensor(args[6]);
@@ -278,16 +293,339 @@ PyObject *decay_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
         const c10::DeviceGuard guard(q->device());
         const at::Tensor out = output(tensor(args[12]), {a.n_tokens, a.heads_q, a.dim_v}, *q);
         a.out = rows(out, *q, true);
-        int rc = decay_workspace_fn(&a, &a.workspace_bytes);
+        int rc = fn.decay_workspace(&a, &a.workspace_bytes);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
         at::Tensor ws;
         if (a.workspace_bytes) {
             ws = at::empty({(int64_t)a.workspace_bytes}, q->options().dtype(at::kByte));
             a.workspace = ws.data_ptr();
         }
-        rc = call(decay_fn, a, stream);
+        rc = call(fn.decay, a, stream);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
         return args[12] != Py_None ? Py_NewRef(args[12]) : THPVariable_Wrap(out);
+    });
+}
+
+// What a call needs beside its arguments, held until the work is enqueued; what the library returned if that is an error.
+template <class A> int with_workspace(int (*size)(const A *, size_t *), A &a, const at::Tensor &like, at::Tensor &ws)
+{
+    const int rc = size(&a, &a.workspace_bytes);
+    if (rc == IDF_OK && a.workspace_bytes) {
+        ws = at::empty({(int64_t)a.workspace_bytes}, like.options().dtype(at::kByte));
+        a.workspace = ws.data_ptr();
+    }
+    return rc;
+}
+
+// A matrix whose values lie next to each other in a row.
+idf_rows matrix(const at::Tensor &t, const at::Tensor &like)
+{
+    need(t.is_cuda() && t.layout() == at::kStrided && t.dim() == 2 && t.device() == like.device() && (t.stride(1) == 1 || t.size(1) <= 1));
+    need(t.size(0) <= 1 || t.stride(0) <= 1 << 25);
+    return idf_rows{t.data_ptr(), t.size(0) > 1 ? t.stride(0) : t.size(1)};
+}
+
+// quantize_rows(stream, x, codes, scales)
+PyObject *quantize_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 4 || !bound) { PyErr_SetString(PyExc_TypeError, "quantize_rows takes 4 arguments"); return nullptr; }
+    return entry([&]() -> PyObject * {
+        void *stream = reinterpret_cast<void *>((uintptr_t)whole(args[0]));
+        const at::Tensor *x = tensor(args[1]);
+        need(x);
+        idf_quantize_args a{};
+        a.precision = precision(*x);
+        a.x = matrix(*x, *x);
+        need(x->size(1) <= INT_MAX - 16);
+        a.n_rows = x->size(0);
+        a.cols = (int)x->size(1);
+        const c10::DeviceGuard guard(x->device());
+        const at::Tensor *given[2] = {tensor(args[2]), tensor(args[3])};
+        const int64_t padded = (a.cols + 15) / 16 * 16;
+        at::Tensor codes = given[0] ? *given[0] : at::empty({a.n_rows, padded}, x->options().dtype(at::kChar));
+        at::Tensor scales = given[1] ? *given[1] : at::empty({a.n_rows}, x->options().dtype(at::kFloat));
+        need(codes.scalar_type() == at::kChar && codes.device() == x->device() && codes.is_contiguous() && codes.dim() == 2 && codes.size(0) == a.n_rows && codes.size(1) == padded);
+        a.codes = static_cast<int8_t *>(codes.data_ptr());
+        a.scales = plain<float>(&scales, at::kFloat, a.n_rows, *x);
+        const int rc = call(fn.quantize, a, stream);
+        if (rc != IDF_OK) return PyLong_FromLong(rc);
+        PyObject *both = PyTuple_New(2);
+        if (!both) throw Unusual();
+        PyTuple_SET_ITEM(both, 0, given[0] ? Py_NewRef(args[2]) : THPVariable_Wrap(codes));
+        PyTuple_SET_ITEM(both, 1, given[1] ? Py_NewRef(args[3]) : THPVariable_Wrap(scales));
+        return both;
+    });
+}
+
+// project_rows(stream, x, weight, weight_scales, bias, x_scales, to_f32, out); to_f32: the type of a new out, 0 or 1, or -1 for x's
+PyObject *project_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 8 || !bound) { PyErr_SetString(PyExc_TypeError, "project_rows takes 8 arguments"); return nullptr; }
+    return entry([&]() -> PyObject * {
+        void *stream = reinterpret_cast<void *>((uintptr_t)whole(args[0]));
+        const at::Tensor *x = tensor(args[1]), *w = tensor(args[2]), *ws_ = tensor(args[3]), *bias = tensor(args[4]), *xs = tensor(args[5]), *given = tensor(args[7]);
+        need(x && w && ws_);
+        idf_project_args a{};
+        const bool codes = x->scalar_type() == at::kChar;
+        a.precision = codes ? IDF_PREC_I8 : precision(*x);
+        need(codes == (xs != nullptr));
+        a.x = matrix(*x, *x);
+        need(!codes || ((uintptr_t)a.x.base % 16 == 0 && a.x.row_stride % 16 == 0));
+        need((uintptr_t)w->data_ptr() % 16 == 0);
+        need(x->size(1) <= INT_MAX - 16 && w->dim() == 2 && w->scalar_type() == at::kChar && w->device() == x->device() && w->is_contiguous() && w->size(0) <= INT_MAX);
+        a.n_rows = x->size(0);
+        a.cols = (int)x->size(1);
+        a.n_out = (int)w->size(0);
+        need(w->size(1) == (a.cols + 15) / 16 * 16);
+        a.weights = static_cast<const int8_t *>(w->data_ptr());
+        a.weight_scales = plain<float>(ws_, at::kFloat, a.n_out, *x);
+        a.bias = plain<float>(bias, at::kFloat, a.n_out, *x);
+        a.x_scales = plain<float>(xs, at::kFloat, a.n_rows, *x);
+        const int64_t to_f32 = whole(args[6]);
+        need(given ? to_f32 < 0 || given->scalar_type() == (to_f32 ? at::kFloat : at::kBFloat16) : !codes || to_f32 >= 0);
+        const at::ScalarType type = given ? given->scalar_type() : to_f32 < 0 ? x->scalar_type() : to_f32 ? at::kFloat : at::kBFloat16;
+        const c10::DeviceGuard guard(x->device());
+        const at::Tensor out = given ? *given : at::empty({a.n_rows, a.n_out}, x->options().dtype(type));
+        need(out.dim() == 2 && out.size(0) == a.n_rows && out.size(1) == a.n_out);
+        a.out_precision = precision(out);
+        a.out = matrix(out, *x);
+        at::Tensor ws;
+        int rc = with_workspace(fn.project_workspace, a, *x, ws);
+        if (rc == IDF_OK) rc = call(fn.project, a, stream);
+        if (rc != IDF_OK) return PyLong_FromLong(rc);
+        return given ? Py_NewRef(args[7]) : THPVariable_Wrap(out);
+    });
+}
+
+// The four tensors of a ring; fills in sizes that the first one has.
+template <class A> void nibble_ring(A &a, PyObject *const *args, const at::Tensor *like)
+{
+    const at::Tensor *t[4];
+    for (int i = 0; i < 4; ++i) {
+        t[i] = tensor(args[i]);
+        need(t[i] && t[i]->scalar_type() == at::kByte && t[i]->is_cuda() && t[i]->is_contiguous() && t[i]->dim() == 4 && (!like || t[i]->device() == like->device()));
+        need(t[i]->device() == t[0]->device());
+        for (int d = 0; d < 3; ++d) need(t[i]->size(d) == t[0]->size(d));
+        need(t[i]->size(3) <= 1024 && t[i]->size(3) * (i % 2 ? 16 : 1) == t[0]->size(3));
+    }
+    need(t[0]->size(0) <= INT_MAX && t[0]->size(1) <= INT_MAX);
+    a.n_streams = (int)t[0]->size(0);
+    a.heads_kv = (int)t[0]->size(1);
+    a.slots = t[0]->size(2);
+    a.head_dim = 2 * (int)t[0]->size(3);
+    a.ring = idf_nibble_ring{static_cast<uint8_t *>(t[0]->data_ptr()), static_cast<uint8_t *>(t[1]->data_ptr()), static_cast<uint8_t *>(t[2]->data_ptr()), static_cast<uint8_t *>(t[3]->data_ptr())};
+}
+
+// Where segments of a ring's streams begin, and which streams they are of.
+template <class A> void places(A &a, const at::Tensor &like, PyObject *starts_, PyObject *offsets_, PyObject *max_tokens, PyObject *ids_)
+{
+    const at::Tensor *starts = tensor(starts_), *offsets = tensor(offsets_), *ids = tensor(ids_);
+    const int64_t count = ids ? ids->numel() : starts ? starts->numel() : a.n_streams;
+    segments(a, like, offsets, max_tokens, count);
+    need(!(ids || starts) || a.n_segments == count);
+    a.starts = plain<int64_t>(starts, at::kLong, a.n_segments, like);
+    a.stream_ids = plain<int32_t>(ids, at::kInt, a.n_segments, like);
+}
+
+// nibble_append(stream, k, v, four of the ring, starts, sinks, frequencies, interleaved, amplitude, k_weight, eps, offsets, max_tokens, stream_ids)
+PyObject *nibble_append(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 17 || !bound) { PyErr_SetString(PyExc_TypeError, "nibble_append takes 17 arguments"); return nullptr; }
+    return entry([&]() -> PyObject * {
+        void *stream = reinterpret_cast<void *>((uintptr_t)whole(args[0]));
+        const at::Tensor *k = tensor(args[1]), *v = tensor(args[2]), *freq = tensor(args[9]);
+        need(k && v);
+        idf_nibble_append_args a{};
+        a.precision = precision(*k);
+        a.k = rows(*k, *k, false);
+        a.v = rows(*v, *k, false);
+        nibble_ring(a, args + 3, k);
+        need(k->sizes() == v->sizes() && k->size(1) == a.heads_kv && k->size(2) == a.head_dim && (!freq || freq->numel() <= 1024));
+        a.n_tokens = k->size(0);
+        places(a, *k, args[7], args[14], args[15], args[16]);
+        a.sinks = small(args[8]);
+        a.frequencies = plain<double>(freq, at::kDouble, -1, *k);
+        a.rotary_dim = freq ? 2 * (int)freq->numel() : 0;
+        a.interleaved = small(args[10]);
+        a.amplitude = real(args[11]);
+        a.k_weight = plain<float>(tensor(args[12]), at::kFloat, a.head_dim, *k);
+        a.eps = real(args[13]);
+        const c10::DeviceGuard guard(k->device());
+        const int rc = call(fn.nibble_append, a, stream);
+        return PyLong_FromLong(rc);
+    });
+}
+
+// nibble_attend(stream, q, four of the ring, starts, window, sinks, scale, offsets, max_tokens, stream_ids, out)
+PyObject *nibble_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 14 || !bound) { PyErr_SetString(PyExc_TypeError, "nibble_attend takes 14 arguments"); return nullptr; }
+    return entry([&]() -> PyObject * {
+        void *stream = reinterpret_cast<void *>((uintptr_t)whole(args[0]));
+        const at::Tensor *q = tensor(args[1]);
+        need(q);
+        idf_nibble_attend_args a{};
+        a.precision = precision(*q);
+        a.q = rows(*q, *q, true);
+        nibble_ring(a, args + 2, q);
+        need(q->size(1) <= INT_MAX && q->size(2) == a.head_dim);
+        a.heads_q = (int)q->size(1);
+        a.n_tokens = q->size(0);
+        places(a, *q, args[6], args[10], args[11], args[12]);
+        a.window = small(args[7]);
+        a.sinks = small(args[8]);
+        a.scale = args[9] == Py_None ? (float)(1.0 / std::sqrt((double)a.head_dim)) : (float)real(args[9]);
+        const c10::DeviceGuard guard(q->device());
+        const at::Tensor out = output(tensor(args[13]), q->sizes(), *q);
+        a.out = rows(out, *q, true);
+        at::Tensor ws;
+        int rc = with_workspace(fn.nibble_workspace, a, *q, ws);
+        if (rc == IDF_OK) rc = call(fn.nibble_attend, a, stream);
+        if (rc != IDF_OK) return PyLong_FromLong(rc);
+        return args[13] != Py_None ? Py_NewRef(args[13]) : THPVariable_Wrap(out);
+    });
+}
+
+// nibble_values(stream, four of the ring, to_f32)
+PyObject *nibble_values(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 6 || !bound) { PyErr_SetString(PyExc_TypeError, "nibble_values takes 6 arguments"); return nullptr; }
+    return entry([&]() -> PyObject * {
+        void *stream = reinterpret_cast<void *>((uintptr_t)whole(args[0]));
+        idf_nibble_values_args a{};
+        nibble_ring(a, args + 1, nullptr);
+        const at::Tensor &like = *tensor(args[1]);
+        a.precision = whole(args[5]) ? IDF_PREC_F32 : IDF_PREC_BF16;
+        const c10::DeviceGuard guard(like.device());
+        at::Tensor out[2];
+        for (at::Tensor &t : out) t = at::empty({a.n_streams, a.slots, a.heads_kv, a.head_dim}, like.options().dtype(a.precision == IDF_PREC_F32 ? at::kFloat : at::kBFloat16));
+        a.k = out[0].data_ptr();
+        a.v = out[1].data_ptr();
+        const int rc = call(fn.nibble_values, a, stream);
+        if (rc != IDF_OK) return PyLong_FromLong(rc);
+        PyObject *both = PyTuple_New(2);
+        if (!both) throw Unusual();
+        for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(both, i, THPVariable_Wrap(out[i]));
+        return both;
+    });
+}
+
+// States [stream][channel] that a call of the recurrence goes from and to.
+int64_t states(const at::Tensor *in, const at::Tensor *to, int64_t channels, const at::Tensor &like)
+{
+    int64_t streams = -1;
+    for (const at::Tensor *s : {in, to}) {
+        if (!s) continue;
+        need(s->dim() == 2 && s->scalar_type() == at::kFloat && s->device() == like.device() && s->is_contiguous() && s->size(1) == channels && s->size(0) <= INT_MAX);
+        need(streams < 0 || streams == s->size(0));
+        streams = s->size(0);
+    }
+    return streams;
+}
+
+// Tokens, segments and streams of a call of the recurrence.
+template <class A> void gate_segments(A &a, const at::Tensor &x, int64_t streams, PyObject *offsets, PyObject *max_tokens, PyObject *n_segments, PyObject *ids_)
+{
+    const at::Tensor *ids = tensor(ids_);
+    const bool told = ids || n_segments != Py_None;
+    const int64_t count = ids ? ids->numel() : n_segments != Py_None ? whole(n_segments) : streams >= 0 ? streams : 1;
+    segments(a, x, tensor(offsets), max_tokens, count);
+    need(!told || a.n_segments == count);
+    a.n_streams = streams >= 0 ? (int)streams : a.n_segments;
+    a.stream_ids = plain<int32_t>(ids, at::kInt, a.n_segments, x);
+}
+
+// gate_scan(stream, x, gates, state, state_out, offsets, max_tokens, n_segments, stream_ids, out, marks): out; marks True: new ones, (out, marks)
+PyObject *gate_scan(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 11 || !bound) { PyErr_SetString(PyExc_TypeError, "gate_scan takes 11 arguments"); return nullptr; }
+    return entry([&]() -> PyObject * {
+        void *stream = reinterpret_cast<void *>((uintptr_t)whole(args[0]));
+        const at::Tensor *x = tensor(args[1]), *g = tensor(args[2]), *in = tensor(args[3]), *to = tensor(args[4]), *given = tensor(args[9]);
+        const at::Tensor *marks = args[10] == Py_True ? nullptr : tensor(args[10]);
+        need(x && g && x->sizes() == g->sizes() && g->scalar_type() == x->scalar_type());
+        idf_gate_scan_args a{};
+        a.precision = precision(*x);
+        a.x = matrix(*x, *x);
+        a.gates = matrix(*g, *x);
+        need(x->size(1) <= INT_MAX);
+        a.channels = (int)x->size(1);
+        a.n_tokens = x->size(0);
+        gate_segments(a, *x, states(in, to, a.channels, *x), args[5], args[6], args[7], args[8]);
+        a.state_in = in ? static_cast<const float *>(in->data_ptr()) : nullptr;
+        a.state_out = to ? static_cast<float *>(to->data_ptr()) : nullptr;
+        const c10::DeviceGuard guard(x->device());
+        const at::Tensor out = output(given, x->sizes(), *x);
+        need(out.scalar_type() == x->scalar_type());
+        a.out = matrix(out, *x);
+        at::Tensor fresh, ws;
+        int rc = IDF_OK;
+        if (marks || args[10] == Py_True) {
+            size_t bytes = 0;
+            rc = fn.gate_marks(&a, &bytes);
+            if (rc != IDF_OK) return PyLong_FromLong(rc);
+            if (!marks) { fresh = at::empty({(int64_t)bytes / 4}, x->options().dtype(at::kFloat)); marks = &fresh; }
+            a.marks = plain<float>(marks, at::kFloat, (int64_t)bytes / 4, *x);
+        }
+        rc = with_workspace(fn.gate_workspace, a, *x, ws);
+        if (rc == IDF_OK) rc = call(fn.gate, a, stream);
+        if (rc != IDF_OK) return PyLong_FromLong(rc);
+        PyObject *got = given ? Py_NewRef(args[9]) : THPVariable_Wrap(out);
+        if (args[10] != Py_True || !got) return got;
+        PyObject *both = PyTuple_New(2);
+        if (!both) { Py_DECREF(got); throw Unusual(); }
+        PyTuple_SET_ITEM(both, 0, got);
+        PyTuple_SET_ITEM(both, 1, THPVariable_Wrap(fresh));
+        return both;
+    });
+}
+
+// gate_scan_backward(stream, x, gates, marks, grad_out, grad_end, offsets, max_tokens, n_segments, stream_ids, n_streams): gradients of x, gates and states
+PyObject *gate_scan_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 11 || !bound) { PyErr_SetString(PyExc_TypeError, "gate_scan_backward takes 11 arguments"); return nullptr; }
+    return entry([&]() -> PyObject * {
+        void *stream = reinterpret_cast<void *>((uintptr_t)whole(args[0]));
+        const at::Tensor *x = tensor(args[1]), *g = tensor(args[2]), *marks = tensor(args[3]), *grad = tensor(args[4]), *end = tensor(args[5]);
+        need(x && g && marks && x->sizes() == g->sizes() && g->scalar_type() == x->scalar_type());
+        idf_gate_scan_backward_args a{};
+        a.precision = precision(*x);
+        a.x = matrix(*x, *x);
+        a.gates = matrix(*g, *x);
+        need(x->size(1) <= INT_MAX);
+        a.channels = (int)x->size(1);
+        a.n_tokens = x->size(0);
+        const int64_t told = args[10] == Py_None ? -1 : whole(args[10]), have = states(end, nullptr, a.channels, *x);
+        need(told < 0 || have < 0 || told == have);
+        gate_segments(a, *x, have >= 0 ? have : told, args[6], args[7], args[8], args[9]);
+        if (grad) {
+            need(grad->sizes() == x->sizes() && grad->scalar_type() == x->scalar_type());
+            a.grad_out = matrix(*grad, *x);
+        }
+        idf_gate_scan_args f{};
+        f.precision = a.precision; f.channels = a.channels; f.n_tokens = a.n_tokens; f.max_tokens = a.max_tokens; f.n_segments = a.n_segments; f.n_streams = a.n_streams;
+        f.offsets = a.offsets; f.stream_ids = a.stream_ids;
+        size_t bytes = 0;
+        int rc = fn.gate_marks(&f, &bytes);
+        if (rc != IDF_OK) return PyLong_FromLong(rc);
+        a.marks = plain<float>(marks, at::kFloat, (int64_t)bytes / 4, *x);
+        a.grad_end = end ? static_cast<const float *>(end->data_ptr()) : nullptr;
+        const c10::DeviceGuard guard(x->device());
+        const auto fresh = [&]() { return a.n_segments ? at::empty(x->sizes(), x->options()) : at::zeros(x->sizes(), x->options()); };
+        const at::Tensor gx = fresh(), gg = fresh(), gs = at::empty({a.n_streams, a.channels}, x->options().dtype(at::kFloat));
+        a.grad_x = matrix(gx, *x);
+        a.grad_gates = matrix(gg, *x);
+        a.grad_state = static_cast<float *>(gs.data_ptr());
+        at::Tensor ws;
+        rc = with_workspace(fn.gate_back_workspace, a, *x, ws);
+        if (rc == IDF_OK) rc = call(fn.gate_back, a, stream);
+        if (rc != IDF_OK) return PyLong_FromLong(rc);
+        PyObject *all = PyTuple_New(3);
+        if (!all) throw Unusual();
+        PyTuple_SET_ITEM(all, 0, THPVariable_Wrap(gx));
+        PyTuple_SET_ITEM(all, 1, THPVariable_Wrap(gg));
+        PyTuple_SET_ITEM(all, 2, THPVariable_Wrap(gs));
+        return all;
     });
 }
 
@@ -297,6 +635,13 @@ PyMethodDef methods[] = {
     {"norm_rotate", FAST(norm_rotate), "idf_norm_rotate on tensors"},
     {"window_attend", FAST(window_attend), "idf_window_attend on tensors"},
     {"decay_attend", FAST(decay_attend), "idf_decay_attend on tensors"},
+    {"quantize_rows", FAST(quantize_rows), "idf_quantize_rows on tensors"},
+    {"project_rows", FAST(project_rows), "idf_project_rows on tensors"},
+    {"nibble_append", FAST(nibble_append), "idf_nibble_append on tensors"},
+    {"nibble_attend", FAST(nibble_attend), "idf_nibble_attend on tensors"},
+    {"nibble_values", FAST(nibble_values), "idf_nibble_values on tensors"},
+    {"gate_scan", FAST(gate_scan), "idf_gate_scan on tensors"},
+    {"gate_scan_backward", FAST(gate_scan_backward), "idf_gate_scan_backward on tensors"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tokens", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,13 +1,14 @@
-"""The operators that mix the tokens of streams (include/idf.h, last section) on torch tensors: argument marshalling only.
+"""The operators that mix the tokens of streams (include/idf.h, last sections) on torch tensors: argument marshalling only.
 
-Everything is enqueued on the current stream of the tensors' device.  There is no backward pass: tensors that require gradients are refused
-where gradients are recorded, taken under torch.no_grad().  Packed tokens [token][head][value]; a tensor whose values lie
+Everything is enqueued on the current stream of the tensors' device.  There is no backward pass but that of gate_scan_recorded: tensors that require
+gradients are refused elsewhere where gradients are recorded, taken under torch.no_grad().  Packed tokens [token][head][value]; a tensor whose values lie
 apart, or whose rows do not begin at multiples of 16 bytes where the library asks for that, is copied first.
 """
 from __future__ import annotations
 
 import ctypes as C
 import math
+from typing import NamedTuple
 
 import numpy as np
 
@@ -45,6 +46,55 @@ class _Decay(C.Structure):
                 [(n, _Tokens) for n in ("q", "k", "v", "out")] +
                 [(n, C.c_void_p) for n in ("log_decay", "state_in", "state_out", "offsets", "stream_ids", "workspace")] +
                 [("workspace_bytes", C.c_size_t)])
+
+
+class _Rows(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("row_stride", C.c_int64)]
+
+
+class _Quantize(C.Structure):
+    _fields_ = [("precision", C.c_int), ("cols", C.c_int), ("n_rows", C.c_int64), ("x", _Rows), ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class _Project(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("precision", "out_precision", "cols", "n_out")] + [("n_rows", C.c_int64), ("x", _Rows), ("out", _Rows)] +
+                [(n, C.c_void_p) for n in ("x_scales", "weights", "weight_scales", "bias", "workspace")] + [("workspace_bytes", C.c_size_t)])
+
+
+class _NibbleRing(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")]
+
+
+class _NibbleAppend(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("precision", "heads_kv", "head_dim", "rotary_dim", "interleaved")] +
+                [("n_tokens", C.c_int64), ("max_tokens", C.c_int64), ("n_segments", C.c_int), ("n_streams", C.c_int), ("slots", C.c_int64),
+                 ("sinks", C.c_int), ("amplitude", C.c_double), ("eps", C.c_double), ("k", _Tokens), ("v", _Tokens), ("ring", _NibbleRing)] +
+                [(n, C.c_void_p) for n in ("frequencies", "k_weight", "offsets", "starts", "stream_ids")])
+
+
+class _NibbleAttend(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("precision", "heads_q", "heads_kv", "head_dim")] +
+                [("n_tokens", C.c_int64), ("max_tokens", C.c_int64), ("n_segments", C.c_int), ("n_streams", C.c_int), ("slots", C.c_int64),
+                 ("window", C.c_int), ("sinks", C.c_int), ("scale", C.c_float), ("q", _Tokens), ("out", _Tokens), ("ring", _NibbleRing)] +
+                [(n, C.c_void_p) for n in ("offsets", "starts", "stream_ids", "workspace")] + [("workspace_bytes", C.c_size_t)])
+
+
+class _NibbleValues(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("precision", "heads_kv", "head_dim", "n_streams")] +
+                [("slots", C.c_int64), ("ring", _NibbleRing), ("k", C.c_void_p), ("v", C.c_void_p)])
+
+
+_GATE_SIZES = [("precision", C.c_int), ("channels", C.c_int), ("n_tokens", C.c_int64), ("max_tokens", C.c_int64), ("n_segments", C.c_int), ("n_streams", C.c_int)]
+
+
+class _GateScan(C.Structure):
+    _fields_ = (_GATE_SIZES + [(n, _Rows) for n in ("x", "gates", "out")] +
+                [(n, C.c_void_p) for n in ("state_in", "state_out", "marks", "offsets", "stream_ids", "workspace")] + [("workspace_bytes", C.c_size_t)])
+
+
+class _GateScanBackward(C.Structure):
+    _fields_ = (_GATE_SIZES + [(n, _Rows) for n in ("x", "gates", "grad_out", "grad_x", "grad_gates")] +
+                [(n, C.c_void_p) for n in ("grad_end", "grad_state", "marks", "offsets", "stream_ids", "workspace")] + [("workspace_bytes", C.c_size_t)])
 
 
 def _direct(name, q, *args):
@@ -271,3 +321,343 @@ def _decay_attend(q, k, v, log_decay, state, state_out, scale, offsets, max_toke
         ws = _workspace(L.idf_decay_workspace, a, q.device)           # noqa: F841 (held until the work is enqueued)
         _check(L.idf_decay_attend(C.byref(a), _stream(q)))
     return out
+
+
+# ---- in few bits, and a recurrence per channel ----
+
+def _matrix(t, like, what, dtype=None):
+    """Rows as the library reads them, of like's device; copied where their values lie apart, or rows further than it takes."""
+    if t.dim() != 2 or t.dtype != (like.dtype if dtype is None else dtype) or t.device != like.device or not t.is_cuda:
+        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.contiguous() if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) > 1 << 25 else t
+
+
+def _as_rows(t):
+    return _Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _out_matrix(out, shape, dtype, device, what):
+    import torch
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(out.shape) != tuple(shape) or out.device != device or shape[1] > 1 and out.stride(1) != 1:
+        raise ValueError(f"{what}: {out.dtype} {tuple(out.shape)} with strides {out.stride()} on {out.device}, wanted {tuple(shape)} on {device}")
+    return out
+
+
+def quantize_rows(x, codes=None, scales=None):
+    """Rows of a matrix in 8 bits with a scale each: (codes, int8 [rows][columns rounded up to 16, zeros behind them], scales float32 [rows])
+    (idf_quantize_rows).  For tokens, and for the rows of a matrix of weights [outputs][columns]."""
+    r = _direct("quantize_rows", x, codes, scales)
+    return r if r is not None else _quantize_rows(x, codes, scales)
+
+
+def _quantize_rows(x, codes, scales):
+    import torch
+    _no_gradients(x=x)
+    x = _matrix(x, x, "x")
+    rows, cols = x.shape
+    padded = -(-cols // 16) * 16
+    for t, dtype, shape in ((codes, torch.int8, (rows, padded)), (scales, torch.float32, (rows,))):
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or t.device != x.device or not t.is_contiguous()):
+            raise ValueError(f"{t.dtype} {tuple(t.shape)} on {t.device}, wanted contiguous {dtype} {shape} on {x.device}")
+    codes = torch.empty(rows, padded, dtype=torch.int8, device=x.device) if codes is None else codes
+    scales = torch.empty(rows, dtype=torch.float32, device=x.device) if scales is None else scales
+    a = _Quantize(_precision(x), cols, rows, _as_rows(x), _ptr(codes), _ptr(scales))
+    with torch.cuda.device(x.device):
+        _check(load_library().idf_quantize_rows(C.byref(a), _stream(x)))
+    return codes, scales
+
+
+def project_rows(x, weight, weight_scales, bias=None, x_scales=None, dtype=None, out=None):
+    """x [rows][columns] times the transpose of a matrix of 8-bit weights [outputs][columns rounded up to 16] with a scale for each output, plus a bias
+    (idf_project_rows).  x in float32 or bfloat16 is taken to 8 bits with a scale for each row on the way; in int8 it comes with its
+    x_scales, and dtype or out says what the result is in (else what x is in)."""
+    import torch
+    to_f32 = {None: -1, torch.float32: 1, torch.bfloat16: 0}.get(dtype)
+    r = None if to_f32 is None else _direct("project_rows", x, weight, weight_scales, bias, x_scales, to_f32, out)
+    return r if r is not None else _project_rows(x, weight, weight_scales, bias, x_scales, dtype, out)
+
+
+def _project_rows(x, weight, weight_scales, bias, x_scales, dtype, out):
+    import torch
+    _no_gradients(x=x, weight_scales=weight_scales, bias=bias, x_scales=x_scales, out=out)
+    x = _matrix(x, x, "x")
+    coded = x.dtype == torch.int8
+    if coded != (x_scales is not None):
+        raise ValueError("x_scales go with x in int8")
+    if coded and dtype is None and out is None:
+        raise ValueError("x in int8 does not say what the result is in: dtype or out")
+    if coded and (x.data_ptr() % 16 or x.shape[0] > 1 and x.stride(0) % 16):
+        x = x.contiguous()
+        x = x.clone() if x.data_ptr() % 16 else x
+    rows, cols = x.shape
+    padded = -(-cols // 16) * 16
+    if weight.dim() != 2 or weight.shape[1] != padded:
+        raise ValueError(f"weight {tuple(weight.shape)}, wanted [outputs][{padded}] for rows of {cols}")
+    weight = _plain(weight, torch.int8, None, x.device, "weight")
+    weight = weight.clone() if weight.data_ptr() % 16 else weight
+    n = weight.shape[0]
+    weight_scales, bias = (_plain(t, torch.float32, (n,), x.device, what) for t, what in ((weight_scales, "weight_scales"), (bias, "bias")))
+    x_scales = _plain(x_scales, torch.float32, (rows,), x.device, "x_scales")
+    out = _out_matrix(out, (rows, n), x.dtype if dtype is None else dtype, x.device, "out")
+    if dtype is not None and out.dtype != dtype:
+        raise ValueError(f"out: {out.dtype}, wanted {dtype}")
+    a = _Project(2 if coded else _precision(x), _precision(out), cols, n, rows, _as_rows(x), _as_rows(out), _ptr(x_scales), _ptr(weight),
+                 _ptr(weight_scales), _ptr(bias), None, 0)
+    L = load_library()
+    with torch.cuda.device(x.device):
+        ws = _workspace(L.idf_project_workspace, a, x.device)         # noqa: F841 (held until the work is enqueued)
+        _check(L.idf_project_rows(C.byref(a), _stream(x)))
+    return out
+
+
+class NibbleRing(NamedTuple):
+    """A ring of keys and values in 4 bits (idf_nibble_ring): codes, uint8 [stream][head][slot][head size / 2], and powers of two,
+    uint8 [stream][head][slot][head size / 32]."""
+    k_codes: object
+    k_scales: object
+    v_codes: object
+    v_scales: object
+
+
+def nibble_ring(n_streams, slots, heads, dim, device="cuda:0"):
+    """An empty NibbleRing: 17 bytes for 32 values."""
+    import torch
+    if dim % 32 or not 32 <= dim <= 256:
+        raise ValueError(f"heads of {dim} values: multiples of 32 up to 256")
+    return NibbleRing(*(torch.zeros(n_streams, heads, slots, dim // by, dtype=torch.uint8, device=device) for by in (2, 32, 2, 32)))
+
+
+def _nibble_ring(ring, device=None):
+    """(the library's ring, streams, heads, slots, head size)"""
+    import torch
+    codes = ring[0]
+    for i, t in enumerate(ring):
+        if t.dtype != torch.uint8 or t.dim() != 4 or not t.is_contiguous() or not t.is_cuda or t.device != (codes.device if device is None else device) or \
+                t.shape[:3] != codes.shape[:3] or t.shape[3] * (16 if i % 2 else 1) != codes.shape[3]:
+            raise ValueError(f"ring: {t.dtype} {tuple(t.shape)} on {t.device}, wanted contiguous uint8 [streams][heads][slots][dim / 2] and [..][dim / 32]")
+    _no_gradients(**dict(zip(NibbleRing._fields, ring)))
+    streams, heads, slots, half = codes.shape
+    return _NibbleRing(*(t.data_ptr() for t in ring)), streams, heads, slots, 2 * half
+
+
+def _places(n, streams, starts, offsets, max_tokens, stream_ids, device):
+    """(offsets, longest segment, segments, starts, stream_ids)"""
+    import torch
+    count = next((t.numel() for t in (stream_ids, starts) if t is not None), streams)
+    offsets, longest, n_segments = _segments(n, offsets, max_tokens, count, device)
+    if offsets is not None and n_segments != count and (stream_ids is not None or starts is not None):
+        raise ValueError(f"{n_segments} segments by offsets, {count} by starts or stream_ids")
+    return (offsets, longest, n_segments, _plain(starts, torch.int64, (n_segments,), device, "starts"),
+            _plain(stream_ids, torch.int32, (n_segments,), device, "stream_ids"))
+
+
+def nibble_append(k, v, ring, starts=None, *, sinks=0, frequencies=None, layout="half", amplitude=1.0, k_weight=None, eps=1e-6, offsets=None,
+                 max_tokens=None, stream_ids=None):
+    """Segments' keys and values [token][head][value] into their streams' rings of 4-bit blocks, keys normalised (where there is a weight) and turned by
+    position (where there are frequencies) on the way, as norm_rotate does it to queries (idf_nibble_append).  Segments as in window_attend."""
+    if layout not in ("half", "interleaved"):
+        raise ValueError(f"layout {layout!r}")
+    r = _direct("nibble_append", k, v, *ring, starts, sinks, frequencies, int(layout == "interleaved"), amplitude, k_weight, eps, offsets, max_tokens, stream_ids)
+    if r is None:
+        _nibble_append(k, v, ring, starts, sinks, frequencies, layout, amplitude, k_weight, eps, offsets, max_tokens, stream_ids)
+
+
+def _nibble_append(k, v, ring, starts, sinks, frequencies, layout, amplitude, k_weight, eps, offsets, max_tokens, stream_ids):
+    import torch
+    _no_gradients(k=k, v=v, frequencies=frequencies, k_weight=k_weight)
+    k, v = _rows(k, k, "k", aligned=False), _rows(v, k, "v", aligned=False)
+    held, streams, heads, slots, dim = _nibble_ring(ring, k.device)
+    n = k.shape[0]
+    if k.shape != v.shape or tuple(k.shape[1:]) != (heads, dim):
+        raise ValueError(f"keys {tuple(k.shape)} and values {tuple(v.shape)} for a ring of {heads} heads of {dim}")
+    offsets, longest, n_segments, starts, stream_ids = _places(n, streams, starts, offsets, max_tokens, stream_ids, k.device)
+    frequencies = _plain(frequencies, torch.float64, None, k.device, "frequencies")
+    k_weight = _plain(k_weight, torch.float32, (dim,), k.device, "k_weight")
+    a = _NibbleAppend(_precision(k), heads, dim, 0 if frequencies is None else 2 * frequencies.numel(), int(layout == "interleaved"), n, longest, n_segments,
+                     streams, slots, sinks, amplitude, eps, _tokens(k), _tokens(v), held, _ptr(frequencies), _ptr(k_weight), _ptr(offsets), _ptr(starts),
+                     _ptr(stream_ids))
+    with torch.cuda.device(k.device):
+        _check(load_library().idf_nibble_append(C.byref(a), _stream(k)))
+
+
+def nibble_attend(q, ring, starts=None, *, window, sinks=0, scale=None, offsets=None, max_tokens=None, stream_ids=None, out=None):
+    """Attention of packed segments' queries over the last `window` tokens of their streams and the first `sinks` ones, their own among them, which have been
+    appended to the rings of 4-bit blocks before (idf_nibble_attend); a ring has room for a segment beside a window.  starts: int64, position of each
+    segment's first query; segments as in window_attend.  scale: 1 / sqrt(head size)."""
+    r = _direct("nibble_attend", q, *ring, starts, window, sinks, scale, offsets, max_tokens, stream_ids, out)
+    return r if r is not None else _nibble_attend(q, ring, starts, window, sinks, scale, offsets, max_tokens, stream_ids, out)
+
+
+def _nibble_attend(q, ring, starts, window, sinks, scale, offsets, max_tokens, stream_ids, out):
+    import torch
+    _no_gradients(q=q, out=out)
+    q = _rows(q, q, "q")
+    held, streams, heads, slots, dim = _nibble_ring(ring, q.device)
+    n, hq = q.shape[:2]
+    if q.shape[2] != dim:
+        raise ValueError(f"queries {tuple(q.shape)} for a ring of {heads} heads of {dim}")
+    offsets, longest, n_segments, starts, stream_ids = _places(n, streams, starts, offsets, max_tokens, stream_ids, q.device)
+    out = _out(out, q.shape, q, "out")
+    a = _NibbleAttend(_precision(q), hq, heads, dim, n, longest, n_segments, streams, slots, window, sinks, 1.0 / math.sqrt(dim) if scale is None else scale,
+                     _tokens(q), _tokens(out), held, _ptr(offsets), _ptr(starts), _ptr(stream_ids), None, 0)
+    L = load_library()
+    with torch.cuda.device(q.device):
+        ws = _workspace(L.idf_nibble_attend_workspace, a, q.device)    # noqa: F841 (held until the work is enqueued)
+        _check(L.idf_nibble_attend(C.byref(a), _stream(q)))
+    return out
+
+
+def nibble_values(ring, dtype=None):
+    """(keys, values) that a NibbleRing stands for, [stream][slot][head][value] in bfloat16 (or float32): rings as window_attend takes them
+    (idf_nibble_values)."""
+    import torch
+    if dtype not in (None, torch.float32, torch.bfloat16):
+        raise ValueError(f"values in {dtype}: float32 or bfloat16")
+    r = _direct("nibble_values", *ring, int(dtype == torch.float32))
+    return r if r is not None else _nibble_values(ring, torch.bfloat16 if dtype is None else dtype)
+
+
+def _nibble_values(ring, dtype):
+    import torch
+    held, streams, heads, slots, dim = _nibble_ring(ring)
+    k, v = (torch.empty(streams, slots, heads, dim, dtype=dtype, device=ring[0].device) for _ in range(2))
+    a = _NibbleValues(_precision(k), heads, dim, streams, slots, held, _ptr(k), _ptr(v))
+    with torch.cuda.device(k.device):
+        _check(load_library().idf_nibble_values(C.byref(a), _stream(k)))
+    return k, v
+
+
+def _gate_sizes(x, gates, states, offsets, max_tokens, n_segments, stream_ids, n_streams=None):
+    """What the structures of the recurrence begin with, and offsets and stream_ids."""
+    import torch
+    n, channels = x.shape
+    if gates.shape != x.shape:
+        raise ValueError(f"x {tuple(x.shape)} and gates {tuple(gates.shape)}")
+    for s in states:
+        if s is None:
+            continue
+        if s.dim() != 2 or s.dtype != torch.float32 or s.device != x.device or not s.is_contiguous() or s.shape[1] != channels or n_streams not in (None, s.shape[0]):
+            raise ValueError(f"state: {s.dtype} {tuple(s.shape)} on {s.device}, wanted contiguous float32 [streams][{channels}]")
+        n_streams = s.shape[0]
+    count = next((c for c in (None if stream_ids is None else stream_ids.numel(), n_segments, n_streams) if c is not None), 1)
+    offsets, longest, n_segments_ = _segments(n, offsets, max_tokens, count, x.device)
+    if offsets is not None and n_segments_ != count and (stream_ids is not None or n_segments is not None):
+        raise ValueError(f"{n_segments_} segments by offsets, {count} by stream_ids or n_segments")
+    stream_ids = _plain(stream_ids, torch.int32, (n_segments_,), x.device, "stream_ids")
+    return (_precision(x), channels, n, longest, n_segments_, n_segments_ if n_streams is None else n_streams), offsets, stream_ids
+
+
+def _marks_floats(sizes, offsets):
+    a, nb = _GateScan(*sizes), C.c_size_t()
+    a.offsets = _ptr(offsets)
+    _check(load_library().idf_gate_scan_marks(C.byref(a), C.byref(nb)))
+    return nb.value // 4
+
+
+def gate_scan(x, gates, state=None, state_out=None, *, offsets=None, max_tokens=None, n_segments=None, stream_ids=None, out=None, marks=None):
+    """h = a h + (1 - a) x per channel along the tokens of packed segments, a = sigmoid(gates): x, gates and the result [token][channel], from `state` (float32
+    [stream][channel], None: zeros) into `state_out` (None: not wanted; may be `state`) (idf_gate_scan).  Segments as in decay_attend.
+    marks True: returns (out, marks), the latter for gate_scan_backward.  gate_scan_recorded is the form that torch's gradients go through."""
+    r = _direct("gate_scan", x, gates, state, state_out, offsets, max_tokens, n_segments, stream_ids, out, marks)
+    return r if r is not None else _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stream_ids, out, marks)
+
+
+def _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stream_ids, out, marks):
+    import torch
+    _no_gradients(x=x, gates=gates, state=state, state_out=state_out, out=out)
+    x, gates = _matrix(x, x, "x"), _matrix(gates, x, "gates")
+    sizes, offsets, stream_ids = _gate_sizes(x, gates, (state, state_out), offsets, max_tokens, n_segments, stream_ids)
+    out = _out_matrix(out, x.shape, x.dtype, x.device, "out")
+    if out.dtype != x.dtype:
+        raise ValueError(f"out: {out.dtype}, wanted {x.dtype}")
+    given = marks
+    if marks is not None:
+        marks = torch.empty(_marks_floats(sizes, offsets), device=x.device) if marks is True else _plain(marks, torch.float32, (_marks_floats(sizes, offsets),), x.device, "marks")
+        if given is not True and marks is not given:
+            raise ValueError("marks have to be contiguous")
+    a = _GateScan(*sizes, _as_rows(x), _as_rows(gates), _as_rows(out), _ptr(state), _ptr(state_out), _ptr(marks), _ptr(offsets), _ptr(stream_ids), None, 0)
+    L = load_library()
+    with torch.cuda.device(x.device):
+        ws = _workspace(L.idf_gate_scan_workspace, a, x.device)       # noqa: F841 (held until the work is enqueued)
+        _check(L.idf_gate_scan(C.byref(a), _stream(x)))
+    return (out, marks) if given is True else out
+
+
+def gate_scan_backward(x, gates, marks, grad_out=None, grad_end=None, *, offsets=None, max_tokens=None, n_segments=None, stream_ids=None, n_streams=None):
+    """Gradients of gate_scan's x, gates and state from those of its result and of state_out (None: zeros), with the marks that the call left
+    (idf_gate_scan_backward).  n_streams where grad_end does not say how many there are."""
+    r = _direct("gate_scan_backward", x, gates, marks, grad_out, grad_end, offsets, max_tokens, n_segments, stream_ids, n_streams)
+    return r if r is not None else _gate_scan_backward(x, gates, marks, grad_out, grad_end, offsets, max_tokens, n_segments, stream_ids, n_streams)
+
+
+def _gate_scan_backward(x, gates, marks, grad_out, grad_end, offsets, max_tokens, n_segments, stream_ids, n_streams):
+    import torch
+    _no_gradients(x=x, gates=gates, grad_out=grad_out, grad_end=grad_end)
+    x, gates = _matrix(x, x, "x"), _matrix(gates, x, "gates")
+    sizes, offsets, stream_ids = _gate_sizes(x, gates, (grad_end,), offsets, max_tokens, n_segments, stream_ids, n_streams)
+    if grad_out is not None:
+        grad_out = _matrix(grad_out, x, "grad_out")
+        if grad_out.shape != x.shape:
+            raise ValueError(f"grad_out {tuple(grad_out.shape)} of x {tuple(x.shape)}")
+    marks = _plain(marks, torch.float32, (_marks_floats(sizes, offsets),), x.device, "marks")
+    grads = [torch.zeros(x.shape, dtype=x.dtype, device=x.device) for _ in range(2)]
+    grad_state = torch.empty(sizes[5], x.shape[1], device=x.device)
+    a = _GateScanBackward(*sizes, _as_rows(x), _as_rows(gates), _Rows(None, 0) if grad_out is None else _as_rows(grad_out), *(_as_rows(t) for t in grads),
+                          _ptr(grad_end), _ptr(grad_state), _ptr(marks), _ptr(offsets), _ptr(stream_ids), None, 0)
+    L = load_library()
+    with torch.cuda.device(x.device):
+        ws = _workspace(L.idf_gate_scan_backward_workspace, a, x.device)          # noqa: F841 (held until the work is enqueued)
+        _check(L.idf_gate_scan_backward(C.byref(a), _stream(x)))
+    return *grads, grad_state
+
+
+_recorded = None             # the autograd function, made with the first call
+
+
+def _make_recorded():
+    import torch
+    from torch.autograd.function import once_differentiable
+
+    class GateScan(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, gates, state, offsets, max_tokens, n_segments):
+            streams = state.shape[0] if state is not None else n_segments if n_segments is not None else 1 if offsets is None else offsets.numel() - 1
+            end = torch.empty(streams, x.shape[1], device=x.device)
+            out, marks = gate_scan(x, gates, state, end, offsets=offsets, max_tokens=max_tokens, n_segments=n_segments, marks=True)
+            ctx.save_for_backward(x, gates, marks, offsets)
+            ctx.sizes = max_tokens, n_segments, streams
+            ctx.set_materialize_grads(False)
+            return out, end
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, grad_out, grad_end):
+            if grad_out is None and grad_end is None:
+                return (None,) * 6
+            x, gates, marks, offsets = ctx.saved_tensors
+            max_tokens, n_segments, streams = ctx.sizes
+            _no_capture(x)
+            dx, dg, ds = gate_scan_backward(x, gates, marks, grad_out, None if grad_end is None else grad_end.contiguous(), offsets=offsets,
+                                            max_tokens=max_tokens, n_segments=n_segments, n_streams=streams)
+            need = ctx.needs_input_grad
+            return dx if need[0] else None, dg if need[1] else None, ds if need[2] else None, None, None, None
+    return GateScan
+
+
+def _no_capture(x):
+    import torch
+    if x.is_cuda and torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("gate_scan_recorded while a stream is captured: torch ends the process there where leaves have recorded outside; "
+                           "gate_scan with marks and gate_scan_backward can be captured")
+
+
+def gate_scan_recorded(x, gates, state=None, *, offsets=None, max_tokens=None, n_segments=None):
+    """gate_scan for training: (out, states behind the segments), both recorded by torch's gradients where x, gates or state require them, once (gradients
+    of gradients are refused).  Segment s is of stream s.  Not for a stream that is being captured into a graph."""
+    global _recorded
+    if _recorded is None:
+        _recorded = _make_recorded()
+    _no_capture(x)
+    return _recorded.apply(x, gates, state, offsets, max_tokens, n_segments)
