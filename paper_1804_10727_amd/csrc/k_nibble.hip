@@ -16,7 +16,7 @@ namespace idf {
 namespace {
 
 constexpr int kBits = 32;                          // values of a block
-constexpr int kStepRows = 16;                      // query rows of a segment and key/value head that the step kernel takes
+constexpr int kStepRows = 32;                      // query rows of a segment and key/value head that the step kernel takes, in one or two tiles of 16
 constexpr int kTileRows = 128;                     // query rows of a workgroup of the tile kernel
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
@@ -317,33 +317,36 @@ __device__ __forceinline__ void exact_row(const idf_nibble_attend_args &a, const
 
 // -- few rows on a long axis: single tokens, short segments --
 
-// A workgroup takes the at most 16 query rows of one segment and key/value head and a part of the keys; its four waves take 32 of them at a time, in turn, each
-// with a softmax of its own, and are joined at the end.  Codes of keys go from memory into the layout of the matrix instruction, a lane having a quarter of a
+// A workgroup takes the at most 16 RT query rows of one segment and key/value head and a part of the keys; its waves take 32 of them at a time, in turn, each
+// with a softmax of its own, and are joined at the end.  Eight waves where there are workgroups for half the machine only (64 x 16 tokens in float32 on 1000 keys of
+// 4 x 64: 20.7 us by four, 17.6 by eight), else four with two rounds each on their way (64 streams on 4096 keys of 8 x 128: one round 61.6, two 56.5; reading alone, with
+// nothing done, takes 52, 5.5 TB/s).  What had cost most were choices on the loaded values next to the loads, which wait for them (72 -> 62).  Codes of keys go from memory into the layout of the matrix instruction, a lane having a quarter of a
 // row, whose place along the summed axis is free; those of values through a piece of LDS that is the wave's own, to be read along the keys.
-template <int DP> struct StepShape {
+template <int PREC, int DP, int RT, int WAVES> struct StepShape {
     static constexpr int KEYS = 32, NT = 2;
+    static constexpr int AHEAD = WAVES == 4 && DP <= 128 && !(PREC == IDF_PREC_F32 && DP == 128 && RT == 2) ? 2 : 1;      // rounds that a wave has on their way
     static constexpr int STRIDE = DP + 16;                                    // of a row of values in LDS: rows that are read together begin in banks of their own
     static constexpr int BLOCKS = DP / kBits;                                 // of a row
     static constexpr int LOADS = (KEYS * BLOCKS + 63) / 64;                   // of 16 bytes of values per lane
     static constexpr int K_WORDS = DP / 32;                                   // words of eight codes of a key per lane
     static constexpr int K_POWERS = DP == 256 ? 2 : 1;
-    static constexpr int WAVE_FLOATS = 16 * DP > KEYS * STRIDE / 2 ? 16 * DP : KEYS * STRIDE / 2;
+    static constexpr int WAVE_FLOATS = 16 * RT * DP > KEYS * STRIDE / 2 ? 16 * RT * DP : KEYS * STRIDE / 2;
 };
 
-template <int PREC, int DP>
-__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_nibble_step(idf_nibble_attend_args a, int splits)
+template <int PREC, int DP, int RT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || DP <= 128 ? 2 : 1) k_nibble_step(idf_nibble_attend_args a, int splits)
 {
     using M = Mfma<IDF_PREC_BF16>;
     using T = typename Elem<PREC>::type;
-    using S = StepShape<DP>;
+    using S = StepShape<PREC, DP, RT, WAVES>;
     constexpr int NT = S::NT, KS = DP / 32, DT = DP / 16, N = Parts<PREC>::N;
-    __shared__ __align__(16) float lds[4 * S::WAVE_FLOATS];
-    __shared__ float stats[2][4][16];
+    extern __shared__ __align__(16) float lds[];
+    __shared__ float stats[2][WAVES][16 * RT];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
     const int split = blockIdx.x, kv = blockIdx.y, group = a.heads_q / a.heads_kv;
     const Segment g = segment_of(a, blockIdx.z, a.starts);
     if (g.len == 0) return;
-    const int rows = min(g.len * group, kStepRows);
+    const int rows = min(g.len * group, 16 * RT);
     const Keys keys(a, g.start, g.start + g.len - 1);
     const Held4<const uint8_t> kh(a.ring.k_codes, a.ring.k_scales, a.slots, a.heads_kv, a.head_dim, g.ring, kv), vh(a.ring.v_codes, a.ring.v_scales, a.slots, a.heads_kv, a.head_dim, g.ring, kv);
     const Partial part = partial_of(a, splits);
@@ -352,73 +355,94 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_nibble_step(idf_nibb
     // this split's entries, whole tiles of them; the waves take them in turn
     const int tiles = (keys.n + S::KEYS - 1) / S::KEYS, per = (tiles + splits - 1) / splits;
     const int t0 = split * per, t1 = min(tiles, t0 + per);
-    const int my_t = col / group;                                             // the query row of this lane
-    const int my_h = kv * group + col - my_t * group;
-    const int64_t p = g.start + min(my_t, g.len - 1);
-    const int hi = (int)(p - keys.shift);
-    const int lo = (int)max(p - a.window - keys.shift, (int64_t)-1);
     const float scale = a.scale * kLog2e;
+    int hi[RT], lo[RT];                                                       // what this lane's query rows see
 
     // of the summed axis a lane has: 64 values a head, 16 grp + 8 s ..; 128, 32 grp + 8 s ..; 256, 32 (grp + 4 (s / 4)) + 8 (s % 4) ..
     auto dim_of = [&](int s) IDF_INLINE { return DP == 64 ? 16 * grp + 8 * s : DP == 128 ? 32 * grp + 8 * s : 32 * (grp + 4 * (s / 4)) + 8 * (s % 4); };
-    bf16x8 q[KS][N];
-    {
-        const T *src = (const T *)a.q.base + (g.begin + my_t) * a.q.token_stride + my_h * a.q.head_stride;
+    bf16x8 q[RT][KS][N];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) load_query<PREC>(src + dim_of(s), col < rows ? a.head_dim - dim_of(s) : 0, q[s]);
+    for (int r = 0; r < RT; ++r) {
+        const int row = 16 * r + col, t = min(row, rows - 1) / group, h = kv * group + min(row, rows - 1) - t * group;
+        const int64_t p = g.start + t;
+        hi[r] = (int)(p - keys.shift);
+        lo[r] = (int)max(p - a.window - keys.shift, (int64_t)-1);
+        const T *src = (const T *)a.q.base + (g.begin + t) * a.q.token_stride + h * a.q.head_stride;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) load_query<PREC>(src + dim_of(s), row < rows ? a.head_dim - dim_of(s) : 0, q[r][s]);
     }
 
     __bf16 *v_lds = (__bf16 *)(lds + wave * S::WAVE_FLOATS);
-    uint32_t kc[NT][S::K_WORDS], kp[NT][S::K_POWERS], vp[S::LOADS];
-    i32x4 vc[S::LOADS];
-    auto load = [&](int tile) IDF_INLINE {
-        const int i0 = tile * S::KEYS;
+    struct Round { uint32_t kc[NT][S::K_WORDS], kp[NT][S::K_POWERS], vp[S::LOADS]; i32x4 vc[S::LOADS]; };
+    // Places behind a row's end are those of its first block again: there queries are zeros, and outputs nobody's.  Rounds that lie in one piece are read
+    // from one address on, the others (first tokens, the ring's end, the list's) look for the place of each entry.
+    uint32_t k_at[S::K_POWERS], k_power_at[S::K_POWERS];
+#pragma unroll
+    for (int x = 0; x < S::K_POWERS; ++x) {
+        const int d = dim_of(4 * x), there = d < a.head_dim ? d : 0;
+        k_at[x] = there / 2;
+        k_power_at[x] = there / kBits;
+    }
+    auto load_from = [&](Round &r, const uint8_t *kc, const uint8_t *kp, const uint8_t *vc, const uint8_t *vp, auto slot_of) IDF_INLINE {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const uint32_t slot = keys.slot(min(i0 + 16 * t + col, keys.n - 1));
+            const uint32_t slot = slot_of(16 * t + col);
 #pragma unroll
             for (int x = 0; x < S::K_POWERS; ++x) {
-                const int d = dim_of(4 * x);
-                const bool there = d < a.head_dim;
-                const uint32_t at = slot * row_codes + (there ? d / 2 : 0);
-                kp[t][x] = kh.scales[slot * row_scales + (there ? d / kBits : 0)];
+                r.kp[t][x] = kp[slot * row_scales + k_power_at[x]];
                 if constexpr (DP == 64) {
-                    const uint2 w = *(const uint2 *)(kh.codes + at);
-                    kc[t][0] = there ? w.x : 0u; kc[t][1] = there ? w.y : 0u;
+                    const uint2 w = *(const uint2 *)(kc + (slot * row_codes + k_at[x]));
+                    r.kc[t][0] = w.x; r.kc[t][1] = w.y;
                 } else {
-                    const i32x4 w = *(const i32x4 *)(kh.codes + at);
+                    const i32x4 w = *(const i32x4 *)(kc + (slot * row_codes + k_at[x]));
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) kc[t][4 * x + s] = there ? (uint32_t)w[s] : 0u;
+                    for (int s = 0; s < 4; ++s) r.kc[t][4 * x + s] = (uint32_t)w[s];
                 }
-                if (!there) kp[t][x] = 127u;
             }
         }
 #pragma unroll
         for (int j = 0; j < S::LOADS; ++j) {
-            const int piece = j * 64 + lane, r = piece / S::BLOCKS, b = piece - r * S::BLOCKS;
-            const bool there = i0 + r < keys.n && b * kBits < a.head_dim;
-            const uint32_t slot = keys.slot(min(i0 + r, keys.n - 1));
-            vc[j] = i32x4{0, 0, 0, 0};
-            vp[j] = 127u;
-            if (there) { vc[j] = *(const i32x4 *)(vh.codes + (slot * row_codes + b * 16)); vp[j] = vh.scales[slot * row_scales + b]; }
+            const int piece = j * 64 + lane, row = min(piece / S::BLOCKS, S::KEYS - 1), b = piece % S::BLOCKS;
+            const uint32_t slot = slot_of(row), block = b * kBits < a.head_dim ? b : 0;
+            r.vp[j] = vp[slot * row_scales + block];
+            r.vc[j] = *(const i32x4 *)(vc + (slot * row_codes + block * 16));
+        }
+    };
+    auto load = [&](int tile, Round &r) IDF_INLINE {
+        const int i0 = tile * S::KEYS;
+        uint32_t at = keys.slot0 + (uint32_t)(i0 - keys.n_first);
+        if (at >= keys.period) at -= keys.period;
+        if (i0 >= keys.n_first && i0 + S::KEYS <= keys.n && at + S::KEYS <= keys.period) {
+            const int64_t slot = (int64_t)keys.sinks + at;
+            load_from(r, kh.codes + slot * row_codes, kh.scales + slot * row_scales, vh.codes + slot * row_codes, vh.scales + slot * row_scales, [](int e) { return (uint32_t)e; });
+        } else {
+            load_from(r, kh.codes, kh.scales, vh.codes, vh.scales, [&](int e) { return keys.slot(min(i0 + e, keys.n - 1)); });
         }
     };
 
-    f32x4 o[DT];
+    f32x4 o[RT][DT];
+    float m[RT], l[RT];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -__FLT_MAX__, l = 0.f;
-    if (t0 + wave < t1) load(t0 + wave);
-    for (int tile = t0 + wave; tile < t1; tile += 4) {
-        f32x4 st[NT];
+    for (int r = 0; r < RT; ++r) {
+        m[r] = -__FLT_MAX__;
+        l[r] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[r][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    auto work = [&](int tile, Round &x_) IDF_INLINE {
+        const auto &kc = x_.kc; const auto &kp = x_.kp; const auto &vp = x_.vp; const auto &vc = x_.vc;
+        f32x4 st[RT][NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            st[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int r = 0; r < RT; ++r) st[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 const bf16x8 k = values8(kc[t][s], power_of(kp[t][s / 4]));
 #pragma unroll
-                for (int x = N - 1; x >= 0; --x) st[t] = M::mma16(k, q[s][x], st[t]);
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int x = N - 1; x >= 0; --x) st[r][t] = M::mma16(k, q[r][s][x], st[r][t]);
             }
         }
         __builtin_amdgcn_wave_barrier();                                      // (LDS serves a wave in order: only the compiler has to keep it)
@@ -431,58 +455,74 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_nibble_step(idf_nibb
                 for (int w = 0; w < 4; ++w) *(bf16x8 *)(v_lds + r * S::STRIDE + b * kBits + 8 * w) = values8((uint32_t)vc[j][w], power);
         }
         __builtin_amdgcn_wave_barrier();
-        if (tile + 4 < t1) load(tile + 4);
+        if (tile + WAVES * S::AHEAD < t1) load(tile + WAVES * S::AHEAD, x_);
 
-        float w[NT * 4], top = m;
+        bf16x8 pf[RT][N];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int r = 0; r < RT; ++r) {
+            float w[NT * 4], top = m[r];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = tile * S::KEYS + 16 * t + 4 * grp + e;
-                const bool seen = i <= hi && (i > lo || i < keys.n_first);
-                w[4 * t + e] = seen ? st[t][e] * scale : -__builtin_inff();
-                top = fmaxf(top, w[4 * t + e]);
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = tile * S::KEYS + 16 * t + 4 * grp + e;
+                    const bool seen = i <= hi[r] && (i > lo[r] || i < keys.n_first);
+                    w[4 * t + e] = seen ? st[r][t][e] * scale : -__builtin_inff();
+                    top = fmaxf(top, w[4 * t + e]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (__ballot(top > m[r])) {
+                const float fade = __builtin_amdgcn_exp2f(m[r] - top);
+                l[r] *= fade;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[r][d] *= fade;
+                m[r] = top;
             }
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (__ballot(top > m)) {
-            const float fade = __builtin_amdgcn_exp2f(m - top);
-            l *= fade;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] *= fade;
-            m = top;
+            for (int e = 0; e < NT * 4; ++e) { w[e] = __builtin_amdgcn_exp2f(w[e] - m[r]); l[r] += w[e]; }
+            in_parts(w, pf[r]);
         }
-#pragma unroll
-        for (int e = 0; e < NT * 4; ++e) { w[e] = __builtin_amdgcn_exp2f(w[e] - m); l += w[e]; }
-        bf16x8 pf[N];
-        in_parts(w, pf);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             const bf16x8 v = read_column(v_lds, S::STRIDE, 16 * d, 4 * grp, 16 + 4 * grp);
 #pragma unroll
-            for (int x = N - 1; x >= 0; --x) o[d] = M::mma16(v, pf[x], o[d]);
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int x = N - 1; x >= 0; --x) o[r][d] = M::mma16(v, pf[r][x], o[r][d]);
         }
-    }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    };
+    Round rounds[S::AHEAD];
+#pragma unroll
+    for (int x = 0; x < S::AHEAD; ++x)
+        if (t0 + wave + WAVES * x < t1) load(t0 + wave + WAVES * x, rounds[x]);
+    for (int tile = t0 + wave; tile < t1; tile += WAVES * S::AHEAD)
+#pragma unroll
+        for (int x = 0; x < S::AHEAD; ++x)
+            if (tile + WAVES * x < t1) work(tile + WAVES * x, rounds[x]);
 
     // the waves' rows joined: [wave][row][value]
     __builtin_amdgcn_wave_barrier();
     float *mine = lds + wave * S::WAVE_FLOATS;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *(f32x4 *)(mine + col * DP + 16 * d + 4 * grp) = o[d];
-    if (grp == 0) { stats[0][wave][col] = m; stats[1][wave][col] = l; }
+    for (int r = 0; r < RT; ++r) {
+        l[r] += __shfl_xor(l[r], 16);
+        l[r] += __shfl_xor(l[r], 32);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) *(f32x4 *)(mine + (16 * r + col) * DP + 16 * d + 4 * grp) = o[r][d];
+        if (grp == 0) { stats[0][wave][16 * r + col] = m[r]; stats[1][wave][16 * r + col] = l[r]; }
+    }
     __syncthreads();
     bool bad = false;
     constexpr int V4 = DP / 4;
-    for (int x = threadIdx.x; x < rows * V4; x += 256) {
+    for (int x = threadIdx.x; x < rows * V4; x += 64 * WAVES) {
         const int r = x / V4, c = (x - r * V4) * 4;
         float top = -__FLT_MAX__, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, stats[0][w][r]);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, stats[0][w][r]);
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float fade = __builtin_amdgcn_exp2f(stats[0][w][r] - top);
             sum += fade * stats[1][w][r];
             v += fade * *(const f32x4 *)(lds + w * S::WAVE_FLOATS + r * DP + c);
@@ -504,7 +544,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_nibble_step(idf_nibb
         }
     }
     if ((N > 1 || g.len > 1) && __syncthreads_or(bad))                        // (a single token sees every key of its list; what is infinite is no number in parts)
-        for (int r = wave; r < rows; r += 4) {
+        for (int r = wave; r < rows; r += WAVES) {
             const int t = r / group;
             exact_row<PREC>(a, g, keys, kv, kv * group + r - t * group, t, t0 * S::KEYS, min(t1 * S::KEYS, keys.n), part, split);
         }
@@ -708,13 +748,14 @@ __global__ void __launch_bounds__(256, PREC != IDF_PREC_BF16 || DP > 128 ? 1 : D
 // How a call of the attention is cut: which kernel, and into how many parts the keys go.
 struct Plan {
     bool step;
-    int tiles, splits;
+    int64_t rows;              // of the longest segment and a key/value head
+    int tiles, splits, waves;
 };
 // Into how many parts a list of keys goes: the number with the least estimated time, as in the window's attention.
 int splits_of(const idf_nibble_attend_args &a, bool step, int64_t pairs, int64_t keys)
 {
     const int64_t round = step ? 128 : 64, rounds = (keys + round - 1) / round, held = 512;
-    const double each = step ? 1.4 : 1.0 + 0.006 * a.head_dim;
+    const double each = step ? 1.25 : 1.0 + 0.006 * a.head_dim;
     const double rows = (double)std::min<int64_t>(a.n_tokens, a.n_segments * longest(a)) * a.heads_q;
     int best = 1;
     double least = 0.0;
@@ -730,19 +771,36 @@ int splits_of(const idf_nibble_attend_args &a, bool step, int64_t pairs, int64_t
 Plan plan_of(const idf_nibble_attend_args &a)
 {
     Plan p;
-    const int64_t rows = longest(a) * (a.heads_q / a.heads_kv);
-    p.step = rows <= kStepRows;
-    p.tiles = p.step ? 1 : (int)((rows + kTileRows - 1) / kTileRows);
+    p.rows = longest(a) * (a.heads_q / a.heads_kv);
+    p.step = p.rows <= (a.precision == IDF_PREC_F32 && a.head_dim > 128 ? kStepRows / 2 : kStepRows);
+    p.tiles = p.step ? 1 : (int)((p.rows + kTileRows - 1) / kTileRows);
     const int64_t pairs = (int64_t)a.n_segments * a.heads_kv * p.tiles;
     const int64_t own = p.step ? longest(a) : std::min<int64_t>(longest(a), kTileRows / (a.heads_q / a.heads_kv) + 1);
     p.splits = splits_of(a, p.step, pairs, std::min<int64_t>(a.window + own, a.slots) + a.sinks);
+    p.waves = pairs * p.splits <= 256 && a.head_dim <= 128 ? 8 : 4;
     return p;
+}
+
+template <int PREC, int DP, int RT, int WAVES>
+hipError_t step(const idf_nibble_attend_args &a, const Plan &p, const LaunchCtx &lc)
+{
+    constexpr int bytes = WAVES * StepShape<PREC, DP, RT, WAVES>::WAVE_FLOATS * (int)sizeof(float);
+    if (bytes > 60000)
+        if (const hipError_t e = allow_lds<bytes>(Kernel<k_nibble_step<PREC, DP, RT, WAVES>>{})) return e;
+    return launch(k_nibble_step<PREC, DP, RT, WAVES>, dim3(p.splits, a.heads_kv, a.n_segments), dim3(64 * WAVES), bytes, lc, a, p.splits);
 }
 
 template <int PREC, int DP>
 hipError_t attend(const idf_nibble_attend_args &a, const Plan &p, const LaunchCtx &lc)
 {
-    if (p.step) return launch(k_nibble_step<PREC, DP>, dim3(p.splits, a.heads_kv, a.n_segments), dim3(256), 0, lc, a, p.splits);
+    if (p.step) {
+        // (what eight waves, or 32 rows, leave of the registers has to hold a round)
+        if constexpr (DP <= 128)
+            if (p.waves == 8) return p.rows <= 16 ? step<PREC, DP, 1, 8>(a, p, lc) : step<PREC, DP, 2, 8>(a, p, lc);
+        if constexpr (DP <= 128 || PREC == IDF_PREC_BF16)
+            if (p.rows > 16) return step<PREC, DP, 2, 4>(a, p, lc);
+        return step<PREC, DP, 1, 4>(a, p, lc);
+    }
     constexpr int bytes = TileShape<DP>::LDS_BYTES;
     if (bytes > 65536)
         if (const hipError_t e = allow_lds<bytes>(Kernel<k_nibble_tile<PREC, DP>>{})) return e;
