@@ -169,7 +169,8 @@ def load_tokens():
         L = load_library()
         from . import build as _build
         native = _load_extension("_tokens", _build.tokens_path(), _build.build_tokens)
-        native.bind(*(C.cast(getattr(L, n), C.c_void_p).value for n in TOKEN_OPS))
+        # (the runtime's own function through the library that is bound to it)
+        native.bind(*(C.cast(getattr(L, n), C.c_void_p).value for n in TOKEN_OPS + ("hipStreamIsCapturing",)))
         _token_ops = native
     return _token_ops
 

@@ -1,13 +1,13 @@
 // A gated recurrence per channel and its gradients (idf_gate_scan, idf_gate_scan_backward).
 //
-//   h_t = a_t h_{t-1} + b_t x_t,  a = sigmoid(g), b = 1 - a = sigmoid(-g), both formed from exp(-g) so that the small one of them is as exact as the large one.
-// Where more than half is kept a step is taken as h += b (x - h): a itself, rounded to a number near one, would be off in the same direction again and
-// again where gates stay the same.  A part of a segment takes a state to (1 - c) h + n, with n what the part gives from nothing, and c and 1 - c = prod(a) both
-// carried (c_t = c + b (1 - c), exact where it is small; the product where that is).
+//   h_t = a_t h_{t-1} + b_t x_t,  a = sigmoid(g), b = 1 - a.  Of a and b the smaller one, e / (1 + e) with e = exp(-|g|), is formed, and a step taken as
+// h + b (x - h) or x + a (h - x): the larger one, rounded to a number near one, would be off in the same direction again and again where gates stay the
+// same.  A part of a segment takes a state h to k h + n, with n what the part gives from nothing and k the product of its a, formed in the same way.
 //   A lane has V neighbouring channels, a wave 64 V of them, and goes along the tokens 16 at a time with the next 16 on their way.  Segments are cut
 // into parts along time where channels and segments are too few for the machine: their summaries first, then every part from the state that
 // those before it give (x and gates are read twice then).  States within a segment before every 16th token are what the backward pass
 // starts from: it forms the 16 states of a block anew, in registers, and goes back through them.
+//   What infinite values, gates that are no numbers and gates beyond +-87 ask for is done where a block has any: once more for that block.
 #include <algorithm>
 
 #include "idf.h"
@@ -21,33 +21,60 @@ constexpr int kBlock = 16;                         // tokens that a wave has in 
 constexpr int kMostGroups = 64;                    // groups of parts of a segment: every part goes through the summaries of those before it
 constexpr float kGateMost = 87.f;
 
-struct Gate { float keep, take; };
+// The smaller one of what a gate keeps and takes in, with the gate's sign: above zero it is what is taken in.
+struct Gate {
+    float s;
+    __device__ __forceinline__ bool open() const { return __builtin_bit_cast(int, s) >= 0; }
+    __device__ __forceinline__ float big() const { return 1.f - __builtin_fabsf(s); }
+    __device__ __forceinline__ float take() const { return open() ? s : big(); }
+};
 template <int PREC> __device__ __forceinline__ Gate gate_of(float g)
 {
     constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.9259629911e-8f, kLn2 = 0.6931471805599453f;
-    g = g > kGateMost ? kGateMost : g;             // (comparisons, so that what is not a number stays)
-    g = g < -kGateMost ? -kGateMost : g;
-    const float p = g * -kLog2e;
+    const float size = __builtin_fabsf(g), p = size * -kLog2e;
     float t = __builtin_amdgcn_exp2f(p);
     // the rounding of the product counts by its size: 5e-6 of t where |g| is 87
-    if (PREC == IDF_PREC_F32) t = __builtin_fmaf(t, kLn2 * (__builtin_fmaf(g, -kLog2e, -p) - g * kLog2eLow), t);
+    if (PREC == IDF_PREC_F32) t = __builtin_fmaf(t, kLn2 * (__builtin_fmaf(size, -kLog2e, -p) - size * kLog2eLow), t);
     const float r = __builtin_amdgcn_rcpf(1.f + t);
-    return {r, t * r};
+    return {__builtin_copysignf(t * r, g)};
 }
-
 __device__ __forceinline__ bool finite(float v) { return __builtin_fabsf(v) < __builtin_inff(); }
 
-// What a part makes of the state before it.
-struct Summary { float keep, gone, made; };        // prod(a); 1 - prod(a); the state from nothing
+// The next state, and what flows to the token before it (l: what comes to this one).
+__device__ __forceinline__ float step_of(const Gate &w, float x, float h) { return __builtin_fmaf(w.s, x - h, w.open() ? h : x); }
+__device__ __forceinline__ float kept_of(const Gate &w, float l) { return __builtin_fmaf(-w.s, l, w.open() ? l : 0.f); }
+
+// The same from the definition, for what the above would make no number: differences of infinite values, gates held to +-87.
+template <int PREC> struct Slow {
+    float keep, take;
+    Gate w;
+    __device__ __forceinline__ Slow(float g)
+    {
+        g = g > kGateMost ? kGateMost : g;         // (comparisons, so that what is not a number stays)
+        g = g < -kGateMost ? -kGateMost : g;
+        w = gate_of<PREC>(g);
+        keep = w.open() ? w.big() : __builtin_fabsf(w.s);
+        take = w.take();
+    }
+    __device__ __forceinline__ float step(float x, float h) const
+    {
+        const float next = step_of(w, x, h);
+        return finite(next) ? next : keep * h + take * x;
+    }
+    __device__ __forceinline__ float kept(float l) const
+    {
+        const float next = kept_of(w, l);
+        return finite(next) ? next : keep * l;
+    }
+};
+
+// What a part makes of the state before it: keep * h + made.
+struct Summary { float keep, made; };
 __device__ __forceinline__ float through(const Summary &s, float h)
 {
-    if (!finite(h)) return (s.keep == 0.f ? h : s.keep * h) + s.made;          // (no product of gates is nothing, but 32 bits may say so)
-    return (s.keep < 0.5f ? s.keep * h : __builtin_fmaf(-s.gone, h, h)) + s.made;
+    return (s.keep == 0.f && !finite(h) ? h : s.keep * h) + s.made;            // (no product of gates is nothing, but 32 bits may say so)
 }
-__device__ __forceinline__ Summary join(const Summary &first, const Summary &then)
-{
-    return {first.keep * then.keep, __builtin_fmaf(then.gone, 1.f - first.gone, first.gone), through(then, first.made)};
-}
+__device__ __forceinline__ Summary join(const Summary &first, const Summary &then) { return {first.keep * then.keep, through(then, first.made)}; }
 
 // How a call is cut: waves of a workgroup take parts of `part` tokens (a multiple of a block) behind each other, groups of them lie along y.
 struct Cut {
@@ -55,10 +82,10 @@ struct Cut {
     __device__ __host__ __forceinline__ int64_t span() const { return (int64_t)part * waves; }
 };
 
-// Summaries in the workspace, [segment][group][1 + waves][3][channels]: of the group, then of its parts.
+// Summaries in the workspace, [segment][group][1 + waves][2][channels]: of the group, then of its parts.
 __device__ __forceinline__ float *summary_at(void *workspace, const Cut &cut, int segment, int group, int part, int channels)
 {
-    return (float *)workspace + ((((int64_t)segment * cut.groups + group) * (1 + cut.waves) + part) * 3) * channels;
+    return (float *)workspace + ((((int64_t)segment * cut.groups + group) * (1 + cut.waves) + part) * 2) * channels;
 }
 // Behind them the states (or gradients) that segments begin with, [segment][channels]: the last part may write to where they came from before others have read.
 __device__ __forceinline__ float *begin_at(void *workspace, const Cut &cut, int n_segments, int segment, int channels)
@@ -68,7 +95,7 @@ __device__ __forceinline__ float *begin_at(void *workspace, const Cut &cut, int 
 template <int V> __device__ __forceinline__ void put(float *to, int channels, int c, const Summary (&s)[V])
 {
 #pragma unroll
-    for (int v = 0; v < V; ++v) { to[c + v] = s[v].keep; to[channels + c + v] = s[v].gone; to[2 * (int64_t)channels + c + v] = s[v].made; }
+    for (int v = 0; v < V; ++v) { to[c + v] = s[v].keep; to[channels + c + v] = s[v].made; }
 }
 
 // The state (or gradient) h goes through n summaries that lie `apart` floats from each other; several are asked for at once.
@@ -81,7 +108,7 @@ template <int V> __device__ __forceinline__ void go_through(const float *from, i
         for (int j = 0; j < kAhead; ++j) {
             const float *at = from + (int64_t)min(i + j, n - 1) * apart + c;
 #pragma unroll
-            for (int v = 0; v < V; ++v) s[j][v] = {at[v], at[channels + v], at[2 * (int64_t)channels + v]};
+            for (int v = 0; v < V; ++v) s[j][v] = {at[v], at[channels + v]};
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j)
@@ -154,31 +181,23 @@ template <int V> __device__ __forceinline__ void join_group(float *lds, const Wo
         for (int v = 0; v < V; ++v) to[v] = begin ? begin[(int64_t)w.g.ring * channels + w.c + v] : 0.f;
     }
     if (w.on) put<V>(summary_at(workspace, cut, w.segment, w.group, 1 + w.wave, channels), channels, w.c, s);
-    float *mine = lds + (w.wave * 64 + (threadIdx.x & 63)) * 3 * V;
+    float *mine = lds + (w.wave * 64 + (threadIdx.x & 63)) * 2 * V;
 #pragma unroll
-    for (int v = 0; v < V; ++v) { mine[3 * v] = s[v].keep; mine[3 * v + 1] = s[v].gone; mine[3 * v + 2] = s[v].made; }
+    for (int v = 0; v < V; ++v) { mine[2 * v] = s[v].keep; mine[2 * v + 1] = s[v].made; }
     lds_barrier();
     if (w.wave != 0 || !w.on) return;
     Summary all[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) all[v] = {1.f, 0.f, 0.f};
+    for (int v = 0; v < V; ++v) all[v] = {1.f, 0.f};
     for (int i = 0; i < cut.waves; ++i) {
-        const float *its = lds + ((backwards ? cut.waves - 1 - i : i) * 64 + (threadIdx.x & 63)) * 3 * V;
+        const float *its = lds + ((backwards ? cut.waves - 1 - i : i) * 64 + (threadIdx.x & 63)) * 2 * V;
 #pragma unroll
-        for (int v = 0; v < V; ++v) all[v] = join(all[v], Summary{its[3 * v], its[3 * v + 1], its[3 * v + 2]});
+        for (int v = 0; v < V; ++v) all[v] = join(all[v], Summary{its[2 * v], its[2 * v + 1]});
     }
     put<V>(summary_at(workspace, cut, w.segment, w.group, 0, channels), channels, w.c, all);
 }
 
 // ---- forward ----
-
-// The next state, and what flows to the token before.
-__device__ __forceinline__ float step_of(const Gate &w, float x, float h)
-{
-    const bool most = w.keep >= 0.5f;
-    return __builtin_fmaf(w.take, most ? x - h : x, most ? h : w.keep * h);
-}
-__device__ __forceinline__ float flow_of(const Gate &w, float l) { return w.keep >= 0.5f ? __builtin_fmaf(-w.take, l, l) : w.keep * l; }
 
 // f(0), f(1), .. of the n first rows of a block, or in the other order; whole blocks without a look at n.
 template <class F> __device__ __forceinline__ void rows_up(int n, F f)
@@ -204,12 +223,12 @@ template <class F> __device__ __forceinline__ void rows_down(int n, F f)
     }
 }
 
-// The states after each of the n first rows of a block.  Where one comes out infinite or not a number the block is taken once more, with
-// what is infinite kept and taken in by the definition, since x - h is no number where both are infinite.
+// The states after each of the n first rows of a block: each(u, h, gates).  Where one comes out infinite or not a number, or a gate is out of bounds,
+// the block is taken once more by the definition.
 template <int PREC, int V, class P, class F>
 __device__ __forceinline__ void states(const P (&x)[kBlock], const P (&g)[kBlock], int n, float (&h)[V], F each)
 {
-    float was[V];
+    float was[V], far = 0.f;
     bool fine = true;
 #pragma unroll
     for (int v = 0; v < V; ++v) was[v] = h[v];
@@ -217,14 +236,16 @@ __device__ __forceinline__ void states(const P (&x)[kBlock], const P (&g)[kBlock
         Gate w[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            w[v] = gate_of<PREC>(Elem<PREC>::to_f32(g[u].v[v]));
+            const float gate = Elem<PREC>::to_f32(g[u].v[v]);
+            far = fmaxf(far, __builtin_fabsf(gate));
+            w[v] = gate_of<PREC>(gate);
             h[v] = step_of(w[v], Elem<PREC>::to_f32(x[u].v[v]), h[v]);
         }
         each(u, h, w);
     });
 #pragma unroll
     for (int v = 0; v < V; ++v) fine = fine && finite(h[v]);
-    if (fine) return;
+    if (fine && far <= kGateMost) return;
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = was[v];
 #pragma unroll
@@ -233,16 +254,16 @@ __device__ __forceinline__ void states(const P (&x)[kBlock], const P (&g)[kBlock
             Gate w[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                w[v] = gate_of<PREC>(Elem<PREC>::to_f32(g[u].v[v]));
-                const float in = Elem<PREC>::to_f32(x[u].v[v]), next = step_of(w[v], in, h[v]);
-                h[v] = finite(next) ? next : w[v].keep * h[v] + w[v].take * in;
+                const Slow<PREC> slow(Elem<PREC>::to_f32(g[u].v[v]));
+                w[v] = slow.w;
+                h[v] = slow.step(Elem<PREC>::to_f32(x[u].v[v]), h[v]);
             }
             each(u, h, w);
         }
 }
 
 template <int PREC, int V>
-__global__ void __launch_bounds__(1024) k_gate_parts(idf_gate_scan_args a, Cut cut)
+__global__ void __launch_bounds__(512) k_gate_parts(idf_gate_scan_args a, Cut cut)
 {
     extern __shared__ float lds[];
     const Work w = work_of<V>(a, cut, blockIdx.y);
@@ -252,7 +273,7 @@ __global__ void __launch_bounds__(1024) k_gate_parts(idf_gate_scan_args a, Cut c
     Summary s[V];
     float h[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) { s[v] = {1.f, 0.f, 0.f}; h[v] = 0.f; }
+    for (int v = 0; v < V; ++v) { s[v] = {1.f, 0.f}; h[v] = 0.f; }
     if (w.t0 < w.t1) { x.load(xs, w.t0, w.t1); g.load(gs, w.t0, w.t1); }
     for (int t = w.t0; t < w.t1; t += kBlock) {
         typename Rows<PREC, V>::P xn[kBlock], gn[kBlock];
@@ -264,8 +285,7 @@ __global__ void __launch_bounds__(1024) k_gate_parts(idf_gate_scan_args a, Cut c
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if (u == 0) s[v] = was[v];
-                s[v].keep *= w[v].keep;
-                s[v].gone = __builtin_fmaf(w[v].take, 1.f - s[v].gone, s[v].gone);
+                s[v].keep = kept_of(w[v], s[v].keep);
             }
         });
 #pragma unroll
@@ -277,7 +297,7 @@ __global__ void __launch_bounds__(1024) k_gate_parts(idf_gate_scan_args a, Cut c
 }
 
 template <int PREC, int V>
-__global__ void __launch_bounds__(1024) k_gate_out(idf_gate_scan_args a, Cut cut)
+__global__ void __launch_bounds__(512) k_gate_out(idf_gate_scan_args a, Cut cut)
 {
     // parts that were read last come first: they are still in the caches
     const Work w = work_of<V>(a, cut, gridDim.y - 1 - blockIdx.y);
@@ -293,7 +313,7 @@ __global__ void __launch_bounds__(1024) k_gate_out(idf_gate_scan_args a, Cut cut
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = begin ? begin[w.c + v] : 0.f;
     if (w.t0 > 0) {
-        const int64_t apart = 3 * (int64_t)a.channels;
+        const int64_t apart = 2 * (int64_t)a.channels;
         go_through<V>(summary_at(a.workspace, cut, w.segment, 0, 0, a.channels), (1 + cut.waves) * apart, w.group, a.channels, w.c, h);
         go_through<V>(summary_at(a.workspace, cut, w.segment, w.group, 1, a.channels), apart, w.wave, a.channels, w.c, h);
     }
@@ -317,9 +337,9 @@ __global__ void __launch_bounds__(1024) k_gate_out(idf_gate_scan_args a, Cut cut
 // ---- backward ----
 
 // What flows from a token to the one before it, m = a l with l = grad_out + m of the token behind it, over the n first rows of a block, the last
-// first; as above, once more where it comes out infinite.
-template <int V, class F, class G>
-__device__ __forceinline__ void flow(int n, float (&m)[V], F grad, G each)
+// first: each(u, l, gates).  As above, once more where it comes out infinite or a gate is out of bounds (far).
+template <int PREC, int V, class P, class F, class G>
+__device__ __forceinline__ void flow(const P (&g)[kBlock], const P (&d)[kBlock], int n, float (&m)[V], float far, F gates, G each)
 {
     float was[V];
     bool fine = true;
@@ -328,17 +348,17 @@ __device__ __forceinline__ void flow(int n, float (&m)[V], F grad, G each)
     rows_down(n, [&](int u) IDF_INLINE {
         float l[V];
         Gate w[V];
-        grad(u, l, w);
+        gates(u, w);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            l[v] += m[v];
-            m[v] = flow_of(w[v], l[v]);
+            l[v] = Elem<PREC>::to_f32(d[u].v[v]) + m[v];
+            m[v] = kept_of(w[v], l[v]);
         }
         each(u, l, w);
     });
 #pragma unroll
     for (int v = 0; v < V; ++v) fine = fine && finite(m[v]);
-    if (fine) return;
+    if (fine && far <= kGateMost) return;
 #pragma unroll
     for (int v = 0; v < V; ++v) m[v] = was[v];
 #pragma unroll
@@ -346,15 +366,24 @@ __device__ __forceinline__ void flow(int n, float (&m)[V], F grad, G each)
         if (u < n) {
             float l[V];
             Gate w[V];
-            grad(u, l, w);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                l[v] += m[v];
-                const float next = flow_of(w[v], l[v]);
-                m[v] = finite(next) ? next : w[v].keep * l[v];
+                const Slow<PREC> slow(Elem<PREC>::to_f32(g[u].v[v]));
+                w[v] = slow.w;
+                l[v] = Elem<PREC>::to_f32(d[u].v[v]) + m[v];
+                m[v] = slow.kept(l[v]);
             }
             each(u, l, w);
         }
+}
+template <int PREC, int V, class P> __device__ __forceinline__ float farthest(const P (&g)[kBlock])
+{
+    float far = 0.f;
+#pragma unroll
+    for (int u = 0; u < kBlock; ++u)
+#pragma unroll
+        for (int v = 0; v < V; ++v) far = fmaxf(far, __builtin_fabsf(Elem<PREC>::to_f32(g[u].v[v])));
+    return far;
 }
 
 template <int PREC, int V>
@@ -369,7 +398,7 @@ __global__ void __launch_bounds__(256) k_gate_back_parts(idf_gate_scan_backward_
     Summary s[V];
     float m[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) { s[v] = {1.f, 0.f, 0.f}; m[v] = 0.f; }
+    for (int v = 0; v < V; ++v) { s[v] = {1.f, 0.f}; m[v] = 0.f; }
     const int from = w.t0 < w.t1 ? w.t0 + (w.t1 - 1 - w.t0) / kBlock * kBlock : w.t0 - kBlock;
     const bool any = a.grad_out.base;
     if (w.t0 < w.t1) { g.load(gs, from, w.t1); if (any) d.load(ds, from, w.t1); }
@@ -377,18 +406,19 @@ __global__ void __launch_bounds__(256) k_gate_back_parts(idf_gate_scan_backward_
         typename R::P gn[kBlock], dn[kBlock] = {};
         if (t > w.t0) { g.load(gn, t - kBlock, w.t1); if (any) d.load(dn, t - kBlock, w.t1); }
         const int n = min(kBlock, w.t1 - t);
-        rows_up(n, [&](int u) IDF_INLINE {
+        float was[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) was[v] = s[v].keep;
+        flow<PREC, V>(gs, ds, n, m, farthest<PREC, V>(gs), [&](int u, Gate (&w)[V]) IDF_INLINE {
+#pragma unroll
+            for (int v = 0; v < V; ++v) w[v] = gate_of<PREC>(Elem<PREC>::to_f32(gs[u].v[v]));
+        }, [&](int u, float (&)[V], Gate (&w)[V]) IDF_INLINE {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Gate w = gate_of<PREC>(Elem<PREC>::to_f32(gs[u].v[v]));
-                s[v].keep *= w.keep;
-                s[v].gone = __builtin_fmaf(w.take, 1.f - s[v].gone, s[v].gone);
+                if (u == n - 1) s[v].keep = was[v];
+                s[v].keep = kept_of(w[v], s[v].keep);
             }
         });
-        flow<V>(n, m, [&](int u, float (&l)[V], Gate (&w)[V]) IDF_INLINE {
-#pragma unroll
-            for (int v = 0; v < V; ++v) { l[v] = Elem<PREC>::to_f32(ds[u].v[v]); w[v] = gate_of<PREC>(Elem<PREC>::to_f32(gs[u].v[v])); }
-        }, [](int, float (&)[V], Gate (&)[V]) {});
 #pragma unroll
         for (int u = 0; u < kBlock; ++u) { gs[u] = gn[u]; ds[u] = dn[u]; }
     }
@@ -398,7 +428,7 @@ __global__ void __launch_bounds__(256) k_gate_back_parts(idf_gate_scan_backward_
 }
 
 template <int PREC, int V>
-__global__ void __launch_bounds__(256) k_gate_back(idf_gate_scan_backward_args a, Cut cut)
+__global__ void __launch_bounds__(256, 2) k_gate_back(idf_gate_scan_backward_args a, Cut cut)
 {
     const Work w = work_of<V>(a, cut, blockIdx.y);
     const bool first = w.group == 0 && w.wave == 0;
@@ -431,6 +461,7 @@ __global__ void __launch_bounds__(256) k_gate_back(idf_gate_scan_backward_args a
 #pragma unroll
         for (int v = 0; v < V; ++v) mark[v] = at[v];
     };
+    const bool on = w.on;
     if (w.t0 < w.t1) load(from, xs, gs, ds, mark);
     float m[V];
     const bool cuts = cut.groups * cut.waves > 1 && w.g.len > 0;
@@ -438,7 +469,7 @@ __global__ void __launch_bounds__(256) k_gate_back(idf_gate_scan_backward_args a
 #pragma unroll
     for (int v = 0; v < V; ++v) m[v] = end ? end[w.c + v] : 0.f;
     if (w.t1 < w.g.len) {
-        const int64_t apart = 3 * (int64_t)a.channels;
+        const int64_t apart = 2 * (int64_t)a.channels;
         // groups and parts that have tokens, the last first
         const int groups = (int)((w.g.len + cut.span() - 1) / cut.span());
         const int parts = (int)((min((int64_t)w.g.len, (w.group + 1) * cut.span()) - w.group * cut.span() + cut.part - 1) / cut.part);
@@ -450,8 +481,9 @@ __global__ void __launch_bounds__(256) k_gate_back(idf_gate_scan_backward_args a
         float mark_n[V];
         if (t > w.t0) load(t - kBlock, xn, gn, dn, mark_n);
         const int n = min(kBlock, w.t1 - t);
-        // what x takes the place of, h before the token - x, and the gates
-        float apart[kBlock][V], keep[kBlock][V], take[kBlock][V], h[V], before[V];
+        // of every token the state before it less x, and its gate
+        float apart[kBlock][V], h[V], before[V];
+        Gate gate[kBlock][V];
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = before[v] = mark[v];
         states<PREC, V>(xs, gs, n, h, [&](int u, float (&h)[V], Gate (&w)[V]) IDF_INLINE {
@@ -459,19 +491,21 @@ __global__ void __launch_bounds__(256) k_gate_back(idf_gate_scan_backward_args a
             for (int v = 0; v < V; ++v) {
                 if (u == 0) before[v] = mark[v];
                 apart[u][v] = before[v] - Elem<PREC>::to_f32(xs[u].v[v]);
-                keep[u][v] = w[v].keep;
-                take[u][v] = w[v].take;
+                gate[u][v] = w[v];
                 before[v] = h[v];
             }
         });
-        flow<V>(n, m, [&](int u, float (&l)[V], Gate (&w)[V]) IDF_INLINE {
+        flow<PREC, V>(gs, ds, n, m, farthest<PREC, V>(gs), [&](int u, Gate (&w)[V]) IDF_INLINE {
 #pragma unroll
-            for (int v = 0; v < V; ++v) { l[v] = Elem<PREC>::to_f32(ds[u].v[v]); w[v].take = take[u][v]; w[v].keep = keep[u][v]; }
-        }, [&](int u, float (&l)[V], Gate (&)[V]) IDF_INLINE {
+            for (int v = 0; v < V; ++v) w[v] = gate[u][v];
+        }, [&](int u, float (&l)[V], Gate (&w)[V]) IDF_INLINE {
             float dx[V], dg[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) { dx[v] = take[u][v] * l[v]; dg[v] = l[v] * apart[u][v] * (keep[u][v] * take[u][v]); }
-            if (w.on) { gx.store(t, u, dx); gg.store(t, u, dg); }
+            for (int v = 0; v < V; ++v) {
+                dx[v] = l[v] * w[v].take();
+                dg[v] = l[v] * apart[u][v] * (__builtin_fabsf(w[v].s) * w[v].big());
+            }
+            if (on) { gx.store(t, u, dx); gg.store(t, u, dg); }
         });
 #pragma unroll
         for (int u = 0; u < kBlock; ++u) { xs[u] = xn[u]; gs[u] = gn[u]; ds[u] = dn[u]; }
@@ -495,24 +529,29 @@ template <class Args> bool pairs(const Args &a, std::initializer_list<const idf_
 bool pairs(const idf_gate_scan_args &a) { return pairs(a, {&a.x, &a.gates, &a.out}); }
 bool pairs(const idf_gate_scan_backward_args &a) { return pairs(a, {&a.x, &a.gates, &a.grad_out, &a.grad_x, &a.grad_gates}); }
 
+// Waves that a call is cut into, by the tokens that there are (us, forward and backward, with 2048 : 4096 : 8192; 16 uneven segments of up to 2048 tokens of 1536 channels
+// 74, 130 : 62, 109 : 60, 109; 65536 tokens of 2048 channels 296, 449 : 311, 470 : 304, 468; 8 segments of 4096 tokens of 1024 channels 76, 125 : 78, 128 : 80, 137).
+constexpr int64_t kWaves = 4096;
 template <class Args> Cut cut_of(const Args &a, int most_waves)
 {
     const int64_t blocks = (longest(a) + kBlock - 1) / kBlock, wide = 64 * (pairs(a) ? 2 : 1);
-    const int64_t lanes = (a.channels + wide - 1) / wide * a.n_segments;       // waves of a call that is not cut
+    const int64_t lanes = (a.channels + wide - 1) / wide;                      // waves of a token
     Cut c = {(int)std::max<int64_t>(blocks, 1) * kBlock, 1, 1};
-    const int64_t parts = std::min<int64_t>({(2048 + lanes - 1) / lanes, blocks / 2, (int64_t)kMostGroups * most_waves});
+    // blocks of a part so that all tokens that there are make kWaves waves, and more where the longest segment has no room for so many parts
+    const int64_t all = std::min<int64_t>(a.n_tokens / kBlock + a.n_segments, a.n_segments * blocks);
+    const int64_t part = std::max<int64_t>({(all * lanes + kWaves - 1) / kWaves, 1, (blocks + kMostGroups * most_waves - 1) / (kMostGroups * most_waves)});
+    const int64_t parts = (blocks + part - 1) / part;
     if (parts < 2) return c;
     c.waves = (int)std::min<int64_t>(parts <= kMostGroups * 4 ? 4 : most_waves, parts);
-    const int64_t groups = std::min<int64_t>((parts + c.waves - 1) / c.waves, kMostGroups);
-    c.part = (int)((blocks + groups * c.waves - 1) / (groups * c.waves)) * kBlock;
+    c.part = (int)part * kBlock;
     c.groups = (int)((blocks * kBlock + c.span() - 1) / c.span());
     return c;
 }
-constexpr int kForwardWaves = 16, kBackwardWaves = 4;
+constexpr int kForwardWaves = 8, kBackwardWaves = 4;
 
 template <class Args> size_t summaries(const Args &a, const Cut &c)
 {
-    return c.groups * c.waves > 1 ? (size_t)a.n_segments * ((size_t)c.groups * (1 + c.waves) * 3 + 1) * a.channels * sizeof(float) : 0;
+    return c.groups * c.waves > 1 ? (size_t)a.n_segments * ((size_t)c.groups * (1 + c.waves) * 2 + 1) * a.channels * sizeof(float) : 0;
 }
 
 template <int PREC, int V>
@@ -521,7 +560,7 @@ hipError_t forward(const idf_gate_scan_args &a, const LaunchCtx &lc)
     const Cut c = cut_of(a, kForwardWaves);
     const dim3 grid((a.channels + 64 * V - 1) / (64 * V), c.groups, a.n_segments), block(64 * c.waves);
     if (c.groups * c.waves > 1)
-        if (const hipError_t e = launch(k_gate_parts<PREC, V>, grid, block, (size_t)c.waves * 64 * 3 * V * sizeof(float), lc, a, c)) return e;
+        if (const hipError_t e = launch(k_gate_parts<PREC, V>, grid, block, (size_t)c.waves * 64 * 2 * V * sizeof(float), lc, a, c)) return e;
     return launch(k_gate_out<PREC, V>, grid, block, 0, lc, a, c);
 }
 template <int PREC, int V>
@@ -530,7 +569,7 @@ hipError_t backward(const idf_gate_scan_backward_args &a, const LaunchCtx &lc)
     const Cut c = cut_of(a, kBackwardWaves);
     const dim3 grid((a.channels + 64 * V - 1) / (64 * V), c.groups, a.n_segments), block(64 * c.waves);
     if (c.groups * c.waves > 1)
-        if (const hipError_t e = launch(k_gate_back_parts<PREC, V>, grid, block, (size_t)c.waves * 64 * 3 * V * sizeof(float), lc, a, c)) return e;
+        if (const hipError_t e = launch(k_gate_back_parts<PREC, V>, grid, block, (size_t)c.waves * 64 * 2 * V * sizeof(float), lc, a, c)) return e;
     return launch(k_gate_back<PREC, V>, grid, block, 0, lc, a, c);
 }
 

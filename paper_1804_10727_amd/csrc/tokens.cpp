@@ -3,6 +3,8 @@
 // the kernels of a single token's step take.
 #include <Python.h>
 
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
@@ -12,6 +14,8 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <optional>
+#include <stdexcept>
 
 #include "idf.h"
 
@@ -36,6 +40,7 @@ struct Functions {
     int (*gate_back_workspace)(const idf_gate_scan_backward_args *, size_t *);
     int (*gate_back)(const idf_gate_scan_backward_args *, void *);
     int (*gate_marks)(const idf_gate_scan_args *, size_t *);
+    int (*is_capturing)(void *, int *);            // the runtime's own
 } fn;
 constexpr int kFunctions = sizeof(Functions) / sizeof(void *);
 bool bound;
@@ -61,13 +66,17 @@ void need(bool ok)
     if (!ok) throw Unusual();
 }
 
-const at::Tensor *tensor(PyObject *o)
+const at::Tensor *recorded_tensor(PyObject *o)
 {
     if (o == Py_None) return nullptr;
     need(THPVariable_CheckExact(o));
-    const at::Tensor &t = THPVariable_Unpack(o);
-    need(!t.requires_grad() || !c10::GradMode::is_enabled());                // (refused there: there is no backward pass)
-    return &t;
+    return &THPVariable_Unpack(o);
+}
+const at::Tensor *tensor(PyObject *o)
+{
+    const at::Tensor *t = recorded_tensor(o);
+    need(!t || !t->requires_grad() || !c10::GradMode::is_enabled());         // (refused there: there is no backward pass)
+    return t;
 }
 
 int precision(const at::Tensor &t)
@@ -580,6 +589,37 @@ PyObject *gate_scan(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// Gradients of the recurrence; segments are those of a.
+struct GateGradients { at::Tensor x, gates, state; };
+int gate_gradients(idf_gate_scan_backward_args &a, const at::Tensor &x, const at::Tensor &g, const at::Tensor &marks, const at::Tensor *grad, const at::Tensor *end, void *stream, GateGradients &to)
+{
+    a.precision = precision(x);
+    a.x = matrix(x, x);
+    a.gates = matrix(g, x);
+    a.channels = (int)x.size(1);
+    a.n_tokens = x.size(0);
+    if (grad) {
+        need(grad->sizes() == x.sizes() && grad->scalar_type() == x.scalar_type());
+        a.grad_out = matrix(*grad, x);
+    }
+    idf_gate_scan_args f{};
+    f.precision = a.precision; f.channels = a.channels; f.n_tokens = a.n_tokens; f.max_tokens = a.max_tokens; f.n_segments = a.n_segments; f.n_streams = a.n_streams;
+    f.offsets = a.offsets; f.stream_ids = a.stream_ids;
+    size_t bytes = 0;
+    int rc = fn.gate_marks(&f, &bytes);
+    if (rc != IDF_OK) return rc;
+    a.marks = plain<float>(&marks, at::kFloat, (int64_t)bytes / 4, x);
+    a.grad_end = end ? static_cast<const float *>(end->data_ptr()) : nullptr;
+    const auto fresh = [&]() { return a.n_segments ? at::empty(x.sizes(), x.options()) : at::zeros(x.sizes(), x.options()); };
+    to = {fresh(), fresh(), at::empty({a.n_streams, a.channels}, x.options().dtype(at::kFloat))};
+    a.grad_x = matrix(to.x, x);
+    a.grad_gates = matrix(to.gates, x);
+    a.grad_state = static_cast<float *>(to.state.data_ptr());
+    at::Tensor ws;
+    rc = with_workspace(fn.gate_back_workspace, a, x, ws);
+    return rc == IDF_OK ? fn.gate_back(&a, stream) : rc;
+}
+
 // gate_scan_backward(stream, x, gates, marks, grad_out, grad_end, offsets, max_tokens, n_segments, stream_ids, n_streams): gradients of x, gates and states
 PyObject *gate_scan_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -587,45 +627,119 @@ PyObject *gate_scan_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     return entry([&]() -> PyObject * {
         void *stream = reinterpret_cast<void *>((uintptr_t)whole(args[0]));
         const at::Tensor *x = tensor(args[1]), *g = tensor(args[2]), *marks = tensor(args[3]), *grad = tensor(args[4]), *end = tensor(args[5]);
-        need(x && g && marks && x->sizes() == g->sizes() && g->scalar_type() == x->scalar_type());
+        need(x && g && marks && x->dim() == 2 && x->size(1) <= INT_MAX && x->sizes() == g->sizes() && g->scalar_type() == x->scalar_type());
         idf_gate_scan_backward_args a{};
-        a.precision = precision(*x);
-        a.x = matrix(*x, *x);
-        a.gates = matrix(*g, *x);
-        need(x->size(1) <= INT_MAX);
-        a.channels = (int)x->size(1);
         a.n_tokens = x->size(0);
-        const int64_t told = args[10] == Py_None ? -1 : whole(args[10]), have = states(end, nullptr, a.channels, *x);
+        const int64_t told = args[10] == Py_None ? -1 : whole(args[10]), have = states(end, nullptr, x->size(1), *x);
         need(told < 0 || have < 0 || told == have);
         gate_segments(a, *x, have >= 0 ? have : told, args[6], args[7], args[8], args[9]);
-        if (grad) {
-            need(grad->sizes() == x->sizes() && grad->scalar_type() == x->scalar_type());
-            a.grad_out = matrix(*grad, *x);
-        }
-        idf_gate_scan_args f{};
-        f.precision = a.precision; f.channels = a.channels; f.n_tokens = a.n_tokens; f.max_tokens = a.max_tokens; f.n_segments = a.n_segments; f.n_streams = a.n_streams;
-        f.offsets = a.offsets; f.stream_ids = a.stream_ids;
-        size_t bytes = 0;
-        int rc = fn.gate_marks(&f, &bytes);
-        if (rc != IDF_OK) return PyLong_FromLong(rc);
-        a.marks = plain<float>(marks, at::kFloat, (int64_t)bytes / 4, *x);
-        a.grad_end = end ? static_cast<const float *>(end->data_ptr()) : nullptr;
         const c10::DeviceGuard guard(x->device());
-        const auto fresh = [&]() { return a.n_segments ? at::empty(x->sizes(), x->options()) : at::zeros(x->sizes(), x->options()); };
-        const at::Tensor gx = fresh(), gg = fresh(), gs = at::empty({a.n_streams, a.channels}, x->options().dtype(at::kFloat));
-        a.grad_x = matrix(gx, *x);
-        a.grad_gates = matrix(gg, *x);
-        a.grad_state = static_cast<float *>(gs.data_ptr());
-        at::Tensor ws;
-        rc = with_workspace(fn.gate_back_workspace, a, *x, ws);
-        if (rc == IDF_OK) rc = call(fn.gate_back, a, stream);
+        GateGradients to;
+        const int rc = gate_gradients(a, *x, *g, *marks, grad, end, stream, to);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
         PyObject *all = PyTuple_New(3);
         if (!all) throw Unusual();
-        PyTuple_SET_ITEM(all, 0, THPVariable_Wrap(gx));
-        PyTuple_SET_ITEM(all, 1, THPVariable_Wrap(gg));
-        PyTuple_SET_ITEM(all, 2, THPVariable_Wrap(gs));
+        PyTuple_SET_ITEM(all, 0, THPVariable_Wrap(to.x));
+        PyTuple_SET_ITEM(all, 1, THPVariable_Wrap(to.gates));
+        PyTuple_SET_ITEM(all, 2, THPVariable_Wrap(to.state));
         return all;
+    });
+}
+
+// The recurrence as torch's gradients go through it.  The backward pass runs on the stream of the forward one, as torch has it.
+struct GateScan : torch::autograd::Function<GateScan> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext *ctx, const at::Tensor &x, const at::Tensor &gates, const std::optional<at::Tensor> &state,
+                                                  const std::optional<at::Tensor> &offsets, int64_t max_tokens, int64_t segments, int64_t stream)
+    {
+        idf_gate_scan_args a{};
+        a.precision = precision(x);
+        a.channels = (int)x.size(1);
+        a.n_tokens = x.size(0);
+        a.max_tokens = max_tokens;
+        a.n_segments = a.n_streams = (int)segments;
+        a.offsets = offsets ? plain<int64_t>(&*offsets, at::kLong, segments + 1, x) : nullptr;
+        a.x = matrix(x, x);
+        a.gates = matrix(gates, x);
+        a.state_in = state ? static_cast<const float *>(state->data_ptr()) : nullptr;
+        const at::Tensor out = at::empty(x.sizes(), x.options()), end = at::empty({segments, x.size(1)}, x.options().dtype(at::kFloat));
+        a.out = matrix(out, x);
+        a.state_out = static_cast<float *>(end.data_ptr());
+        size_t bytes = 0;
+        need(fn.gate_marks(&a, &bytes) == IDF_OK);
+        const at::Tensor marks = at::empty({(int64_t)bytes / 4}, x.options().dtype(at::kFloat));
+        a.marks = static_cast<float *>(marks.data_ptr());
+        at::Tensor ws;
+        need(with_workspace(fn.gate_workspace, a, x, ws) == IDF_OK && fn.gate(&a, reinterpret_cast<void *>((uintptr_t)stream)) == IDF_OK);
+        ctx->save_for_backward({x, gates, marks, offsets ? *offsets : at::Tensor()});
+        ctx->saved_data["max_tokens"] = max_tokens;
+        ctx->saved_data["segments"] = segments;
+        ctx->saved_data["stream"] = stream;
+        ctx->saved_data["has_state"] = state.has_value();
+        ctx->set_materialize_grads(false);
+        return {out, end};
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext *ctx, torch::autograd::variable_list grads)
+    {
+        torch::autograd::variable_list answer(7);
+        if (!grads[0].defined() && !grads[1].defined()) return answer;
+        const auto saved = ctx->get_saved_variables();
+        const at::Tensor &x = saved[0], &offsets = saved[3];
+        void *stream = reinterpret_cast<void *>((uintptr_t)ctx->saved_data["stream"].toInt());
+        int capturing = 0;
+        if (fn.is_capturing(stream, &capturing) != 0 || capturing)
+            throw std::runtime_error("gate_scan_recorded's backward pass while a stream is captured: gate_scan_backward can be captured");
+        const bool twice = c10::GradMode::is_enabled();
+        GateGradients to;
+        {
+            const c10::AutoGradMode off(false);
+            const c10::DeviceGuard guard(x.device());
+            const at::Tensor grad = grads[0].defined() ? grads[0].contiguous() : at::Tensor(), end = grads[1].defined() ? grads[1].contiguous() : at::Tensor();
+            idf_gate_scan_backward_args a{};
+            a.max_tokens = ctx->saved_data["max_tokens"].toInt();
+            a.n_segments = a.n_streams = (int)ctx->saved_data["segments"].toInt();
+            a.offsets = offsets.defined() ? static_cast<const int64_t *>(offsets.data_ptr()) : nullptr;
+            // (rows that lie too far apart, which the forward call did not take either, are no case here)
+            if (gate_gradients(a, x, saved[1], saved[2], grad.defined() ? &grad : nullptr, end.defined() ? &end : nullptr, stream, to) != IDF_OK)
+                throw std::runtime_error("gate_scan_backward was refused");
+        }
+        answer[0] = to.x; answer[1] = to.gates; answer[2] = to.state;
+        if (twice) {                               // (gradients of these are refused, when somebody asks for them)
+            torch::autograd::variable_list of(answer.begin(), answer.begin() + 3);
+            for (at::Tensor &t : of) t.set_requires_grad(true);
+            auto refusal = std::make_shared<torch::autograd::DelayedError>("gate_scan_recorded has no gradients of gradients", 3);
+            of = (*refusal)(std::move(of));
+            std::copy(of.begin(), of.end(), answer.begin());
+        }
+        // (tensors alone are counted: a state that was not given is none)
+        const size_t given = ctx->saved_data["has_state"].toBool() ? 3 : 2;
+        for (size_t i = 0; i < 3; ++i)
+            if (i >= given || !ctx->needs_input_grad(i)) answer[i] = at::Tensor();
+        return answer;
+    }
+};
+
+// gate_scan_recorded(stream, x, gates, state, offsets, max_tokens, n_segments): (out, states behind the segments)
+PyObject *gate_scan_recorded(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 7 || !bound) { PyErr_SetString(PyExc_TypeError, "gate_scan_recorded takes 7 arguments"); return nullptr; }
+    return entry([&]() -> PyObject * {
+        const int64_t stream = whole(args[0]);
+        const at::Tensor *x = recorded_tensor(args[1]), *g = recorded_tensor(args[2]), *state = recorded_tensor(args[3]), *offsets = tensor(args[4]);
+        need(x && g && x->dim() == 2 && x->size(1) <= INT_MAX && x->sizes() == g->sizes() && g->scalar_type() == x->scalar_type());
+        (void)precision(*x);
+        (void)matrix(*x, *x);
+        (void)matrix(*g, *x);
+        idf_gate_scan_args a{};
+        a.n_tokens = x->size(0);
+        gate_segments(a, *x, states(state, nullptr, x->size(1), *x), args[4], args[5], args[6], Py_None);
+        need(!state || state->size(0) == a.n_segments);
+        const c10::DeviceGuard guard(x->device());
+        const auto got = GateScan::apply(*x, *g, state ? std::optional<at::Tensor>(*state) : std::nullopt, offsets ? std::optional<at::Tensor>(*offsets) : std::nullopt, a.max_tokens,
+                                         (int64_t)a.n_segments, stream);
+        PyObject *both = PyTuple_New(2);
+        if (!both) throw Unusual();
+        for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(both, i, THPVariable_Wrap(got[i]));
+        return both;
     });
 }
 
@@ -642,6 +756,7 @@ PyMethodDef methods[] = {
     {"nibble_values", FAST(nibble_values), "idf_nibble_values on tensors"},
     {"gate_scan", FAST(gate_scan), "idf_gate_scan on tensors"},
     {"gate_scan_backward", FAST(gate_scan_backward), "idf_gate_scan_backward on tensors"},
+    {"gate_scan_recorded", FAST(gate_scan_recorded), "both of them as torch's gradients go through them"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tokens", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

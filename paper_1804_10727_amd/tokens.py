@@ -623,7 +623,9 @@ def _make_recorded():
     class GateScan(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, gates, state, offsets, max_tokens, n_segments):
-            streams = state.shape[0] if state is not None else n_segments if n_segments is not None else 1 if offsets is None else offsets.numel() - 1
+            streams = n_segments if n_segments is not None else offsets.numel() - 1 if offsets is not None else 1 if state is None else state.shape[0]
+            if state is not None and state.shape[0] != streams:
+                raise ValueError(f"{state.shape[0]} states of {streams} segments")
             end = torch.empty(streams, x.shape[1], device=x.device)
             out, marks = gate_scan(x, gates, state, end, offsets=offsets, max_tokens=max_tokens, n_segments=n_segments, marks=True)
             ctx.save_for_backward(x, gates, marks, offsets)
@@ -657,7 +659,10 @@ def gate_scan_recorded(x, gates, state=None, *, offsets=None, max_tokens=None, n
     """gate_scan for training: (out, states behind the segments), both recorded by torch's gradients where x, gates or state require them, once (gradients
     of gradients are refused).  Segment s is of stream s.  Not for a stream that is being captured into a graph."""
     global _recorded
+    _no_capture(x)
+    r = _direct("gate_scan_recorded", x, gates, state, offsets, max_tokens, n_segments)
+    if r is not None:
+        return r
     if _recorded is None:
         _recorded = _make_recorded()
-    _no_capture(x)
     return _recorded.apply(x, gates, state, offsets, max_tokens, n_segments)

@@ -83,13 +83,13 @@ def test_segments_of_one_length(dtype):
     check((1,) * 70, 96, dtype, even=True)
 
 
-@pytest.mark.parametrize("n", [200, 20000])
+@pytest.mark.parametrize("n", [16, 200, 20000])
 def test_a_state_that_is_what_comes_in_stays(n):
     """Gates that keep nearly everything, and values equal to the state: what is kept, rounded by itself to a number near one, would move it.  A part from
     nothing is rounded at every step, half a step each."""
     x, gates = torch.full((n, 64), 0.37, device=DEV), torch.full((n, 64), 12.0, device=DEV)
     out = idf.gate_scan(x, gates, x[:1].contiguous())
-    assert torch.equal(out, x) if n == 200 else (out - x).abs().max() <= 2 * 2048 * W * 0.37
+    assert torch.equal(out, x) if n == 16 else (out - x).abs().max() <= 2 * 2048 * W * 0.37       # (16 tokens are never cut)
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
