@@ -18,6 +18,7 @@ namespace {
 constexpr int kBits = 32;                          // values of a block
 constexpr int kStepRows = 32;                      // query rows of a segment and key/value head that the step kernel takes, in one or two tiles of 16
 constexpr int kTileRows = 128;                     // query rows of a workgroup of the tile kernel
+constexpr int kMostTokens = 8;                     // of a workgroup that appends
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 
@@ -63,19 +64,159 @@ __device__ __forceinline__ float to_odd(double d)
     return __builtin_bit_cast(float, bits);
 }
 
-// A lane has eight values of a head, four lanes a block.  Keys are formed in 64 bits, whose instructions run as fast as those of 32 here: a value next to
-// the middle between two codes goes to the same one however sums and products are ordered, and memory bounds the launch all the same.
+// The smallest power with most <= 7 * 2^power, 7 being 1.75 * 2^2: from the exponent and the mantissa of most, held to what a block can have.
+__device__ __forceinline__ int power_for(float most)
+{
+    const uint32_t bits = __builtin_bit_cast(uint32_t, most);
+    return min(max((int)(bits >> 23) - 127 - ((bits & 0x7fffffu) <= 0x600000u ? 2 : 1), -100), 125);
+}
+__device__ __forceinline__ int power_for(double most)
+{
+    const uint64_t bits = __builtin_bit_cast(uint64_t, most);
+    return min(max((int)(bits >> 52) - 1023 - ((bits & 0xfffffffffffffull) <= 0xc000000000000ull ? 2 : 1), -100), 125);
+}
+
+// A lane's neighbours within four and within a row of 16, without a way through LDS: v with those of lanes that lie apart by a mask, or mirrored.
+template <int CTRL> __device__ __forceinline__ float moved(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 15, 15, false)); }
+template <int CTRL> __device__ __forceinline__ double moved(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t low = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)b, CTRL, 15, 15, false), high = (uint32_t)__builtin_amdgcn_mov_dpp((int)(b >> 32), CTRL, 15, 15, false);
+    return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+}
+constexpr int kApart1 = 0xb1, kApart2 = 0x4e, kMirror8 = 0x141, kMirror16 = 0x140;           // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror
+template <class F> __device__ __forceinline__ F block_max(F v)
+{
+    v = __builtin_elementwise_max(v, moved<kApart1>(v));
+    return __builtin_elementwise_max(v, moved<kApart2>(v));
+}
+// Over 1 << lanes_log2 lanes, four at least.
+__device__ __forceinline__ double lanes_sum(double v, int lanes_log2)
+{
+    v += moved<kApart1>(v);
+    v += moved<kApart2>(v);
+    if (lanes_log2 > 2) v += moved<kMirror8>(v);
+    if (lanes_log2 > 3) v += moved<kMirror16>(v);
+    if (lanes_log2 > 4) v += __shfl_xor(v, 16);
+    return v;
+}
+
+__device__ __forceinline__ uint32_t to_codes(const float (&f)[8], float by)
+{
+    uint32_t codes = 0u;
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[0], f[1], by, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], by, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], by, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], by, 3);
+    return codes;
+}
+
+// Eight values of a lane, a block being four neighbouring lanes': codes, and the byte of the power.  EXACT: y are the values themselves; else they were rounded from 64
+// bits, and close says whether one of them lies on a middle between two codes, or the largest on the border between two powers (a multiple of a quarter of the
+// power), where that rounding may have decided.
+template <bool EXACT> __device__ __forceinline__ uint32_t encode(const float (&y)[8], uint32_t &byte, bool &close)
+{
+    float most = 0.f, none = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        none = __builtin_fmaf(y[e], 0.f, none);
+        most = fmaxf(most, __builtin_fabsf(y[e]));
+    }
+    if (!(none == 0.f)) most = __builtin_inff();
+    most = block_max(most);
+    byte = 255u;
+    close = !EXACT;                                // (what is finite in 64 bits may be none of float32)
+    if (!(most < __builtin_inff())) return 0u;
+    const int power = power_for(most);
+    byte = (uint32_t)(power + 127);
+    const float four = power_of((uint32_t)(129 - power));                     // 4 / 2^power
+    float f[8], off = 1.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        f[e] = y[e] * four;
+        if (!EXACT) off = fminf(off, __builtin_amdgcn_fractf(f[e]));
+        f[e] = __builtin_amdgcn_fmed3f(f[e], -24.f, 24.f);                    // (beyond 6: 6)
+    }
+    close = !EXACT && off == 0.f;
+    return to_codes(f, 4.f);
+}
+// The same of 64 bits.
+__device__ __forceinline__ uint32_t encode_exact(const double (&y)[8], uint32_t &byte)
+{
+    double most = 0.0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = __builtin_fabs(y[e]) <= 0x1.fffffffffffffp+1023 ? fmax(most, __builtin_fabs(y[e])) : __builtin_inf();
+    most = block_max(most);
+    byte = 255u;
+    if (!(most < __builtin_inf())) return 0u;
+    const int power = power_for(most);
+    byte = (uint32_t)(power + 127);
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __builtin_amdgcn_fmed3f(to_odd(y[e] * __builtin_bit_cast(double, (uint64_t)(1023 - power) << 52)), -6.f, 6.f);
+    return to_codes(f, 1.f);
+}
+
+// A lane has eight values of a head, four lanes a block; a workgroup a few tokens with all their heads, so that slots, cosines and sines are formed once per
+// token.  Keys that are normalised or turned are formed in 64 bits, whose instructions run as fast as those of 32 here: a value next to the middle between two codes goes to
+// the same one however sums and products are ordered.
 template <int PREC, bool ALIGNED>
-__global__ void __launch_bounds__(256) k_nibble_append(idf_nibble_append_args a, int lanes_log2, int tokens_per_group)
+__global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args a, int lanes_log2, int tokens_per_group)
 {
     using E = Elem<PREC>;
     using T = typename E::type;
     using P = Pack<T, 8>;
     extern __shared__ double2 turn[];              // [token][rotary_dim / 2]: amplitude * (cos, sin)
+    __shared__ int64_t slots[kMostTokens];         // of each token; negative: none
+    __shared__ __align__(16) float weight[256];
     const Segment g = segment_of(a, blockIdx.y, a.starts);
     const int t0 = blockIdx.x * tokens_per_group;
     if (t0 >= g.len) return;
     const int n = min(tokens_per_group, g.len - t0), half = a.rotary_dim / 2;
+    const int lane = threadIdx.x & ((1 << lanes_log2) - 1), c = lane * 8, heads = a.heads_kv, d = a.head_dim;
+    const bool on = c < d, plain = !a.k_weight && !half;
+    const float per_token = 1.f / (float)(2 * heads);
+    const double per_value = 1.0 / d;
+    // a row of a head, and what lies in a pair with this lane's values in the other half of what is turned; the next one is on its way while this one is worked on
+    struct Row { int t, h; bool key; P x, other; };
+    const int total = n * 2 * heads, step = 256 >> lanes_log2;
+    auto fetch = [&](int row) IDF_INLINE {
+        Row r;
+        r.t = (int)(((float)row + 0.5f) * per_token);                          // (fewer than 2^15 rows: exact)
+        const int which = row - r.t * 2 * heads;
+        r.key = which < heads;
+        r.h = r.key ? which : which - heads;
+        r.x = P{};
+        r.other = P{};
+        if (!on) return r;
+        const idf_tokens &from = r.key ? a.k : a.v;
+        const T *src = (const T *)from.base + (g.begin + t0 + r.t) * from.token_stride + r.h * from.head_stride;
+        auto load = [&](int c) IDF_INLINE {
+            P x;
+            if (ALIGNED) return *(const P *)(src + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x.v[e] = src[c + e];
+            return x;
+        };
+        r.x = load(c);
+        if (r.key && c < a.rotary_dim && !a.interleaved) {
+            if (half % 8 == 0) {
+                r.other = load(c < half ? c + half : c - half);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < a.rotary_dim) r.other.v[e] = src[c + e < half ? c + e + half : c + e - half];
+            }
+        }
+        return r;
+    };
+    const int row0 = threadIdx.x >> lanes_log2;
+    Row next = row0 < total ? fetch(row0) : Row{};
+    if ((int)threadIdx.x < n) {
+        const int64_t period = a.slots - a.sinks, p = g.start + t0 + threadIdx.x;
+        slots[threadIdx.x] = p < a.sinks ? p : t0 + (int)threadIdx.x < g.len - period ? -1 : a.sinks + (p - a.sinks) % period;
+    }
+    if (a.k_weight && (int)threadIdx.x < a.head_dim) weight[threadIdx.x] = a.k_weight[threadIdx.x];
     for (int i = threadIdx.x; i < n * half; i += 256) {
         const int t = i / half;
         double s, c;
@@ -83,39 +224,37 @@ __global__ void __launch_bounds__(256) k_nibble_append(idf_nibble_append_args a,
         turn[i] = make_double2(a.amplitude * c, a.amplitude * s);
     }
     __syncthreads();
-    const int64_t period = a.slots - a.sinks;
-    const int lane = threadIdx.x & ((1 << lanes_log2) - 1), c = lane * 8, heads = a.heads_kv, d = a.head_dim;
-    const bool on = c < d;
-    for (int row = threadIdx.x >> lanes_log2; row < n * 2 * heads; row += 256 >> lanes_log2) {
-        const int t = row / (2 * heads), which = row - t * 2 * heads, h = which < heads ? which : which - heads;
-        const int64_t p = g.start + t0 + t;
-        if (p >= a.sinks && t0 + t < g.len - period) continue;
-        const bool key = which < heads;
-        const idf_tokens &from = key ? a.k : a.v;
-        const T *src = (const T *)from.base + (g.begin + t0 + t) * from.token_stride + h * from.head_stride;
-        auto load = [&](int c, double (&y)[8]) IDF_INLINE {
-            if (ALIGNED) {
-                const P x = *(const P *)(src + c);
+    for (int row = row0; row < total; row += step) {
+        const Row now = next;
+        if (row + step < total) next = fetch(row + step);
+        const int t = now.t, h = now.h;
+        const bool key = now.key;
+        const int64_t slot = slots[t];
+        if (slot < 0) continue;
+        uint32_t codes, byte;
+        if (!key || plain) {
+            float x[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = E::to_f32(x.v[e]);
-            } else {
+            for (int e = 0; e < 8; ++e) x[e] = E::to_f32(now.x.v[e]);
+            bool close;
+            codes = encode<true>(x, byte, close);
+        } else {
+            double y[8], norm = 1.0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = E::to_f32(src[c + e]);
-            }
-        };
-        double y[8] = {};
-        if (on) load(c, y);
-        if (key) {
-            double norm = 1.0;
+            for (int e = 0; e < 8; ++e) y[e] = E::to_f32(now.x.v[e]);
             if (a.k_weight) {
                 double sum = 0.0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum += y[e] * y[e];
-                for (int m = 1; m < 1 << lanes_log2; m <<= 1) sum += __shfl_xor(sum, m);
-                norm = 1.0 / sqrt(sum / d + a.eps);
+                // 1 / sqrt by the instruction's start (some 26 bits) and two steps
+                sum = lanes_sum(sum, lanes_log2) * per_value + a.eps;
+                norm = __builtin_amdgcn_rsq(sum);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) norm = norm * __builtin_fma(-0.5 * sum * norm, norm, 1.5);
+                if (sum == __builtin_inf()) norm = 0.0;
                 if (on)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] *= norm * a.k_weight[c + e];
+                    for (int e = 0; e < 8; ++e) y[e] *= norm * weight[c + e];
             }
             if (on && c < a.rotary_dim) {
                 const double2 *cs = turn + t * half;
@@ -129,82 +268,62 @@ __global__ void __launch_bounds__(256) k_nibble_append(idf_nibble_append_args a,
                         y[e + 1] = w * r.x + u * r.y;
                     }
                 } else {
-                    double other[8] = {};
-                    if (half % 8 == 0) {
-                        load(c < half ? c + half : c - half, other);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (c + e < a.rotary_dim) other[e] = E::to_f32(src[c + e < half ? c + e + half : c + e - half]);
-                    }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const int i = c + e, j = i < half ? i + half : i - half;
                         if (i >= a.rotary_dim) continue;
-                        if (a.k_weight) other[e] *= norm * a.k_weight[j];
+                        const double q = E::to_f32(now.other.v[e]), o = a.k_weight ? q * (norm * weight[j]) : q;
                         const double2 r = cs[i < half ? i : j];
-                        y[e] = i < half ? y[e] * r.x - other[e] * r.y : y[e] * r.x + other[e] * r.y;
+                        y[e] = y[e] * r.x + (i < half ? -o : o) * r.y;
                     }
                 }
             }
-        }
-        double most = 0.0;
-        bool fine = true;
+            float near[8];
+            bool close;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const double v = __builtin_fabs(y[e]);
-            fine = fine && v < __builtin_inf();
-            most = fmax(most, v);
-        }
-        if (!fine) most = __builtin_inf();
-        most = fmax(most, __shfl_xor(most, 1));
-        most = fmax(most, __shfl_xor(most, 2));
-        fine = most < __builtin_inf();
-        // the smallest power with most <= 7 * 2^power: 7 is 1.75 * 2^2
-        const uint64_t bits = __builtin_bit_cast(uint64_t, most);
-        int power = (int)(bits >> 52) - 1023 - ((bits & 0xfffffffffffffull) <= 0xc000000000000ull ? 2 : 1);
-        power = fine ? min(max(power, -100), 125) : 0;
-        const double down = __builtin_bit_cast(double, (uint64_t)(1023 - power) << 52);
-        uint32_t codes = 0u;
-        if (fine) {
-            float f[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = fminf(fmaxf(to_odd(y[e] * down), -6.f), 6.f);
-            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[0], f[1], 1.f, 0);
-            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], 1.f, 1);
-            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], 1.f, 2);
-            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], 1.f, 3);
+            for (int e = 0; e < 8; ++e) near[e] = (float)y[e];
+            codes = encode<false>(near, byte, close);
+            if (__ballot(close)) codes = encode_exact(y, byte);
         }
         const Held4<uint8_t> to(key ? a.ring.k_codes : a.ring.v_codes, key ? a.ring.k_scales : a.ring.v_scales, a.slots, heads, d, g.ring, h);
-        const int64_t slot = p < a.sinks ? p : a.sinks + (p - a.sinks) % period;
         if (on) *(uint32_t *)(to.codes + slot * (d / 2) + c / 2) = codes;
-        if (on && lane % 4 == 0) to.scales[slot * (d / kBits) + lane / 4] = (uint8_t)(fine ? power + 127 : 255);
+        if (on && lane % 4 == 0) to.scales[slot * (d / kBits) + lane / 4] = (uint8_t)byte;
     }
 }
 
 // ---- what a ring stands for ----
 
-// A lane takes a block: 16 bytes of codes and one of the power to 32 values.  Bound by memory, most of it what is written.
+// A workgroup takes a head of a stream's keys or values and some of its slots, a lane eight values at a time: lanes read and write next to each other.  Bound by memory, most
+// of it what is written.
 template <int PREC>
-__global__ void __launch_bounds__(256) k_nibble_values(idf_nibble_values_args a, int64_t n)
+__global__ void __launch_bounds__(256) k_nibble_values(idf_nibble_values_args a)
 {
     using T = typename Elem<PREC>::type;
-    const int blocks = a.head_dim / kBits;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < 2 * n; i += (int64_t)gridDim.x * 256) {
-        const bool key = i < n;
-        const int64_t at = key ? i : i - n, row = at / blocks, token = row / a.heads_kv;
-        const int b = (int)(at - row * blocks), h = (int)(row - token * a.heads_kv);
-        const int64_t stream = token / a.slots, slot = token - stream * a.slots, from = (stream * a.heads_kv + h) * a.slots + slot;
-        const i32x4 codes = *(const i32x4 *)((key ? a.ring.k_codes : a.ring.v_codes) + from * (a.head_dim / 2) + b * 16);
-        const float power = power_of((key ? a.ring.k_scales : a.ring.v_scales)[from * blocks + b]);
-        T *to = (T *)(key ? a.k : a.v) + at * kBits;
+    constexpr int kAhead = 4;
+    const int lanes = a.head_dim / 8, rows = 256 / lanes, row = threadIdx.x / lanes, at = threadIdx.x - row * lanes;
+    if (row >= rows) return;
+    const int64_t head = blockIdx.y, stream = head / a.heads_kv, h = head - stream * a.heads_kv;
+    const bool key = blockIdx.z == 0;
+    const uint8_t *codes = (key ? a.ring.k_codes : a.ring.v_codes) + head * a.slots * (a.head_dim / 2) + at * 4;
+    const uint8_t *scales = (key ? a.ring.k_scales : a.ring.v_scales) + head * a.slots * (a.head_dim / kBits) + at / 4;
+    T *to = (T *)(key ? a.k : a.v) + (stream * a.slots * a.heads_kv + h) * a.head_dim + at * 8;
+    const int64_t step = (int64_t)gridDim.x * rows;
+    for (int64_t s = (int64_t)blockIdx.x * rows + row; s < a.slots; s += kAhead * step) {
+        uint32_t c[kAhead], p[kAhead];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const bf16x8 v = values8((uint32_t)codes[w], power);
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t slot = min(s + u * step, a.slots - 1);
+            c[u] = *(const uint32_t *)(codes + slot * (a.head_dim / 2));
+            p[u] = scales[slot * (a.head_dim / kBits)];
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (s + u * step >= a.slots) break;
+            const bf16x8 v = values8(c[u], power_of(p[u]));
             Pack<T, 8> out;
 #pragma unroll
             for (int e = 0; e < 8; ++e) out.v[e] = Elem<PREC>::from_f32((float)v[e]);
-            *(Pack<T, 8> *)(to + 8 * w) = out;
+            *(Pack<T, 8> *)(to + (s + u * step) * a.heads_kv * a.head_dim) = out;
         }
     }
 }
@@ -825,7 +944,7 @@ hipError_t append(const idf_nibble_append_args &a, const LaunchCtx &lc)
     while (8 << lanes_log2 < a.head_dim) ++lanes_log2;
     // workgroups for every compute unit first, then as many tokens as share a barrier
     const int64_t n = longest(a);
-    const int per = (int)std::max<int64_t>(1, std::min<int64_t>({n * a.n_segments / 1024, 8, n}));
+    const int per = (int)std::max<int64_t>(1, std::min<int64_t>({std::min<int64_t>(a.n_tokens, n * a.n_segments) / 1024, kMostTokens, n}));
     const dim3 grid((unsigned)((n + per - 1) / per), a.n_segments);
     const size_t lds = (size_t)per * (a.rotary_dim / 2) * sizeof(double2);
     return aligned ? launch(k_nibble_append<PREC, true>, grid, dim3(256), lds, lc, a, lanes_log2, per) : launch(k_nibble_append<PREC, false>, grid, dim3(256), lds, lc, a, lanes_log2, per);
@@ -840,9 +959,21 @@ hipError_t launch_nibble_append(const idf_nibble_append_args &a, const LaunchCtx
 
 hipError_t launch_nibble_values(const idf_nibble_values_args &a, const LaunchCtx &lc)
 {
-    const int64_t n = (int64_t)a.n_streams * a.slots * a.heads_kv * (a.head_dim / kBits);
-    const dim3 grid((unsigned)std::min<int64_t>((2 * n + 255) / 256, 1 << 16));
-    return a.precision == IDF_PREC_F32 ? launch(k_nibble_values<IDF_PREC_F32>, grid, dim3(256), 0, lc, a, n) : launch(k_nibble_values<IDF_PREC_BF16>, grid, dim3(256), 0, lc, a, n);
+    const int rows = 256 / (a.head_dim / 8);
+    const int64_t heads = (int64_t)a.n_streams * a.heads_kv;
+    // (a launch's second axis: more heads go in several launches)
+    for (int64_t first = 0; first < heads; first += 65536 / a.heads_kv * a.heads_kv - a.heads_kv) {
+        idf_nibble_values_args part = a;
+        const int64_t n = std::min<int64_t>(heads - first, 65536 / a.heads_kv * a.heads_kv - a.heads_kv), row = first * a.slots;
+        const int eb = a.precision == IDF_PREC_F32 ? 4 : 2;
+        part.ring = {a.ring.k_codes + row * (a.head_dim / 2), a.ring.k_scales + row * (a.head_dim / kBits), a.ring.v_codes + row * (a.head_dim / 2), a.ring.v_scales + row * (a.head_dim / kBits)};
+        part.k = (char *)a.k + row * a.head_dim * eb;
+        part.v = (char *)a.v + row * a.head_dim * eb;
+        const dim3 grid((unsigned)std::min<int64_t>((a.slots + rows * 4 - 1) / (rows * 4), std::max<int64_t>(1, 8192 / n)), (unsigned)n, 2);
+        const hipError_t e = a.precision == IDF_PREC_F32 ? launch(k_nibble_values<IDF_PREC_F32>, grid, dim3(256), 0, lc, part) : launch(k_nibble_values<IDF_PREC_BF16>, grid, dim3(256), 0, lc, part);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 size_t nibble_attend_workspace(const idf_nibble_attend_args &a) { return split_workspace(a, plan_of(a).splits); }
