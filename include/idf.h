@@ -553,7 +553,7 @@ int idf_quantize_rows(const idf_quantize_args *a, void *hip_stream);
  *   precision: that of x.  IDF_PREC_F32, IDF_PREC_BF16: rows are taken to codes and scales as by idf_quantize_rows, within the call;
  * IDF_PREC_I8: codes with x_scales [n_rows], cols and x.row_stride multiples of 16 and x.base 16-byte aligned.  out_precision IDF_PREC_F32 or
  * IDF_PREC_BF16.  weights int8 [n_out][cols rounded up to 16], 16-byte aligned; weight_scales, bias float32 [n_out], bias NULL: none.  out must not
- * overlap an input.  cols <= 65536, n_out <= 2^24. */
+ * overlap an input.  cols <= 65536, n_out <= 2^24, n_rows * n_out <= 2^37. */
 typedef struct {
     int precision, out_precision, cols, n_out;
     int64_t n_rows;
@@ -580,7 +580,7 @@ typedef struct {
 
 /* Segments' keys and values into their streams' rings, keys normalised and turned on the way as by idf_norm_rotate (a null weight: not
  * normalised; rotary_dim 0: not turned), in float64: a code does not depend on how that is rounded.  Of a segment longer than the ring its newest tokens are
- * written, and the first ones of the stream.  slots > sinks.  k and v need not be aligned.  starts NULL: 0. */
+ * written, and the first ones of the stream; segments of up to 2^26.  slots > sinks.  k and v need not be aligned.  starts NULL: 0. */
 typedef struct {
     int precision, heads_kv, head_dim, rotary_dim, interleaved;
     int64_t n_tokens, max_tokens;

@@ -79,18 +79,21 @@ __device__ __forceinline__ Summary join(const Summary &first, const Summary &the
 // How a call is cut: waves of a workgroup take parts of `part` tokens (a multiple of a block) behind each other, groups of them lie along y.
 struct Cut {
     int part, waves, groups;
+    int64_t rows;                                  // of summaries
     __device__ __host__ __forceinline__ int64_t span() const { return (int64_t)part * waves; }
 };
 
-// Summaries in the workspace, [segment][group][1 + waves][2][channels]: of the group, then of its parts.
-__device__ __forceinline__ float *summary_at(void *workspace, const Cut &cut, int segment, int group, int part, int channels)
+// Summaries in the workspace, [row][1 + waves][2][channels], a row for each group that has tokens: of the group, then of its parts.  As with the marks a segment's
+// first one goes by the tokens before it, so that there are as many as the tokens need and not as many as all segments would if they were as long as the longest.
+__device__ __forceinline__ float *summary_at(void *workspace, const Cut &cut, int64_t row, int part, int channels)
 {
-    return (float *)workspace + ((((int64_t)segment * cut.groups + group) * (1 + cut.waves) + part) * 2) * channels;
+    return (float *)workspace + ((row * (1 + cut.waves) + part) * 2) * channels;
 }
+__device__ __forceinline__ int64_t first_row(const Cut &cut, int64_t begin, int segment) { return (uint32_t)begin / (uint32_t)cut.span() + segment; }
 // Behind them the states (or gradients) that segments begin with, [segment][channels]: the last part may write to where they came from before others have read.
-__device__ __forceinline__ float *begin_at(void *workspace, const Cut &cut, int n_segments, int segment, int channels)
+__device__ __forceinline__ float *begin_at(void *workspace, const Cut &cut, int segment, int channels)
 {
-    return summary_at(workspace, cut, n_segments, 0, 0, channels) + (int64_t)segment * channels;
+    return summary_at(workspace, cut, cut.rows, 0, channels) + (int64_t)segment * channels;
 }
 template <int V> __device__ __forceinline__ void put(float *to, int channels, int c, const Summary (&s)[V])
 {
@@ -173,14 +176,15 @@ __device__ __forceinline__ float *marks_at(float *marks, const Work &w, int t, i
     return marks + (w.g.begin / kBlock + w.segment + t / kBlock) * channels + w.c;
 }
 
-template <int V> __device__ __forceinline__ void join_group(float *lds, const Work &w, const Cut &cut, void *workspace, int n_segments, int channels, const float *begin, const Summary (&s)[V], bool backwards)
+template <int V> __device__ __forceinline__ void join_group(float *lds, const Work &w, const Cut &cut, void *workspace, int channels, const float *begin, const Summary (&s)[V], bool backwards)
 {
     if (w.on && w.group == 0 && w.wave == 0) {
-        float *to = begin_at(workspace, cut, n_segments, w.segment, channels) + w.c;
+        float *to = begin_at(workspace, cut, w.segment, channels) + w.c;
 #pragma unroll
         for (int v = 0; v < V; ++v) to[v] = begin ? begin[(int64_t)w.g.ring * channels + w.c + v] : 0.f;
     }
-    if (w.on) put<V>(summary_at(workspace, cut, w.segment, w.group, 1 + w.wave, channels), channels, w.c, s);
+    const int64_t row = first_row(cut, w.g.begin, w.segment) + w.group;
+    if (w.on) put<V>(summary_at(workspace, cut, row, 1 + w.wave, channels), channels, w.c, s);
     float *mine = lds + (w.wave * 64 + (threadIdx.x & 63)) * 2 * V;
 #pragma unroll
     for (int v = 0; v < V; ++v) { mine[2 * v] = s[v].keep; mine[2 * v + 1] = s[v].made; }
@@ -194,7 +198,7 @@ template <int V> __device__ __forceinline__ void join_group(float *lds, const Wo
 #pragma unroll
         for (int v = 0; v < V; ++v) all[v] = join(all[v], Summary{its[2 * v], its[2 * v + 1]});
     }
-    put<V>(summary_at(workspace, cut, w.segment, w.group, 0, channels), channels, w.c, all);
+    put<V>(summary_at(workspace, cut, row, 0, channels), channels, w.c, all);
 }
 
 // ---- forward ----
@@ -293,7 +297,7 @@ __global__ void __launch_bounds__(512) k_gate_parts(idf_gate_scan_args a, Cut cu
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) s[v].made = h[v];
-    join_group<V>(lds, w, cut, a.workspace, a.n_segments, a.channels, a.state_in, s, false);
+    join_group<V>(lds, w, cut, a.workspace, a.channels, a.state_in, s, false);
 }
 
 template <int PREC, int V>
@@ -309,13 +313,13 @@ __global__ void __launch_bounds__(512) k_gate_out(idf_gate_scan_args a, Cut cut)
     if (w.t0 < w.t1) { x.load(xs, w.t0, w.t1); g.load(gs, w.t0, w.t1); }
     float h[V];
     const bool cuts = cut.groups * cut.waves > 1 && w.g.len > 0;
-    const float *begin = cuts ? begin_at(a.workspace, cut, a.n_segments, w.segment, a.channels) : a.state_in ? a.state_in + (int64_t)w.g.ring * a.channels : nullptr;
+    const float *begin = cuts ? begin_at(a.workspace, cut, w.segment, a.channels) : a.state_in ? a.state_in + (int64_t)w.g.ring * a.channels : nullptr;
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = begin ? begin[w.c + v] : 0.f;
     if (w.t0 > 0) {
-        const int64_t apart = 2 * (int64_t)a.channels;
-        go_through<V>(summary_at(a.workspace, cut, w.segment, 0, 0, a.channels), (1 + cut.waves) * apart, w.group, a.channels, w.c, h);
-        go_through<V>(summary_at(a.workspace, cut, w.segment, w.group, 1, a.channels), apart, w.wave, a.channels, w.c, h);
+        const int64_t apart = 2 * (int64_t)a.channels, row = first_row(cut, w.g.begin, w.segment);
+        go_through<V>(summary_at(a.workspace, cut, row, 0, a.channels), (1 + cut.waves) * apart, w.group, a.channels, w.c, h);
+        go_through<V>(summary_at(a.workspace, cut, row + w.group, 1, a.channels), apart, w.wave, a.channels, w.c, h);
     }
     for (int t = w.t0; t < w.t1; t += kBlock) {
         typename Rows<PREC, V>::P xn[kBlock], gn[kBlock];
@@ -424,7 +428,7 @@ __global__ void __launch_bounds__(256) k_gate_back_parts(idf_gate_scan_backward_
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) s[v].made = m[v];
-    join_group<V>(lds, w, cut, a.workspace, a.n_segments, a.channels, a.grad_end, s, true);
+    join_group<V>(lds, w, cut, a.workspace, a.channels, a.grad_end, s, true);
 }
 
 template <int PREC, int V>
@@ -465,16 +469,16 @@ __global__ void __launch_bounds__(256, 2) k_gate_back(idf_gate_scan_backward_arg
     if (w.t0 < w.t1) load(from, xs, gs, ds, mark);
     float m[V];
     const bool cuts = cut.groups * cut.waves > 1 && w.g.len > 0;
-    const float *end = cuts ? begin_at(a.workspace, cut, a.n_segments, w.segment, a.channels) : a.grad_end ? a.grad_end + (int64_t)w.g.ring * a.channels : nullptr;
+    const float *end = cuts ? begin_at(a.workspace, cut, w.segment, a.channels) : a.grad_end ? a.grad_end + (int64_t)w.g.ring * a.channels : nullptr;
 #pragma unroll
     for (int v = 0; v < V; ++v) m[v] = end ? end[w.c + v] : 0.f;
     if (w.t1 < w.g.len) {
-        const int64_t apart = 2 * (int64_t)a.channels;
+        const int64_t apart = 2 * (int64_t)a.channels, row = first_row(cut, w.g.begin, w.segment);
         // groups and parts that have tokens, the last first
         const int groups = (int)((w.g.len + cut.span() - 1) / cut.span());
         const int parts = (int)((min((int64_t)w.g.len, (w.group + 1) * cut.span()) - w.group * cut.span() + cut.part - 1) / cut.part);
-        go_through<V>(summary_at(a.workspace, cut, w.segment, groups - 1, 0, a.channels), -(1 + cut.waves) * apart, groups - 1 - w.group, a.channels, w.c, m);
-        go_through<V>(summary_at(a.workspace, cut, w.segment, w.group, parts, a.channels), -apart, parts - 1 - w.wave, a.channels, w.c, m);
+        go_through<V>(summary_at(a.workspace, cut, row + groups - 1, 0, a.channels), -(1 + cut.waves) * apart, groups - 1 - w.group, a.channels, w.c, m);
+        go_through<V>(summary_at(a.workspace, cut, row + w.group, parts, a.channels), -apart, parts - 1 - w.wave, a.channels, w.c, m);
     }
     for (int t = from; t >= w.t0; t -= kBlock) {
         typename R::P xn[kBlock], gn[kBlock], dn[kBlock] = {};
@@ -536,7 +540,7 @@ template <class Args> Cut cut_of(const Args &a, int most_waves)
 {
     const int64_t blocks = (longest(a) + kBlock - 1) / kBlock, wide = 64 * (pairs(a) ? 2 : 1);
     const int64_t lanes = (a.channels + wide - 1) / wide;                      // waves of a token
-    Cut c = {(int)std::max<int64_t>(blocks, 1) * kBlock, 1, 1};
+    Cut c = {(int)std::max<int64_t>(blocks, 1) * kBlock, 1, 1, 0};
     // blocks of a part so that all tokens that there are make kWaves waves, and more where the longest segment has no room for so many parts
     const int64_t all = std::min<int64_t>(a.n_tokens / kBlock + a.n_segments, a.n_segments * blocks);
     const int64_t part = std::max<int64_t>({(all * lanes + kWaves - 1) / kWaves, 1, (blocks + kMostGroups * most_waves - 1) / (kMostGroups * most_waves)});
@@ -545,13 +549,14 @@ template <class Args> Cut cut_of(const Args &a, int most_waves)
     c.waves = (int)std::min<int64_t>(parts <= kMostGroups * 4 ? 4 : most_waves, parts);
     c.part = (int)part * kBlock;
     c.groups = (int)((blocks * kBlock + c.span() - 1) / c.span());
+    c.rows = a.n_tokens / c.span() + a.n_segments;
     return c;
 }
 constexpr int kForwardWaves = 8, kBackwardWaves = 4;
 
 template <class Args> size_t summaries(const Args &a, const Cut &c)
 {
-    return c.groups * c.waves > 1 ? (size_t)a.n_segments * ((size_t)c.groups * (1 + c.waves) * 2 + 1) * a.channels * sizeof(float) : 0;
+    return c.groups * c.waves > 1 ? ((size_t)c.rows * (1 + c.waves) * 2 + a.n_segments) * a.channels * sizeof(float) : 0;
 }
 
 template <int PREC, int V>

@@ -21,6 +21,8 @@ constexpr int64_t kMostNibbleSlots = 1 << 24;           // places in a ring of 4
 constexpr int kMostCols = 65536;                   // sums of so many products of 8-bit codes stay below 2^31
 constexpr int kMostOuts = 1 << 24;
 constexpr int64_t kMostMatrixRows = (1 << 24) - 1; // a workgroup each: 2^32 threads
+constexpr int64_t kMostOutputs = (int64_t)1 << 37;  // of a product: 2^21 tiles of 256 x 256, which products that large go in
+constexpr int64_t kMostAppended = 1 << 26;        // tokens of a segment that go to a ring of 4-bit blocks, eight to a workgroup: a launch's first axis again
 constexpr int64_t kMostRowStride = 1 << 25;        // sixteen rows lie within 32 bits of bytes
 constexpr int kMostChannels = 1 << 20;
 
@@ -148,6 +150,7 @@ int check_project(const idf_project_args *a)
     if (a->cols < 1 || a->cols > kMostCols || (a->precision == IDF_PREC_I8 && a->cols % 16)) return fail(IDF_EUNSUPPORTED, "rows of %d values", a->cols);
     if (a->n_out < 1 || a->n_out > kMostOuts) return fail(IDF_EUNSUPPORTED, "%d outputs", a->n_out);
     if (a->n_rows < 0 || a->n_rows > kMostMatrixRows) return fail(IDF_EINVAL, "%lld rows", (long long)a->n_rows);
+    if (a->n_rows * a->n_out > kMostOutputs) return fail(IDF_EUNSUPPORTED, "%lld rows of %d outputs: more than a launch takes", (long long)a->n_rows, a->n_out);
     return IDF_OK;
 }
 
@@ -347,7 +350,7 @@ int idf_nibble_append(const idf_nibble_append_args *a, void *hip_stream)
     if (int rc = check_nibble(a->ring, a->head_dim, a->slots, a->sinks)) return rc;
     if (a->rotary_dim < 0 || a->rotary_dim > a->head_dim || a->rotary_dim % 2) return fail(IDF_EINVAL, "rotation of %d of %d values", a->rotary_dim, a->head_dim);
     if (!(a->eps >= 0.0) || !std::isfinite(a->amplitude)) return fail(IDF_EINVAL, "eps %g, amplitude %g", a->eps, a->amplitude);
-    if (longest(*a) > kMostTokens) return fail(IDF_EUNSUPPORTED, "segments of up to %lld tokens", (long long)longest(*a));
+    if (longest(*a) > kMostAppended) return fail(IDF_EUNSUPPORTED, "segments of up to %lld tokens", (long long)longest(*a));
     if (a->n_segments == 0 || longest(*a) == 0) return IDF_OK;
     const int eb = bytes_of(a->precision);
     for (const idf_tokens *t : {&a->k, &a->v}) {

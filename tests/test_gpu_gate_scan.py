@@ -303,3 +303,11 @@ def test_on_a_stream_of_its_own():
     torch.cuda.current_stream().wait_stream(side)
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("long_first", [True, False])
+def test_one_long_segment_among_many_short_ones(dtype, long_first):
+    """Summaries lie by the tokens before a segment: none of them lies on another's, wherever the long segment stands and ends."""
+    short = [i * 7 % 5 for i in range(90)] + [16, 32, 31, 160, 161, 0, 0]
+    check([2500] + short if long_first else short + [2500, 1, 0, 1100, 3], 70, dtype, seed=21)
