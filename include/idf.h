@@ -631,7 +631,8 @@ int idf_nibble_values(const idf_nibble_values_args *a, void *hip_stream);
  * with gates held to -87 .. 87 (neither what is kept nor what is taken in is ever nothing: an infinite state stays infinite).  state_in, state_out: float32
  * [n_streams][channels], from the state of the segment's stream before it to the one after it, as in idf_decay_attend.  States are float32 throughout.
  *   marks (NULL: not wanted): what the backward pass needs beside x and gates, states within the segments, idf_gate_scan_marks bytes, 256-byte
- * aligned.  Rows need no alignment beyond their values'.  1 <= channels <= 2^20; segments of up to 2^30 tokens. */
+ * aligned.  Rows need no alignment beyond their values'.  1 <= channels <= 2^20; segments of up to 2^30 tokens; where one has more than 128,
+ * (n_tokens / 128 + n_segments) * channels / 64 < 2^23. */
 typedef struct {
     int precision, channels;
     int64_t n_tokens, max_tokens;

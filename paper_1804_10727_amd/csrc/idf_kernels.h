@@ -134,6 +134,8 @@ hipError_t launch_nibble_append(const idf_nibble_append_args &a, const LaunchCtx
 hipError_t launch_nibble_values(const idf_nibble_values_args &a, const LaunchCtx &lc);
 size_t nibble_attend_workspace(const idf_nibble_attend_args &a);
 hipError_t launch_nibble_attend(const idf_nibble_attend_args &a, const LaunchCtx &lc);
+int64_t gate_scan_tiles(const idf_gate_scan_args &a);                     // workgroups of a launch, 0: not too many
+int64_t gate_scan_tiles(const idf_gate_scan_backward_args &a);
 size_t gate_scan_marks(int64_t n_tokens, int n_segments, int channels);
 size_t gate_scan_workspace(const idf_gate_scan_args &a);
 hipError_t launch_gate_scan(const idf_gate_scan_args &a, const LaunchCtx &lc);

@@ -3,11 +3,11 @@
 //   h_t = a_t h_{t-1} + b_t x_t,  a = sigmoid(g), b = 1 - a.  Of a and b the smaller one, e / (1 + e) with e = exp(-|g|), is formed, and a step taken as
 // h + b (x - h) or x + a (h - x): the larger one, rounded to a number near one, would be off in the same direction again and again where gates stay the
 // same.  A part of a segment takes a state h to k h + n, with n what the part gives from nothing and k the product of its a, formed in the same way.
-//   A lane has V neighbouring channels, a wave 64 V of them, and goes along the tokens 16 at a time with the next 16 on their way.  Segments are cut
-// into parts along time where channels and segments are too few for the machine: their summaries first, then every part from the state that
-// those before it give (x and gates are read twice then).  States within a segment before every 16th token are what the backward pass
-// starts from: it forms the 16 states of a block anew, in registers, and goes back through them.
-//   What infinite values, gates that are no numbers and gates beyond +-87 ask for is done where a block has any: once more for that block.
+//   A lane has V neighbouring channels, a wave 64 V of them and 16 or 32 tokens, which it reads once: they stay in registers with their gates while the state that
+// they begin with is found out.  A tile is up to eight waves behind each other, one workgroup; a long segment has many, which hand summaries on through memory.
+// States within a segment before every 16th token are what the backward pass starts from: it forms the 16 states of a block anew, in registers, and
+// goes back through them.
+//   What infinite values and gates that are no numbers ask for is done where a block has any: once more for that block, by the definition and from memory.
 #include <algorithm>
 
 #include "idf.h"
@@ -18,7 +18,6 @@ namespace idf {
 namespace {
 
 constexpr int kBlock = 16;                         // tokens that a wave has in registers
-constexpr int kMostGroups = 64;                    // groups of parts of a segment: every part goes through the summaries of those before it
 constexpr float kGateMost = 87.f;
 
 // The smaller one of what a gate keeps and takes in, with the gate's sign: above zero it is what is taken in.
@@ -76,55 +75,21 @@ __device__ __forceinline__ float through(const Summary &s, float h)
 }
 __device__ __forceinline__ Summary join(const Summary &first, const Summary &then) { return {first.keep * then.keep, through(then, first.made)}; }
 
-// How a call is cut: waves of a workgroup take parts of `part` tokens (a multiple of a block) behind each other, groups of them lie along y.
-struct Cut {
-    int part, waves, groups;
-    int64_t rows;                                  // of summaries
-    __device__ __host__ __forceinline__ int64_t span() const { return (int64_t)part * waves; }
+// V values as they lie in memory: two of 16 bits stay in one register until they are asked for.
+template <int PREC, int V> struct Raw {
+    using T = typename Elem<PREC>::type;
+    T bits;
+    __device__ __forceinline__ float get(int) const { return Elem<PREC>::to_f32(bits); }
 };
-
-// Summaries in the workspace, [row][1 + waves][2][channels], a row for each group that has tokens: of the group, then of its parts.  As with the marks a segment's
-// first one goes by the tokens before it, so that there are as many as the tokens need and not as many as all segments would if they were as long as the longest.
-__device__ __forceinline__ float *summary_at(void *workspace, const Cut &cut, int64_t row, int part, int channels)
-{
-    return (float *)workspace + ((row * (1 + cut.waves) + part) * 2) * channels;
-}
-__device__ __forceinline__ int64_t first_row(const Cut &cut, int64_t begin, int segment) { return (uint32_t)begin / (uint32_t)cut.span() + segment; }
-// Behind them the states (or gradients) that segments begin with, [segment][channels]: the last part may write to where they came from before others have read.
-__device__ __forceinline__ float *begin_at(void *workspace, const Cut &cut, int segment, int channels)
-{
-    return summary_at(workspace, cut, cut.rows, 0, channels) + (int64_t)segment * channels;
-}
-template <int V> __device__ __forceinline__ void put(float *to, int channels, int c, const Summary (&s)[V])
-{
-#pragma unroll
-    for (int v = 0; v < V; ++v) { to[c + v] = s[v].keep; to[channels + c + v] = s[v].made; }
-}
-
-// The state (or gradient) h goes through n summaries that lie `apart` floats from each other; several are asked for at once.
-template <int V> __device__ __forceinline__ void go_through(const float *from, int64_t apart, int n, int channels, int c, float (&h)[V])
-{
-    constexpr int kAhead = 8;
-    for (int i = 0; i < n; i += kAhead) {
-        Summary s[kAhead][V];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const float *at = from + (int64_t)min(i + j, n - 1) * apart + c;
-#pragma unroll
-            for (int v = 0; v < V; ++v) s[j][v] = {at[v], at[channels + v]};
-        }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (i + j < n)
-#pragma unroll
-                for (int v = 0; v < V; ++v) h[v] = through(s[j][v], h[v]);
-    }
-}
+template <> struct Raw<IDF_PREC_BF16, 2> {
+    uint32_t bits;
+    __device__ __forceinline__ float get(int v) const { return __builtin_bit_cast(float, v ? bits & 0xffff0000u : bits << 16); }
+};
 
 // A matrix from a segment's first row on: an address that is the wave's own per block, and offsets of 32 bits in it (rows lie at most 2^25 values apart).
 template <int PREC, int V> struct Rows {
     using T = typename Elem<PREC>::type;
-    using P = Pack<T, V>;
+    using P = Raw<PREC, V>;
     const char *base;
     uint32_t stride, lane;                         // in bytes
     __device__ __forceinline__ Rows(const idf_rows &r, int64_t row, int c)
@@ -141,12 +106,13 @@ template <int PREC, int V> struct Rows {
             for (int u = 0; u < kBlock; ++u) to[u] = *(const P *)(at + (lane + (uint32_t)min(u, n - 1 - t) * stride));
         }
     }
+    __device__ __forceinline__ P row(int t) const { return *(const P *)(base + (int64_t)t * stride + lane); }
     __device__ __forceinline__ void store(int t, int u, const float (&v)[V]) const
     {
-        P p;
+        Pack<T, V> p;
 #pragma unroll
         for (int i = 0; i < V; ++i) p.v[i] = Elem<PREC>::from_f32(v[i]);
-        *(P *)(const_cast<char *>(base) + (int64_t)t * stride + (lane + u * stride)) = p;
+        *(Pack<T, V> *)(const_cast<char *>(base) + (int64_t)t * stride + (lane + u * stride)) = p;
     }
 };
 
@@ -156,367 +122,479 @@ struct Work {
     int segment, group, wave, c, t0, t1;
     bool on;
 };
-template <int V, class Args> __device__ __forceinline__ Work work_of(const Args &a, const Cut &cut, int group)
-{
-    Work w;
-    w.segment = blockIdx.z;
-    w.group = group;
-    w.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    w.g = segment_of(a, w.segment, nullptr);
-    w.c = (blockIdx.x * 64 + (threadIdx.x & 63)) * V;
-    w.on = w.c < a.channels;
-    if (!w.on) w.c = a.channels - V;               // (reads what is there, stores nothing)
-    w.t0 = (int)min((int64_t)w.g.len, group * cut.span() + (int64_t)w.wave * cut.part);
-    w.t1 = min(w.g.len, w.t0 + cut.part);
-    return w;
-}
 // the first token of a segment has a row of marks of its own, whatever the others' lengths are
 __device__ __forceinline__ float *marks_at(float *marks, const Work &w, int t, int channels)
 {
     return marks + (w.g.begin / kBlock + w.segment + t / kBlock) * channels + w.c;
 }
 
-template <int V> __device__ __forceinline__ void join_group(float *lds, const Work &w, const Cut &cut, void *workspace, int channels, const float *begin, const Summary (&s)[V], bool backwards)
+// Rows that no segment has have no gradient: those in front of the first one, and from a segment's last token to the next one.
+template <int PREC, int V> __device__ __forceinline__ void clear_between(const idf_gate_scan_backward_args &a, const Work &w)
 {
-    if (w.on && w.group == 0 && w.wave == 0) {
-        float *to = begin_at(workspace, cut, w.segment, channels) + w.c;
+    const float zero[V] = {};
+    auto clear = [&](int64_t from, int64_t to) {
+        for (int64_t t = from; t < to; ++t)
+            if (w.on) {
+                Rows<PREC, V>(a.grad_x, t, w.c).store(0, 0, zero);
+                Rows<PREC, V>(a.grad_gates, t, w.c).store(0, 0, zero);
+            }
+    };
+    const bool last = w.segment + 1 == a.n_segments;
+    if (a.offsets && w.segment == 0) clear(0, w.g.begin);
+    clear(w.g.begin + w.g.len, last ? a.n_tokens : a.offsets ? min(max(a.offsets[w.segment + 1], (int64_t)0), a.n_tokens) : w.g.begin + a.max_tokens);
+}
+
+// ---- tiles ----
+
+// A tile is W waves of K blocks each, one behind the other.  Its tokens are read once and stay in registers with their gates: every wave first makes its summary, and goes
+// through its tokens again when it knows what it begins with.  A segment of one tile needs no more than its workgroup for that.  Tiles of longer ones tell
+// each other through memory: each makes its summary known, and gathers those of the tiles since the last row whose number is a multiple of chain_of(K), in front of
+// which a state is made known too (that way follows the tokens one by one, 4096 in 2.5 us; eight rows to a state left 65536 tokens of 1024 channels at 162 us instead of 108).
+// What is combined and in what order does not depend on who comes first.  A word that is not there yet is all ones (no
+// number that is stored has these bits) and holds all that it tells, so that nothing else has to be seen with it.  Tiles are numbered in the order in which workgroups begin,
+// and wait for lower numbers only, which have begun; a tile makes known what others may wait for whatever its segment looks like.
+//   Bound by memory: x, gates and results once, and 4 to 12 bytes a channel that tiles tell each other for every 128 or 256 tokens.  65536 tokens of 2048 channels, bfloat16:
+// forward 189 us, 4.3 TB/s, backward 309, 4.35; 262144 of 2048 in float32 5.7 TB/s both.  (Summaries in a launch of their own, and everything read again from
+// the states that they give, 308 and 436.)  All of it in 128 registers, for two workgroups to a compute unit: what one waits for the other hides.
+constexpr int kTileWaves = 8;
+constexpr int each_of(int blocks) { return 4 / blocks; }                     // tiles that a wave gathers
+constexpr int chain_of(int blocks) { return kTileWaves * each_of(blocks); }
+constexpr int kMostTries = 1 << 22;                // seconds; what is not there then is taken as no number
+constexpr uint64_t kAbsent = ~(uint64_t)0;
+struct Tiling {
+    int span, cols;                                // tokens of a tile, tiles side by side
+    int64_t rows;                                  // of tiles behind each other
+};
+// In the workspace: a counter in 256 bytes, [row][channels] summaries of 8 bytes, [row / kChain][channels] states.
+__device__ __forceinline__ uint64_t *told_at(void *workspace, int64_t row, int channels) { return (uint64_t *)((char *)workspace + 256) + row * channels; }
+__device__ __forceinline__ uint32_t *state_at(void *workspace, const Tiling &tl, int64_t link, int channels)
+{
+    return (uint32_t *)told_at(workspace, tl.rows, channels) + link * channels;
+}
+__device__ __forceinline__ uint32_t told(float v) { return v == v ? __builtin_bit_cast(uint32_t, v) : 0x7fc00000u; }
+
+template <class Word> __device__ __forceinline__ void tell(Word *to, Word w) { __hip_atomic_store(to, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// V neighbouring words of each of n rows that lie `apart` words from each other, once all that the wave asks for are there
+template <int V, int N, class Word> __device__ __forceinline__ void hear(const Word *from, int64_t apart, int n, Word (&to)[N][V])
+{
+    for (int tries = 0;; ++tries) {
+        bool there = true;
 #pragma unroll
-        for (int v = 0; v < V; ++v) to[v] = begin ? begin[(int64_t)w.g.ring * channels + w.c + v] : 0.f;
+        for (int i = 0; i < N; ++i)
+            if (i < n)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    to[i][v] = __hip_atomic_load(from + i * apart + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    there = there && to[i][v] != (Word)kAbsent;
+                }
+        if (__all(there) || tries == kMostTries) return;
+        __builtin_amdgcn_s_sleep(1);
     }
-    const int64_t row = first_row(cut, w.g.begin, w.segment) + w.group;
-    if (w.on) put<V>(summary_at(workspace, cut, row, 1 + w.wave, channels), channels, w.c, s);
-    float *mine = lds + (w.wave * 64 + (threadIdx.x & 63)) * 2 * V;
+}
+
+__global__ void __launch_bounds__(256) k_gate_absent(uint4 *to, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) to[i] = uint4{~0u, ~0u, ~0u, ~0u};
+}
+
+// The segment that a row of tiles is one of: the last one whose first row is not behind it.
+template <class Args> __device__ __forceinline__ int64_t first_row(const Args &a, const Tiling &tl, int s)
+{
+    const int64_t begin = a.offsets ? min(max(a.offsets[s], (int64_t)0), a.n_tokens) : s * a.max_tokens;
+    return (uint32_t)begin / (uint32_t)tl.span + s;
+}
+template <class Args> __device__ __forceinline__ int segment_at(const Args &a, const Tiling &tl, int64_t row)
+{
+    int at = 0, n = a.n_segments;
+    while (n > 1) {
+        const int step = (n + 63) / 64, i = (threadIdx.x & 63) * step;
+        const uint64_t below = __ballot(i < n && first_row(a, tl, at + min(i, n - 1)) <= row);
+        const int k = below ? (63 - __builtin_clzll(below)) * step : 0;
+        at += k;
+        n = min(step, n - k);
+    }
+    return __builtin_amdgcn_readfirstlane(at);
+}
+
+// What a workgroup's waves tell each other: summaries of the waves, then of the tiles before this one, and what all of them begin with.
+template <int V> struct Board {
+    float own[kTileWaves][64][2 * V], before[kTileWaves][64][2 * V], start[64][V];
+};
+template <int V> __device__ __forceinline__ void pin(float (&at)[2 * V], const Summary (&s)[V])
+{
 #pragma unroll
-    for (int v = 0; v < V; ++v) { mine[2 * v] = s[v].keep; mine[2 * v + 1] = s[v].made; }
+    for (int v = 0; v < V; ++v) { at[2 * v] = s[v].keep; at[2 * v + 1] = s[v].made; }
+}
+template <int V> __device__ __forceinline__ void through(const float (&at)[2 * V], float (&h)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = through(Summary{at[2 * v], at[2 * v + 1]}, h[v]);
+}
+
+// A tile's place: which row and channels, and the tokens of each wave.
+struct Tile {
+    Work w;
+    int64_t row;
+    int order, waves;                              // order: of this wave among its tile's, in the direction that the states go
+    bool edge;                                     // nothing of the segment comes before it in that direction
+    int links;                                     // tiles before it, as far as the state that it begins with, and whether there is one
+    bool linked;
+};
+template <int V, int K, bool CHAIN, bool BACK, class Args> __device__ __forceinline__ bool tile_of(const Args &a, const Tiling &tl, Tile &x)
+{
+    constexpr int kChain = chain_of(K);
+    x.waves = blockDim.x >> 6;
+    int col = blockIdx.x, segment = blockIdx.y;
+    x.row = 0;
+    if (CHAIN) {
+        __shared__ uint32_t ticket;
+        if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add((uint32_t *)a.workspace, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u;
+        __syncthreads();
+        const uint32_t n = __builtin_amdgcn_readfirstlane(ticket);
+        const int64_t row = n / (uint32_t)tl.cols;
+        if (row >= tl.rows) return false;
+        col = (int)(n - (uint32_t)row * (uint32_t)tl.cols);
+        x.row = BACK ? tl.rows - 1 - row : row;
+        segment = segment_at(a, tl, x.row);
+    }
+    Work &w = x.w;
+    w.segment = segment;
+    w.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    w.g = segment_of(a, segment, nullptr);
+    w.c = (col * 64 + (int)(threadIdx.x & 63)) * V;
+    w.on = w.c < a.channels;
+    if (!w.on) w.c = a.channels - V;
+    const int64_t first = CHAIN ? first_row(a, tl, segment) : 0, tokens = K * kBlock;
+    w.group = (int)(x.row - first);
+    if (w.group < 0) { w.group = 1; w.g.len = 0; w.g.valid = false; }             // (offsets that do not go up)
+    const int64_t t0 = (int64_t)w.group * tl.span + w.wave * tokens;
+    w.t0 = (int)min((int64_t)w.g.len, t0);
+    w.t1 = (int)min((int64_t)w.g.len, t0 + tokens);
+    x.order = BACK ? x.waves - 1 - w.wave : w.wave;
+    const int64_t last = first + (w.g.len > 0 ? (w.g.len - 1) / tl.span : 0);
+    x.edge = BACK ? x.row == last : w.group == 0;
+    const int64_t block = x.row / kChain * kChain;
+    x.links = (int)(BACK ? min(last, block + kChain - 1) - x.row : x.row - max(first, block));
+    x.linked = BACK ? block + kChain - 1 < last : first < block;
+    return true;
+}
+
+// From the waves' summaries to what each begins with.  All waves of a workgroup come here.
+template <int V, int K, bool CHAIN, bool BACK, class Args>
+__device__ __forceinline__ void begin_of(const Args &a, const Tiling &tl, const Tile &x, Board<V> &b, const float *begin, const Summary (&s)[V], float (&h)[V])
+{
+    constexpr int kEach = each_of(K), kChain = chain_of(K);
+    const int lane = threadIdx.x & 63, c = x.w.c;
+    if (x.order == x.waves - 1 && (!CHAIN || x.edge)) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) b.start[lane][v] = begin ? begin[(int64_t)x.w.g.ring * a.channels + c + v] : 0.f;
+    }
+    pin<V>(b.own[x.order][lane], s);
     lds_barrier();
-    if (w.wave != 0 || !w.on) return;
-    Summary all[V];
+    if (CHAIN) {
+        if (x.order == 0) {
+            Summary all[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) all[v] = {1.f, 0.f};
-    for (int i = 0; i < cut.waves; ++i) {
-        const float *its = lds + ((backwards ? cut.waves - 1 - i : i) * 64 + (threadIdx.x & 63)) * 2 * V;
+            for (int v = 0; v < V; ++v) all[v] = {1.f, 0.f};
+            for (int i = 0; i < x.waves; ++i)
 #pragma unroll
-        for (int v = 0; v < V; ++v) all[v] = join(all[v], Summary{its[2 * v], its[2 * v + 1]});
-    }
-    put<V>(summary_at(workspace, cut, row, 0, channels), channels, w.c, all);
-}
-
-// ---- forward ----
-
-// f(0), f(1), .. of the n first rows of a block, or in the other order; whole blocks without a look at n.
-template <class F> __device__ __forceinline__ void rows_up(int n, F f)
-{
-    if (n >= kBlock) {
-#pragma unroll
-        for (int u = 0; u < kBlock; ++u) f(u);
-    } else {
-#pragma unroll
-        for (int u = 0; u < kBlock; ++u)
-            if (u < n) f(u);
-    }
-}
-template <class F> __device__ __forceinline__ void rows_down(int n, F f)
-{
-    if (n >= kBlock) {
-#pragma unroll
-        for (int u = kBlock - 1; u >= 0; --u) f(u);
-    } else {
-#pragma unroll
-        for (int u = kBlock - 1; u >= 0; --u)
-            if (u < n) f(u);
-    }
-}
-
-// The states after each of the n first rows of a block: each(u, h, gates).  Where one comes out infinite or not a number, or a gate is out of bounds,
-// the block is taken once more by the definition.
-template <int PREC, int V, class P, class F>
-__device__ __forceinline__ void states(const P (&x)[kBlock], const P (&g)[kBlock], int n, float (&h)[V], F each)
-{
-    float was[V], far = 0.f;
-    bool fine = true;
-#pragma unroll
-    for (int v = 0; v < V; ++v) was[v] = h[v];
-    rows_up(n, [&](int u) IDF_INLINE {
-        Gate w[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float gate = Elem<PREC>::to_f32(g[u].v[v]);
-            far = fmaxf(far, __builtin_fabsf(gate));
-            w[v] = gate_of<PREC>(gate);
-            h[v] = step_of(w[v], Elem<PREC>::to_f32(x[u].v[v]), h[v]);
-        }
-        each(u, h, w);
-    });
-#pragma unroll
-    for (int v = 0; v < V; ++v) fine = fine && finite(h[v]);
-    if (fine && far <= kGateMost) return;
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = was[v];
-#pragma unroll
-    for (int u = 0; u < kBlock; ++u)
-        if (u < n) {
-            Gate w[V];
+                for (int v = 0; v < V; ++v) all[v] = join(all[v], Summary{b.own[i][lane][2 * v], b.own[i][lane][2 * v + 1]});
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Slow<PREC> slow(Elem<PREC>::to_f32(g[u].v[v]));
-                w[v] = slow.w;
-                h[v] = slow.step(Elem<PREC>::to_f32(x[u].v[v]), h[v]);
+                if (x.edge) all[v] = {0.f, through(all[v], b.start[lane][v])};         // (whatever comes before is another segment's)
+                if (x.w.on) tell(told_at(a.workspace, x.row, a.channels) + c + v, told(all[v].keep) | (uint64_t)told(all[v].made) << 32);
             }
-            each(u, h, w);
         }
+        // the tiles before this one, kEach to a wave
+        if (x.order * kEach < x.links) {
+            const int from = x.order * kEach, n = min(kEach, x.links - from);
+            const int64_t row = BACK ? x.row + x.links - from : x.row - x.links + from;
+            uint64_t word[kEach][V];
+            hear<V, kEach>(told_at(a.workspace, row, a.channels) + c, BACK ? -(int64_t)a.channels : a.channels, n, word);
+            Summary all[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) all[v] = {1.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (i < n)
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        all[v] = join(all[v], Summary{__builtin_bit_cast(float, (uint32_t)word[i][v]), __builtin_bit_cast(float, (uint32_t)(word[i][v] >> 32))});
+            pin<V>(b.before[x.order][lane], all);
+        }
+        if (x.order == x.waves - 1 && !x.edge) {
+            uint32_t word[1][V] = {};
+            if (x.linked) hear<V, 1>(state_at(a.workspace, tl, x.row / kChain, a.channels) + c, 0, 1, word);
+#pragma unroll
+            for (int v = 0; v < V; ++v) b.start[lane][v] = __builtin_bit_cast(float, word[0][v]);
+        }
+        lds_barrier();
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = b.start[lane][v];
+    if (CHAIN) {
+        for (int i = 0; i * kEach < x.links; ++i) through<V>(b.before[i][lane], h);
+        const int64_t next = BACK ? x.row / kChain - 1 : x.row / kChain + 1;
+        if (x.order == 0 && x.row % kChain == (BACK ? 0 : kChain - 1) && next >= 0) {
+            float end[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) end[v] = h[v];
+            for (int i = 0; i < x.waves; ++i) through<V>(b.own[i][lane], end);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (x.w.on) tell(state_at(a.workspace, tl, next, a.channels) + c + v, told(end[v]));
+        }
+    }
+    for (int i = 0; i < x.order; ++i) through<V>(b.own[i][lane], h);
+}
+// A tile without tokens makes known that it changes nothing.
+template <int V, int K, bool BACK, class Args> __device__ __forceinline__ void pass_over(const Args &a, const Tiling &tl, const Tile &x)
+{
+    constexpr int kChain = chain_of(K);
+    if (x.w.wave != 0 || !x.w.on) return;
+    const int64_t next = BACK ? x.row / kChain - 1 : x.row / kChain + 1;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        tell(told_at(a.workspace, x.row, a.channels) + x.w.c + v, (uint64_t)told(1.f));
+        if (x.row % kChain == (BACK ? 0 : kChain - 1) && next >= 0) tell(state_at(a.workspace, tl, next, a.channels) + x.w.c + v, told(0.f));
+    }
 }
 
-template <int PREC, int V>
-__global__ void __launch_bounds__(512) k_gate_parts(idf_gate_scan_args a, Cut cut)
+// A gate held to its bounds.
+template <int PREC> __device__ __forceinline__ Gate held_gate(float g)
 {
-    extern __shared__ float lds[];
-    const Work w = work_of<V>(a, cut, blockIdx.y);
-    if (w.group * cut.span() >= w.g.len) return;
-    const Rows<PREC, V> x(a.x, w.g.begin, w.c), g(a.gates, w.g.begin, w.c);
-    typename Rows<PREC, V>::P xs[kBlock], gs[kBlock];
+    return gate_of<PREC>(__builtin_fabsf(g) > kGateMost ? __builtin_copysignf(kGateMost, g) : g);
+}
+
+template <int PREC, int V, int K, bool CHAIN>
+__global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_tile(idf_gate_scan_args a, Tiling tl)
+{
+    __shared__ Board<V> board;
+    Tile tile;
+    if (!tile_of<V, K, CHAIN, false>(a, tl, tile)) return;
+    const Work &w = tile.w;
+    if (w.g.len <= (int64_t)w.group * tl.span) {
+        if (CHAIN) pass_over<V, K, false>(a, tl, tile);
+        if (w.g.valid && w.group == 0 && w.wave == 0 && w.on && a.state_out)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int64_t i = (int64_t)w.g.ring * a.channels + w.c + v;
+                a.state_out[i] = a.state_in ? a.state_in[i] : 0.f;
+            }
+        return;
+    }
+    using R = Rows<PREC, V>;
+    const R x(a.x, w.g.begin, w.c), g(a.gates, w.g.begin, w.c), out(a.out, w.g.begin, w.c);
+    typename R::P xs[K][kBlock], gs[K][kBlock];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (w.t0 + k * kBlock < w.t1) { g.load(gs[k], w.t0 + k * kBlock, w.t1); x.load(xs[k], w.t0 + k * kBlock, w.t1); }
+    float gate[K][kBlock][V], h[V];
     Summary s[V];
-    float h[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) { s[v] = {1.f, 0.f}; h[v] = 0.f; }
-    if (w.t0 < w.t1) { x.load(xs, w.t0, w.t1); g.load(gs, w.t0, w.t1); }
-    for (int t = w.t0; t < w.t1; t += kBlock) {
-        typename Rows<PREC, V>::P xn[kBlock], gn[kBlock];
-        if (t + kBlock < w.t1) { x.load(xn, t + kBlock, w.t1); g.load(gn, t + kBlock, w.t1); }
-        Summary was[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) was[v] = s[v];
-        states<PREC, V>(xs, gs, min(kBlock, w.t1 - t), h, [&](int u, float (&)[V], Gate (&w)[V]) IDF_INLINE {
+    // the rows of a block by the definition, from memory: h, and each row's gates
+    auto slow = [&](int t, int n, auto each) IDF_INLINE {
+        for (int u = 0; u < n; ++u) {
+            const typename R::P xr = x.row(t + u), gr = g.row(t + u);
+            Gate one[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                if (u == 0) s[v] = was[v];
-                s[v].keep = kept_of(w[v], s[v].keep);
+                const Slow<PREC> it(gr.get(v));
+                h[v] = it.step(xr.get(v), h[v]);
+                one[v] = it.w;
             }
-        });
+            each(u, one);
+        }
+    };
 #pragma unroll
-        for (int u = 0; u < kBlock; ++u) { xs[u] = xn[u]; gs[u] = gn[u]; }
+    for (int k = 0; k < K; ++k) {
+        const int t = w.t0 + k * kBlock, n = w.t1 - t;
+        if (n <= 0) break;
+        float was[V], kept[V];
+        bool fine = true;
+#pragma unroll
+        for (int v = 0; v < V; ++v) { was[v] = h[v]; kept[v] = s[v].keep; }
+#pragma unroll
+        for (int u = 0; u < kBlock; ++u)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                // (a row that is not there leaves the state as it is)
+                const Gate one = u < n ? held_gate<PREC>(gs[k][u].get(v)) : Gate{0.f};
+                gate[k][u][v] = one.s;
+                h[v] = step_of(one, xs[k][u].get(v), h[v]);
+                s[v].keep = kept_of(one, s[v].keep);
+            }
+#pragma unroll
+        for (int v = 0; v < V; ++v) fine = fine && finite(h[v]);
+        if (!fine) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) { h[v] = was[v]; s[v].keep = kept[v]; }
+            slow(t, min(n, kBlock), [&](int, Gate (&one)[V]) IDF_INLINE {
+#pragma unroll
+                for (int v = 0; v < V; ++v) s[v].keep = kept_of(one[v], s[v].keep);
+            });
+        }
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) s[v].made = h[v];
-    join_group<V>(lds, w, cut, a.workspace, a.channels, a.state_in, s, false);
-}
-
-template <int PREC, int V>
-__global__ void __launch_bounds__(512) k_gate_out(idf_gate_scan_args a, Cut cut)
-{
-    // parts that were read last come first: they are still in the caches
-    const Work w = work_of<V>(a, cut, gridDim.y - 1 - blockIdx.y);
-    if (!w.g.valid) return;
-    const bool last = w.t1 == w.g.len && (w.t0 < w.t1 || (w.g.len == 0 && w.group == 0 && w.wave == 0));
-    if (w.t0 >= w.t1 && !last) return;
-    const Rows<PREC, V> x(a.x, w.g.begin, w.c), g(a.gates, w.g.begin, w.c), out(a.out, w.g.begin, w.c);
-    typename Rows<PREC, V>::P xs[kBlock], gs[kBlock];
-    if (w.t0 < w.t1) { x.load(xs, w.t0, w.t1); g.load(gs, w.t0, w.t1); }
-    float h[V];
-    const bool cuts = cut.groups * cut.waves > 1 && w.g.len > 0;
-    const float *begin = cuts ? begin_at(a.workspace, cut, w.segment, a.channels) : a.state_in ? a.state_in + (int64_t)w.g.ring * a.channels : nullptr;
+    begin_of<V, K, CHAIN, false>(a, tl, tile, board, a.state_in, s, h);
 #pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = begin ? begin[w.c + v] : 0.f;
-    if (w.t0 > 0) {
-        const int64_t apart = 2 * (int64_t)a.channels, row = first_row(cut, w.g.begin, w.segment);
-        go_through<V>(summary_at(a.workspace, cut, row, 0, a.channels), (1 + cut.waves) * apart, w.group, a.channels, w.c, h);
-        go_through<V>(summary_at(a.workspace, cut, row + w.group, 1, a.channels), apart, w.wave, a.channels, w.c, h);
-    }
-    for (int t = w.t0; t < w.t1; t += kBlock) {
-        typename Rows<PREC, V>::P xn[kBlock], gn[kBlock];
-        if (t + kBlock < w.t1) { x.load(xn, t + kBlock, w.t1); g.load(gn, t + kBlock, w.t1); }
+    for (int k = 0; k < K; ++k) {
+        const int t = w.t0 + k * kBlock, n = w.t1 - t;
+        if (n <= 0) break;
         if (a.marks && w.on) {
             float *to = marks_at(a.marks, w, t, a.channels);
 #pragma unroll
             for (int v = 0; v < V; ++v) to[v] = h[v];
         }
-        states<PREC, V>(xs, gs, min(kBlock, w.t1 - t), h, [&](int u, float (&h)[V], Gate (&)[V]) IDF_INLINE { if (w.on) out.store(t, u, h); });
+        float was[V];
+        bool fine = true;
 #pragma unroll
-        for (int u = 0; u < kBlock; ++u) { xs[u] = xn[u]; gs[u] = gn[u]; }
+        for (int v = 0; v < V; ++v) was[v] = h[v];
+#pragma unroll
+        for (int u = 0; u < kBlock; ++u) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[v] = step_of(Gate{gate[k][u][v]}, xs[k][u].get(v), h[v]);
+            if (u < n && w.on) out.store(t, u, h);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) fine = fine && finite(h[v]);
+        if (!fine) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[v] = was[v];
+            slow(t, min(n, kBlock), [&](int u, Gate (&)[V]) IDF_INLINE { if (w.on) out.store(t, u, h); });
+        }
     }
-    if (last && a.state_out && w.on)
+    if (w.t0 < w.t1 && w.t1 == w.g.len && a.state_out && w.on)
 #pragma unroll
         for (int v = 0; v < V; ++v) a.state_out[(int64_t)w.g.ring * a.channels + w.c + v] = h[v];
 }
 
-// ---- backward ----
-
-// What flows from a token to the one before it, m = a l with l = grad_out + m of the token behind it, over the n first rows of a block, the last
-// first: each(u, l, gates).  As above, once more where it comes out infinite or a gate is out of bounds (far).
-template <int PREC, int V, class P, class F, class G>
-__device__ __forceinline__ void flow(const P (&g)[kBlock], const P (&d)[kBlock], int n, float (&m)[V], float far, F gates, G each)
+template <int PREC, int V, bool CHAIN>
+__global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_back_tile(idf_gate_scan_backward_args a, Tiling tl)
 {
-    float was[V];
-    bool fine = true;
-#pragma unroll
-    for (int v = 0; v < V; ++v) was[v] = m[v];
-    rows_down(n, [&](int u) IDF_INLINE {
-        float l[V];
-        Gate w[V];
-        gates(u, w);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            l[v] = Elem<PREC>::to_f32(d[u].v[v]) + m[v];
-            m[v] = kept_of(w[v], l[v]);
-        }
-        each(u, l, w);
-    });
-#pragma unroll
-    for (int v = 0; v < V; ++v) fine = fine && finite(m[v]);
-    if (fine && far <= kGateMost) return;
-#pragma unroll
-    for (int v = 0; v < V; ++v) m[v] = was[v];
-#pragma unroll
-    for (int u = kBlock - 1; u >= 0; --u)
-        if (u < n) {
-            float l[V];
-            Gate w[V];
+    __shared__ Board<V> board;
+    Tile tile;
+    if (!tile_of<V, 1, CHAIN, true>(a, tl, tile)) return;
+    const Work &w = tile.w;
+    if (w.group == 0 && w.wave == 0) clear_between<PREC, V>(a, w);
+    if (w.g.len <= (int64_t)w.group * tl.span) {
+        if (CHAIN) pass_over<V, 1, true>(a, tl, tile);
+        if (w.g.valid && w.group == 0 && w.wave == 0 && w.on && a.grad_state)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Slow<PREC> slow(Elem<PREC>::to_f32(g[u].v[v]));
-                w[v] = slow.w;
-                l[v] = Elem<PREC>::to_f32(d[u].v[v]) + m[v];
-                m[v] = slow.kept(l[v]);
+                const int64_t i = (int64_t)w.g.ring * a.channels + w.c + v;
+                a.grad_state[i] = a.grad_end ? a.grad_end[i] : 0.f;
             }
-            each(u, l, w);
-        }
-}
-template <int PREC, int V, class P> __device__ __forceinline__ float farthest(const P (&g)[kBlock])
-{
-    float far = 0.f;
-#pragma unroll
-    for (int u = 0; u < kBlock; ++u)
-#pragma unroll
-        for (int v = 0; v < V; ++v) far = fmaxf(far, __builtin_fabsf(Elem<PREC>::to_f32(g[u].v[v])));
-    return far;
-}
-
-template <int PREC, int V>
-__global__ void __launch_bounds__(256) k_gate_back_parts(idf_gate_scan_backward_args a, Cut cut)
-{
-    extern __shared__ float lds[];
-    const Work w = work_of<V>(a, cut, blockIdx.y);
-    if (w.group * cut.span() >= w.g.len) return;
-    using R = Rows<PREC, V>;
-    const R g(a.gates, w.g.begin, w.c), d(a.grad_out, w.g.begin, w.c);
-    typename R::P gs[kBlock], ds[kBlock] = {};
-    Summary s[V];
-    float m[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) { s[v] = {1.f, 0.f}; m[v] = 0.f; }
-    const int from = w.t0 < w.t1 ? w.t0 + (w.t1 - 1 - w.t0) / kBlock * kBlock : w.t0 - kBlock;
-    const bool any = a.grad_out.base;
-    if (w.t0 < w.t1) { g.load(gs, from, w.t1); if (any) d.load(ds, from, w.t1); }
-    for (int t = from; t >= w.t0; t -= kBlock) {
-        typename R::P gn[kBlock], dn[kBlock] = {};
-        if (t > w.t0) { g.load(gn, t - kBlock, w.t1); if (any) d.load(dn, t - kBlock, w.t1); }
-        const int n = min(kBlock, w.t1 - t);
-        float was[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) was[v] = s[v].keep;
-        flow<PREC, V>(gs, ds, n, m, farthest<PREC, V>(gs), [&](int u, Gate (&w)[V]) IDF_INLINE {
-#pragma unroll
-            for (int v = 0; v < V; ++v) w[v] = gate_of<PREC>(Elem<PREC>::to_f32(gs[u].v[v]));
-        }, [&](int u, float (&)[V], Gate (&w)[V]) IDF_INLINE {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (u == n - 1) s[v].keep = was[v];
-                s[v].keep = kept_of(w[v], s[v].keep);
-            }
-        });
-#pragma unroll
-        for (int u = 0; u < kBlock; ++u) { gs[u] = gn[u]; ds[u] = dn[u]; }
+        return;
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) s[v].made = m[v];
-    join_group<V>(lds, w, cut, a.workspace, a.channels, a.grad_end, s, true);
-}
-
-template <int PREC, int V>
-__global__ void __launch_bounds__(256, 2) k_gate_back(idf_gate_scan_backward_args a, Cut cut)
-{
-    const Work w = work_of<V>(a, cut, blockIdx.y);
-    const bool first = w.group == 0 && w.wave == 0;
-    if (w.t0 >= w.t1 && !first) return;
     using R = Rows<PREC, V>;
-    if (first) {                                   // rows that no segment has have no gradient: those in front of the first one, and from a segment's last token to the next one
-        auto clear = [&](int64_t from, int64_t to) {
-            const float zero[V] = {};
-            for (int64_t t = from; t < to; ++t)
-                if (w.on) {
-                    R(a.grad_x, t, w.c).store(0, 0, zero);
-                    R(a.grad_gates, t, w.c).store(0, 0, zero);
-                }
-        };
-        const bool last = w.segment + 1 == a.n_segments;
-        if (a.offsets && w.segment == 0) clear(0, w.g.begin);
-        clear(w.g.begin + w.g.len, last ? a.n_tokens : a.offsets ? min(max(a.offsets[w.segment + 1], (int64_t)0), a.n_tokens) : w.g.begin + a.max_tokens);
-    }
-    if (!w.g.valid) return;
     const R x(a.x, w.g.begin, w.c), g(a.gates, w.g.begin, w.c), d(a.grad_out, w.g.begin, w.c), gx(a.grad_x, w.g.begin, w.c), gg(a.grad_gates, w.g.begin, w.c);
-    typename R::P xs[kBlock], gs[kBlock], ds[kBlock] = {};
-    float mark[V];
     const bool any = a.grad_out.base;
-    const int from = w.t0 < w.t1 ? w.t0 + (w.t1 - 1 - w.t0) / kBlock * kBlock : w.t0 - kBlock;
-    auto load = [&](int t, typename R::P (&xs)[kBlock], typename R::P (&gs)[kBlock], typename R::P (&ds)[kBlock], float (&mark)[V]) IDF_INLINE {
-        x.load(xs, t, w.t1);
+    const int t = w.t0, n = w.t1 - w.t0;
+    typename R::P xs[kBlock], gs[kBlock], ds[kBlock] = {};
+    float mark[V] = {}, gate[kBlock][V], apart[kBlock][V], h[V], m[V];
+    if (n > 0) {
         g.load(gs, t, w.t1);
+        x.load(xs, t, w.t1);
         if (any) d.load(ds, t, w.t1);
         const float *at = marks_at(const_cast<float *>(a.marks), w, t, a.channels);
 #pragma unroll
         for (int v = 0; v < V; ++v) mark[v] = at[v];
-    };
-    const bool on = w.on;
-    if (w.t0 < w.t1) load(from, xs, gs, ds, mark);
-    float m[V];
-    const bool cuts = cut.groups * cut.waves > 1 && w.g.len > 0;
-    const float *end = cuts ? begin_at(a.workspace, cut, w.segment, a.channels) : a.grad_end ? a.grad_end + (int64_t)w.g.ring * a.channels : nullptr;
-#pragma unroll
-    for (int v = 0; v < V; ++v) m[v] = end ? end[w.c + v] : 0.f;
-    if (w.t1 < w.g.len) {
-        const int64_t apart = 2 * (int64_t)a.channels, row = first_row(cut, w.g.begin, w.segment);
-        // groups and parts that have tokens, the last first
-        const int groups = (int)((w.g.len + cut.span() - 1) / cut.span());
-        const int parts = (int)((min((int64_t)w.g.len, (w.group + 1) * cut.span()) - w.group * cut.span() + cut.part - 1) / cut.part);
-        go_through<V>(summary_at(a.workspace, cut, row + groups - 1, 0, a.channels), -(1 + cut.waves) * apart, groups - 1 - w.group, a.channels, w.c, m);
-        go_through<V>(summary_at(a.workspace, cut, row + w.group, parts, a.channels), -apart, parts - 1 - w.wave, a.channels, w.c, m);
     }
-    for (int t = from; t >= w.t0; t -= kBlock) {
-        typename R::P xn[kBlock], gn[kBlock], dn[kBlock] = {};
-        float mark_n[V];
-        if (t > w.t0) load(t - kBlock, xn, gn, dn, mark_n);
-        const int n = min(kBlock, w.t1 - t);
-        // of every token the state before it less x, and its gate
-        float apart[kBlock][V], h[V], before[V];
-        Gate gate[kBlock][V];
+    Summary s[V];
+    bool ahead = true, fine = true;                // no state, no gradient of the block is infinite or not a number
 #pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = before[v] = mark[v];
-        states<PREC, V>(xs, gs, n, h, [&](int u, float (&h)[V], Gate (&w)[V]) IDF_INLINE {
+    for (int v = 0; v < V; ++v) { s[v] = {1.f, 0.f}; m[v] = 0.f; h[v] = mark[v]; }
+    if (n > 0) {
+#pragma unroll
+        for (int u = 0; u < kBlock; ++u)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                if (u == 0) before[v] = mark[v];
-                apart[u][v] = before[v] - Elem<PREC>::to_f32(xs[u].v[v]);
-                gate[u][v] = w[v];
-                before[v] = h[v];
+                const Gate one = u < n ? held_gate<PREC>(gs[u].get(v)) : Gate{0.f};
+                const float value = xs[u].get(v);
+                gate[u][v] = one.s;
+                apart[u][v] = h[v] - value;
+                h[v] = step_of(one, value, h[v]);
             }
-        });
-        flow<PREC, V>(gs, ds, n, m, farthest<PREC, V>(gs), [&](int u, Gate (&w)[V]) IDF_INLINE {
 #pragma unroll
-            for (int v = 0; v < V; ++v) w[v] = gate[u][v];
-        }, [&](int u, float (&l)[V], Gate (&w)[V]) IDF_INLINE {
+        for (int u = kBlock - 1; u >= 0; --u)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Gate one = {gate[u][v]};
+                m[v] = kept_of(one, (u < n ? ds[u].get(v) : 0.f) + m[v]);
+                s[v].keep = kept_of(one, s[v].keep);
+            }
+#pragma unroll
+        for (int v = 0; v < V; ++v) { ahead = ahead && finite(h[v]); fine = fine && finite(m[v]); }
+        if (!fine) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) { s[v].keep = 1.f; m[v] = 0.f; }
+            for (int u = n - 1; u >= 0; --u) {
+                const typename R::P gr = g.row(t + u), dr = any ? d.row(t + u) : typename R::P{};
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const Slow<PREC> it(gr.get(v));
+                    m[v] = it.kept(dr.get(v) + m[v]);
+                    s[v].keep = kept_of(it.w, s[v].keep);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[v].made = m[v];
+    begin_of<V, 1, CHAIN, true>(a, tl, tile, board, a.grad_end, s, m);
+    if (n > 0) {
+        float was[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) was[v] = m[v];
+        auto put_row = [&](int u, int v, Gate one, float l, float apart, float (&dx)[V], float (&dg)[V]) IDF_INLINE {
+            dx[v] = l * one.take();
+            dg[v] = l * apart * (__builtin_fabsf(one.s) * one.big());
+        };
+#pragma unroll
+        for (int u = kBlock - 1; u >= 0; --u) {
             float dx[V], dg[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                dx[v] = l[v] * w[v].take();
-                dg[v] = l[v] * apart[u][v] * (__builtin_fabsf(w[v].s) * w[v].big());
+                const Gate one = {gate[u][v]};
+                const float l = (u < n ? ds[u].get(v) : 0.f) + m[v];
+                m[v] = kept_of(one, l);
+                put_row(u, v, one, l, apart[u][v], dx, dg);
             }
-            if (on) { gx.store(t, u, dx); gg.store(t, u, dg); }
-        });
+            if (u < n && w.on) { gx.store(t, u, dx); gg.store(t, u, dg); }
+        }
+        fine = ahead;
 #pragma unroll
-        for (int u = 0; u < kBlock; ++u) { xs[u] = xn[u]; gs[u] = gn[u]; ds[u] = dn[u]; }
+        for (int v = 0; v < V; ++v) fine = fine && finite(m[v]);
+        if (!fine) {                               // by the definition, from memory: the state before each token from the block's first one on
 #pragma unroll
-        for (int v = 0; v < V; ++v) mark[v] = mark_n[v];
+            for (int v = 0; v < V; ++v) m[v] = was[v];
+            for (int u = n - 1; u >= 0; --u) {
+                const typename R::P dr = any ? d.row(t + u) : typename R::P{};
+                typename R::P xr = x.row(t), gr = g.row(t);
+#pragma unroll
+                for (int v = 0; v < V; ++v) h[v] = mark[v];
+                for (int i = 0; i < u; ++i) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) h[v] = Slow<PREC>(gr.get(v)).step(xr.get(v), h[v]);
+                    xr = x.row(t + i + 1);
+                    gr = g.row(t + i + 1);
+                }
+                float dx[V], dg[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const Slow<PREC> it(gr.get(v));
+                    const float l = dr.get(v) + m[v];
+                    m[v] = it.kept(l);
+                    put_row(u, v, it.w, l, h[v] - xr.get(v), dx, dg);
+                }
+                if (w.on) { gx.store(t, u, dx); gg.store(t, u, dg); }
+            }
+        }
     }
-    if (first && a.grad_state && w.on)
+    if (w.group == 0 && w.wave == 0 && a.grad_state && w.on)
 #pragma unroll
         for (int v = 0; v < V; ++v) a.grad_state[(int64_t)w.g.ring * a.channels + w.c + v] = m[v];
 }
@@ -533,56 +611,68 @@ template <class Args> bool pairs(const Args &a, std::initializer_list<const idf_
 bool pairs(const idf_gate_scan_args &a) { return pairs(a, {&a.x, &a.gates, &a.out}); }
 bool pairs(const idf_gate_scan_backward_args &a) { return pairs(a, {&a.x, &a.gates, &a.grad_out, &a.grad_x, &a.grad_gates}); }
 
-// Waves that a call is cut into, by the tokens that there are (us, forward and backward, with 2048 : 4096 : 8192; 16 uneven segments of up to 2048 tokens of 1536 channels
-// 74, 130 : 62, 109 : 60, 109; 65536 tokens of 2048 channels 296, 449 : 311, 470 : 304, 468; 8 segments of 4096 tokens of 1024 channels 76, 125 : 78, 128 : 80, 137).
-constexpr int64_t kWaves = 4096;
-template <class Args> Cut cut_of(const Args &a, int most_waves)
+// How a call goes: blocks to a wave, waves to a tile, and whether segments have several tiles.
+struct Way {
+    int blocks, waves;
+    bool chain;
+    Tiling tl;
+};
+template <class Args> Way way_of(const Args &a, bool back)
 {
     const int64_t blocks = (longest(a) + kBlock - 1) / kBlock, wide = 64 * (pairs(a) ? 2 : 1);
-    const int64_t lanes = (a.channels + wide - 1) / wide;                      // waves of a token
-    Cut c = {(int)std::max<int64_t>(blocks, 1) * kBlock, 1, 1, 0};
-    // blocks of a part so that all tokens that there are make kWaves waves, and more where the longest segment has no room for so many parts
-    const int64_t all = std::min<int64_t>(a.n_tokens / kBlock + a.n_segments, a.n_segments * blocks);
-    const int64_t part = std::max<int64_t>({(all * lanes + kWaves - 1) / kWaves, 1, (blocks + kMostGroups * most_waves - 1) / (kMostGroups * most_waves)});
-    const int64_t parts = (blocks + part - 1) / part;
-    if (parts < 2) return c;
-    c.waves = (int)std::min<int64_t>(parts <= kMostGroups * 4 ? 4 : most_waves, parts);
-    c.part = (int)part * kBlock;
-    c.groups = (int)((blocks * kBlock + c.span() - 1) / c.span());
-    c.rows = a.n_tokens / c.span() + a.n_segments;
-    return c;
+    Way y = {1, kTileWaves, false, {}};
+    y.tl.cols = (int)((a.channels + wide - 1) / wide);
+    if (blocks <= kTileWaves * (back ? 1 : 2)) {
+        y.blocks = blocks <= kTileWaves ? 1 : 2;
+        y.waves = (int)std::max<int64_t>(1, (blocks + y.blocks - 1) / y.blocks);
+        y.tl.span = y.waves * y.blocks * kBlock;
+        return y;
+    }
+    y.chain = true;
+    // (us, 16 : 32 tokens of a wave, forward: 20000 tokens of 64 channels 22.5 : 24.2, 16 uneven segments of 15462 tokens of 1536 51.6 : 52.3, 2 of 8192 of 1024 45.6 : 41.7,
+    // 65536 of 2048 206 : 189; backward 32 do not fit the registers)
+    if (!back && (a.n_tokens / (2 * kTileWaves * kBlock) + a.n_segments) * y.tl.cols >= 512) y.blocks = 2;
+    y.tl.span = kTileWaves * y.blocks * kBlock;
+    y.tl.rows = a.n_tokens / y.tl.span + a.n_segments;
+    return y;
 }
-constexpr int kForwardWaves = 8, kBackwardWaves = 4;
-
-template <class Args> size_t summaries(const Args &a, const Cut &c)
+template <class Args> size_t workspace_of(const Args &a, const Way &y)
 {
-    return c.groups * c.waves > 1 ? ((size_t)c.rows * (1 + c.waves) * 2 + a.n_segments) * a.channels * sizeof(float) : 0;
+    if (!y.chain) return 0;
+    return (256 + ((size_t)y.tl.rows * sizeof(uint64_t) + (size_t)(y.tl.rows / chain_of(y.blocks) + 1) * sizeof(uint32_t)) * a.channels + 15) / 16 * 16;
+}
+template <class Args> hipError_t nothing_told(const Args &a, const Way &y, const LaunchCtx &lc)
+{
+    const int64_t n = (int64_t)workspace_of(a, y) / 16;
+    return launch(k_gate_absent, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 4096)), dim3(256), 0, lc, (uint4 *)a.workspace, n);
 }
 
 template <int PREC, int V>
 hipError_t forward(const idf_gate_scan_args &a, const LaunchCtx &lc)
 {
-    const Cut c = cut_of(a, kForwardWaves);
-    const dim3 grid((a.channels + 64 * V - 1) / (64 * V), c.groups, a.n_segments), block(64 * c.waves);
-    if (c.groups * c.waves > 1)
-        if (const hipError_t e = launch(k_gate_parts<PREC, V>, grid, block, (size_t)c.waves * 64 * 2 * V * sizeof(float), lc, a, c)) return e;
-    return launch(k_gate_out<PREC, V>, grid, block, 0, lc, a, c);
+    const Way y = way_of(a, false);
+    const dim3 block(64 * y.waves), grid = y.chain ? dim3((unsigned)(y.tl.rows * y.tl.cols)) : dim3(y.tl.cols, a.n_segments);
+    if (!y.chain) return launch(y.blocks == 1 ? k_gate_tile<PREC, V, 1, false> : k_gate_tile<PREC, V, 2, false>, grid, block, 0, lc, a, y.tl);
+    if (const hipError_t e = nothing_told(a, y, lc)) return e;
+    return launch(y.blocks == 1 ? k_gate_tile<PREC, V, 1, true> : k_gate_tile<PREC, V, 2, true>, grid, block, 0, lc, a, y.tl);
 }
 template <int PREC, int V>
 hipError_t backward(const idf_gate_scan_backward_args &a, const LaunchCtx &lc)
 {
-    const Cut c = cut_of(a, kBackwardWaves);
-    const dim3 grid((a.channels + 64 * V - 1) / (64 * V), c.groups, a.n_segments), block(64 * c.waves);
-    if (c.groups * c.waves > 1)
-        if (const hipError_t e = launch(k_gate_back_parts<PREC, V>, grid, block, (size_t)c.waves * 64 * 2 * V * sizeof(float), lc, a, c)) return e;
-    return launch(k_gate_back<PREC, V>, grid, block, 0, lc, a, c);
+    const Way y = way_of(a, true);
+    const dim3 block(64 * y.waves), grid = y.chain ? dim3((unsigned)(y.tl.rows * y.tl.cols)) : dim3(y.tl.cols, a.n_segments);
+    if (!y.chain) return launch(k_gate_back_tile<PREC, V, false>, grid, block, 0, lc, a, y.tl);
+    if (const hipError_t e = nothing_told(a, y, lc)) return e;
+    return launch(k_gate_back_tile<PREC, V, true>, grid, block, 0, lc, a, y.tl);
 }
 
 }  // namespace
 
+int64_t gate_scan_tiles(const idf_gate_scan_args &a) { const Way y = way_of(a, false); return y.tl.rows * y.tl.cols; }
+int64_t gate_scan_tiles(const idf_gate_scan_backward_args &a) { const Way y = way_of(a, true); return y.tl.rows * y.tl.cols; }
 size_t gate_scan_marks(int64_t n_tokens, int n_segments, int channels) { return (size_t)(n_tokens / kBlock + n_segments + 1) * channels * sizeof(float); }
-size_t gate_scan_workspace(const idf_gate_scan_args &a) { return summaries(a, cut_of(a, kForwardWaves)); }
-size_t gate_scan_workspace(const idf_gate_scan_backward_args &a) { return summaries(a, cut_of(a, kBackwardWaves)); }
+size_t gate_scan_workspace(const idf_gate_scan_args &a) { return workspace_of(a, way_of(a, false)); }
+size_t gate_scan_workspace(const idf_gate_scan_backward_args &a) { return workspace_of(a, way_of(a, true)); }
 
 hipError_t launch_gate_scan(const idf_gate_scan_args &a, const LaunchCtx &lc)
 {

@@ -184,6 +184,8 @@ int check_gate(const Args *a)
     if (int rc = check_packing(*a)) return rc;
     if (a->channels < 1 || a->channels > kMostChannels) return fail(IDF_EUNSUPPORTED, "%d channels", a->channels);
     if (longest(*a) > kMostTokens) return fail(IDF_EUNSUPPORTED, "segments of up to %lld tokens", (long long)longest(*a));
+    if (gate_scan_tiles(*a) >= kMostPairs)
+        return fail(IDF_EUNSUPPORTED, "%lld tokens in %d segments of %d channels: more than a launch takes", (long long)a->n_tokens, a->n_segments, a->channels);
     return IDF_OK;
 }
 

@@ -100,10 +100,10 @@ def gate_plans(rt):
                         for max_tokens in (0, 1, 15, 17, 4096, 1 << 20):
                             need = holds_its_plan(rt, "idf_gate_scan_backward" if back else "idf_gate_scan", lambda **kw: gate_args(**kw, back=back),
                                                   dict(rows=rows, max_tokens=max_tokens, channels=channels, precision=precision, segments=segments),
-                                                  lambda need: {None: 1 + (need > 0), b"k_gate_back_parts" if back else b"k_gate_parts": need > 0})
+                                                  lambda need: {None: 1 + (need > 0), b"k_gate_absent": need > 0, b"k_gate_back_tile" if back else b"k_gate_tile": 1})
                             seen.add(need > 0)
-                            # states, and a few floats for every 16 tokens and every segment
-                            assert need <= (rows // 16 + 2 * segments) * channels * 4 * 18
+                            # one launch for segments of one tile; twelve bytes a channel for every 128 tokens and every segment are enough
+                            assert (need > 0) == (min(rows, max_tokens) > (128 if back else 256)) and need <= (rows // 128 + segments + 1) * channels * 12 + 256 + 16
     assert seen == {False, True}
 
 
@@ -122,6 +122,11 @@ def more_than_a_launch_takes(rt):
         t = tokens._Tokens(AT, 32, 32)
         a = tokens._NibbleAppend(1, 1, 32, 32, 0, n, (1 << 31) - 1, 1, 1, 64, 2, 1.0, 1e-6, t, t, tokens._NibbleRing(AT, AT, AT, AT), AT, None, AT, AT, None)
         assert call(rt, "idf_nibble_append", a) == rc and rt.host_launches(None) == (rc == 0)
+    for rows, channels, rc in ((1 << 29, 1 << 6, 0), (1 << 30, 1 << 8, -5), ((1 << 31) - 1, 65, -5), (1 << 18, 1 << 16, 0), (1 << 18, 1 << 20, -5)):
+        for back in (False, True):
+            a = gate_args(rows, 4096, channels, 0, 1000, back, AT, 1 << 50)
+            a.offsets = AT
+            assert call(rt, "idf_gate_scan_backward" if back else "idf_gate_scan", a) == rc and (rt.host_launches(None) > 0) == (rc == 0), (rows, channels, back)
     # heads of many streams go in several launches
     for streams, heads, launches in ((1, 1, 1), (64, 1000, 1), (65, 1000, 2), (200000, 1, 4)):
         a = tokens._NibbleValues(1, heads, 32, streams, 5, tokens._NibbleRing(AT, AT, AT, AT), AT, AT)

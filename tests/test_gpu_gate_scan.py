@@ -311,3 +311,91 @@ def test_one_long_segment_among_many_short_ones(dtype, long_first):
     """Summaries lie by the tokens before a segment: none of them lies on another's, wherever the long segment stands and ends."""
     short = [i * 7 % 5 for i in range(90)] + [16, 32, 31, 160, 161, 0, 0]
     check([2500] + short if long_first else short + [2500, 1, 0, 1100, 3], 70, dtype, seed=21)
+
+
+@pytest.mark.parametrize("offsets", [[0, -5, 4000, 1000, 6000], [6000, 5, 3000, 1 << 40, 0], [0, 5999, 20, 5990, 300], [4000, 4000, 10, 10, 6000], [-1] * 5, [1 << 62] * 5],
+                         ids=str)
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_offsets_that_nobody_meant_end_in_bounds(offsets, dtype):
+    """Tiles of long segments wait for each other: whatever the offsets say, they all end, and nothing beside the rows is written."""
+    x, gates, _, d, _ = (t.to(DEV) for t in make((6000,), 192, dtype))
+    guard = torch.full((6002, 192), 5.0, dtype=dtype, device=DEV)
+    kw = dict(offsets=torch.tensor(offsets, device=DEV), max_tokens=6000)
+    _, marks = idf.gate_scan(x, gates, out=guard[1:6001], marks=True, **kw)
+    idf.gate_scan_backward(x, gates, marks, d, **kw)
+    torch.cuda.synchronize()
+    assert torch.all(guard[0] == 5.0) and torch.all(guard[6001] == 5.0)
+
+
+def test_long_segments_of_no_stream_and_rows_of_no_segment():
+    """A stream that is none between others, bounds shorter than what the offsets leave, empty segments: tiles that have nothing to do hold up nobody."""
+    lengths, streams = (2500, 0, 3000, 1, 2600), 5
+    x, gates, _, d, _ = (t.to(DEV) for t in make((9000,), 70, torch.float32, seed=31))
+    state, end = (torch.randn(streams, 70, generator=torch.Generator().manual_seed(s)).to(DEV) for s in (32, 33))
+    offsets = torch.tensor([100, 2700, 2700, 5800, 5801, 8500], device=DEV)
+    for ids in ([4, 0, 2, 1, 3], [4, 0, -1, 1, 3], [-7, 0, 2, 99, 3]):
+        kw = dict(stream_ids=torch.tensor(ids, dtype=torch.int32, device=DEV), offsets=offsets, max_tokens=3000)
+        s, out = state.clone(), torch.full_like(x, 7.0)
+        _, marks = idf.gate_scan(x, gates, s, s, out=out, marks=True, **kw)
+        dx, dg, ds = idf.gate_scan_backward(x, gates, marks, d, end, **kw)
+        mine = torch.zeros(9000, dtype=torch.bool)
+        for i, b in enumerate(ids):
+            rows = slice(int(offsets[i]), min(int(offsets[i + 1]), int(offsets[i]) + 3000))
+            if not 0 <= b < streams:
+                continue
+            mine[rows] = True
+            hs, _, errors = oracle.gate_scan(f64(x[rows]), f64(gates[rows]), f64(state[b]))
+            within(out[rows], hs, W * (errors + np.abs(hs)))
+            want = oracle.gate_scan_backward(f64(x[rows]), f64(gates[rows]), f64(state[b]), f64(d[rows]), f64(end[b]))
+            for got, w, e in ((dx[rows], want[0], want[3]), (dg[rows], want[1], want[4]), (ds[b], want[2], want[5])):
+                within(got, w, W * (np.abs(w) + e) + 1e-30)
+            within(s[b], hs[-1] if len(hs) else f64(state[b]), W * errors[-1] + 1e-30 if len(hs) else np.full(70, 1e-30))
+        assert torch.all(out[~mine] == 7.0) and not dx[~mine].any() and not dg[~mine].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_numbers_of_all_ones(dtype):
+    """Not numbers whose bits are all set, in values, gates, states and gradients: as any other that is not a number."""
+    n = 3000
+    x, gates, state, d, end = (t.to(DEV) for t in make((n,), 128, dtype, seed=34))
+    want = idf.gate_scan(x, gates, state)
+    ones = torch.full((1,), -1, dtype=torch.int32 if dtype == torch.float32 else torch.int16, device=DEV).view(dtype)
+    x[5, 3], gates[700, 9], d[2000, 20] = ones[0], ones[0], ones[0]
+    state[0, 15], end[0, 17] = (torch.full((1,), -1, dtype=torch.int32, device=DEV).view(torch.float32)[0] for _ in range(2))
+    to = torch.empty_like(state)
+    out, marks = idf.gate_scan(x, gates, state, to, marks=True)
+    dx, dg, ds = idf.gate_scan_backward(x, gates, marks, d, end)
+    bad = torch.zeros(n, 128, dtype=torch.bool, device=DEV)
+    bad[5:, 3] = bad[700:, 9] = bad[:, 15] = True
+    assert torch.equal(torch.isnan(out), bad) and torch.equal(out[~bad], want[~bad]) and torch.equal(torch.isnan(to[0]), bad[-1])
+    nan = torch.isnan(ds[0])
+    assert nan[9] and nan[20] and nan[17] and int(nan.sum()) == 3
+    assert torch.isnan(dx[:2001, 20]).all() and not torch.isnan(dx[2001:, 20]).any() and torch.isnan(dx[:, 17]).all()
+
+
+def test_two_calls_at_once():
+    """Tiles of two calls on two streams are on the machine together, more of them than it holds: each waits for its own call's only."""
+    sets = [tuple(t.to(DEV) for t in make((9000, 7000), 1024, torch.bfloat16, seed=s)) for s in (35, 36)]
+    kw = ragged((9000, 7000))
+
+    def both(x, gates, state, d, end):
+        to = torch.empty_like(state)
+        out, marks = idf.gate_scan(x, gates, state, to, marks=True, **kw)
+        return (out, to, *idf.gate_scan_backward(x, gates, marks, d, end, **kw))
+    want = [both(*s) for s in sets]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(both(*sets[i]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i in range(2) for run in got[i] for a, b in zip(run, want[i]))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("lengths", [(4096 + 1,), (8192 * 2 + 255, 1, 4095), (128, 129, 255, 256, 257, 2047, 2048, 2049)], ids=str)
+def test_segments_that_end_about_a_tile(lengths, dtype):
+    """Ends at, before and behind the borders of waves, tiles and of the rows that a state is told for."""
+    check(lengths, 66, dtype, seed=37)
