@@ -31,7 +31,8 @@ __device__ __forceinline__ int code_of(float x, float per, float most)
     return c;
 }
 
-// A row by THREADS threads, which keep as many of its values as their registers hold, and read the others a second time.
+// A row by THREADS threads, which keep as many of its values as their registers hold, and read the others a second time.  Bound by memory: 16384 x 4096 from
+// bfloat16 in 48 us, 4.2 TB/s, from float32 in 60, 5.6.
 template <int PREC, int THREADS>
 __global__ void __launch_bounds__(256) k_quantize_rows(idf_quantize_args a, bool aligned)
 {
@@ -75,7 +76,9 @@ __global__ void __launch_bounds__(256) k_quantize_rows(idf_quantize_args a, bool
     if (THREADS > 64) {
         if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = most;
         __syncthreads();
-        most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        const float *mine = top + threadIdx.x / THREADS * (THREADS / 64);
+        most = fmaxf(mine[0], mine[1]);
+        if (THREADS == 256) most = fmaxf(most, fmaxf(mine[2], mine[3]));
     }
     if (!there) return;
     fine = most < __builtin_inff();
@@ -422,8 +425,13 @@ hipError_t quantize(const idf_quantize_args &a, const LaunchCtx &lc)
 {
     const int eb = PREC == IDF_PREC_F32 ? 4 : 2;
     const bool aligned = (uintptr_t)a.x.base % (8 * eb) == 0 && a.x.row_stride % 8 == 0;
-    if (a.cols <= 2048) return launch(k_quantize_rows<PREC, 64>, dim3((unsigned)((a.n_rows + 3) / 4)), dim3(256), 0, lc, a, aligned);
-    return launch(k_quantize_rows<PREC, 256>, dim3((unsigned)a.n_rows), dim3(256), 0, lc, a, aligned);
+    // many rows: as few threads as keep all of one; few rows: as many threads as share one (us by 64, 128, 256; bfloat16, 16384 x 2048 26.5, 27.7, 35.7; 16384 x 4096
+    // 63, 48, 57; 777 x 1096 5.1, 4.8, 4.4; 64 x 4096 12.5, 7.2, 4.7; 64 x 512 3.6, 3.5, 3.9)
+    const int threads = a.n_rows >= 2048 ? (a.cols <= 2048 ? 64 : a.cols <= 4096 ? 128 : 256) : a.cols <= 512 ? 64 : 256;
+    const dim3 grid((unsigned)((a.n_rows * threads + 255) / 256));
+    if (threads == 64) return launch(k_quantize_rows<PREC, 64>, grid, dim3(256), 0, lc, a, aligned);
+    if (threads == 128) return launch(k_quantize_rows<PREC, 128>, grid, dim3(256), 0, lc, a, aligned);
+    return launch(k_quantize_rows<PREC, 256>, grid, dim3(256), 0, lc, a, aligned);
 }
 
 }  // namespace

@@ -182,3 +182,16 @@ def test_refusals_of_tensors():
             call()
     with pytest.raises(idf.IdfError):
         idf.project_rows(x.detach().half(), w, ws)
+
+
+@pytest.mark.parametrize("rows,cols", [(2047, 513), (2049, 2049), (2050, 4096), (2051, 4097), (2049, 100), (3, 513), (2047, 4096)])
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_rows_that_share_a_workgroup(rows, cols, dtype):
+    """One, two and four rows to a workgroup, the last one half empty: each has a scale of its own, beside rows of zeros and rows that are not finite."""
+    x, *_ = make(rows, cols, 1, dtype, seed=rows)
+    x[1], x[2, cols - 1] = 0, float("inf")
+    codes, scales = idf.quantize_rows(x.to(DEV))
+    fine = torch.arange(rows) != 2
+    want, want_scales = oracle.quantize_rows(f64(x)[fine])
+    assert np.array_equal(f64(codes)[fine][:, :cols], want) and not codes[:, cols:].any()
+    assert np.all(np.abs(f64(scales)[fine] - want_scales) <= W * want_scales) and torch.isnan(scales[2])
