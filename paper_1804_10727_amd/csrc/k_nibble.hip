@@ -159,7 +159,8 @@ __device__ __forceinline__ uint32_t encode_exact(const double (&y)[8], uint32_t 
 
 // A lane has eight values of a head, four lanes a block; a workgroup a few tokens with all their heads, so that slots, cosines and sines are formed once per
 // token.  Keys that are normalised or turned are formed in 64 bits, whose instructions run as fast as those of 32 here: a value next to the middle between two codes goes to
-// the same one however sums and products are ordered.
+// the same one however sums and products are ordered.  What is read and written asks for 17 us of 15,104 tokens with 8 heads of 128 in bfloat16; it takes 46, by
+// the instructions (with every code decided in 64 bits 97; with a workgroup per token 52).  One token of 64 streams: 5.7 us.
 template <int PREC, bool ALIGNED>
 __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args a, int lanes_log2, int tokens_per_group)
 {
@@ -294,7 +295,7 @@ __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args
 // ---- what a ring stands for ----
 
 // A workgroup takes a head of a stream's keys or values and some of its slots, a lane eight values at a time: lanes read and write next to each other.  Bound by memory, most
-// of it what is written.
+// of it what is written: 8 streams of 4100 slots with 8 heads of 128 to bfloat16 in 28 us, 170 MB, 6.0 TB/s.
 template <int PREC>
 __global__ void __launch_bounds__(256) k_nibble_values(idf_nibble_values_args a)
 {
@@ -672,7 +673,9 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || DP <= 128 ? 2 : 1) k
 // -- many rows --
 
 // A workgroup takes 128 query rows of one segment and key/value head and walks over their keys, 64 at a time; a wave has 32 of the rows.  Codes of a round
-// go through registers into LDS as bfloat16, the next round's being asked for while this one's are worked on.
+// go through registers into LDS as bfloat16, the next round's being asked for while this one's are worked on.  Bound by the matrix instructions and what feeds them: 2
+// streams of 8192 tokens on windows of 4096, 32 heads of 128 on 8, in bfloat16 1113 us, 990 TFLOP/s, two thirds of what a large product reaches (1495); the exponentials
+// and the weights' way to bfloat16 are the rest.
 template <int DP> struct TileShape {
     static constexpr int KEYS = 64, BLOCKS = DP / kBits;
     static constexpr int K_STRIDE = DP + 8;                                   // neighbouring rows begin 16 bytes apart in the banks

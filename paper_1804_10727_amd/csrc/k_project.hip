@@ -151,7 +151,8 @@ __device__ const int8_t kZeros[16] __attribute__((aligned(16))) = {};
 // A workgroup takes BM rows of x by BN outputs, a wave 16 MT by 16 NT of them; codes go from memory into LDS directly, 128 of a row at a time, those of the next
 // STAGES times on their way while these are multiplied.  A row's eight pieces of 16 bytes lie in LDS at place piece ^ (row & 7): what a matrix instruction's
 // lanes read together, 16 rows by four neighbouring pieces, lies in banks of its own.  Workgroups of one die (every eighth) take tiles next to each other.
-// Results leave by way of LDS, whole lines of a row at a time.
+// Results leave by way of LDS, whole lines of a row at a time.  Many rows are bound by the matrix instructions (16384 x 4096 x 6144: 370 us, 2,230 TOP/s, as fast as the library's
+// product of 8-bit numbers alone), few ones by the weights (64 x 4096 x 6144: 25 MB in 9.4 us).
 template <int N> __device__ __forceinline__ void wait_and_meet()
 {
 #if defined(__HIP_DEVICE_COMPILE__)
