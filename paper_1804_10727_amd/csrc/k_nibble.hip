@@ -676,6 +676,8 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || DP <= 128 ? 2 : 1) k
 // go through registers into LDS as bfloat16, the next round's being asked for while this one's are worked on.  Bound by the matrix instructions and what feeds them: 2
 // streams of 8192 tokens on windows of 4096, 32 heads of 128 on 8, in bfloat16 1113 us, 990 TFLOP/s, two thirds of what a large product reaches (1495); the exponentials
 // and the weights' way to bfloat16 are the rest.
+// In LDS a block's four pieces of eight values change places, x to x ^ turn: eight lanes that write a piece each, of blocks that follow each other, then write to banks of
+// their own (written in order two or four of them met in one; 1113 us where this takes 1069).
 template <int DP> struct TileShape {
     static constexpr int KEYS = 64, BLOCKS = DP / kBits;
     static constexpr int K_STRIDE = DP + 8;                                   // neighbouring rows begin 16 bytes apart in the banks
@@ -683,7 +685,19 @@ template <int DP> struct TileShape {
     static constexpr int PIECES = KEYS * BLOCKS;                              // of keys, and as many of values
     static constexpr int LOADS = 2 * PIECES / 256;
     static constexpr int LDS_BYTES = KEYS * (K_STRIDE + V_STRIDE) * 2;
+    static __device__ __forceinline__ int k_turn(int block) { return DP == 64 ? 0 : DP == 128 ? block & 2 : block >> 1 & 3; }
+    static __device__ __forceinline__ int v_turn(int row, int block) { return DP == 64 ? row & 3 : DP == 128 ? (row & 1) | (block & 2) : block >> 1 & 3; }
 };
+// read_column of the values over 32 lanes, of a block's columns.
+template <int DP> __device__ __forceinline__ bf16x8 read_block(const __bf16 *lds, int block, int r0, int r1)
+{
+    using S = TileShape<DP>;
+    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+    const int lane = threadIdx.x & 31, r = lane >> 2 & 3, at = r * S::V_STRIDE + block * kBits + (((lane >> 3 & 2) | (lane >> 1 & 1)) ^ S::v_turn(r, block)) * 8 + (lane & 1) * 4;
+    const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(lds + r0 * S::V_STRIDE + at));
+    const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(lds + r1 * S::V_STRIDE + at));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
 
 template <int PREC, int DP>
 __global__ void __launch_bounds__(256, PREC != IDF_PREC_BF16 || DP > 128 ? 1 : DP > 64 ? 2 : 4) k_nibble_tile(idf_nibble_attend_args a, int splits)
@@ -761,8 +775,9 @@ __global__ void __launch_bounds__(256, PREC != IDF_PREC_BF16 || DP > 128 ? 1 : D
             const int piece = key ? x : x - S::PIECES, r = piece / S::BLOCKS, b = piece - r * S::BLOCKS;
             __bf16 *to = (key ? k_lds + r * S::K_STRIDE : v_lds + r * S::V_STRIDE) + b * kBits;
             const float power = power_of(powers[j]);
+            const int turn = key ? S::k_turn(b) : S::v_turn(r, b);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) *(bf16x8 *)(to + 8 * w) = values8((uint32_t)codes[j][w], power);
+            for (int w = 0; w < 4; ++w) *(bf16x8 *)(to + 8 * (w ^ turn)) = values8((uint32_t)codes[j][w], power);
         }
         __syncthreads();
         if (t + 1 < t1) load(t + 1);
@@ -776,7 +791,7 @@ __global__ void __launch_bounds__(256, PREC != IDF_PREC_BF16 || DP > 128 ? 1 : D
             for (int e = 0; e < 16; ++e) st[kt][e] = 0.f;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                const bf16x8 k = M::load(k_lds + (32 * kt + col) * S::K_STRIDE + 16 * s + 8 * half);
+                const bf16x8 k = M::load(k_lds + (32 * kt + col) * S::K_STRIDE + s / 2 * kBits + (((2 * s & 2) | half) ^ S::k_turn(s / 2)) * 8);
 #pragma unroll
                 for (int x = N - 1; x >= 0; --x) st[kt] = M::mma32(k, q[s][x], st[kt]);
             }
@@ -826,7 +841,7 @@ __global__ void __launch_bounds__(256, PREC != IDF_PREC_BF16 || DP > 128 ? 1 : D
             in_parts(w, pf);
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-                const bf16x8 v = read_column(v_lds, S::V_STRIDE, 32 * d + (lane & 16), 16 * s + 4 * half, 16 * s + 8 + 4 * half);
+                const bf16x8 v = read_block<DP>(v_lds, d, 16 * s + 4 * half, 16 * s + 8 + 4 * half);
 #pragma unroll
                 for (int x = N - 1; x >= 0; --x) o[d] = M::mma32(v, pf[x], o[d]);
             }
