@@ -674,7 +674,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || DP <= 128 ? 2 : 1) k
 
 // A workgroup takes 128 query rows of one segment and key/value head and walks over their keys, 64 at a time; a wave has 32 of the rows.  Codes of a round
 // go through registers into LDS as bfloat16, the next round's being asked for while this one's are worked on.  Bound by the matrix instructions and what feeds them: 2
-// streams of 8192 tokens on windows of 4096, 32 heads of 128 on 8, in bfloat16 1113 us, 990 TFLOP/s, two thirds of what a large product reaches (1495); the exponentials
+// streams of 8192 tokens on windows of 4096, 32 heads of 128 on 8, in bfloat16 1069 us, 1030 TFLOP/s, 69 % of what a large product reaches (1495); the exponentials
 // and the weights' way to bfloat16 are the rest.
 // In LDS a block's four pieces of eight values change places, x to x ^ turn: eight lanes that write a piece each, of blocks that follow each other, then write to banks of
 // their own (written in order two or four of them met in one; 1113 us where this takes 1069).
