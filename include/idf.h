@@ -630,6 +630,7 @@ int idf_nibble_values(const idf_nibble_values_args *a, void *hip_stream);
 /* A gated recurrence per channel:  h_t = a_t h_{t-1} + (1 - a_t) x_t,  a_t = 1 / (1 + exp(-g_t)),  out_t = h_t,
  * with gates held to -87 .. 87 (neither what is kept nor what is taken in is ever nothing: an infinite state stays infinite).  state_in, state_out: float32
  * [n_streams][channels], from the state of the segment's stream before it to the one after it, as in idf_decay_attend.  States are float32 throughout.
+ * out must not overlap x or gates.
  *   marks (NULL: not wanted): what the backward pass needs beside x and gates, states within the segments, idf_gate_scan_marks bytes, 256-byte
  * aligned.  Rows need no alignment beyond their values'.  1 <= channels <= 2^20; segments of up to 2^30 tokens; where one has more than 128,
  * (n_tokens / 128 + n_segments) * channels / 64 < 2^23. */
@@ -653,7 +654,8 @@ int idf_gate_scan(const idf_gate_scan_args *a, void *hip_stream);
  *   l_t = grad_out_t + a_{t+1} l_{t+1} (the last one with grad_end in place of a l),  grad_x_t = (1 - a_t) l_t,
  *   grad_gates_t = l_t (h_{t-1} - x_t) a_t (1 - a_t),  grad_state = a_1 l_1.
  * grad_out.base, grad_end (of state_out) NULL: zeros; grad_state (of state_in) NULL: not wanted.  grad_end and grad_state float32 [n_streams][channels], may be
- * the same; a segment without tokens hands grad_end on.  Rows of grad_x and grad_gates that none of the segments has are set to zero. */
+ * the same; a segment without tokens hands grad_end on; of streams that no segment is of, grad_state stays as it was.  Rows of grad_x and grad_gates
+ * that none of the segments has are set to zero.  Neither may overlap the other, x, gates or grad_out. */
 typedef struct {
     int precision, channels;
     int64_t n_tokens, max_tokens;

@@ -567,6 +567,11 @@ PyObject *gate_scan(PyObject *, PyObject *const *args, Py_ssize_t n)
         const at::Tensor out = output(given, x->sizes(), *x);
         need(out.scalar_type() == x->scalar_type());
         a.out = matrix(out, *x);
+        if (given)                                 // (what may share places with it is looked at more closely the long way round)
+            for (const idf_rows *r : {&a.x, &a.gates}) {
+                const auto end = [&](const idf_rows &m) { return (uintptr_t)m.base + ((a.n_tokens ? a.n_tokens - 1 : 0) * m.row_stride + a.channels) * x->element_size(); };
+                need(end(*r) <= (uintptr_t)a.out.base || end(a.out) <= (uintptr_t)r->base);
+            }
         at::Tensor fresh, ws;
         int rc = IDF_OK;
         if (marks || args[10] == Py_True) {
@@ -611,7 +616,9 @@ int gate_gradients(idf_gate_scan_backward_args &a, const at::Tensor &x, const at
     a.marks = plain<float>(&marks, at::kFloat, (int64_t)bytes / 4, x);
     a.grad_end = end ? static_cast<const float *>(end->data_ptr()) : nullptr;
     const auto fresh = [&]() { return a.n_segments ? at::empty(x.sizes(), x.options()) : at::zeros(x.sizes(), x.options()); };
-    to = {fresh(), fresh(), at::empty({a.n_streams, a.channels}, x.options().dtype(at::kFloat))};
+    // (streams that no segment is of have no gradient)
+    const auto state = x.options().dtype(at::kFloat);
+    to = {fresh(), fresh(), !a.stream_ids && a.n_streams == a.n_segments ? at::empty({a.n_streams, a.channels}, state) : at::zeros({a.n_streams, a.channels}, state)};
     a.grad_x = matrix(to.x, x);
     a.grad_gates = matrix(to.gates, x);
     a.grad_state = static_cast<float *>(to.state.data_ptr());

@@ -564,6 +564,21 @@ def gate_scan(x, gates, state=None, state_out=None, *, offsets=None, max_tokens=
     return r if r is not None else _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stream_ids, out, marks)
 
 
+def _share(a, b):
+    """Whether two matrices of one size share places: where rows lie alike they may be columns of one larger matrix, else it is enough that they reach into each other."""
+    rows, cols = a.shape
+    if not a.numel():
+        return False
+    strides = [t.stride(0) if rows > 1 else cols for t in (a, b)]
+    apart = (b.data_ptr() - a.data_ptr()) // a.element_size()
+    if not -(rows - 1) * strides[1] - cols < apart < (rows - 1) * strides[0] + cols:
+        return False
+    if strides[0] != strides[1] or not strides[0]:
+        return True
+    k, rest = divmod(apart, strides[0])
+    return (abs(k) < rows and rest < cols) or (abs(k + 1) < rows and strides[0] - rest < cols)
+
+
 def _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stream_ids, out, marks):
     import torch
     _no_gradients(x=x, gates=gates, state=state, state_out=state_out, out=out)
@@ -572,6 +587,8 @@ def _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stre
     out = _out_matrix(out, x.shape, x.dtype, x.device, "out")
     if out.dtype != x.dtype:
         raise ValueError(f"out: {out.dtype}, wanted {x.dtype}")
+    if _share(out, x) or _share(out, gates):
+        raise ValueError("out shares places with x or gates")
     given = marks
     if marks is not None:
         marks = torch.empty(_marks_floats(sizes, offsets), device=x.device) if marks is True else _plain(marks, torch.float32, (_marks_floats(sizes, offsets),), x.device, "marks")
@@ -587,7 +604,7 @@ def _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stre
 
 def gate_scan_backward(x, gates, marks, grad_out=None, grad_end=None, *, offsets=None, max_tokens=None, n_segments=None, stream_ids=None, n_streams=None):
     """Gradients of gate_scan's x, gates and state from those of its result and of state_out (None: zeros), with the marks that the call left
-    (idf_gate_scan_backward).  n_streams where grad_end does not say how many there are."""
+    (idf_gate_scan_backward).  n_streams where grad_end does not say how many there are; streams that no segment is of get zeros."""
     r = _direct("gate_scan_backward", x, gates, marks, grad_out, grad_end, offsets, max_tokens, n_segments, stream_ids, n_streams)
     return r if r is not None else _gate_scan_backward(x, gates, marks, grad_out, grad_end, offsets, max_tokens, n_segments, stream_ids, n_streams)
 
@@ -603,7 +620,7 @@ def _gate_scan_backward(x, gates, marks, grad_out, grad_end, offsets, max_tokens
             raise ValueError(f"grad_out {tuple(grad_out.shape)} of x {tuple(x.shape)}")
     marks = _plain(marks, torch.float32, (_marks_floats(sizes, offsets),), x.device, "marks")
     grads = [torch.zeros(x.shape, dtype=x.dtype, device=x.device) for _ in range(2)]
-    grad_state = torch.empty(sizes[5], x.shape[1], device=x.device)
+    grad_state = torch.zeros(sizes[5], x.shape[1], device=x.device)        # (streams that no segment is of have no gradient here)
     a = _GateScanBackward(*sizes, _as_rows(x), _as_rows(gates), _Rows(None, 0) if grad_out is None else _as_rows(grad_out), *(_as_rows(t) for t in grads),
                           _ptr(grad_end), _ptr(grad_state), _ptr(marks), _ptr(offsets), _ptr(stream_ids), None, 0)
     L = load_library()

@@ -208,3 +208,19 @@ def test_recurrence_is_the_formula():
     for t in range(4):
         h = a[t] * h + (1 - a[t]) * x[t]
         assert np.allclose(hs[t], h, rtol=1e-14)
+
+
+def test_matrices_that_share_places():
+    """Against the set of all their places: columns beside each other, rows in between, one beginning within the other."""
+    import random
+    rng, seen = random.Random(3), set()
+    buf = torch.zeros(400)
+    for _ in range(3000):
+        rows, cols, stride = rng.choice([1, 2, 5]), rng.choice([1, 3, 8]), rng.choice([8, 9, 17, 40])
+        a, b = (buf.as_strided((rows, cols), (stride, 1), rng.randrange(0, 200)) for _ in range(2))
+        places = [{t.storage_offset() + r * stride + c for r in range(rows) for c in range(cols)} for t in (a, b)]
+        assert tokens._share(a, b) == bool(places[0] & places[1]), (rows, cols, stride, a.storage_offset(), b.storage_offset())
+        seen.add(tokens._share(a, b))
+    assert seen == {False, True}
+    assert tokens._share(buf[:40].view(4, 10), buf[:60].view(4, 15)[:, :10]) and not tokens._share(buf[:40].view(4, 10), buf[40:100].view(4, 15)[:, :10])
+    assert tokens._share(buf[:40].view(4, 10), buf[5:15].expand(4, 10)) and not tokens._share(buf[:0].view(0, 10), buf[:0].view(0, 10))

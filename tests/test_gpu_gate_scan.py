@@ -399,3 +399,28 @@ def test_two_calls_at_once():
 def test_segments_that_end_about_a_tile(lengths, dtype):
     """Ends at, before and behind the borders of waves, tiles and of the rows that a state is told for."""
     check(lengths, 66, dtype, seed=37)
+
+
+def test_out_that_shares_places_is_refused():
+    """The result over x or gates is refused; beside them in one matrix it is taken."""
+    both = torch.randn(300, 192, generator=torch.Generator().manual_seed(40)).to(DEV)
+    x, gates, out = both[:, :64], both[:, 64:128], both[:, 128:]
+    want = idf.gate_scan(x, gates)
+    assert idf.gate_scan(x, gates, out=out) is out and torch.equal(out, want)
+    for bad in (x, gates, both[:, 32:96], both[:, 1:65]):
+        with pytest.raises(ValueError, match="shares"):
+            idf.gate_scan(x, gates, out=bad)
+    with pytest.raises(ValueError, match="shares"):
+        y = both[:, :64].contiguous()
+        idf.gate_scan(y, y, out=y)
+
+
+def test_streams_that_no_segment_is_of_have_no_gradient():
+    x, gates, _, d, _ = (t.to(DEV) for t in make((40,), 32, torch.float32, seed=41))
+    _, marks = idf.gate_scan(x, gates, marks=True)
+    for kw in (dict(n_streams=5), dict(n_streams=5, stream_ids=torch.tensor([3], dtype=torch.int32, device=DEV))):
+        at = 3 if "stream_ids" in kw else 0
+        filler = torch.full((5, 32), float("nan"), device=DEV)
+        del filler                                 # (its memory is likely to be taken next)
+        ds = idf.gate_scan_backward(x, gates, marks, d, n_segments=1, **kw)[2]
+        assert ds.shape == (5, 32) and ds[at].any() and not ds[[i for i in range(5) if i != at]].any()
