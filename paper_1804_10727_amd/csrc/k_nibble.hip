@@ -439,7 +439,7 @@ __device__ __forceinline__ void exact_row(const idf_nibble_attend_args &a, const
 
 // A workgroup takes the at most 16 RT query rows of one segment and key/value head and a part of the keys; its waves take 32 of them at a time, in turn, each
 // with a softmax of its own, and are joined at the end.  Eight waves where there are workgroups for half the machine only (64 x 16 tokens in float32 on 1000 keys of
-// 4 x 64: 20.7 us by four, 17.6 by eight), else four with two rounds each on their way (64 streams on 4096 keys of 8 x 128: one round 61.6, two 56.5; reading alone, with
+// 4 x 64: 20.7 us by four, 17.6 by eight, before what is said of LDS below), else four with two rounds each on their way (64 streams on 4096 keys of 8 x 128: one round 61.6, two 56.5; reading alone, with
 // nothing done, takes 52, 5.5 TB/s).  What had cost most were choices on the loaded values next to the loads, which wait for them (72 -> 62).  Codes of keys go from memory into the layout of the matrix instruction, a lane having a quarter of a
 // row, whose place along the summed axis is free; those of values through a piece of LDS that is the wave's own, to be read along the keys.
 template <int PREC, int DP, int RT, int WAVES> struct StepShape {
@@ -450,8 +450,21 @@ template <int PREC, int DP, int RT, int WAVES> struct StepShape {
     static constexpr int LOADS = (KEYS * BLOCKS + 63) / 64;                   // of 16 bytes of values per lane
     static constexpr int K_WORDS = DP / 32;                                   // words of eight codes of a key per lane
     static constexpr int K_POWERS = DP == 256 ? 2 : 1;
-    static constexpr int WAVE_FLOATS = 16 * RT * DP > KEYS * STRIDE / 2 ? 16 * RT * DP : KEYS * STRIDE / 2;
+    static constexpr int OUT = DP + 4;                                        // of a row of sums there
+    static constexpr int WAVE_FLOATS = 16 * RT * OUT > KEYS * STRIDE / 2 ? 16 * RT * OUT : KEYS * STRIDE / 2;
 };
+// In LDS a block's four pieces of eight values change places, x to x ^ turn: eight lanes that write a piece each, of blocks that follow each other, then write to banks of
+// their own; rows of sums that are joined there begin four banks apart.  (Without either the 16 tokens of 64 streams above took 16.8 us in a call, with them 15.5; a token on
+// 65,536 keys 22.5 and 21.2.)  read_turned: the values of read_column that lie so, of columns 16 d on.
+template <int DP> __device__ __forceinline__ int step_turn(int row, int block) { return DP == 64 ? row >> 1 & 1 : DP == 128 ? block >> 1 & 1 : block >> 1 & 3; }
+template <int DP> __device__ __forceinline__ bf16x8 read_turned(const __bf16 *lds, int stride, int d, int r0, int r1)
+{
+    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+    const int lane = threadIdx.x & 15, r = lane >> 2, at = r * stride + d / 2 * kBits + (((d & 1) << 1 | (lane >> 1 & 1)) ^ step_turn<DP>(r, d / 2)) * 8 + (lane & 1) * 4;
+    const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(lds + r0 * stride + at));
+    const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(lds + r1 * stride + at));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
 
 template <int PREC, int DP, int RT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || DP <= 128 ? 2 : 1) k_nibble_step(idf_nibble_attend_args a, int splits)
@@ -572,7 +585,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || DP <= 128 ? 2 : 1) k
             const float power = power_of(vp[j]);
             if (S::KEYS * S::BLOCKS % 64 == 0 || piece < S::KEYS * S::BLOCKS)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) *(bf16x8 *)(v_lds + r * S::STRIDE + b * kBits + 8 * w) = values8((uint32_t)vc[j][w], power);
+                for (int w = 0; w < 4; ++w) *(bf16x8 *)(v_lds + r * S::STRIDE + b * kBits + 8 * (w ^ step_turn<DP>(r, b))) = values8((uint32_t)vc[j][w], power);
         }
         __builtin_amdgcn_wave_barrier();
         if (tile + WAVES * S::AHEAD < t1) load(tile + WAVES * S::AHEAD, x_);
@@ -605,7 +618,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || DP <= 128 ? 2 : 1) k
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-            const bf16x8 v = read_column(v_lds, S::STRIDE, 16 * d, 4 * grp, 16 + 4 * grp);
+            const bf16x8 v = read_turned<DP>(v_lds, S::STRIDE, d, 4 * grp, 16 + 4 * grp);
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -629,7 +642,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || DP <= 128 ? 2 : 1) k
         l[r] += __shfl_xor(l[r], 16);
         l[r] += __shfl_xor(l[r], 32);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) *(f32x4 *)(mine + (16 * r + col) * DP + 16 * d + 4 * grp) = o[r][d];
+        for (int d = 0; d < DT; ++d) *(f32x4 *)(mine + (16 * r + col) * S::OUT + 16 * d + 4 * grp) = o[r][d];
         if (grp == 0) { stats[0][wave][16 * r + col] = m[r]; stats[1][wave][16 * r + col] = l[r]; }
     }
     __syncthreads();
@@ -645,7 +658,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || DP <= 128 ? 2 : 1) k
         for (int w = 0; w < WAVES; ++w) {
             const float fade = __builtin_amdgcn_exp2f(stats[0][w][r] - top);
             sum += fade * stats[1][w][r];
-            v += fade * *(const f32x4 *)(lds + w * S::WAVE_FLOATS + r * DP + c);
+            v += fade * *(const f32x4 *)(lds + w * S::WAVE_FLOATS + r * S::OUT + c);
         }
         if (c >= a.head_dim) continue;
         const int t = r / group, h = kv * group + r - t * group;
