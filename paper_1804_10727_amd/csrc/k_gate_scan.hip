@@ -154,7 +154,7 @@ template <int PREC, int V> __device__ __forceinline__ void clear_between(const i
 // number that is stored has these bits) and holds all that it tells, so that nothing else has to be seen with it.  Tiles are numbered in the order in which workgroups begin,
 // and wait for lower numbers only, which have begun; a tile makes known what others may wait for whatever its segment looks like.
 //   Bound by memory: x, gates and results once, and 4 to 12 bytes a channel that tiles tell each other for every 128 or 256 tokens.  65536 tokens of 2048 channels, bfloat16:
-// forward 189 us, 4.3 TB/s, backward 309, 4.35; 262144 of 2048 in float32 5.7 TB/s both.  (Summaries in a launch of their own, and everything read again from
+// forward 185 us, 4.35 TB/s, backward 291, 4.6; 262144 of 2048 in float32 5.7 TB/s both.  (Summaries in a launch of their own, and everything read again from
 // the states that they give, 308 and 436.)  All of it in 128 registers, for two workgroups to a compute unit: what one waits for the other hides.
 constexpr int kTileWaves = 8;
 constexpr int each_of(int blocks) { return 4 / blocks; }                     // tiles that a wave gathers
@@ -217,18 +217,32 @@ template <class Args> __device__ __forceinline__ int segment_at(const Args &a, c
 }
 
 // What a workgroup's waves tell each other: summaries of the waves, then of the tiles before this one, and what all of them begin with.
-template <int V> struct Board {
-    float own[kTileWaves][64][2 * V], before[kTileWaves][64][2 * V], start[64][V];
+template <int V> struct alignas(16) Board {
+    alignas(16) float own[kTileWaves][64][2 * V], before[kTileWaves][64][2 * V], start[64][V];
 };
 template <int V> __device__ __forceinline__ void pin(float (&at)[2 * V], const Summary (&s)[V])
 {
+    Pack<float, 2 * V> p;                          // (in one piece: four lanes would meet in a bank)
 #pragma unroll
-    for (int v = 0; v < V; ++v) { at[2 * v] = s[v].keep; at[2 * v + 1] = s[v].made; }
+    for (int v = 0; v < V; ++v) { p.v[2 * v] = s[v].keep; p.v[2 * v + 1] = s[v].made; }
+    *(Pack<float, 2 * V> *)at = p;
 }
 template <int V> __device__ __forceinline__ void through(const float (&at)[2 * V], float (&h)[V])
 {
+    const Pack<float, 2 * V> p = *(const Pack<float, 2 * V> *)at;
 #pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = through(Summary{at[2 * v], at[2 * v + 1]}, h[v]);
+    for (int v = 0; v < V; ++v) h[v] = through(Summary{p.v[2 * v], p.v[2 * v + 1]}, h[v]);
+}
+
+// f(0) .. f(n - 1), as the compiler unrolls it or step by step (unrolled, the forward pass spills: 198 us where it takes 185; step by step, the backward pass takes 318 and not 292).
+template <bool UNROLL, class F> __device__ __forceinline__ void go(int n, F f)
+{
+    if constexpr (UNROLL) {
+        for (int i = 0; i < n; ++i) f(i);
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) f(i);
+    }
 }
 
 // A tile's place: which row and channels, and the tokens of each wave.
@@ -296,9 +310,10 @@ __device__ __forceinline__ void begin_of(const Args &a, const Tiling &tl, const 
             Summary all[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) all[v] = {1.f, 0.f};
-            for (int i = 0; i < x.waves; ++i)
+            go<BACK>(x.waves, [&](int i) IDF_INLINE {
 #pragma unroll
                 for (int v = 0; v < V; ++v) all[v] = join(all[v], Summary{b.own[i][lane][2 * v], b.own[i][lane][2 * v + 1]});
+            });
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if (x.edge) all[v] = {0.f, through(all[v], b.start[lane][v])};         // (whatever comes before is another segment's)
@@ -333,19 +348,19 @@ __device__ __forceinline__ void begin_of(const Args &a, const Tiling &tl, const 
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = b.start[lane][v];
     if (CHAIN) {
-        for (int i = 0; i * kEach < x.links; ++i) through<V>(b.before[i][lane], h);
+        go<BACK>((x.links + kEach - 1) / kEach, [&](int i) IDF_INLINE { through<V>(b.before[i][lane], h); });
         const int64_t next = BACK ? x.row / kChain - 1 : x.row / kChain + 1;
         if (x.order == 0 && x.row % kChain == (BACK ? 0 : kChain - 1) && next >= 0) {
             float end[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) end[v] = h[v];
-            for (int i = 0; i < x.waves; ++i) through<V>(b.own[i][lane], end);
+            go<BACK>(x.waves, [&](int i) IDF_INLINE { through<V>(b.own[i][lane], end); });
 #pragma unroll
             for (int v = 0; v < V; ++v)
                 if (x.w.on) tell(state_at(a.workspace, tl, next, a.channels) + c + v, told(end[v]));
         }
     }
-    for (int i = 0; i < x.order; ++i) through<V>(b.own[i][lane], h);
+    go<BACK>(x.order, [&](int i) IDF_INLINE { through<V>(b.own[i][lane], h); });
 }
 // A tile without tokens makes known that it changes nothing.
 template <int V, int K, bool BACK, class Args> __device__ __forceinline__ void pass_over(const Args &a, const Tiling &tl, const Tile &x)
