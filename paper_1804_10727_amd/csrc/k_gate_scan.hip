@@ -128,22 +128,6 @@ __device__ __forceinline__ float *marks_at(float *marks, const Work &w, int t, i
     return marks + (w.g.begin / kBlock + w.segment + t / kBlock) * channels + w.c;
 }
 
-// Rows that no segment has have no gradient: those in front of the first one, and from a segment's last token to the next one.
-template <int PREC, int V> __device__ __forceinline__ void clear_between(const idf_gate_scan_backward_args &a, const Work &w)
-{
-    const float zero[V] = {};
-    auto clear = [&](int64_t from, int64_t to) {
-        for (int64_t t = from; t < to; ++t)
-            if (w.on) {
-                Rows<PREC, V>(a.grad_x, t, w.c).store(0, 0, zero);
-                Rows<PREC, V>(a.grad_gates, t, w.c).store(0, 0, zero);
-            }
-    };
-    const bool last = w.segment + 1 == a.n_segments;
-    if (a.offsets && w.segment == 0) clear(0, w.g.begin);
-    clear(w.g.begin + w.g.len, last ? a.n_tokens : a.offsets ? min(max(a.offsets[w.segment + 1], (int64_t)0), a.n_tokens) : w.g.begin + a.max_tokens);
-}
-
 // ---- tiles ----
 
 // A tile is W waves of K blocks each, one behind the other.  Its tokens are read once and stay in registers with their gates: every wave first makes its summary, and goes
@@ -248,7 +232,7 @@ template <bool UNROLL, class F> __device__ __forceinline__ void go(int n, F f)
 // A tile's place: which row and channels, and the tokens of each wave.
 struct Tile {
     Work w;
-    int64_t row;
+    int64_t row, place;                            // place: of the row among the segment's
     int order, waves;                              // order: of this wave among its tile's, in the direction that the states go
     bool edge;                                     // nothing of the segment comes before it in that direction
     int links;                                     // tiles before it, as far as the state that it begins with, and whether there is one
@@ -279,7 +263,8 @@ template <int V, int K, bool CHAIN, bool BACK, class Args> __device__ __forceinl
     w.on = w.c < a.channels;
     if (!w.on) w.c = a.channels - V;
     const int64_t first = CHAIN ? first_row(a, tl, segment) : 0, tokens = K * kBlock;
-    w.group = (int)(x.row - first);
+    x.place = x.row - first;
+    w.group = (int)x.place;
     if (w.group < 0) { w.group = 1; w.g.len = 0; w.g.valid = false; }             // (offsets that do not go up)
     const int64_t t0 = (int64_t)w.group * tl.span + w.wave * tokens;
     w.t0 = (int)min((int64_t)w.g.len, t0);
@@ -486,6 +471,36 @@ __global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_tile(idf_gate_scan_
         for (int v = 0; v < V; ++v) a.state_out[(int64_t)w.g.ring * a.channels + w.c + v] = h[v];
 }
 
+// Rows that no segment has have no gradient: those in front of the first one, and from a segment's last token to the next one.  In a chain a wave clears what lies where its
+// tokens would be, else the waves of all workgroups of the segment share them (65,472 rows behind 64 single tokens of 1024 channels: 2,415 us by one wave, 131 so;
+// behind 4 segments of 1000 2,326 and 76).
+template <int PREC, int V, bool CHAIN> __device__ __forceinline__ void clear_between(const idf_gate_scan_backward_args &a, const Tiling &tl, const Tile &x)
+{
+    const Work &w = x.w;
+    auto clear = [&](int64_t from, int64_t to) {
+        const float zero[V] = {};
+        for (int64_t t = from; t < to; ++t)
+            if (w.on) {
+                Rows<PREC, V>(a.grad_x, t, w.c).store(0, 0, zero);
+                Rows<PREC, V>(a.grad_gates, t, w.c).store(0, 0, zero);
+            }
+    };
+    const int64_t end = w.g.begin + w.g.len;
+    const int64_t next = w.segment + 1 == a.n_segments ? a.n_tokens : a.offsets ? min(max(a.offsets[w.segment + 1], (int64_t)0), a.n_tokens) : w.g.begin + a.max_tokens;
+    if (CHAIN) {
+        const int64_t mine = w.wave * kBlock, behind = w.g.begin + x.place * tl.span + mine;
+        if (x.place >= 0) clear(max(end, behind), min(next, behind + kBlock));
+        // (rows of tiles in front of the first segment's, and what that one leaves of the tile it begins in)
+        const int64_t front = x.row * tl.span + mine;
+        if (w.segment == 0 && x.place <= 0) clear(front, min(w.g.begin, front + kBlock));
+    } else {
+        const int64_t of = (int64_t)gridDim.z * x.waves, i = (int64_t)blockIdx.z * x.waves + w.wave;
+        auto share = [&](int64_t from, int64_t to) { if (to > from) clear(from + (to - from) * i / of, from + (to - from) * (i + 1) / of); };
+        share(end, next);
+        if (w.segment == 0) share(0, w.g.begin);
+    }
+}
+
 template <int PREC, int V, bool CHAIN>
 __global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_back_tile(idf_gate_scan_backward_args a, Tiling tl)
 {
@@ -493,7 +508,8 @@ __global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_back_tile(idf_gate_
     Tile tile;
     if (!tile_of<V, 1, CHAIN, true>(a, tl, tile)) return;
     const Work &w = tile.w;
-    if (w.group == 0 && w.wave == 0) clear_between<PREC, V>(a, w);
+    clear_between<PREC, V, CHAIN>(a, tl, tile);
+    if (!CHAIN && blockIdx.z > 0) return;
     if (w.g.len <= (int64_t)w.group * tl.span) {
         if (CHAIN) pass_over<V, 1, true>(a, tl, tile);
         if (w.g.valid && w.group == 0 && w.wave == 0 && w.on && a.grad_state)
@@ -675,7 +691,9 @@ template <int PREC, int V>
 hipError_t backward(const idf_gate_scan_backward_args &a, const LaunchCtx &lc)
 {
     const Way y = way_of(a, true);
-    const dim3 block(64 * y.waves), grid = y.chain ? dim3((unsigned)(y.tl.rows * y.tl.cols)) : dim3(y.tl.cols, a.n_segments);
+    // (more workgroups where there are rows to clear for sure)
+    const int64_t over = std::max<int64_t>(0, a.n_tokens - a.n_segments * longest(a));
+    const dim3 block(64 * y.waves), grid = y.chain ? dim3((unsigned)(y.tl.rows * y.tl.cols)) : dim3(y.tl.cols, a.n_segments, (unsigned)std::min<int64_t>(64, 1 + over / 256));
     if (!y.chain) return launch(k_gate_back_tile<PREC, V, false>, grid, block, 0, lc, a, y.tl);
     if (const hipError_t e = nothing_told(a, y, lc)) return e;
     return launch(k_gate_back_tile<PREC, V, true>, grid, block, 0, lc, a, y.tl);

@@ -424,3 +424,21 @@ def test_streams_that_no_segment_is_of_have_no_gradient():
         del filler                                 # (its memory is likely to be taken next)
         ds = idf.gate_scan_backward(x, gates, marks, d, n_segments=1, **kw)[2]
         assert ds.shape == (5, 32) and ds[at].any() and not ds[[i for i in range(5) if i != at]].any()
+
+
+@pytest.mark.parametrize("lengths,front,behind", [((1, 1, 0, 1), 5, 3000), ((40, 0, 17), 900, 2000), ((700, 3, 0, 500), 300, 0), ((700, 3, 0, 500), 1000, 5000), ((128,), 0, 1), ((129,), 127, 129)])
+def test_padded_batches(lengths, front, behind):
+    """Many rows in front of the first segment and behind the last one, and behind segments that are cut at max_tokens: no gradient, whichever workgroup clears them."""
+    n = front + sum(lengths) + behind
+    x, gates, _, d, _ = (t.to(DEV) for t in make((n,), 130, torch.bfloat16, seed=50))
+    offsets = (front + torch.tensor([0] + list(lengths)).cumsum(0)).to(DEV)
+    for longest in (max(lengths), max(1, max(lengths) - 200)):
+        kw = dict(offsets=offsets, max_tokens=longest)
+        _, marks = idf.gate_scan(x, gates, marks=True, **kw)
+        filler = [torch.full_like(x, float("nan")) for _ in range(2)]
+        del filler                                 # (their memory is likely to be taken for the gradients)
+        dx, dg, _ = idf.gate_scan_backward(x, gates, marks, d, **kw)
+        mine = torch.zeros(n, dtype=torch.bool)
+        for b, length in enumerate(lengths):
+            mine[int(offsets[b]):int(offsets[b]) + min(length, longest)] = True
+        assert not dx[~mine].any() and not dg[~mine].any() and dx[mine].any(1).all() and torch.isfinite(dg).all()
