@@ -159,8 +159,8 @@ __device__ __forceinline__ uint32_t encode_exact(const double (&y)[8], uint32_t 
 
 // A lane has eight values of a head, four lanes a block; a workgroup a few tokens with all their heads, so that slots, cosines and sines are formed once per
 // token.  Keys that are normalised or turned are formed in 64 bits, whose instructions run as fast as those of 32 here: a value next to the middle between two codes goes to
-// the same one however sums and products are ordered.  What is read and written asks for 17 us of 15,104 tokens with 8 heads of 128 in bfloat16; it takes 46, by
-// the instructions (with every code decided in 64 bits 97; with a workgroup per token 52).  One token of 64 streams: 5.7 us.
+// the same one however sums and products are ordered.  What is read and written asks for 17 us of 15,104 tokens with 8 heads of 128 in bfloat16; it takes 39.5, by
+// the vector instructions (with every code decided in 64 bits 97; with a workgroup per token 52; with keys on the same two of a workgroup's waves, and so on two SIMDs of four, 46).  One token of 64 streams: 5.7 us.
 template <int PREC, bool ALIGNED>
 __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args a, int lanes_log2, int tokens_per_group)
 {
@@ -185,8 +185,8 @@ __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args
         Row r;
         r.t = (int)(((float)row + 0.5f) * per_token);                          // (fewer than 2^15 rows: exact)
         const int which = row - r.t * 2 * heads;
-        r.key = which < heads;
-        r.h = r.key ? which : which - heads;
+        r.key = (which < heads) != (bool)((t0 + r.t) & 1);                     // (keys take longer: a wave has those of every other token)
+        r.h = which < heads ? which : which - heads;
         r.x = P{};
         r.other = P{};
         if (!on) return r;
