@@ -157,6 +157,28 @@ __device__ __forceinline__ uint32_t encode_exact(const double (&y)[8], uint32_t 
     return to_codes(f, 1.f);
 }
 
+// Eight values as they lie in memory: those of 16 bits stay two to a register until they are asked for.
+template <int PREC> struct alignas(16) Eight {
+    using T = typename Elem<PREC>::type;
+    uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ float get(int e) const
+    {
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[e]);
+        else return __builtin_bit_cast(float, e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    }
+    __device__ __forceinline__ static uint32_t bits(T v) { if constexpr (sizeof(T) == 4) return __builtin_bit_cast(uint32_t, v); else return __builtin_bit_cast(uint16_t, v); }
+    // eight values from there, or the n first of them (with whatever behind them)
+    __device__ __forceinline__ void load(const T *from, bool aligned, int n)
+    {
+        if (aligned && n >= 8) { *this = *(const Eight *)from; return; }
+#pragma unroll
+        for (int i = 0; i < (int)(2 * sizeof(T)); ++i) w[i] = 0u;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) w[e * sizeof(T) / 4] |= bits(from[e]) << (sizeof(T) == 4 ? 0 : 16 * (e % 2));
+    }
+};
+
 // A lane has eight values of a head, four lanes a block; a workgroup a few tokens with all their heads, so that slots, cosines and sines are formed once per
 // token.  Keys that are normalised or turned are formed in 64 bits, whose instructions run as fast as those of 32 here: a value next to the middle between two codes goes to
 // the same one however sums and products are ordered.  What is read and written asks for 17 us of 15,104 tokens with 8 heads of 128 in bfloat16; it takes 39.5, by
@@ -164,9 +186,7 @@ __device__ __forceinline__ uint32_t encode_exact(const double (&y)[8], uint32_t 
 template <int PREC, bool ALIGNED>
 __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args a, int lanes_log2, int tokens_per_group)
 {
-    using E = Elem<PREC>;
-    using T = typename E::type;
-    using P = Pack<T, 8>;
+    using T = typename Elem<PREC>::type;
     extern __shared__ double2 turn[];              // [token][rotary_dim / 2]: amplitude * (cos, sin)
     __shared__ int64_t slots[kMostTokens];         // of each token; negative: none
     __shared__ __align__(16) float weight[256];
@@ -179,40 +199,32 @@ __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args
     const float per_token = 1.f / (float)(2 * heads);
     const double per_value = 1.0 / d;
     // a row of a head, and what lies in a pair with this lane's values in the other half of what is turned; the next one is on its way while this one is worked on
-    struct Row { int t, h; bool key; P x, other; };
+    struct Row { int t, h; bool key; Eight<PREC> x, other; };
     const int total = n * 2 * heads, step = 256 >> lanes_log2;
-    auto fetch = [&](int row) IDF_INLINE {
-        Row r;
+    const T *const k0 = (const T *)a.k.base + (g.begin + t0) * a.k.token_stride, *const v0 = (const T *)a.v.base + (g.begin + t0) * a.v.token_stride;
+    auto fetch = [&](int row, Row &r) IDF_INLINE {
         r.t = (int)(((float)row + 0.5f) * per_token);                          // (fewer than 2^15 rows: exact)
         const int which = row - r.t * 2 * heads;
         r.key = (which < heads) != (bool)((t0 + r.t) & 1);                     // (keys take longer: a wave has those of every other token)
         r.h = which < heads ? which : which - heads;
-        r.x = P{};
-        r.other = P{};
-        if (!on) return r;
-        const idf_tokens &from = r.key ? a.k : a.v;
-        const T *src = (const T *)from.base + (g.begin + t0 + r.t) * from.token_stride + r.h * from.head_stride;
-        auto load = [&](int c) IDF_INLINE {
-            P x;
-            if (ALIGNED) return *(const P *)(src + c);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x.v[e] = src[c + e];
-            return x;
-        };
-        r.x = load(c);
+        if (!on) return;
+        const T *src = r.key ? k0 + r.t * a.k.token_stride + r.h * a.k.head_stride : v0 + r.t * a.v.token_stride + r.h * a.v.head_stride;
+        r.x.load(src + c, ALIGNED, 8);
         if (r.key && c < a.rotary_dim && !a.interleaved) {
             if (half % 8 == 0) {
-                r.other = load(c < half ? c + half : c - half);
+                r.other.load(src + (c < half ? c + half : c - half), ALIGNED, 8);
             } else {
+                Pack<T, 8> p = {};
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (c + e < a.rotary_dim) r.other.v[e] = src[c + e < half ? c + e + half : c + e - half];
+                    if (c + e < a.rotary_dim) p.v[e] = src[c + e < half ? c + e + half : c + e - half];
+                r.other.load(p.v, false, 8);
             }
         }
-        return r;
     };
     const int row0 = threadIdx.x >> lanes_log2;
-    Row next = row0 < total ? fetch(row0) : Row{};
+    Row next = {};                                 // (lanes that have no values keep zeros)
+    if (row0 < total) fetch(row0, next);
     if ((int)threadIdx.x < n) {
         const int64_t period = a.slots - a.sinks, p = g.start + t0 + threadIdx.x;
         slots[threadIdx.x] = p < a.sinks ? p : t0 + (int)threadIdx.x < g.len - period ? -1 : a.sinks + (p - a.sinks) % period;
@@ -225,9 +237,10 @@ __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args
         turn[i] = make_double2(a.amplitude * c, a.amplitude * s);
     }
     __syncthreads();
+    const uint64_t ring = (uint64_t)g.ring * heads * a.slots;
     for (int row = row0; row < total; row += step) {
         const Row now = next;
-        if (row + step < total) next = fetch(row + step);
+        if (row + step < total) fetch(row + step, next);
         const int t = now.t, h = now.h;
         const bool key = now.key;
         const int64_t slot = slots[t];
@@ -236,13 +249,13 @@ __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args
         if (!key || plain) {
             float x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = E::to_f32(now.x.v[e]);
+            for (int e = 0; e < 8; ++e) x[e] = now.x.get(e);
             bool close;
             codes = encode<true>(x, byte, close);
         } else {
             double y[8], norm = 1.0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = E::to_f32(now.x.v[e]);
+            for (int e = 0; e < 8; ++e) y[e] = now.x.get(e);
             if (a.k_weight) {
                 double sum = 0.0;
 #pragma unroll
@@ -273,7 +286,7 @@ __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args
                     for (int e = 0; e < 8; ++e) {
                         const int i = c + e, j = i < half ? i + half : i - half;
                         if (i >= a.rotary_dim) continue;
-                        const double q = E::to_f32(now.other.v[e]), o = a.k_weight ? q * (norm * weight[j]) : q;
+                        const double q = now.other.get(e), o = a.k_weight ? q * (norm * weight[j]) : q;
                         const double2 r = cs[i < half ? i : j];
                         y[e] = y[e] * r.x + (i < half ? -o : o) * r.y;
                     }
@@ -286,9 +299,9 @@ __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args
             codes = encode<false>(near, byte, close);
             if (__ballot(close)) codes = encode_exact(y, byte);
         }
-        const Held4<uint8_t> to(key ? a.ring.k_codes : a.ring.v_codes, key ? a.ring.k_scales : a.ring.v_scales, a.slots, heads, d, g.ring, h);
-        if (on) *(uint32_t *)(to.codes + slot * (d / 2) + c / 2) = codes;
-        if (on && lane % 4 == 0) to.scales[slot * (d / kBits) + lane / 4] = (uint8_t)byte;
+        const uint64_t place = ring + (uint64_t)(uint32_t)h * (uint32_t)a.slots + (uint32_t)slot;
+        if (on) *(uint32_t *)((key ? a.ring.k_codes : a.ring.v_codes) + (place * (uint32_t)(d / 2) + c / 2)) = codes;
+        if (on && lane % 4 == 0) (key ? a.ring.k_scales : a.ring.v_scales)[place * (uint32_t)(d / kBits) + lane / 4] = (uint8_t)byte;
     }
 }
 
