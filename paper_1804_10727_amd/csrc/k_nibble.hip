@@ -181,7 +181,7 @@ template <int PREC> struct alignas(16) Eight {
 
 // A lane has eight values of a head, four lanes a block; a workgroup a few tokens with all their heads, so that slots, cosines and sines are formed once per
 // token.  Keys that are normalised or turned are formed in 64 bits, whose instructions run as fast as those of 32 here: a value next to the middle between two codes goes to
-// the same one however sums and products are ordered.  What is read and written asks for 17 us of 15,104 tokens with 8 heads of 128 in bfloat16; it takes 39.5, by
+// the same one however sums and products are ordered.  What is read and written asks for 17 us of 15,104 tokens with 8 heads of 128 in bfloat16; it takes 38.5, by
 // the vector instructions (with every code decided in 64 bits 97; with a workgroup per token 52; with keys on the same two of a workgroup's waves, and so on two SIMDs of four, 46).  One token of 64 streams: 5.7 us.
 template <int PREC, bool ALIGNED>
 __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args a, int lanes_log2, int tokens_per_group)
