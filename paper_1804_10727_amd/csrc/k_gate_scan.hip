@@ -17,7 +17,7 @@ namespace idf {
 
 namespace {
 
-constexpr int kBlock = 16;                         // tokens that a wave has in registers
+constexpr int kBlock = 16;                         // tokens of a block
 constexpr float kGateMost = 87.f;
 
 // The smaller one of what a gate keeps and takes in, with the gate's sign: above zero it is what is taken in.
