@@ -923,7 +923,7 @@ int splits_of(const idf_nibble_attend_args &a, bool step, int64_t pairs, int64_t
     const double rows = (double)std::min<int64_t>(a.n_tokens, a.n_segments * longest(a)) * a.heads_q;
     int best = 1;
     double least = 0.0;
-    for (int64_t per = rounds; per >= 1; per = per > 8 ? per * 7 / 8 : per - 1) {
+    for (int64_t per = rounds; per >= 1; per = per > 32 ? per * 7 / 8 : per - 1) {
         const int64_t n = (rounds + per - 1) / per;
         if (n > 1 && (n > kMostSplits || pairs * n > held)) break;
         const double each = !step ? 1.0 + 0.006 * a.head_dim : eight_waves(a, pairs * n) ? 0.65 : 1.25;
