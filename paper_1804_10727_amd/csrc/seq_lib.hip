@@ -450,23 +450,34 @@ int idf_gate_scan_backward_workspace(const idf_gate_scan_backward_args *a, size_
 int idf_gate_scan_backward(const idf_gate_scan_backward_args *a, void *hip_stream)
 {
     if (int rc = check_gate(a)) return rc;
-    if (a->n_segments == 0 || (a->n_tokens == 0 && !a->grad_state)) return IDF_OK;
+    if (a->n_tokens == 0 && (a->n_segments == 0 || !a->grad_state)) return IDF_OK;
     const int eb = bytes_of(a->precision);
     if (a->n_tokens) {
-        int rc = check_rows("x", a->x, eb, false, a->n_tokens, a->channels);
-        if (!rc) rc = check_rows("gates", a->gates, eb, false, a->n_tokens, a->channels);
-        if (!rc && a->grad_out.base) rc = check_rows("grad_out", a->grad_out, eb, false, a->n_tokens, a->channels);
+        int rc = IDF_OK;
+        if (a->n_segments) {
+            rc = check_rows("x", a->x, eb, false, a->n_tokens, a->channels);
+            if (!rc) rc = check_rows("gates", a->gates, eb, false, a->n_tokens, a->channels);
+            if (!rc && a->grad_out.base) rc = check_rows("grad_out", a->grad_out, eb, false, a->n_tokens, a->channels);
+        }
         if (!rc) rc = check_rows("grad_x", a->grad_x, eb, true, a->n_tokens, a->channels);
         if (!rc) rc = check_rows("grad_gates", a->grad_gates, eb, true, a->n_tokens, a->channels);
         if (rc) return rc;
-        if (!a->marks) return fail(IDF_EINVAL, "marks: null pointer");
+        if (a->n_segments && !a->marks) return fail(IDF_EINVAL, "marks: null pointer");
     }
     if ((uintptr_t)a->marks % 256) return fail(IDF_EINVAL, "marks have to be 256-byte aligned");
     if (((uintptr_t)a->grad_end | (uintptr_t)a->grad_state) % 4) return fail(IDF_EINVAL, "gradients of states: not aligned to their values");
-    if (int rc = check_workspace(a->workspace, a->workspace_bytes, gate_scan_workspace(*a))) return rc;
+    idf_gate_scan_backward_args b = *a;
+    if (b.n_segments == 0) {                       // rows of none: as those behind one segment without tokens, which has no state
+        b.n_segments = 1;
+        b.max_tokens = 0;
+        b.offsets = nullptr;
+        b.stream_ids = nullptr;
+        b.grad_state = nullptr;
+    }
+    if (int rc = check_workspace(b.workspace, b.workspace_bytes, gate_scan_workspace(b))) return rc;
     LaunchCtx lc;
     lc.st = (hipStream_t)hip_stream;
-    const hipError_t e = launch_gate_scan_backward(*a, lc);
+    const hipError_t e = launch_gate_scan_backward(b, lc);
     return e == hipSuccess ? IDF_OK : dev_fail(e, "gate_scan_backward");
 }
 

@@ -615,10 +615,9 @@ int gate_gradients(idf_gate_scan_backward_args &a, const at::Tensor &x, const at
     if (rc != IDF_OK) return rc;
     a.marks = plain<float>(&marks, at::kFloat, (int64_t)bytes / 4, x);
     a.grad_end = end ? static_cast<const float *>(end->data_ptr()) : nullptr;
-    const auto fresh = [&]() { return a.n_segments ? at::empty(x.sizes(), x.options()) : at::zeros(x.sizes(), x.options()); };
     // (streams that no segment is of have no gradient)
     const auto state = x.options().dtype(at::kFloat);
-    to = {fresh(), fresh(), !a.stream_ids && a.n_streams == a.n_segments ? at::empty({a.n_streams, a.channels}, state) : at::zeros({a.n_streams, a.channels}, state)};
+    to = {at::empty(x.sizes(), x.options()), at::empty(x.sizes(), x.options()), !a.stream_ids && a.n_streams == a.n_segments ? at::empty({a.n_streams, a.channels}, state) : at::zeros({a.n_streams, a.channels}, state)};
     a.grad_x = matrix(to.x, x);
     a.grad_gates = matrix(to.gates, x);
     a.grad_state = static_cast<float *>(to.state.data_ptr());

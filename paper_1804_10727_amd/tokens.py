@@ -619,7 +619,7 @@ def _gate_scan_backward(x, gates, marks, grad_out, grad_end, offsets, max_tokens
         if grad_out.shape != x.shape:
             raise ValueError(f"grad_out {tuple(grad_out.shape)} of x {tuple(x.shape)}")
     marks = _plain(marks, torch.float32, (_marks_floats(sizes, offsets),), x.device, "marks")
-    grads = [torch.zeros(x.shape, dtype=x.dtype, device=x.device) for _ in range(2)]
+    grads = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for _ in range(2)]
     grad_state = torch.zeros(sizes[5], x.shape[1], device=x.device)        # (streams that no segment is of have no gradient here)
     a = _GateScanBackward(*sizes, _as_rows(x), _as_rows(gates), _Rows(None, 0) if grad_out is None else _as_rows(grad_out), *(_as_rows(t) for t in grads),
                           _ptr(grad_end), _ptr(grad_state), _ptr(marks), _ptr(offsets), _ptr(stream_ids), None, 0)

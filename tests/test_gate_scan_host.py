@@ -1,0 +1,29 @@
+"""What calls of the gated recurrence launch where there is little or nothing to go over, on a stand-in for the HIP runtime (no GPU)."""
+import pytest
+
+import host_runtime
+from test_few_bits_host import AT, call, gate_args, workspace
+
+
+@pytest.fixture(scope="session")
+def runtime(tmp_path_factory):
+    return host_runtime.build(tmp_path_factory.mktemp("runtime"))
+
+
+def rows_of_no_segment(rt):
+    """The backward pass sets them to zero where there are no segments at all, too: one launch, no workspace, whatever max_tokens says."""
+    for precision in (0, 1):
+        for rows, max_tokens in ((100, 100), (100, 0), (300000, 1 << 20)):
+            a = gate_args(rows, max_tokens, 64, precision, 0, back=True)
+            a.offsets = AT
+            assert workspace("idf_gate_scan_backward", a) == 0
+            assert call(rt, "idf_gate_scan_backward", a) == 0 and rt.host_launches(None) == rt.host_launches(b"k_gate_back_tile") == 1
+            a.grad_gates.base = None
+            assert call(rt, "idf_gate_scan_backward", a) == -1 and rt.host_launches(None) == 0
+    a = gate_args(0, 0, 64, 0, 0, back=True)
+    a.offsets = AT
+    assert call(rt, "idf_gate_scan_backward", a) == 0 and rt.host_launches(None) == 0
+
+
+def test_rows_of_no_segment(runtime):
+    host_runtime.run(runtime, "test_gate_scan_host", "rows_of_no_segment")
