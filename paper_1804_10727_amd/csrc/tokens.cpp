@@ -75,7 +75,8 @@ const at::Tensor *recorded_tensor(PyObject *o)
 const at::Tensor *tensor(PyObject *o)
 {
     const at::Tensor *t = recorded_tensor(o);
-    need(!t || !t->requires_grad() || !c10::GradMode::is_enabled());         // (refused there: there is no backward pass)
+    // (refused there: there is no backward pass, and no tangent of a result)
+    need(!t || ((!t->requires_grad() || !c10::GradMode::is_enabled()) && !t->_fw_grad(0).defined()));
     return t;
 }
 

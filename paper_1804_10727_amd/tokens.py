@@ -1,8 +1,9 @@
 """The operators that mix the tokens of streams (include/idf.h, last sections) on torch tensors: argument marshalling only.
 
 Everything is enqueued on the current stream of the tensors' device.  There is no backward pass but that of gate_scan_recorded: tensors that require
-gradients are refused elsewhere where gradients are recorded, taken under torch.no_grad().  Packed tokens [token][head][value]; a tensor whose values lie
-apart, or whose rows do not begin at multiples of 16 bytes where the library asks for that, is copied first.
+gradients are refused elsewhere where gradients are recorded, taken under torch.no_grad(); tensors that carry a tangent of torch's forward mode are
+refused everywhere.  Packed tokens [token][head][value]; a tensor whose values lie apart, or whose rows do not begin at multiples of 16 bytes where the
+library asks for that, is copied first.
 """
 from __future__ import annotations
 
@@ -117,6 +118,8 @@ def _no_gradients(**tensors):
     for what, t in tensors.items():
         if torch.is_grad_enabled() and getattr(t, "requires_grad", False):
             raise ValueError(f"{what} requires gradients, and there is no backward pass: detach it, or call under torch.no_grad()")
+        if isinstance(t, torch.Tensor) and torch.autograd.forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError(f"{what} carries a tangent, and results have none: unpack it first")
 
 
 def _precision(t):

@@ -44,3 +44,36 @@ def test_gradients_without_segments(rows, channels, dtype):
         del filler                                 # (their memory is likely to be taken for the gradients)
         got = f(x, gates, marks, d, offsets=offsets, max_tokens=rows)
         assert not got[0].any() and not got[1].any() and not got[2].any()
+
+
+def test_tangents_are_refused():
+    """Forward mode: refused by every call, not answered with a derivative of zero; what carries no tangent is taken beside it."""
+    x, gates, d = make(40, 64, torch.float32)
+    w, ws = idf.quantize_rows(torch.randn(32, 64, device=DEV))
+    ring, heads = idf.nibble_ring(1, 64, 1, 64, DEV), x[:, None]
+    _, marks = idf.gate_scan(x, gates, marks=True)
+    state = torch.zeros(1, 64, device=DEV)
+    with torch.autograd.forward_ad.dual_level():
+        t = torch.autograd.forward_ad.make_dual(x, torch.ones_like(x))
+        h = t[:, None]
+        for call in (lambda: idf.gate_scan(t, gates), lambda: idf.gate_scan(x, t), lambda: idf.gate_scan(x, gates, t[:1]), lambda: idf.gate_scan_backward(x, gates, marks, t), lambda: idf.quantize_rows(t),
+                     lambda: idf.project_rows(t, w, ws), lambda: idf.project_rows(x, w, ws, bias=t[0, :32]), lambda: idf.nibble_append(h, heads, ring), lambda: idf.nibble_attend(h, ring, window=9),
+                     lambda: idf.norm_rotate(h, heads, torch.arange(40, device=DEV), idf.rotary_frequencies(64, device=DEV)[0]), lambda: idf.window_attend(heads, h, heads, window=9),
+                     lambda: idf.decay_attend(heads, heads, h, torch.zeros(1, device=DEV))):
+            for mode in (torch.enable_grad, torch.no_grad):
+                with mode(), pytest.raises(ValueError, match="tangent"):
+                    call()
+        with pytest.raises((NotImplementedError, RuntimeError)):
+            idf.gate_scan_recorded(t, gates, state)
+        assert torch.equal(idf.gate_scan(x, gates, state), idf.gate_scan(t.detach(), gates, state))
+        with torch.autograd.forward_ad._set_fwd_grad_enabled(False):
+            assert torch.equal(idf.gate_scan(t, gates, state), idf.gate_scan(x, gates, state))
+
+
+@pytest.mark.parametrize("call", [lambda x, g: idf.gate_scan(x, g), lambda x, g: idf.gate_scan_recorded(x, g)[0]], ids=["gate_scan", "recorded"])
+def test_torchs_transforms_are_refused(call):
+    """vmap, grad and jvp hand over tensors without memory of their own."""
+    x, gates, _ = make(40, 64, torch.float32)
+    for f in (lambda: torch.func.vmap(call)(x[None], gates[None]), lambda: torch.func.grad(lambda y: call(y, gates).sum())(x), lambda: torch.func.jvp(lambda y: call(y, gates), (x,), (x,))):
+        with pytest.raises((RuntimeError, ValueError, NotImplementedError)):
+            f()
