@@ -630,7 +630,7 @@ int idf_nibble_values(const idf_nibble_values_args *a, void *hip_stream);
 /* A gated recurrence per channel:  h_t = a_t h_{t-1} + (1 - a_t) x_t,  a_t = 1 / (1 + exp(-g_t)),  out_t = h_t,
  * with gates held to -87 .. 87 (neither what is kept nor what is taken in is ever nothing: an infinite state stays infinite).  state_in, state_out: float32
  * [n_streams][channels], from the state of the segment's stream before it to the one after it, as in idf_decay_attend.  States are float32 throughout.
- * out must not overlap x or gates.
+ * out must not overlap x or gates.  clear_rows: whether rows of out that none of the segments has are set to zero (0: left as they are).
  *   marks (NULL: not wanted): what the backward pass needs beside x and gates, states within the segments, idf_gate_scan_marks bytes, 256-byte
  * aligned.  Rows need no alignment beyond their values'.  1 <= channels <= 2^20; segments of up to 2^30 tokens; where one has more than 128,
  * (n_tokens / 128 + n_segments) * channels / 64 < 2^23. */
@@ -645,6 +645,7 @@ typedef struct {
     const int32_t *stream_ids;
     void *workspace;
     size_t workspace_bytes;
+    int clear_rows;
 } idf_gate_scan_args;
 int idf_gate_scan_marks(const idf_gate_scan_args *a, size_t *bytes);
 int idf_gate_scan_workspace(const idf_gate_scan_args *a, size_t *bytes);

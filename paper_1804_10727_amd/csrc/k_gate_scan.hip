@@ -366,6 +366,35 @@ template <int PREC> __device__ __forceinline__ Gate held_gate(float g)
     return gate_of<PREC>(__builtin_fabsf(g) > kGateMost ? __builtin_copysignf(kGateMost, g) : g);
 }
 
+// Rows that no segment has, which are cleared where somebody asks for it, and always of gradients: those in front of the first segment, and from a segment's last token to
+// the next one.  In a chain a wave clears what lies where its tokens would be, else the waves of all workgroups of the segment share them (65,472 rows behind 64
+// single tokens of 1024 channels, backward: 2,415 us by one wave, 131 so; behind 4 segments of 1000 2,326 and 76).
+template <int K, bool CHAIN, class Args, class Clear> __device__ __forceinline__ void rows_between(const Args &a, const Tiling &tl, const Tile &x, Clear clear)
+{
+    constexpr int kTokens = K * kBlock;            // of a wave
+    const Work &w = x.w;
+    const int64_t end = w.g.begin + w.g.len;
+    const int64_t next = w.segment + 1 == a.n_segments ? a.n_tokens : a.offsets ? min(max(a.offsets[w.segment + 1], (int64_t)0), a.n_tokens) : w.g.begin + a.max_tokens;
+    if (CHAIN) {
+        const int64_t mine = w.wave * kTokens, behind = w.g.begin + x.place * tl.span + mine;
+        if (x.place >= 0) clear(max(end, behind), min(next, behind + kTokens));
+        // (rows of tiles in front of the first segment's, and what that one leaves of the tile it begins in)
+        const int64_t front = x.row * tl.span + mine;
+        if (w.segment == 0 && x.place <= 0) clear(front, min(w.g.begin, front + kTokens));
+    } else {
+        const int64_t of = (int64_t)gridDim.z * x.waves, i = (int64_t)blockIdx.z * x.waves + w.wave;
+        auto share = [&](int64_t from, int64_t to) { if (to > from) clear(from + (to - from) * i / of, from + (to - from) * (i + 1) / of); };
+        share(end, next);
+        if (w.segment == 0) share(0, w.g.begin);
+    }
+}
+template <int PREC, int V> __device__ __forceinline__ void clear_rows(const idf_rows &r, const Work &w, int64_t from, int64_t to)
+{
+    const float zero[V] = {};
+    for (int64_t t = from; t < to; ++t)
+        if (w.on) Rows<PREC, V>(r, t, w.c).store(0, 0, zero);
+}
+
 template <int PREC, int V, int K, bool CHAIN>
 __global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_tile(idf_gate_scan_args a, Tiling tl)
 {
@@ -373,6 +402,8 @@ __global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_tile(idf_gate_scan_
     Tile tile;
     if (!tile_of<V, K, CHAIN, false>(a, tl, tile)) return;
     const Work &w = tile.w;
+    if (a.clear_rows) rows_between<K, CHAIN>(a, tl, tile, [&](int64_t from, int64_t to) IDF_INLINE { clear_rows<PREC, V>(a.out, w, from, to); });
+    if (!CHAIN && blockIdx.z > 0) return;
     if (w.g.len <= (int64_t)w.group * tl.span) {
         if (CHAIN) pass_over<V, K, false>(a, tl, tile);
         if (w.g.valid && w.group == 0 && w.wave == 0 && w.on && a.state_out)
@@ -471,36 +502,6 @@ __global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_tile(idf_gate_scan_
         for (int v = 0; v < V; ++v) a.state_out[(int64_t)w.g.ring * a.channels + w.c + v] = h[v];
 }
 
-// Rows that no segment has have no gradient: those in front of the first one, and from a segment's last token to the next one.  In a chain a wave clears what lies where its
-// tokens would be, else the waves of all workgroups of the segment share them (65,472 rows behind 64 single tokens of 1024 channels: 2,415 us by one wave, 131 so;
-// behind 4 segments of 1000 2,326 and 76).
-template <int PREC, int V, bool CHAIN> __device__ __forceinline__ void clear_between(const idf_gate_scan_backward_args &a, const Tiling &tl, const Tile &x)
-{
-    const Work &w = x.w;
-    auto clear = [&](int64_t from, int64_t to) {
-        const float zero[V] = {};
-        for (int64_t t = from; t < to; ++t)
-            if (w.on) {
-                Rows<PREC, V>(a.grad_x, t, w.c).store(0, 0, zero);
-                Rows<PREC, V>(a.grad_gates, t, w.c).store(0, 0, zero);
-            }
-    };
-    const int64_t end = w.g.begin + w.g.len;
-    const int64_t next = w.segment + 1 == a.n_segments ? a.n_tokens : a.offsets ? min(max(a.offsets[w.segment + 1], (int64_t)0), a.n_tokens) : w.g.begin + a.max_tokens;
-    if (CHAIN) {
-        const int64_t mine = w.wave * kBlock, behind = w.g.begin + x.place * tl.span + mine;
-        if (x.place >= 0) clear(max(end, behind), min(next, behind + kBlock));
-        // (rows of tiles in front of the first segment's, and what that one leaves of the tile it begins in)
-        const int64_t front = x.row * tl.span + mine;
-        if (w.segment == 0 && x.place <= 0) clear(front, min(w.g.begin, front + kBlock));
-    } else {
-        const int64_t of = (int64_t)gridDim.z * x.waves, i = (int64_t)blockIdx.z * x.waves + w.wave;
-        auto share = [&](int64_t from, int64_t to) { if (to > from) clear(from + (to - from) * i / of, from + (to - from) * (i + 1) / of); };
-        share(end, next);
-        if (w.segment == 0) share(0, w.g.begin);
-    }
-}
-
 template <int PREC, int V, bool CHAIN>
 __global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_back_tile(idf_gate_scan_backward_args a, Tiling tl)
 {
@@ -508,7 +509,10 @@ __global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_back_tile(idf_gate_
     Tile tile;
     if (!tile_of<V, 1, CHAIN, true>(a, tl, tile)) return;
     const Work &w = tile.w;
-    clear_between<PREC, V, CHAIN>(a, tl, tile);
+    rows_between<1, CHAIN>(a, tl, tile, [&](int64_t from, int64_t to) IDF_INLINE {
+        clear_rows<PREC, V>(a.grad_x, w, from, to);
+        clear_rows<PREC, V>(a.grad_gates, w, from, to);
+    });
     if (!CHAIN && blockIdx.z > 0) return;
     if (w.g.len <= (int64_t)w.group * tl.span) {
         if (CHAIN) pass_over<V, 1, true>(a, tl, tile);
@@ -678,11 +682,14 @@ template <class Args> hipError_t nothing_told(const Args &a, const Way &y, const
     return launch(k_gate_absent, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 4096)), dim3(256), 0, lc, (uint4 *)a.workspace, n);
 }
 
+// Workgroups for a segment where one would do: more of them where there are rows to clear for sure.
+template <class Args> unsigned clearing(const Args &a) { return (unsigned)std::min<int64_t>(64, 1 + std::max<int64_t>(0, a.n_tokens - a.n_segments * longest(a)) / 256); }
+
 template <int PREC, int V>
 hipError_t forward(const idf_gate_scan_args &a, const LaunchCtx &lc)
 {
     const Way y = way_of(a, false);
-    const dim3 block(64 * y.waves), grid = y.chain ? dim3((unsigned)(y.tl.rows * y.tl.cols)) : dim3(y.tl.cols, a.n_segments);
+    const dim3 block(64 * y.waves), grid = y.chain ? dim3((unsigned)(y.tl.rows * y.tl.cols)) : dim3(y.tl.cols, a.n_segments, a.clear_rows ? clearing(a) : 1);
     if (!y.chain) return launch(y.blocks == 1 ? k_gate_tile<PREC, V, 1, false> : k_gate_tile<PREC, V, 2, false>, grid, block, 0, lc, a, y.tl);
     if (const hipError_t e = nothing_told(a, y, lc)) return e;
     return launch(y.blocks == 1 ? k_gate_tile<PREC, V, 1, true> : k_gate_tile<PREC, V, 2, true>, grid, block, 0, lc, a, y.tl);
@@ -691,9 +698,7 @@ template <int PREC, int V>
 hipError_t backward(const idf_gate_scan_backward_args &a, const LaunchCtx &lc)
 {
     const Way y = way_of(a, true);
-    // (more workgroups where there are rows to clear for sure)
-    const int64_t over = std::max<int64_t>(0, a.n_tokens - a.n_segments * longest(a));
-    const dim3 block(64 * y.waves), grid = y.chain ? dim3((unsigned)(y.tl.rows * y.tl.cols)) : dim3(y.tl.cols, a.n_segments, (unsigned)std::min<int64_t>(64, 1 + over / 256));
+    const dim3 block(64 * y.waves), grid = y.chain ? dim3((unsigned)(y.tl.rows * y.tl.cols)) : dim3(y.tl.cols, a.n_segments, clearing(a));
     if (!y.chain) return launch(k_gate_back_tile<PREC, V, false>, grid, block, 0, lc, a, y.tl);
     if (const hipError_t e = nothing_told(a, y, lc)) return e;
     return launch(k_gate_back_tile<PREC, V, true>, grid, block, 0, lc, a, y.tl);

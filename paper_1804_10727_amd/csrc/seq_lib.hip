@@ -189,6 +189,26 @@ int check_gate(const Args *a)
     return IDF_OK;
 }
 
+// Rows that are none's where a call has no segments: as those behind one segment without tokens, which has no state.
+idf_gate_scan_args without_segments(idf_gate_scan_args a)
+{
+    a.n_segments = 1;
+    a.max_tokens = 0;
+    a.offsets = nullptr;
+    a.stream_ids = nullptr;
+    a.state_out = nullptr;
+    return a;
+}
+idf_gate_scan_backward_args without_segments(idf_gate_scan_backward_args a)
+{
+    a.n_segments = 1;
+    a.max_tokens = 0;
+    a.offsets = nullptr;
+    a.stream_ids = nullptr;
+    a.grad_state = nullptr;
+    return a;
+}
+
 int check_workspace(void *p, size_t have, size_t need)
 {
     if (need == 0) return IDF_OK;
@@ -422,20 +442,23 @@ int idf_gate_scan_workspace(const idf_gate_scan_args *a, size_t *bytes)
 int idf_gate_scan(const idf_gate_scan_args *a, void *hip_stream)
 {
     if (int rc = check_gate(a)) return rc;
-    if (a->n_segments == 0 || (longest(*a) == 0 && !a->state_out)) return IDF_OK;
+    const bool clear = a->clear_rows && a->n_tokens;
+    if (!clear && (a->n_segments == 0 || (longest(*a) == 0 && !a->state_out))) return IDF_OK;
     const int eb = bytes_of(a->precision);
-    if (longest(*a)) {
+    if (a->n_segments && longest(*a)) {
         int rc = check_rows("x", a->x, eb, false, a->n_tokens, a->channels);
         if (!rc) rc = check_rows("gates", a->gates, eb, false, a->n_tokens, a->channels);
-        if (!rc) rc = check_rows("out", a->out, eb, true, a->n_tokens, a->channels);
         if (rc) return rc;
     }
+    if (clear || longest(*a))
+        if (int rc = check_rows("out", a->out, eb, true, a->n_tokens, a->channels)) return rc;
     if ((uintptr_t)a->marks % 256) return fail(IDF_EINVAL, "marks have to be 256-byte aligned");
     if (((uintptr_t)a->state_in | (uintptr_t)a->state_out) % 4) return fail(IDF_EINVAL, "states: not aligned to their values");
-    if (int rc = check_workspace(a->workspace, a->workspace_bytes, gate_scan_workspace(*a))) return rc;
+    const idf_gate_scan_args b = a->n_segments ? *a : without_segments(*a);
+    if (int rc = check_workspace(b.workspace, b.workspace_bytes, gate_scan_workspace(b))) return rc;
     LaunchCtx lc;
     lc.st = (hipStream_t)hip_stream;
-    const hipError_t e = launch_gate_scan(*a, lc);
+    const hipError_t e = launch_gate_scan(b, lc);
     return e == hipSuccess ? IDF_OK : dev_fail(e, "gate_scan");
 }
 
@@ -466,14 +489,7 @@ int idf_gate_scan_backward(const idf_gate_scan_backward_args *a, void *hip_strea
     }
     if ((uintptr_t)a->marks % 256) return fail(IDF_EINVAL, "marks have to be 256-byte aligned");
     if (((uintptr_t)a->grad_end | (uintptr_t)a->grad_state) % 4) return fail(IDF_EINVAL, "gradients of states: not aligned to their values");
-    idf_gate_scan_backward_args b = *a;
-    if (b.n_segments == 0) {                       // rows of none: as those behind one segment without tokens, which has no state
-        b.n_segments = 1;
-        b.max_tokens = 0;
-        b.offsets = nullptr;
-        b.stream_ids = nullptr;
-        b.grad_state = nullptr;
-    }
+    const idf_gate_scan_backward_args b = a->n_segments ? *a : without_segments(*a);
     if (int rc = check_workspace(b.workspace, b.workspace_bytes, gate_scan_workspace(b))) return rc;
     LaunchCtx lc;
     lc.st = (hipStream_t)hip_stream;

@@ -568,6 +568,7 @@ PyObject *gate_scan(PyObject *, PyObject *const *args, Py_ssize_t n)
         const at::Tensor out = output(given, x->sizes(), *x);
         need(out.scalar_type() == x->scalar_type());
         a.out = matrix(out, *x);
+        a.clear_rows = !given && a.offsets;        // (a new result holds nothing yet)
         if (given)                                 // (what may share places with it is looked at more closely the long way round)
             for (const idf_rows *r : {&a.x, &a.gates}) {
                 const auto end = [&](const idf_rows &m) { return (uintptr_t)m.base + ((a.n_tokens ? a.n_tokens - 1 : 0) * m.row_stride + a.channels) * x->element_size(); };
@@ -671,6 +672,7 @@ struct GateScan : torch::autograd::Function<GateScan> {
         const at::Tensor out = at::empty(x.sizes(), x.options()), end = at::empty({segments, x.size(1)}, x.options().dtype(at::kFloat));
         a.out = matrix(out, x);
         a.state_out = static_cast<float *>(end.data_ptr());
+        a.clear_rows = a.offsets != nullptr;
         size_t bytes = 0;
         need(fn.gate_marks(&a, &bytes) == IDF_OK);
         const at::Tensor marks = at::empty({(int64_t)bytes / 4}, x.options().dtype(at::kFloat));

@@ -90,7 +90,7 @@ _GATE_SIZES = [("precision", C.c_int), ("channels", C.c_int), ("n_tokens", C.c_i
 
 class _GateScan(C.Structure):
     _fields_ = (_GATE_SIZES + [(n, _Rows) for n in ("x", "gates", "out")] +
-                [(n, C.c_void_p) for n in ("state_in", "state_out", "marks", "offsets", "stream_ids", "workspace")] + [("workspace_bytes", C.c_size_t)])
+                [(n, C.c_void_p) for n in ("state_in", "state_out", "marks", "offsets", "stream_ids", "workspace")] + [("workspace_bytes", C.c_size_t), ("clear_rows", C.c_int)])
 
 
 class _GateScanBackward(C.Structure):
@@ -561,7 +561,8 @@ def _marks_floats(sizes, offsets):
 
 def gate_scan(x, gates, state=None, state_out=None, *, offsets=None, max_tokens=None, n_segments=None, stream_ids=None, out=None, marks=None):
     """h = a h + (1 - a) x per channel along the tokens of packed segments, a = sigmoid(gates): x, gates and the result [token][channel], from `state` (float32
-    [stream][channel], None: zeros) into `state_out` (None: not wanted; may be `state`) (idf_gate_scan).  Segments as in decay_attend.
+    [stream][channel], None: zeros) into `state_out` (None: not wanted; may be `state`) (idf_gate_scan).  Segments as in decay_attend; rows that none of them
+    has are zeros in a new result, and stay as they are in `out`.
     marks True: returns (out, marks), the latter for gate_scan_backward.  gate_scan_recorded is the form that torch's gradients go through."""
     r = _direct("gate_scan", x, gates, state, state_out, offsets, max_tokens, n_segments, stream_ids, out, marks)
     return r if r is not None else _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stream_ids, out, marks)
@@ -587,6 +588,7 @@ def _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stre
     _no_gradients(x=x, gates=gates, state=state, state_out=state_out, out=out)
     x, gates = _matrix(x, x, "x"), _matrix(gates, x, "gates")
     sizes, offsets, stream_ids = _gate_sizes(x, gates, (state, state_out), offsets, max_tokens, n_segments, stream_ids)
+    clear = out is None and offsets is not None    # (a new result holds nothing yet)
     out = _out_matrix(out, x.shape, x.dtype, x.device, "out")
     if out.dtype != x.dtype:
         raise ValueError(f"out: {out.dtype}, wanted {x.dtype}")
@@ -597,7 +599,7 @@ def _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stre
         marks = torch.empty(_marks_floats(sizes, offsets), device=x.device) if marks is True else _plain(marks, torch.float32, (_marks_floats(sizes, offsets),), x.device, "marks")
         if given is not True and marks is not given:
             raise ValueError("marks have to be contiguous")
-    a = _GateScan(*sizes, _as_rows(x), _as_rows(gates), _as_rows(out), _ptr(state), _ptr(state_out), _ptr(marks), _ptr(offsets), _ptr(stream_ids), None, 0)
+    a = _GateScan(*sizes, _as_rows(x), _as_rows(gates), _as_rows(out), _ptr(state), _ptr(state_out), _ptr(marks), _ptr(offsets), _ptr(stream_ids), None, 0, clear)
     L = load_library()
     with torch.cuda.device(x.device):
         ws = _workspace(L.idf_gate_scan_workspace, a, x.device)       # noqa: F841 (held until the work is enqueued)
@@ -677,7 +679,7 @@ def _no_capture(x):
 
 def gate_scan_recorded(x, gates, state=None, *, offsets=None, max_tokens=None, n_segments=None):
     """gate_scan for training: (out, states behind the segments), both recorded by torch's gradients where x, gates or state require them, once (gradients
-    of gradients are refused).  Segment s is of stream s.  Not for a stream that is being captured into a graph."""
+    of gradients are refused).  Segment s is of stream s; rows that no segment has are zeros.  Not for a stream that is being captured into a graph."""
     global _recorded
     _no_capture(x)
     r = _direct("gate_scan_recorded", x, gates, state, offsets, max_tokens, n_segments)

@@ -77,3 +77,40 @@ def test_torchs_transforms_are_refused(call):
     for f in (lambda: torch.func.vmap(call)(x[None], gates[None]), lambda: torch.func.grad(lambda y: call(y, gates).sum())(x), lambda: torch.func.jvp(lambda y: call(y, gates), (x,), (x,))):
         with pytest.raises((RuntimeError, ValueError, NotImplementedError)):
             f()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("channels", [64, 33])
+@pytest.mark.parametrize("offsets,longest", [([0], 1), ([3, 4, 4, 9], 5), ([0, 100, 300], 60), ([7, 250, 250, 600], 250), ([300, 1000, 1000, 4000], 2500), ([100, 9000, 30000], 20000), ([0, 40], 0)], ids=str)
+def test_new_results_are_zero_where_no_segment_is(offsets, longest, channels, dtype):
+    """In front of, behind and between segments, and beyond max_tokens: what a call makes itself holds zeros there, recorded or not; what is given stays."""
+    n = offsets[-1] + 700
+    x, gates, d = make(n, channels, dtype, seed=n)
+    kw = dict(offsets=torch.tensor(offsets, device=DEV), max_tokens=longest)
+    mine = torch.zeros(n, dtype=torch.bool)
+    for a, b in zip(offsets, offsets[1:]):
+        mine[a:min(b, a + longest)] = True
+    given = torch.full_like(x, 7.0)
+    idf.gate_scan(x, gates, out=given, **kw)
+    assert torch.all(given[~mine] == 7.0)
+    leaf = x.clone().requires_grad_()
+    long = tokens._make_recorded().apply
+    for call in (lambda: idf.gate_scan(x, gates, **kw), lambda: tokens._gate_scan(x, gates, None, None, kw["offsets"], longest, None, None, None, None), lambda: idf.gate_scan(x, gates, marks=True, **kw)[0],
+                 lambda: idf.gate_scan_recorded(leaf, gates, **kw)[0], lambda: long(leaf, gates, None, kw["offsets"], longest, None)[0]):
+        filler = torch.full_like(x, float("nan"))
+        del filler                                 # (its memory is likely to be taken for the result)
+        got = call().detach()
+        assert not got[~mine].any() and torch.equal(got[mine], given[mine])
+
+
+def test_padding_multiplied_away_leaves_no_nan():
+    """A loss over a padded batch, its padding masked by multiplication."""
+    x, gates, d = make(2000, 64, torch.float32, seed=3)
+    filler = [torch.full_like(x, float("nan")) for _ in range(4)]
+    del filler
+    leaf = x.clone().requires_grad_()
+    out, ends = idf.gate_scan_recorded(leaf, gates, offsets=torch.tensor([0, 500, 900], device=DEV), max_tokens=500)
+    mask = torch.zeros(2000, 1, device=DEV)
+    mask[:900] = 1
+    ((out * mask * d).sum() + ends.sum()).backward()
+    assert torch.isfinite(leaf.grad).all() and not leaf.grad[900:].any() and leaf.grad[:900].any(1).all()
