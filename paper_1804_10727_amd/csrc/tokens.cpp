@@ -335,6 +335,15 @@ idf_rows matrix(const at::Tensor &t, const at::Tensor &like)
     return idf_rows{t.data_ptr(), t.size(0) > 1 ? t.stride(0) : t.size(1)};
 }
 
+// From the first byte of a matrix to behind its last one; a result that reaches into what is read is looked at more closely the long way round.
+struct Reach { uintptr_t from, to; };
+Reach reach(const idf_rows &m, int64_t rows, int64_t cols, int64_t bytes)
+{
+    return {(uintptr_t)m.base, rows && cols ? (uintptr_t)m.base + ((rows - 1) * m.row_stride + cols) * bytes : (uintptr_t)m.base};
+}
+Reach reach(const at::Tensor &t) { return {(uintptr_t)t.data_ptr(), (uintptr_t)t.data_ptr() + t.numel() * t.element_size()}; }          // (without gaps)
+void need_apart(const Reach &a, const Reach &b) { need(a.to <= b.from || b.to <= a.from); }
+
 // quantize_rows(stream, x, codes, scales)
 PyObject *quantize_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -399,6 +408,12 @@ PyObject *project_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
         need(out.dim() == 2 && out.size(0) == a.n_rows && out.size(1) == a.n_out);
         a.out_precision = precision(out);
         a.out = matrix(out, *x);
+        if (given) {
+            const Reach to = reach(a.out, a.n_rows, a.n_out, out.element_size());
+            need_apart(to, reach(a.x, a.n_rows, a.cols, x->element_size()));
+            for (const at::Tensor *t : {w, ws_, bias, xs})
+                if (t) need_apart(to, reach(*t));
+        }
         at::Tensor ws;
         int rc = with_workspace(fn.project_workspace, a, *x, ws);
         if (rc == IDF_OK) rc = call(fn.project, a, stream);
@@ -569,11 +584,9 @@ PyObject *gate_scan(PyObject *, PyObject *const *args, Py_ssize_t n)
         need(out.scalar_type() == x->scalar_type());
         a.out = matrix(out, *x);
         a.clear_rows = !given && a.offsets;        // (a new result holds nothing yet)
-        if (given)                                 // (what may share places with it is looked at more closely the long way round)
-            for (const idf_rows *r : {&a.x, &a.gates}) {
-                const auto end = [&](const idf_rows &m) { return (uintptr_t)m.base + ((a.n_tokens ? a.n_tokens - 1 : 0) * m.row_stride + a.channels) * x->element_size(); };
-                need(end(*r) <= (uintptr_t)a.out.base || end(a.out) <= (uintptr_t)r->base);
-            }
+        if (given)
+            for (const idf_rows *r : {&a.x, &a.gates})
+                need_apart(reach(a.out, a.n_tokens, a.channels, x->element_size()), reach(*r, a.n_tokens, a.channels, x->element_size()));
         at::Tensor fresh, ws;
         int rc = IDF_OK;
         if (marks || args[10] == Py_True) {

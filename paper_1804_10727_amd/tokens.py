@@ -348,6 +348,25 @@ def _out_matrix(out, shape, dtype, device, what):
     return out
 
 
+def _share(a, b):
+    """Whether two matrices (or rows) share places: where their rows lie alike they may be columns of one larger matrix, else it is enough that they reach into each other."""
+    if not a.numel() or not b.numel():
+        return False
+    (rows_a, wide_a), (rows_b, wide_b) = ((t.numel() // t.shape[-1], t.shape[-1] * t.element_size()) for t in (a, b))
+    strides = [t.stride(0) * t.element_size() if t.dim() == 2 else 0 for t in (a, b)]
+    strides = [s if rows > 1 else 0 for s, rows in zip(strides, (rows_a, rows_b))]
+    apart = b.data_ptr() - a.data_ptr()
+    if not -(rows_b - 1) * strides[1] - wide_b < apart < (rows_a - 1) * strides[0] + wide_a:
+        return False
+    stride = max(strides)
+    if any(s != stride for s, rows in zip(strides, (rows_a, rows_b)) if rows > 1) or max(wide_a, wide_b) > stride:
+        return True
+    # row j of b begins `rest` behind row j + k of a
+    k, rest = divmod(apart, stride)
+    both = [max(0, -d) < min(rows_b, rows_a - d) for d in (k, k + 1)]
+    return (both[0] and rest < wide_a) or (both[1] and stride - rest < wide_b)
+
+
 def quantize_rows(x, codes=None, scales=None):
     """Rows of a matrix in 8 bits with a scale each: (codes, int8 [rows][columns rounded up to 16, zeros behind them], scales float32 [rows])
     (idf_quantize_rows).  For tokens, and for the rows of a matrix of weights [outputs][columns]."""
@@ -375,7 +394,7 @@ def _quantize_rows(x, codes, scales):
 def project_rows(x, weight, weight_scales, bias=None, x_scales=None, dtype=None, out=None):
     """x [rows][columns] times the transpose of a matrix of 8-bit weights [outputs][columns rounded up to 16] with a scale for each output, plus a bias
     (idf_project_rows).  x in float32 or bfloat16 is taken to 8 bits with a scale for each row on the way; in int8 it comes with its
-    x_scales, and dtype or out says what the result is in (else what x is in)."""
+    x_scales, and dtype or out says what the result is in (else what x is in).  out may lie beside what is read, not over it."""
     import torch
     to_f32 = {None: -1, torch.float32: 1, torch.bfloat16: 0}.get(dtype)
     r = None if to_f32 is None else _direct("project_rows", x, weight, weight_scales, bias, x_scales, to_f32, out)
@@ -406,6 +425,8 @@ def _project_rows(x, weight, weight_scales, bias, x_scales, dtype, out):
     out = _out_matrix(out, (rows, n), x.dtype if dtype is None else dtype, x.device, "out")
     if dtype is not None and out.dtype != dtype:
         raise ValueError(f"out: {out.dtype}, wanted {dtype}")
+    if any(t is not None and _share(out, t) for t in (x, weight, weight_scales, bias, x_scales)):
+        raise ValueError("out shares places with what is read")
     a = _Project(2 if coded else _precision(x), _precision(out), cols, n, rows, _as_rows(x), _as_rows(out), _ptr(x_scales), _ptr(weight),
                  _ptr(weight_scales), _ptr(bias), None, 0)
     L = load_library()
@@ -566,21 +587,6 @@ def gate_scan(x, gates, state=None, state_out=None, *, offsets=None, max_tokens=
     marks True: returns (out, marks), the latter for gate_scan_backward.  gate_scan_recorded is the form that torch's gradients go through."""
     r = _direct("gate_scan", x, gates, state, state_out, offsets, max_tokens, n_segments, stream_ids, out, marks)
     return r if r is not None else _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stream_ids, out, marks)
-
-
-def _share(a, b):
-    """Whether two matrices of one size share places: where rows lie alike they may be columns of one larger matrix, else it is enough that they reach into each other."""
-    rows, cols = a.shape
-    if not a.numel():
-        return False
-    strides = [t.stride(0) if rows > 1 else cols for t in (a, b)]
-    apart = (b.data_ptr() - a.data_ptr()) // a.element_size()
-    if not -(rows - 1) * strides[1] - cols < apart < (rows - 1) * strides[0] + cols:
-        return False
-    if strides[0] != strides[1] or not strides[0]:
-        return True
-    k, rest = divmod(apart, strides[0])
-    return (abs(k) < rows and rest < cols) or (abs(k + 1) < rows and strides[0] - rest < cols)
 
 
 def _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stream_ids, out, marks):
