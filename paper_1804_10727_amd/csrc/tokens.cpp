@@ -14,6 +14,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <exception>
 #include <optional>
 #include <stdexcept>
 
@@ -58,8 +59,11 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
-// Thrown where arguments are not of the usual kinds, or wrong: the call then goes the long way round, which converts them or raises.
-struct Unusual {};
+// Thrown where arguments are not of the usual kinds, or wrong: the call then goes the long way round, which converts them or raises.  Where there is no long way, in a
+// backward pass, torch makes an error of it: its threads catch what is an exception, and end the process with anything else.
+struct Unusual : std::exception {
+    const char *what() const noexcept override { return "tensors of another kind or size than this call takes"; }
+};
 
 void need(bool ok)
 {
@@ -615,6 +619,7 @@ int gate_gradients(idf_gate_scan_backward_args &a, const at::Tensor &x, const at
 {
     a.precision = precision(x);
     a.x = matrix(x, x);
+    need(g.sizes() == x.sizes() && g.scalar_type() == x.scalar_type());
     a.gates = matrix(g, x);
     a.channels = (int)x.size(1);
     a.n_tokens = x.size(0);
@@ -695,6 +700,8 @@ struct GateScan : torch::autograd::Function<GateScan> {
         ctx->save_for_backward({x, gates, marks, offsets ? *offsets : at::Tensor()});
         ctx->saved_data["max_tokens"] = max_tokens;
         ctx->saved_data["segments"] = segments;
+        ctx->saved_data["tokens"] = x.size(0);
+        ctx->saved_data["channels"] = x.size(1);
         ctx->saved_data["stream"] = stream;
         ctx->saved_data["has_state"] = state.has_value();
         ctx->set_materialize_grads(false);
@@ -719,7 +726,9 @@ struct GateScan : torch::autograd::Function<GateScan> {
             idf_gate_scan_backward_args a{};
             a.max_tokens = ctx->saved_data["max_tokens"].toInt();
             a.n_segments = a.n_streams = (int)ctx->saved_data["segments"].toInt();
-            a.offsets = offsets.defined() ? static_cast<const int64_t *>(offsets.data_ptr()) : nullptr;
+            // (what was saved may come back by way of a hook of the program's)
+            need(x.dim() == 2 && x.size(0) == ctx->saved_data["tokens"].toInt() && x.size(1) == ctx->saved_data["channels"].toInt());
+            a.offsets = offsets.defined() ? plain<int64_t>(&offsets, at::kLong, a.n_segments + 1, x) : nullptr;
             // (rows that lie too far apart, which the forward call did not take either, are no case here)
             if (gate_gradients(a, x, saved[1], saved[2], grad.defined() ? &grad : nullptr, end.defined() ? &end : nullptr, stream, to) != IDF_OK)
                 throw std::runtime_error("gate_scan_backward was refused");

@@ -114,3 +114,42 @@ def test_padding_multiplied_away_leaves_no_nan():
     mask[:900] = 1
     ((out * mask * d).sum() + ends.sum()).backward()
     assert torch.isfinite(leaf.grad).all() and not leaf.grad[900:].any() and leaf.grad[:900].any(1).all()
+
+
+def recorded(dtype, lengths=(300, 0, 45)):
+    x, gates, d = make(sum(lengths), 66, dtype, seed=5)
+    kw = dict(offsets=torch.tensor([0] + list(lengths)).cumsum(0).to(DEV), max_tokens=max(lengths))
+    leaves = [t.clone().requires_grad_() for t in (x, gates)] + [torch.randn(len(lengths), 66, generator=torch.Generator().manual_seed(6)).to(DEV).requires_grad_()]
+    out, ends = idf.gate_scan_recorded(*leaves, **kw)
+    torch.autograd.backward([out, ends], [d, torch.ones_like(ends)])
+    return leaves, kw, d, [t.grad for t in leaves]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_saved_tensors_by_way_of_hooks(dtype):
+    """Kept on the host, or laid out anew, in the meantime: the same gradients.  Of another type or size when they come back: an error of torch's, nothing is read."""
+    leaves, kw, d, want = recorded(dtype)
+
+    def again(hooks):
+        mine = [t.detach().clone().requires_grad_() for t in leaves]
+        with hooks:
+            out, ends = idf.gate_scan_recorded(*mine, **kw)
+        torch.autograd.backward([out, ends], [d, torch.ones_like(ends)])
+        return [t.grad for t in mine]
+    hooks = torch.autograd.graph.saved_tensors_hooks
+    for keep in (torch.autograd.graph.save_on_cpu(), hooks(lambda t: t.clone(), lambda t: t), hooks(lambda t: t, lambda t: t.t().contiguous().t() if t.dim() == 2 and t.shape[1] == 1 else t.clone())):
+        assert all(torch.equal(a, b) for a, b in zip(again(keep), want))
+    for change in (lambda t: t.half() if t.dim() == 2 else t, lambda t: t[:-1] if t.dim() == 2 else t, lambda t: t[:, :-2].contiguous() if t.dim() == 2 else t, lambda t: t.cpu(),
+                   lambda t: t[:-1] if t.dtype == torch.int64 else t, lambda t: t.int() if t.dtype == torch.int64 else t, lambda t: t[:5] if t.dim() == 1 and t.is_floating_point() else t):
+        with pytest.raises(RuntimeError):
+            again(hooks(lambda t: t, change))
+    torch.cuda.synchronize()
+
+
+def test_leaves_changed_before_the_backward_pass_are_refused():
+    leaves, kw, d, _ = recorded(torch.float32)
+    x, gates = leaves[0].detach().clone().requires_grad_(), leaves[1].detach().clone()
+    out, _ = idf.gate_scan_recorded(x, gates, **kw)
+    gates += 1
+    with pytest.raises(RuntimeError, match="modified"):
+        out.backward(d)
