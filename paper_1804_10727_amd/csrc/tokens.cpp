@@ -3,6 +3,7 @@
 // the kernels of a single token's step take.
 #include <Python.h>
 
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -154,6 +155,9 @@ template <class F> PyObject *entry(F f)
         return f();
     } catch (const Unusual &) {
         Py_RETURN_NONE;
+    } catch (python_error &e) {                    // (Python's own, raised within the call: a hook of the program's, or torch's checkpoints, which end a run by one)
+        e.restore();
+        return nullptr;
     } catch (...) {                                // (tensors without memory of their own, no memory left: the long way says so)
         if (PyErr_Occurred()) PyErr_Clear();
         Py_RETURN_NONE;

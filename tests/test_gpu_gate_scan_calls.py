@@ -4,6 +4,7 @@ import ctypes as C
 import numpy as np
 import pytest
 import torch
+import torch.utils.checkpoint
 
 import paper_1804_10727_amd as idf
 from oracle import few_bits as oracle
@@ -144,6 +145,46 @@ def test_saved_tensors_by_way_of_hooks(dtype):
         with pytest.raises(RuntimeError):
             again(hooks(lambda t: t, change))
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_checkpointed(dtype, reentrant):
+    leaves, kw, d, want = recorded(dtype)
+    mine = [t.detach().clone().requires_grad_() for t in leaves]
+    out, ends = torch.utils.checkpoint.checkpoint(lambda *a: idf.gate_scan_recorded(*a, **kw), *mine, use_reentrant=reentrant)
+    torch.autograd.backward([out, ends], [d, torch.ones_like(ends)])
+    assert all(torch.equal(t.grad, w) for t, w in zip(mine, want))
+
+
+def test_errors_of_hooks_are_the_programs():
+    class Stop(Exception):
+        pass
+
+    def stop(t):
+        raise Stop
+    x, gates, _ = make(40, 64, torch.float32)
+    leaf = x.clone().requires_grad_()
+    with torch.autograd.graph.saved_tensors_hooks(stop, lambda t: t), pytest.raises(Stop):
+        idf.gate_scan_recorded(leaf, gates)
+    out, _ = idf.gate_scan_recorded(leaf, gates)
+    out.sum().backward()
+    assert torch.isfinite(leaf.grad).all()
+
+
+def test_two_checkpoints_behind_each_other():
+    """A stack of two layers, each run again for its gradients, some of the leaves shared."""
+    x, gates, d = make(700, 64, torch.float32, seed=9)
+    kw = dict(offsets=torch.tensor([0, 300, 700], device=DEV), max_tokens=400)
+
+    def layer(h, g, w):
+        return idf.gate_scan_recorded(torch.tanh(h * w), g * w, **kw)[0]
+    grads = []
+    for run in (lambda f, *a: f(*a), lambda f, *a: torch.utils.checkpoint.checkpoint(f, *a, use_reentrant=False)):
+        a, g, w = (t.clone().requires_grad_() for t in (x, gates, torch.linspace(0.5, 1.5, 64, device=DEV)))
+        run(layer, run(layer, a, g, w), g, w).backward(d)
+        grads.append([t.grad for t in (a, g, w)])
+    assert all(torch.equal(p, q) for p, q in zip(*grads))
 
 
 def test_leaves_changed_before_the_backward_pass_are_refused():
