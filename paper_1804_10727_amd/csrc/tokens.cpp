@@ -16,6 +16,7 @@
 #include <cstdint>
 #include <cstring>
 #include <exception>
+#include <initializer_list>
 #include <optional>
 #include <stdexcept>
 
@@ -148,6 +149,13 @@ at::Tensor output(const at::Tensor *given, at::IntArrayRef shape, const at::Tens
     return at::empty(shape, like.options());
 }
 
+// What a call has written into tensors of the caller's counts as a change in place: torch refuses gradients that would start from what they held before.
+void written(std::initializer_list<const at::Tensor *> tensors)
+{
+    for (const at::Tensor *t : tensors)
+        if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 // Every entry: what the library returned if that is an error, None where the arguments go the long way round, else the outputs.
 template <class F> PyObject *entry(F f)
 {
@@ -190,11 +198,13 @@ PyObject *norm_rotate(PyObject *, PyObject *const *args, Py_ssize_t n)
         a.k_weight = plain<float>(tensor(args[8]), at::kFloat, a.head_dim, *q);
         a.eps = (float)real(args[9]);
         const c10::DeviceGuard guard(q->device());
-        const at::Tensor q_out = output(tensor(args[10]), q->sizes(), *q), k_out = output(tensor(args[11]), k->sizes(), *q);
+        const at::Tensor *given[2] = {tensor(args[10]), tensor(args[11])};
+        const at::Tensor q_out = output(given[0], q->sizes(), *q), k_out = output(given[1], k->sizes(), *q);
         a.q_out = rows(q_out, *q, false);
         a.k_out = rows(k_out, *q, false);
         const int rc = call(fn.norm_rotate, a, stream);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
+        written({given[0], given[1]});
         PyObject *both = PyTuple_New(2);
         if (!both) throw Unusual();
         PyTuple_SET_ITEM(both, 0, args[10] != Py_None ? Py_NewRef(args[10]) : THPVariable_Wrap(q_out));
@@ -256,7 +266,8 @@ PyObject *window_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
         a.sinks = small(args[8]);
         a.scale = args[9] == Py_None ? (float)(1.0 / std::sqrt((double)a.head_dim)) : (float)real(args[9]);
         const c10::DeviceGuard guard(q->device());
-        const at::Tensor out = output(tensor(args[13]), q->sizes(), *q);
+        const at::Tensor *given = tensor(args[13]);
+        const at::Tensor out = output(given, q->sizes(), *q);
         a.out = rows(out, *q, true);
         int rc = fn.window_workspace(&a, &a.workspace_bytes);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
@@ -267,6 +278,7 @@ PyObject *window_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
         }
         rc = call(fn.window, a, stream);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
+        written({given, k_ring, v_ring});
         return args[13] != Py_None ? Py_NewRef(args[13]) : THPVariable_Wrap(out);
     });
 }
@@ -309,7 +321,8 @@ PyObject *decay_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
         a.stream_ids = plain<int32_t>(ids, at::kInt, a.n_segments, *q);
         a.scale = args[7] == Py_None ? (float)(1.0 / std::sqrt((double)a.dim_k)) : (float)real(args[7]);
         const c10::DeviceGuard guard(q->device());
-        const at::Tensor out = output(tensor(args[12]), {a.n_tokens, a.heads_q, a.dim_v}, *q);
+        const at::Tensor *given = tensor(args[12]);
+        const at::Tensor out = output(given, {a.n_tokens, a.heads_q, a.dim_v}, *q);
         a.out = rows(out, *q, true);
         int rc = fn.decay_workspace(&a, &a.workspace_bytes);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
@@ -320,6 +333,7 @@ PyObject *decay_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
         }
         rc = call(fn.decay, a, stream);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
+        written({given, to});
         return args[12] != Py_None ? Py_NewRef(args[12]) : THPVariable_Wrap(out);
     });
 }
@@ -376,6 +390,7 @@ PyObject *quantize_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
         a.scales = plain<float>(&scales, at::kFloat, a.n_rows, *x);
         const int rc = call(fn.quantize, a, stream);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
+        written({given[0], given[1]});
         PyObject *both = PyTuple_New(2);
         if (!both) throw Unusual();
         PyTuple_SET_ITEM(both, 0, given[0] ? Py_NewRef(args[2]) : THPVariable_Wrap(codes));
@@ -426,6 +441,7 @@ PyObject *project_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
         int rc = with_workspace(fn.project_workspace, a, *x, ws);
         if (rc == IDF_OK) rc = call(fn.project, a, stream);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
+        written({given});
         return given ? Py_NewRef(args[7]) : THPVariable_Wrap(out);
     });
 }
@@ -485,6 +501,7 @@ PyObject *nibble_append(PyObject *, PyObject *const *args, Py_ssize_t n)
         a.eps = real(args[13]);
         const c10::DeviceGuard guard(k->device());
         const int rc = call(fn.nibble_append, a, stream);
+        if (rc == IDF_OK) written({tensor(args[3]), tensor(args[4]), tensor(args[5]), tensor(args[6])});
         return PyLong_FromLong(rc);
     });
 }
@@ -509,12 +526,14 @@ PyObject *nibble_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
         a.sinks = small(args[8]);
         a.scale = args[9] == Py_None ? (float)(1.0 / std::sqrt((double)a.head_dim)) : (float)real(args[9]);
         const c10::DeviceGuard guard(q->device());
-        const at::Tensor out = output(tensor(args[13]), q->sizes(), *q);
+        const at::Tensor *given = tensor(args[13]);
+        const at::Tensor out = output(given, q->sizes(), *q);
         a.out = rows(out, *q, true);
         at::Tensor ws;
         int rc = with_workspace(fn.nibble_workspace, a, *q, ws);
         if (rc == IDF_OK) rc = call(fn.nibble_attend, a, stream);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
+        written({given});
         return args[13] != Py_None ? Py_NewRef(args[13]) : THPVariable_Wrap(out);
     });
 }
@@ -607,6 +626,7 @@ PyObject *gate_scan(PyObject *, PyObject *const *args, Py_ssize_t n)
         rc = with_workspace(fn.gate_workspace, a, *x, ws);
         if (rc == IDF_OK) rc = call(fn.gate, a, stream);
         if (rc != IDF_OK) return PyLong_FromLong(rc);
+        written({given, to, marks == &fresh ? nullptr : marks});
         PyObject *got = given ? Py_NewRef(args[9]) : THPVariable_Wrap(out);
         if (args[10] != Py_True || !got) return got;
         PyObject *both = PyTuple_New(2);

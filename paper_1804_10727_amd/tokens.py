@@ -169,6 +169,12 @@ def _out(out, shape, like, what, aligned=True):
     return out
 
 
+def _written(*tensors):
+    """What a call has written into tensors of the caller's counts as a change in place: torch refuses gradients that would start from what they held before."""
+    import torch
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 def _stream(t):
     import torch
     return C.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
@@ -211,6 +217,7 @@ def _norm_rotate(q, k, positions, frequencies, layout, amplitude, q_weight, k_we
                     _tokens(q_out), _tokens(k_out), _ptr(positions), _ptr(frequencies), _ptr(q_weight), _ptr(k_weight), amplitude, eps)
     with torch.cuda.device(q.device):
         _check(load_library().idf_norm_rotate(C.byref(a), _stream(q)))
+    _written(q_out, k_out)
     return q_out, k_out
 
 
@@ -282,6 +289,7 @@ def _window_attend(q, k, v, k_ring, v_ring, starts, window, sinks, scale, offset
     with torch.cuda.device(q.device):
         ws = _workspace(L.idf_window_workspace, a, q.device)          # noqa: F841 (held until the work is enqueued)
         _check(L.idf_window_attend(C.byref(a), _stream(q)))
+    _written(out, k_ring, v_ring)
     return out
 
 
@@ -323,6 +331,7 @@ def _decay_attend(q, k, v, log_decay, state, state_out, scale, offsets, max_toke
     with torch.cuda.device(q.device):
         ws = _workspace(L.idf_decay_workspace, a, q.device)           # noqa: F841 (held until the work is enqueued)
         _check(L.idf_decay_attend(C.byref(a), _stream(q)))
+    _written(out, state_out)
     return out
 
 
@@ -388,6 +397,7 @@ def _quantize_rows(x, codes, scales):
     a = _Quantize(_precision(x), cols, rows, _as_rows(x), _ptr(codes), _ptr(scales))
     with torch.cuda.device(x.device):
         _check(load_library().idf_quantize_rows(C.byref(a), _stream(x)))
+    _written(codes, scales)
     return codes, scales
 
 
@@ -433,6 +443,7 @@ def _project_rows(x, weight, weight_scales, bias, x_scales, dtype, out):
     with torch.cuda.device(x.device):
         ws = _workspace(L.idf_project_workspace, a, x.device)         # noqa: F841 (held until the work is enqueued)
         _check(L.idf_project_rows(C.byref(a), _stream(x)))
+    _written(out)
     return out
 
 
@@ -504,6 +515,7 @@ def _nibble_append(k, v, ring, starts, sinks, frequencies, layout, amplitude, k_
                      _ptr(stream_ids))
     with torch.cuda.device(k.device):
         _check(load_library().idf_nibble_append(C.byref(a), _stream(k)))
+    _written(*ring)
 
 
 def nibble_attend(q, ring, starts=None, *, window, sinks=0, scale=None, offsets=None, max_tokens=None, stream_ids=None, out=None):
@@ -530,6 +542,7 @@ def _nibble_attend(q, ring, starts, window, sinks, scale, offsets, max_tokens, s
     with torch.cuda.device(q.device):
         ws = _workspace(L.idf_nibble_attend_workspace, a, q.device)    # noqa: F841 (held until the work is enqueued)
         _check(L.idf_nibble_attend(C.byref(a), _stream(q)))
+    _written(out)
     return out
 
 
@@ -610,6 +623,7 @@ def _gate_scan(x, gates, state, state_out, offsets, max_tokens, n_segments, stre
     with torch.cuda.device(x.device):
         ws = _workspace(L.idf_gate_scan_workspace, a, x.device)       # noqa: F841 (held until the work is enqueued)
         _check(L.idf_gate_scan(C.byref(a), _stream(x)))
+    _written(out, state_out, marks)
     return (out, marks) if given is True else out
 
 
