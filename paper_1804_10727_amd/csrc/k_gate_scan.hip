@@ -43,6 +43,9 @@ __device__ __forceinline__ bool finite(float v) { return __builtin_fabsf(v) < __
 __device__ __forceinline__ float step_of(const Gate &w, float x, float h) { return __builtin_fmaf(w.s, x - h, w.open() ? h : x); }
 __device__ __forceinline__ float kept_of(const Gate &w, float l) { return __builtin_fmaf(-w.s, l, w.open() ? l : 0.f); }
 
+// What a gate's gradient goes by: a (1 - a).
+__device__ __forceinline__ float slope_of(const Gate &w) { return __builtin_fabsf(w.s) * w.big(); }
+
 // The same from the definition, for what the above would make no number: differences of infinite values, gates held to +-87.
 template <int PREC> struct Slow {
     float keep, take;
@@ -584,10 +587,6 @@ __global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_back_tile(idf_gate_
         float was[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) was[v] = m[v];
-        auto put_row = [&](int u, int v, Gate one, float l, float apart, float (&dx)[V], float (&dg)[V]) IDF_INLINE {
-            dx[v] = l * one.take();
-            dg[v] = l * apart * (__builtin_fabsf(one.s) * one.big());
-        };
 #pragma unroll
         for (int u = kBlock - 1; u >= 0; --u) {
             float dx[V], dg[V];
@@ -596,7 +595,8 @@ __global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_back_tile(idf_gate_
                 const Gate one = {gate[u][v]};
                 const float l = (u < n ? ds[u].get(v) : 0.f) + m[v];
                 m[v] = kept_of(one, l);
-                put_row(u, v, one, l, apart[u][v], dx, dg);
+                dx[v] = l * one.take();
+                dg[v] = l * apart[u][v] * slope_of(one);
             }
             if (u < n && w.on) { gx.store(t, u, dx); gg.store(t, u, dg); }
         }
@@ -623,7 +623,10 @@ __global__ void __launch_bounds__(64 * kTileWaves, 4) k_gate_back_tile(idf_gate_
                     const Slow<PREC> it(gr.get(v));
                     const float l = dr.get(v) + m[v];
                     m[v] = it.kept(l);
-                    put_row(u, v, it.w, l, h[v] - xr.get(v), dx, dg);
+                    dx[v] = l * it.take;
+                    // (a state and a value of opposite signs may be further apart than a number goes, and the product of gates brings them back)
+                    const float slope = slope_of(it.w), value = xr.get(v), way = l * (h[v] - value);
+                    dg[v] = finite(way) ? way * slope : l * (h[v] * slope - value * slope);
                 }
                 if (w.on) { gx.store(t, u, dx); gg.store(t, u, dg); }
             }

@@ -194,3 +194,29 @@ def test_leaves_changed_before_the_backward_pass_are_refused():
     gates += 1
     with pytest.raises(RuntimeError, match="modified"):
         out.backward(d)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n", [5, 40, 3000])
+def test_states_and_values_far_apart(n, dtype):
+    """Values near the largest number, of either sign: a difference between a state and a value goes beyond it, what gates make of that does not.  Where it flows
+    into no gradient there is none, and not what is no number."""
+    g = torch.Generator().manual_seed(n)
+    x, gates = torch.randn(n, 64, generator=g).to(dtype), (torch.randn(n, 64, generator=g) + 1).to(dtype)
+    d, state = torch.zeros(n, 64, dtype=dtype), torch.randn(1, 64, generator=g)
+    big = 3.2e38
+    x[n // 2, 3], state[0, 3] = big, -big
+    x[n - 1, 7], x[n - 2, 7] = -big, big
+    x[:, 11] = torch.where(torch.arange(n) % 2 == 0, big, -big).to(dtype)
+    d[:, 20:] = torch.randn(n, 44, generator=g).to(dtype)
+    x[n // 3, 30], x[n // 3 + 1, 30], d[:, 30] = big, -big, (d[:, 30].float() * 1e-30).to(dtype)
+    end = torch.zeros(1, 64)
+    out, marks = idf.gate_scan(x.to(DEV), gates.to(DEV), state.to(DEV), marks=True)
+    got = idf.gate_scan_backward(x.to(DEV), gates.to(DEV), marks, d.to(DEV), end.to(DEV))
+    hs, _, errors = oracle.gate_scan(f64(x), f64(gates), f64(state[0]))
+    dx, dg, ds, ex, eg, es = oracle.gate_scan_backward(f64(x), f64(gates), f64(state[0]), f64(d), f64(end[0]))
+    u = torch.finfo(dtype).eps / 2
+    # (a gradient here is the difference of two products that are rounded once more: 2 W of their sizes, which eg, of them and their gates' errors, holds many times over)
+    for t, want, bound in ((out, hs, u * np.abs(hs) + W * errors), (got[0], dx, u * np.abs(dx) + W * ex + 1e-36), (got[1], dg, u * np.abs(dg) + W * eg + 1e-36), (got[2][0], ds, W * es + 1e-30)):
+        assert np.isfinite(f64(t)).all() and np.all(np.abs(f64(t) - want) <= bound)
+    assert not got[1][:, :20].any() and got[1][n // 3 + 1, 30] != 0
