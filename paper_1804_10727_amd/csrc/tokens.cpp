@@ -696,6 +696,12 @@ PyObject *gate_scan_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+bool captured(void *stream)
+{
+    int capturing = 0;
+    return fn.is_capturing(stream, &capturing) != 0 || capturing;
+}
+
 // The recurrence as torch's gradients go through it.  The backward pass runs on the stream of the forward one, as torch has it.
 struct GateScan : torch::autograd::Function<GateScan> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext *ctx, const at::Tensor &x, const at::Tensor &gates, const std::optional<at::Tensor> &state,
@@ -738,8 +744,7 @@ struct GateScan : torch::autograd::Function<GateScan> {
         const auto saved = ctx->get_saved_variables();
         const at::Tensor &x = saved[0], &offsets = saved[3];
         void *stream = reinterpret_cast<void *>((uintptr_t)ctx->saved_data["stream"].toInt());
-        int capturing = 0;
-        if (fn.is_capturing(stream, &capturing) != 0 || capturing)
+        if (captured(stream))
             throw std::runtime_error("gate_scan_recorded's backward pass while a stream is captured: gate_scan_backward can be captured");
         const bool twice = c10::GradMode::is_enabled();
         GateGradients to;
@@ -779,6 +784,7 @@ PyObject *gate_scan_recorded(PyObject *, PyObject *const *args, Py_ssize_t n)
     if (n != 7 || !bound) { PyErr_SetString(PyExc_TypeError, "gate_scan_recorded takes 7 arguments"); return nullptr; }
     return entry([&]() -> PyObject * {
         const int64_t stream = whole(args[0]);
+        need(!captured(reinterpret_cast<void *>((uintptr_t)stream)));           // (refused there)
         const at::Tensor *x = recorded_tensor(args[1]), *g = recorded_tensor(args[2]), *state = recorded_tensor(args[3]), *offsets = tensor(args[4]);
         need(x && g && x->dim() == 2 && x->size(1) <= INT_MAX && x->sizes() == g->sizes() && g->scalar_type() == x->scalar_type());
         (void)precision(*x);

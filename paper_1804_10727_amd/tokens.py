@@ -692,7 +692,11 @@ def _make_recorded():
 
 def _no_capture(x):
     import torch
-    if x.is_cuda and torch.cuda.is_current_stream_capturing():
+    if not x.is_cuda:
+        return
+    with torch.cuda.device(x.device):              # (the stream that is asked about is the current device's)
+        capturing = torch.cuda.is_current_stream_capturing()
+    if capturing:
         raise RuntimeError("gate_scan_recorded while a stream is captured: torch ends the process there where leaves have recorded outside; "
                            "gate_scan with marks and gate_scan_backward can be captured")
 
@@ -701,10 +705,10 @@ def gate_scan_recorded(x, gates, state=None, *, offsets=None, max_tokens=None, n
     """gate_scan for training: (out, states behind the segments), both recorded by torch's gradients where x, gates or state require them, once (gradients
     of gradients are refused).  Segment s is of stream s; rows that no segment has are zeros.  Not for a stream that is being captured into a graph."""
     global _recorded
-    _no_capture(x)
     r = _direct("gate_scan_recorded", x, gates, state, offsets, max_tokens, n_segments)
     if r is not None:
         return r
+    _no_capture(x)
     if _recorded is None:
         _recorded = _make_recorded()
     return _recorded.apply(x, gates, state, offsets, max_tokens, n_segments)
