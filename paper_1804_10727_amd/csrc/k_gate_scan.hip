@@ -142,7 +142,8 @@ __device__ __forceinline__ float *marks_at(float *marks, const Work &w, int t, i
 // and wait for lower numbers only, which have begun; a tile makes known what others may wait for whatever its segment looks like.
 //   Bound by memory: x, gates and results once, and 4 to 12 bytes a channel that tiles tell each other for every 128 or 256 tokens.  65536 tokens of 2048 channels, bfloat16:
 // forward 185 us, 4.35 TB/s, backward 291, 4.6; 262144 of 2048 in float32 5.7 TB/s both.  (Summaries in a launch of their own, and everything read again from
-// the states that they give, 308 and 436.)  All of it in 128 registers, for two workgroups to a compute unit: what one waits for the other hides.
+// the states that they give, 308 and 436.)  All of it in 128 registers, for two workgroups to a compute unit: what one waits for the other hides.  (Backward with two channels to a lane
+// it is 3 to 6 more, which go to scratch memory.)
 constexpr int kTileWaves = 8;
 constexpr int each_of(int blocks) { return 4 / blocks; }                     // tiles that a wave gathers
 constexpr int chain_of(int blocks) { return kTileWaves * each_of(blocks); }

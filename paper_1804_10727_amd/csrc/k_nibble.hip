@@ -181,8 +181,10 @@ template <int PREC> struct alignas(16) Eight {
 
 // A lane has eight values of a head, four lanes a block; a workgroup a few tokens with all their heads, so that slots, cosines and sines are formed once per
 // token.  Keys that are normalised or turned are formed in 64 bits, whose instructions run as fast as those of 32 here: a value next to the middle between two codes goes to
-// the same one however sums and products are ordered.  What is read and written asks for 17 us of 15,104 tokens with 8 heads of 128 in bfloat16; it takes 38.5, by
-// the vector instructions (with every code decided in 64 bits 97; with a workgroup per token 52; with keys on the same two of a workgroup's waves, and so on two SIMDs of four, 46).  One token of 64 streams: 5.7 us.
+// the same one however sums and products are ordered.  (So it would by 32 bits with a border of their error about every middle, and 64 for what lies in it; not built.)
+//   What is read and written asks for 17 us of 15,104 tokens with 8 heads of 128 in bfloat16; it takes 38.5, by the vector instructions and 5 to 12 registers that go to scratch
+// memory (with every code decided in 64 bits 97; with a workgroup per token 52; with keys on the same two of a workgroup's waves, and so on two SIMDs of four, 46).  One token
+// of 64 streams: 5.7 us.
 template <int PREC, bool ALIGNED>
 __global__ void __launch_bounds__(256, 4) k_nibble_append(idf_nibble_append_args a, int lanes_log2, int tokens_per_group)
 {
@@ -451,7 +453,7 @@ __device__ __forceinline__ void exact_row(const idf_nibble_attend_args &a, const
 // -- few rows on a long axis: single tokens, short segments --
 
 // A workgroup takes the at most 16 RT query rows of one segment and key/value head and a part of the keys; its waves take 32 of them at a time, in turn, each
-// with a softmax of its own, and are joined at the end.  Eight waves where there are workgroups for half the machine only (64 x 16 tokens in float32 on 1000 keys of
+// with a softmax of its own, and are joined at the end.  Eight waves where one workgroup to a compute unit is enough (64 x 16 tokens in float32 on 1000 keys of
 // 4 x 64: 20.7 us by four, 17.6 by eight, before what is said of LDS below), else four with two rounds each on their way (64 streams on 4096 keys of 8 x 128: one round 61.6, two 56.5; reading alone, with
 // nothing done, takes 52, 5.5 TB/s).  What had cost most were choices on the loaded values next to the loads, which wait for them (72 -> 62).  Codes of keys go from memory into the layout of the matrix instruction, a lane having a quarter of a
 // row, whose place along the summed axis is free; those of values through a piece of LDS that is the wave's own, to be read along the keys.

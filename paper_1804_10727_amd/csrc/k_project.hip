@@ -31,8 +31,9 @@ __device__ __forceinline__ int code_of(float x, float per, float most)
     return c;
 }
 
-// A row by THREADS threads, which keep as many of its values as their registers hold, and read the others a second time.  Bound by memory: 16384 x 4096 from
-// bfloat16 in 48 us, 4.2 TB/s, from float32 in 60, 5.6.
+// A row by THREADS threads, which keep as many of its values as their registers hold, and read the others a second time.  Many rows are bound by memory: 16384 x 4096 from
+// bfloat16 in 48 us, 4.2 TB/s, from float32 in 60, 5.6.  Few ones by its latency, 64 x 4096 in 4: a piece is a whole one or single values, which the compiler joins in scratch memory
+// (32 or 64 bytes a lane), so that each waits for its own loads before the next one is asked for.
 template <int PREC, int THREADS>
 __global__ void __launch_bounds__(256) k_quantize_rows(idf_quantize_args a, bool aligned)
 {
@@ -311,69 +312,40 @@ __global__ void __launch_bounds__(64 * WM * WN, PER_CU * WM * WN / 4) k_project_
     }
 }
 
-// Few rows: what is read is the weights.  A workgroup takes 16 NT outputs of up to 16 MT rows, its WAVES waves a part of the summed axis each; codes go from memory
+// Up to 16 rows: what is read is the weights.  A workgroup takes 16 outputs, its WAVES waves a part of the summed axis each; codes go from memory
 // straight into the layout of the matrix instruction, whole batches of them on their way at a time, and the waves' sums are added up in LDS.
-template <class Out, int MT, int NT, int WAVES>
+template <class Out, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) k_project_few(Product a)
 {
-    constexpr int kAhead = MT >= 4 ? 4 : 8;        // steps of 64 codes
-    __shared__ __align__(16) i32x4 sums[WAVES][MT * NT][64];
+    constexpr int kAhead = 8;                      // steps of 64 codes
+    __shared__ __align__(16) i32x4 sums[WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
-    const int n0 = blockIdx.x * 16 * NT;
-    const int64_t m0 = (int64_t)blockIdx.y * 16 * MT;
+    const int n0 = blockIdx.x * 16;
     const int steps = (a.w_ld + 63) / 64, per = (steps + WAVES - 1) / WAVES, s0 = min(steps, wave * per), s1 = min(steps, s0 + per);
-    const int8_t *w[NT], *x[MT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) w[j] = a.w + (int64_t)min(n0 + j * 16 + col, a.n_out - 1) * a.w_ld + grp * 16;
-#pragma unroll
-    for (int i = 0; i < MT; ++i) x[i] = a.x + min(m0 + i * 16 + col, a.n_rows - 1) * a.x_ld + grp * 16;
-    i32x4 acc[MT][NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-    auto multiply = [&](const i32x4 (&wf)[NT], const i32x4 (&xf)[MT]) IDF_INLINE {
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[j], xf[i], acc[i][j], 0, 0, 0);
-    };
+    const int8_t *const w = a.w + (int64_t)min(n0 + col, a.n_out - 1) * a.w_ld + grp * 16, *const x = a.x + min((int64_t)col, a.n_rows - 1) * a.x_ld + grp * 16;
+    i32x4 acc = {0, 0, 0, 0};
     int s = s0;
     for (; s + kAhead <= s1 && (s + kAhead) * 64 <= a.w_ld; s += kAhead) {
-        i32x4 wf[kAhead][NT], xf[kAhead][MT];
+        i32x4 wf[kAhead], xf[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
+        for (int u = 0; u < kAhead; ++u) wf[u] = *(const i32x4 *)(w + (s + u) * 64);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) wf[u][j] = *(const i32x4 *)(w[j] + (s + u) * 64);
+        for (int u = 0; u < kAhead; ++u) xf[u] = *(const i32x4 *)(x + (s + u) * 64);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-            for (int i = 0; i < MT; ++i) xf[u][i] = *(const i32x4 *)(x[i] + (s + u) * 64);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) multiply(wf[u], xf[u]);
+        for (int u = 0; u < kAhead; ++u) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[u], xf[u], acc, 0, 0, 0);
     }
     for (; s < s1; ++s) {
         const bool there = s * 64 + grp * 16 < a.w_ld;
-        i32x4 wf[NT], xf[MT];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) wf[j] = there ? *(const i32x4 *)(w[j] + s * 64) : i32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < MT; ++i) xf[i] = there ? *(const i32x4 *)(x[i] + s * 64) : i32x4{0, 0, 0, 0};
-        multiply(wf, xf);
+        const i32x4 wf = there ? *(const i32x4 *)(w + s * 64) : i32x4{0, 0, 0, 0}, xf = there ? *(const i32x4 *)(x + s * 64) : i32x4{0, 0, 0, 0};
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf, xf, acc, 0, 0, 0);
     }
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
+    sums[wave][lane] = acc;
     __syncthreads();
-    for (int t = wave; t < MT * NT; t += WAVES) {
-        i32x4 sum = sums[0][t][lane];
+    if (wave > 0) return;
+    i32x4 sum = sums[0][lane];
 #pragma unroll
-        for (int v = 1; v < WAVES; ++v) sum += sums[v][t][lane];
-        const int n = n0 + (t % NT) * 16 + grp * 4;
-        const int64_t r = m0 + (t / NT) * 16 + col;
-        if (r < a.n_rows) store_four<Out>(a, r, n, a.x_scales[r], sum, four_of(a, n));
-    }
+    for (int v = 1; v < WAVES; ++v) sum += sums[v][lane];
+    if (col < a.n_rows) store_four<Out>(a, col, n0 + grp * 4, a.x_scales[col], sum, four_of(a, n0 + grp * 4));
 }
 
 template <class Out, int WM, int WN, int MT, int NT, int STAGES, int PER_CU> hipError_t tile(const Product &p, const LaunchCtx &lc)
@@ -384,17 +356,17 @@ template <class Out, int WM, int WN, int MT, int NT, int STAGES, int PER_CU> hip
         if (const hipError_t e = allow_lds<S::LDS_BYTES>(Kernel<k_project_tile<Out, WM, WN, MT, NT, STAGES, PER_CU>>{})) return e;
     return launch(kernel, dim3((unsigned)((p.n_rows + S::BM - 1) / S::BM * ((p.n_out + S::BN - 1) / S::BN))), dim3(64 * WM * WN), S::LDS_BYTES, lc, p);
 }
-template <class Out, int MT, int NT, int WAVES> hipError_t few(const Product &p, const LaunchCtx &lc)
+template <class Out, int WAVES> hipError_t few(const Product &p, const LaunchCtx &lc)
 {
-    return launch(k_project_few<Out, MT, NT, WAVES>, dim3((p.n_out + 16 * NT - 1) / (16 * NT), (unsigned)((p.n_rows + 16 * MT - 1) / (16 * MT))), dim3(64 * WAVES), 0, lc, p);
+    return launch(k_project_few<Out, WAVES>, dim3((p.n_out + 15) / 16), dim3(64 * WAVES), 0, lc, p);
 }
 
-// Which tiles a product goes in: those of the least estimated time.  A step of BK codes takes a workgroup that has its compute unit to itself `alone` us, and `full` us each
-// of per_cu that share it (measured with weights that come from memory; rows x columns x outputs, us by 64 x 32, 64 x 64, 64 x 128, 128 x 128, 256 x 256: 64 x 4096 x 6144
+// Which tiles a product goes in: those of the least estimated time.  A step of BK codes takes a workgroup that has its compute unit to itself `alone` us, and `full` us
+// per_cu of them that share it; 256 x 256 always has one to itself (measured with weights that come from memory; rows x columns x outputs, us by 64 x 32, 64 x 64, 64 x 128, 128 x 128, 256 x 256: 64 x 4096 x 6144
 // 10.7, 13.0, -, -, -; 256 23, 20, 18.5, 31, -; 1024 -, -, 43, 40, 53; 2048 -, -, 78, 70, 58; 16384 -, -, -, 445, 370, 2,230 TOP/s).  One workgroup of 16 rows has no
 // tile: their weights are read by waves that share the summed axis (16 x 8192 x 1024 9.3, in tiles 14.8; 16 x 4096 x 6144 10.5 and 9.9).
 struct Tiles { int rows, outs, per_cu; float alone, full; };
-constexpr Tiles kTiles[] = {{64, 32, 2, 0.26f, 0.39f}, {64, 64, 2, 0.33f, 0.54f}, {64, 128, 2, 0.50f, 0.82f}, {128, 128, 2, 0.90f, 1.15f}, {256, 256, 1, 1.60f, 1.93f}};
+constexpr Tiles kTiles[] = {{64, 32, 2, 0.26f, 0.39f}, {64, 64, 2, 0.33f, 0.54f}, {64, 128, 2, 0.50f, 0.82f}, {128, 128, 2, 0.90f, 1.15f}, {256, 256, 1, 1.93f, 1.93f}};
 int tiles_of(const Product &p)
 {
     int best = 0;
@@ -411,7 +383,7 @@ int tiles_of(const Product &p)
 template <class Out>
 hipError_t product(const Product &p, const LaunchCtx &lc)
 {
-    if (p.n_rows <= 16) return few<Out, 1, 1, 8>(p, lc);
+    if (p.n_rows <= 16) return few<Out, 8>(p, lc);
     switch (tiles_of(p)) {
     case 0: return tile<Out, 2, 2, 2, 1, 6, 2>(p, lc);
     case 1: return tile<Out, 2, 2, 2, 2, 4, 2>(p, lc);
