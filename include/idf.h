@@ -600,7 +600,7 @@ int idf_nibble_append(const idf_nibble_append_args *a, void *hip_stream);
 /* idf_window_attend over what the ring holds alone: the queries' own tokens have been appended before.  starts: position of each segment's first
  * query.  The ring has to have room for a segment beside a window, slots - sinks >= window + max_tokens - 1 (of the tokens that there are), since its later
  * tokens take the slots of earlier ones.  Whatever the ring holds of positions beyond the segment's last query, and of positions that fell out of the window,
- * is not seen.  The values are those of idf_nibble_values, exactly. */
+ * is not seen.  The values are those of idf_nibble_values, exactly.  Sums over the keys are float32 and divided behind the last one: values beyond 2^96 may add up to infinity. */
 typedef struct {
     int precision, heads_q, heads_kv, head_dim;
     int64_t n_tokens, max_tokens;
@@ -631,6 +631,7 @@ int idf_nibble_values(const idf_nibble_values_args *a, void *hip_stream);
  * with gates held to -87 .. 87 (neither what is kept nor what is taken in is ever nothing: an infinite state stays infinite).  state_in, state_out: float32
  * [n_streams][channels], from the state of the segment's stream before it to the one after it, as in idf_decay_attend.  States are float32 throughout.
  * out must not overlap x or gates.  clear_rows: whether rows of out that none of the segments has are set to zero (0: left as they are).
+ *   Parts of a long segment wait for each other on the device, for seconds at most: what is not there then is taken as no number, and shows as such.
  *   marks (NULL: not wanted): what the backward pass needs beside x and gates, states within the segments, idf_gate_scan_marks bytes, 256-byte
  * aligned.  Rows need no alignment beyond their values'.  1 <= channels <= 2^20; segments of up to 2^30 tokens; where one has more than 128,
  * (n_tokens / 128 + n_segments) * channels / 64 < 2^23. */

@@ -3,7 +3,8 @@
 Everything is enqueued on the current stream of the tensors' device.  There is no backward pass but that of gate_scan_recorded: tensors that require
 gradients are refused elsewhere where gradients are recorded, taken under torch.no_grad(); tensors that carry a tangent of torch's forward mode are
 refused everywhere.  Packed tokens [token][head][value]; a tensor whose values lie apart, or whose rows do not begin at multiples of 16 bytes where the
-library asks for that, is copied first.
+library asks for that, is copied first.  Rows of a result that no segment has are left as they are, where a call makes the result itself as its memory
+was (but for the recurrence's: zeros).
 """
 from __future__ import annotations
 

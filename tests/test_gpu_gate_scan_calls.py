@@ -45,6 +45,11 @@ def test_gradients_without_segments(rows, channels, dtype):
         del filler                                 # (their memory is likely to be taken for the gradients)
         got = f(x, gates, marks, d, offsets=offsets, max_tokens=rows)
         assert not got[0].any() and not got[1].any() and not got[2].any()
+    leaves = [t.clone().requires_grad_() for t in (x, gates)]
+    out, ends = idf.gate_scan_recorded(*leaves, offsets=offsets, max_tokens=rows)
+    assert not out.any() and ends.shape == (0, channels)
+    out.backward(d)
+    assert not leaves[0].grad.any() and not leaves[1].grad.any()
 
 
 def test_tangents_are_refused():
